@@ -408,9 +408,90 @@ infs_status infs_get_kernel_info(const infs_ctx* ctx, infs_kernel_info* out);
 infs_status infs_timing_begin(infs_ctx* ctx);
 infs_status infs_timing_end(infs_ctx* ctx, double* kernel_ms, double* region_ms, int64_t* launches);
 
-/* Message of the last failed call on ctx (NULL ctx: last failed infs_create / infs_sched_create
-   of this thread).  Never NULL. */
+/* Message of the last failed call on ctx (NULL ctx: last failed infs_create, infs_sched_create or call
+   without a context of this thread).  Never NULL. */
 const char* infs_last_error(const infs_ctx* ctx);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rotary positions on rows of Q and K: what a model applies between its projections and
+ * infs_prefill_shared / infs_decode_step / infs_probe_step, which take rows as they are to be attended.
+ * A pair (a, b) of elements of a head at position p turns by the angle t = p * f_j of its pair j:
+ *     out_a = A (x_a cos t - x_b sin t),    out_b = A (x_b cos t + x_a sin t),
+ * (a, b) = (j, j + rotary_dim/2) or (2j, 2j + 1), j = 0 .. rotary_dim/2 - 1; the head's elements from
+ * rotary_dim on are copied.  Angles are formed in double, rows rotated in fp32 and rounded once.
+ * ------------------------------------------------------------------------------------------- */
+#define INFS_ROTARY_MAX_DIM 256
+
+typedef enum infs_rotary_layout {
+    INFS_ROTARY_HALF = 0,        /* pair j: elements j and j + rotary_dim/2 */
+    INFS_ROTARY_INTERLEAVED = 1  /* pair j: elements 2j and 2j + 1 */
+} infs_rotary_layout;
+
+/* Frequencies: f_j = base^(-2j / rotary_dim), scaled for contexts longer than the trained ones. */
+typedef enum infs_rotary_scaling {
+    INFS_ROTARY_NONE = 0,
+    INFS_ROTARY_LINEAR = 1, /* f_j / factor (position interpolation) */
+    INFS_ROTARY_NTK = 2,    /* base * factor^(rotary_dim / (rotary_dim - 2)) in the place of base */
+    INFS_ROTARY_YARN = 3,   /* from f_j to f_j / factor along a ramp over j, between the pair that makes `high`
+                               turns over trained_len positions (rounded down) and the one that makes `low`
+                               (rounded up); amplitude 0.1 ln(factor) + 1 unless given (arXiv 2309.00071) */
+    INFS_ROTARY_BANDS = 4   /* pairs of fewer than `low` turns over trained_len positions f_j / factor, of more than
+                               `high` turns f_j, between them a mix that is linear in the turns */
+} infs_rotary_scaling;
+
+typedef struct infs_rotary_config {
+    int32_t head_dim;    /* elements of a head, 2 .. INFS_ROTARY_MAX_DIM */
+    int32_t rotary_dim;  /* elements of it that are rotated: even, 2 .. head_dim */
+    int32_t layout;      /* infs_rotary_layout */
+    int32_t scaling;     /* infs_rotary_scaling */
+    double base;         /* above 1 */
+    double factor;       /* scaling: >= 1 */
+    double low, high;    /* YARN (usually 1 and 32), BANDS (usually 1 and 4): turns, 0 < low < high */
+    double amplitude;    /* A; 0: the scaling's own (YARN above, else 1) */
+    int32_t trained_len; /* YARN, BANDS: positions the frequencies were trained on, >= 1 */
+} infs_rotary_config;
+
+/* Rows of one tensor: element e of head h of row t of layer l lies at in + (l * in_layer + t * in_row +
+   h * in_head + e) elements, and goes to out alike.  A stride of 0 is the dense one ([layers, rows, heads,
+   head_dim]).  out may be in where their strides agree; otherwise the two may not overlap.  Any alignment to
+   an element; rows whose addresses and strides are multiples of 16 bytes take the fast path. */
+typedef struct infs_rows {
+    const void* in;
+    void* out;
+    int32_t heads;       /* 1 .. 4096 */
+    int64_t in_row, in_head, in_layer;     /* elements */
+    int64_t out_row, out_head, out_layer;
+} infs_rows;
+
+/* A configuration: frequencies on the host, no device memory; it may be used from several threads, on any
+   stream and device, and destroyed while launches that used it still run. */
+typedef struct infs_rotary infs_rotary;
+infs_status infs_rotary_create(const infs_rotary_config* cfg, infs_rotary** out);
+void infs_rotary_destroy(infs_rotary* r);
+
+/* The n = rotary_dim / 2 frequencies (angle per position) and the amplitude of a configuration. */
+infs_status infs_rotary_frequencies(const infs_rotary* r, double* freq_out, int32_t n, double* amplitude_out);
+
+/* Rotate `tokens` rows of Q and K (either may be NULL) on hip_stream: a prompt before its prefill, or a
+   training batch.  Token t is at position positions_dev[t], or first_position + t without them (any sign;
+   up to 2^31 - 1).  inverse != 0 turns the other way: the gradient of the rows with respect to the inputs.
+   dtype: infs_dtype.  One launch; nothing is allocated, so it may be captured.  Messages:
+   infs_last_error(NULL). */
+infs_status infs_rotate_rows(const infs_rotary* r, void* hip_stream, int32_t dtype, int64_t tokens, const infs_rows* q,
+                             const infs_rows* k, const int32_t* positions_dev, int32_t first_position, int32_t inverse);
+
+/* Rotate the rows of one running step, before its decode calls: row s of q (Hq heads) and k (Hkv heads) is
+   slot s's, at position prompt_len + current length, the one this step's token takes; rows of idle slots are
+   neither read nor written.  num_layers layers in one launch (1 .. the context's; they differ in the rows
+   alone).  q or k may be NULL.  E_ARG also when head_dim or the head counts are not the context's;
+   E_STATE: a live slot's prompt has no prefix. */
+infs_status infs_rotate_step(infs_ctx* ctx, const infs_rotary* r, int32_t num_layers, const infs_rows* q,
+                             const infs_rows* k);
+
+/* The same for the rows of a probe step of samples first_sample .. first_sample+n-1 (infs_probe_step's
+   arguments): position prompt_len + the sample's probe length. */
+infs_status infs_rotate_probe(infs_ctx* ctx, const infs_rotary* r, int32_t prompt, int32_t first_sample, int32_t n,
+                              const uint8_t* live_host, int32_t num_layers, const infs_rows* q, const infs_rows* k);
 
 /* ---------------------------------------------------------------------------------------------
  * Host scheduler (CPU only, no device): chooses which sample a freed slot receives.

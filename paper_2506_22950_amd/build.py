@@ -24,7 +24,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 # (inst_*.hip) that compile in parallel; the device code is in decode.h.
 SOURCES = ["kernels.hip", "inst_wave_f32_d64.hip", "inst_wave_f32_d128.hip", "inst_wave_bf16_d64.hip",
            "inst_wave_bf16_d128.hip", "inst_mfma_d64.hip", "inst_mfma_d128a.hip", "inst_mfma_d128b.hip",
-           "inst_kv8a.hip", "inst_kv8b.hip", "scratch.hip", "runtime.cpp", "sched.cpp"]
+           "inst_kv8a.hip", "inst_kv8b.hip", "scratch.hip", "rotary.hip", "runtime.cpp", "sched.cpp", "ops.cpp"]
 CALIB_SOURCES = ["calib.hip"]
 
 
@@ -80,7 +80,7 @@ def build(verbose: bool = False) -> str:
     return LIB
 
 
-# Host-only sanitizer build: the host runtime (runtime.cpp, sched.cpp) with
+# Host-only sanitizer build: the host runtime (runtime.cpp, sched.cpp, ops.cpp) with
 # AddressSanitizer and UndefinedBehaviorSanitizer, the kernel objects as built
 # by build().  Sanitizers apply to host code only: each -fsanitize= follows
 # -Xarch_host, so no device code is instrumented.  The library is written as
@@ -88,7 +88,7 @@ def build(verbose: bool = False) -> str:
 # needs the sanitizer runtime preloaded (sanitizer_runtime()).
 SAN_DIR = os.path.join(HERE, "_san")
 SAN_LIB = os.path.join(SAN_DIR, "libinfs.so")
-SAN_SOURCES = ["runtime.cpp", "sched.cpp"]
+SAN_SOURCES = ["runtime.cpp", "sched.cpp", "ops.cpp"]
 
 
 def sanitizer_runtime() -> str:

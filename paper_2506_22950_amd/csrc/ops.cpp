@@ -1,0 +1,150 @@
+// Host side of the operators that need no context: rotary configurations and
+// rows.  Arguments are checked before anything is enqueued; messages go to
+// infs_last_error(NULL) of the calling thread.
+#include "ops.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+namespace infs {
+
+infs_status pack_rotary_rows(const infs_rows* r, const char* what, int head_dim, int64_t tokens, int layers, size_t es,
+                             RotaryRows* out) {
+  *out = RotaryRows{};
+  if (r->heads < 1 || r->heads > 4096) return op_fail(INFS_E_ARG, "%s: heads must be in [1, 4096]", what);
+  const int64_t s[6] = {r->in_row, r->in_head, r->in_layer, r->out_row, r->out_head, r->out_layer};
+  for (int64_t x : s)
+    if (x < 0 || x > (int64_t(1) << 40)) return op_fail(INFS_E_ARG, "%s: strides must be in [0, 2^40] elements", what);
+  const int64_t head = head_dim, row = head * r->heads, layer = row * tokens;
+  out->in_head = r->in_head ? r->in_head : head;
+  out->in_row = r->in_row ? r->in_row : row;
+  out->in_layer = r->in_layer ? r->in_layer : layer;
+  out->out_head = r->out_head ? r->out_head : head;
+  out->out_row = r->out_row ? r->out_row : row;
+  out->out_layer = r->out_layer ? r->out_layer : layer;
+  // strides of axes longer than one: heads may not overlap
+  if ((r->heads > 1 && (out->in_head < head || out->out_head < head)) ||
+      (tokens > 1 && (out->in_row < head || out->out_row < head)) ||
+      (layers > 1 && (out->in_layer < head || out->out_layer < head)))
+    return op_fail(INFS_E_ARG, "%s: strides below one head's %d elements", what, head_dim);
+  if (((uintptr_t)r->in | (uintptr_t)r->out) % es) return op_fail(INFS_E_ARG, "%s: rows must be aligned to an element", what);
+  if (r->in == r->out && ((r->heads > 1 && out->in_head != out->out_head) || (tokens > 1 && out->in_row != out->out_row) ||
+                          (layers > 1 && out->in_layer != out->out_layer)))
+    return op_fail(INFS_E_ARG, "%s: rows rotated in place need equal strides", what);
+  out->in = (const char*)r->in;
+  out->out = (char*)r->out;
+  out->heads = r->heads;
+  return INFS_OK;
+}
+
+void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a) {
+  std::copy(r.freq, r.freq + r.pairs, a->freq);
+  a->head_dim = r.cfg.head_dim;
+  a->pairs = r.pairs;
+  a->amplitude = (float)r.amplitude;
+  a->sign = inverse ? -1.f : 1.f;
+}
+
+}  // namespace infs
+
+using infs::op_fail;
+
+extern "C" {
+
+infs_status infs_rotary_create(const infs_rotary_config* cfg, infs_rotary** out) {
+  if (!out) return op_fail(INFS_E_ARG, "out is null");
+  *out = nullptr;
+  if (!cfg) return op_fail(INFS_E_ARG, "cfg is null");
+  const infs_rotary_config& k = *cfg;
+  if (k.head_dim < 2 || k.head_dim > INFS_ROTARY_MAX_DIM)
+    return op_fail(INFS_E_ARG, "head_dim must be in [2, %d]", INFS_ROTARY_MAX_DIM);
+  if (k.rotary_dim < 2 || k.rotary_dim > k.head_dim || k.rotary_dim % 2)
+    return op_fail(INFS_E_ARG, "rotary_dim must be even and in [2, head_dim]");
+  if (k.layout != INFS_ROTARY_HALF && k.layout != INFS_ROTARY_INTERLEAVED)
+    return op_fail(INFS_E_ARG, "layout must be INFS_ROTARY_HALF or INFS_ROTARY_INTERLEAVED");
+  if (k.scaling < INFS_ROTARY_NONE || k.scaling > INFS_ROTARY_BANDS) return op_fail(INFS_E_ARG, "unknown scaling");
+  if (!(k.base > 1.0) || !std::isfinite(k.base)) return op_fail(INFS_E_ARG, "base must be finite and above 1");
+  const bool scaled = k.scaling != INFS_ROTARY_NONE, ramped = k.scaling == INFS_ROTARY_YARN || k.scaling == INFS_ROTARY_BANDS;
+  if (scaled && (!(k.factor >= 1.0) || !std::isfinite(k.factor)))
+    return op_fail(INFS_E_ARG, "factor must be finite and at least 1");
+  if (k.scaling == INFS_ROTARY_NTK && k.rotary_dim < 4)
+    return op_fail(INFS_E_ARG, "INFS_ROTARY_NTK needs a rotary_dim of at least 4");
+  if (ramped && k.trained_len < 1) return op_fail(INFS_E_ARG, "trained_len must be at least 1");
+  if (ramped && (!(k.low > 0.0) || !(k.high > k.low) || !std::isfinite(k.high)))
+    return op_fail(INFS_E_ARG, "low and high must be finite with 0 < low < high");
+  if (!(k.amplitude >= 0.0) || !std::isfinite(k.amplitude))
+    return op_fail(INFS_E_ARG, "amplitude must be finite and >= 0");
+  infs_rotary* r = new (std::nothrow) infs_rotary;
+  if (!r) return op_fail(INFS_E_NOMEM, "host allocation failed");
+  r->cfg = k;
+  r->pairs = k.rotary_dim / 2;
+  const double rd = k.rotary_dim, s = scaled ? k.factor : 1.0, two_pi = 6.283185307179586476925;
+  const double base = k.scaling == INFS_ROTARY_NTK ? k.base * std::pow(s, rd / (rd - 2.0)) : k.base;
+  // YARN: the pair index whose frequency makes `turns` turns over the trained positions
+  auto pair_of = [&](double turns) { return rd * std::log(k.trained_len / (turns * two_pi)) / (2.0 * std::log(k.base)); };
+  double lo = 0, hi = 0;
+  if (k.scaling == INFS_ROTARY_YARN) {
+    lo = std::max(std::floor(pair_of(k.high)), 0.0);
+    hi = std::min(std::ceil(pair_of(k.low)), rd - 1.0);
+  }
+  for (int j = 0; j < r->pairs; ++j) {
+    double f = std::pow(base, -2.0 * j / rd);
+    if (k.scaling == INFS_ROTARY_LINEAR) {
+      f /= s;
+    } else if (k.scaling == INFS_ROTARY_YARN) {
+      const double mix = std::min(1.0, std::max(0.0, (j - lo) / std::max(hi - lo, 0.001)));
+      f = f / s * mix + f * (1.0 - mix);
+    } else if (k.scaling == INFS_ROTARY_BANDS) {
+      const double turns = k.trained_len * f / two_pi;
+      const double mix = std::min(1.0, std::max(0.0, (turns - k.low) / (k.high - k.low)));
+      f = (1.0 - mix) * f / s + mix * f;
+    }
+    r->freq[j] = f;
+  }
+  r->amplitude = k.amplitude > 0.0 ? k.amplitude : k.scaling == INFS_ROTARY_YARN ? 0.1 * std::log(s) + 1.0 : 1.0;
+  *out = r;
+  return INFS_OK;
+}
+
+void infs_rotary_destroy(infs_rotary* r) { delete r; }
+
+infs_status infs_rotary_frequencies(const infs_rotary* r, double* freq_out, int32_t n, double* amplitude_out) {
+  if (!r || !freq_out || !amplitude_out) return op_fail(INFS_E_ARG, "null argument");
+  if (n != r->pairs) return op_fail(INFS_E_ARG, "n must equal rotary_dim / 2 = %d", r->pairs);
+  std::copy(r->freq, r->freq + n, freq_out);
+  *amplitude_out = r->amplitude;
+  return INFS_OK;
+}
+
+infs_status infs_rotate_rows(const infs_rotary* r, void* hip_stream, int32_t dtype, int64_t tokens, const infs_rows* q,
+                             const infs_rows* k, const int32_t* positions_dev, int32_t first_position, int32_t inverse) {
+  if (!r) return op_fail(INFS_E_ARG, "null rotary configuration");
+  if (dtype != INFS_F32 && dtype != INFS_BF16) return op_fail(INFS_E_ARG, "dtype must be INFS_F32 or INFS_BF16");
+  if (tokens < 0 || tokens > INT32_MAX) return op_fail(INFS_E_ARG, "tokens must be in [0, 2^31)");
+  if (!q && !k) return op_fail(INFS_E_ARG, "no rows given");
+  if (!positions_dev && (int64_t)first_position + tokens - 1 > INT32_MAX)
+    return op_fail(INFS_E_ARG, "positions beyond 2^31 - 1");
+  if ((uintptr_t)positions_dev & 3) return op_fail(INFS_E_ARG, "positions must be aligned to 4 bytes");
+  infs::RotaryArgs a{};
+  infs_status st = INFS_OK;
+  const size_t es = dtype == INFS_BF16 ? 2 : 4;
+  const infs_rows* rows[2] = {q, k};
+  for (int i = 0; i < 2 && st == INFS_OK; ++i) {
+    if (!rows[i]) continue;
+    st = infs::pack_rotary_rows(rows[i], i ? "k" : "q", r->cfg.head_dim, tokens, 1, es, i ? &a.k : &a.q);
+    if (st == INFS_OK && tokens > 0 && (!rows[i]->in || !rows[i]->out)) st = op_fail(INFS_E_ARG, "null rows");
+  }
+  if (st != INFS_OK || tokens == 0) return st;
+  infs::set_rotary(*r, inverse != 0, &a);
+  a.positions = positions_dev;
+  a.first = first_position;
+  a.tokens = (int32_t)tokens;
+  infs::StreamDevice dev((hipStream_t)hip_stream);
+  hipError_t e = dev.status();
+  if (e == hipSuccess)
+    e = infs::launch_rotate(a, dtype == INFS_BF16, r->cfg.layout == INFS_ROTARY_INTERLEAVED, 1, (hipStream_t)hip_stream);
+  return e == hipSuccess ? INFS_OK : op_fail(INFS_E_DEVICE, "rotating rows failed: %s", hipGetErrorString(e));
+}
+
+}  // extern "C"

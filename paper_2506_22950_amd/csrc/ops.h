@@ -1,0 +1,82 @@
+// Launch entry points of the row and page operators (rotary.hip), and the
+// error and device helpers their host code shares.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "infs.h"
+#include "plan.h"
+
+// Host only: the frequencies a rotary configuration gives.
+struct infs_rotary {
+  infs_rotary_config cfg{};
+  int pairs = 0;
+  double freq[INFS_ROTARY_MAX_DIM / 2] = {};  // angle per position of pair j
+  double amplitude = 1.0;
+};
+
+namespace infs {
+
+// Records the message infs_last_error(NULL) gives on this thread; returns st.
+infs_status op_fail(infs_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
+// Makes the device of `stream` current for its lifetime (the null stream: the current one stays).
+class StreamDevice {
+ public:
+  explicit StreamDevice(hipStream_t stream) {
+    if (!stream) return;
+    int dev = 0;
+    status_ = hipGetDevice(&before_);
+    if (status_ == hipSuccess) status_ = hipStreamGetDevice(stream, &dev);
+    if (status_ == hipSuccess && dev != before_) {
+      status_ = hipSetDevice(dev);
+      changed_ = status_ == hipSuccess;
+    }
+  }
+  ~StreamDevice() {
+    if (changed_) (void)hipSetDevice(before_);
+  }
+  StreamDevice(const StreamDevice&) = delete;
+  StreamDevice& operator=(const StreamDevice&) = delete;
+  hipError_t status() const { return status_; }
+
+ private:
+  int before_ = 0;
+  bool changed_ = false;
+  hipError_t status_ = hipSuccess;
+};
+
+// ---- rotary positions --------------------------------------------------------
+constexpr int kRotaryThreads = 256;
+constexpr int kRotaryTable = 256;  // (cos, sin) entries of a work-group
+static_assert(INFS_ROTARY_MAX_DIM / 2 <= kRotaryTable, "a token's pairs fit the table");
+
+struct RotaryRows {
+  const char* in;
+  char* out;
+  int64_t in_row, in_head, in_layer, out_row, out_head, out_layer;  // elements
+  int32_t heads;                                                    // 0: no such rows
+};
+
+struct RotaryArgs {
+  double freq[INFS_ROTARY_MAX_DIM / 2];
+  RotaryRows q, k;
+  const int32_t* positions;  // or null: pos[] of the slots (live != 0), else first + token
+  uint64_t live;             // slots: bit t set where token t is rotated (0: every token)
+  int32_t tokens, first, head_dim, pairs;
+  int32_t tokens_per_wg;     // tokens_per_wg * pairs <= kRotaryTable
+  float amplitude, sign;     // of cos and sin; sign of the angle
+  int32_t pos[kMaxSlots];
+};
+static_assert(sizeof(RotaryArgs) <= 4096, "kernel argument block must fit 4 KiB");
+
+// Rotate `layers` layers of rows; fills in tokens_per_wg.
+hipError_t launch_rotate(RotaryArgs& args, bool bf16, bool interleaved, int layers, hipStream_t stream);
+
+// Checks and packs one side's rows (op_fail on E_ARG).  es: element bytes.
+infs_status pack_rotary_rows(const infs_rows* r, const char* what, int head_dim, int64_t tokens, int layers, size_t es,
+                             RotaryRows* out);
+// The configuration's part of the launch arguments.
+void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a);
+
+}  // namespace infs

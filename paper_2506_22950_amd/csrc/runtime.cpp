@@ -16,6 +16,7 @@
 
 #include "infs.h"
 #include "kernels.h"
+#include "ops.h"
 #include "step_plan.h"
 #include "plan.h"
 
@@ -118,6 +119,20 @@ struct infs_ctx {
   std::string err = "no error";
   Timing timing;
 };
+
+namespace infs {
+
+infs_status op_fail(infs_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_thread_error = buf;
+  return st;
+}
+
+}  // namespace infs
 
 namespace {
 
@@ -1517,6 +1532,75 @@ infs_status infs_timing_end(infs_ctx* c, double* kernel_ms, double* region_ms, i
   *region_ms = ms;
   *launches = t.launches;
   return INFS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Rotate the n rows of a running or probe step: row s at position pos[s] where bit s of live is set.
+infs_status rotate_slots(infs_ctx* c, const infs_rotary* r, int32_t num_layers, const infs_rows* q, const infs_rows* k,
+                         int n, uint64_t live, const int32_t* pos) {
+  if (!r) return fail(c, INFS_E_ARG, "null rotary configuration");
+  if (num_layers < 1 || num_layers > c->L) return fail(c, INFS_E_ARG, "num_layers must be in [1, %d]", c->L);
+  if (!q && !k) return fail(c, INFS_E_ARG, "no rows given");
+  if (r->cfg.head_dim != c->D) return fail(c, INFS_E_ARG, "rotary head_dim %d is not the context's %d", r->cfg.head_dim, c->D);
+  infs::RotaryArgs a{};
+  const infs_rows* rows[2] = {q, k};
+  const int heads[2] = {c->Hq, c->Hkv};
+  for (int i = 0; i < 2; ++i) {
+    if (!rows[i]) continue;
+    const char* what = i ? "k" : "q";
+    if (rows[i]->heads != heads[i]) return fail(c, INFS_E_ARG, "%s: %d heads, the context has %d", what, rows[i]->heads, heads[i]);
+    if (!c->dry && (!rows[i]->in || !rows[i]->out)) return fail(c, INFS_E_ARG, "%s: null rows", what);
+    const infs_status st = infs::pack_rotary_rows(rows[i], what, c->D, n, num_layers, c->es, i ? &a.k : &a.q);
+    if (st != INFS_OK) return fail(c, st, "%s", g_thread_error.c_str());
+  }
+  if (c->dry || live == 0) return INFS_OK;
+  infs::set_rotary(*r, false, &a);
+  a.live = live;
+  a.tokens = n;
+  std::copy(pos, pos + n, a.pos);
+  HIP_TRY(c, infs::launch_rotate(a, c->key.bf16 != 0, r->cfg.layout == INFS_ROTARY_INTERLEAVED, num_layers, c->stream));
+  return INFS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+infs_status infs_rotate_step(infs_ctx* c, const infs_rotary* r, int32_t num_layers, const infs_rows* q,
+                             const infs_rows* k) {
+  CHECK_CTX(c);
+  uint64_t live = 0;
+  int32_t pos[infs::kMaxSlots] = {};
+  for (int s = 0; s < c->S; ++s) {
+    if (c->slot_sample[s] < 0) continue;
+    const int p = s / c->m;
+    if (c->plen[p] < 0) return fail(c, INFS_E_STATE, "prompt %d has live slots but no prefilled prefix", p);
+    live |= uint64_t(1) << s;
+    pos[s] = c->plen[p] + c->slot_len[s];
+  }
+  return rotate_slots(c, r, num_layers, q, k, c->S, live, pos);
+}
+
+infs_status infs_rotate_probe(infs_ctx* c, const infs_rotary* r, int32_t prompt, int32_t first_sample, int32_t n,
+                              const uint8_t* live_host, int32_t num_layers, const infs_rows* q, const infs_rows* k) {
+  CHECK_CTX(c);
+  if (c->probe_k == 0) return fail(c, INFS_E_STATE, "rotate_probe needs a context with probe_tokens > 0");
+  if (prompt < 0 || prompt >= c->NP) return fail(c, INFS_E_ARG, "prompt %d out of range [0, %d)", prompt, c->NP);
+  if (n < 1 || n > c->probe_batch) return fail(c, INFS_E_ARG, "n=%d out of range [1, %d]", n, c->probe_batch);
+  if (first_sample < 0 || first_sample > c->G - n)
+    return fail(c, INFS_E_ARG, "samples %d..%d out of range [0, %d)", first_sample, first_sample + n - 1, c->G);
+  uint64_t live = 0;
+  int32_t pos[infs::kMaxSlots] = {};
+  for (int j = 0; j < n; ++j) {
+    if (live_host && !live_host[j]) continue;
+    if (c->plen[prompt] < 0) return fail(c, INFS_E_STATE, "prompt %d has no prefilled prefix", prompt);
+    live |= uint64_t(1) << j;
+    pos[j] = c->plen[prompt] + c->probe_len[prompt][first_sample + j];
+  }
+  return rotate_slots(c, r, num_layers, q, k, n, live, pos);
 }
 
 }  // extern "C"

@@ -28,6 +28,8 @@ FPTAS_EPSILON = 0.1
 FLAG_DRY_RUN = 1
 FLAG_KV_FP8 = 2
 STATIC_SCRATCH_BYTES = 16 << 20
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_NONE, ROTARY_LINEAR, ROTARY_NTK, ROTARY_YARN, ROTARY_BANDS = 0, 1, 2, 3, 4
 
 # Every symbol include/infs.h declares.
 EXPORTS = (
@@ -40,6 +42,8 @@ EXPORTS = (
     "infs_get_kernel_info", "infs_set_exchange", "infs_exchange_mode", "infs_decode_step_static",
     "infs_sched_optimum", "infs_decode_step_layers", "infs_step_launch_workgroups", "infs_set_step_split",
     "infs_step_split_plan", "infs_step_launch_plan", "infs_probe_step_layers",
+    "infs_rotary_create", "infs_rotary_destroy", "infs_rotary_frequencies", "infs_rotate_rows",
+    "infs_rotate_step", "infs_rotate_probe",
 )
 
 
@@ -63,6 +67,19 @@ class Config(ctypes.Structure):
 class KernelInfo(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("bf16", "head_dim", "hpk", "mfma", "prefix_rows", "kv_fp8",
                                              "probe_mfma", "probe_prefix_rows")]
+
+
+class RotaryConfig(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("amplitude", ctypes.c_double),
+                ("trained_len", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("heads", ctypes.c_int32),
+                ("in_row", ctypes.c_int64), ("in_head", ctypes.c_int64), ("in_layer", ctypes.c_int64),
+                ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64), ("out_layer", ctypes.c_int64)]
 
 
 class Stats(ctypes.Structure):
@@ -129,6 +146,13 @@ def load():
         "infs_read_prefix": (I32, [P, I32, I32, P, P]),
         "infs_read_response": (I32, [P, I32, I32, P, P]),
         "infs_set_merge_wait": (I32, [P, I32]),
+        "infs_rotary_create": (I32, [ctypes.POINTER(RotaryConfig), ctypes.POINTER(P)]),
+        "infs_rotary_destroy": (None, [P]),
+        "infs_rotary_frequencies": (I32, [P, ctypes.POINTER(ctypes.c_double), I32, ctypes.POINTER(ctypes.c_double)]),
+        "infs_rotate_rows": (I32, [P, P, I32, I64, ctypes.POINTER(Rows), ctypes.POINTER(Rows), P, I32, I32]),
+        "infs_rotate_step": (I32, [P, P, I32, ctypes.POINTER(Rows), ctypes.POINTER(Rows)]),
+        "infs_rotate_probe": (I32, [P, P, I32, I32, I32, ctypes.POINTER(ctypes.c_uint8), I32, ctypes.POINTER(Rows),
+                                    ctypes.POINTER(Rows)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -165,6 +189,58 @@ def make_config(**kw) -> Config:
     for k, v in kw.items():
         setattr(c, k, v)
     return c
+
+
+def make_rotary_config(**kw) -> RotaryConfig:
+    c = RotaryConfig()
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def rotary_rows(x, out, heads, in_strides=(0, 0, 0), out_strides=(0, 0, 0)) -> Rows:
+    """infs_rows: rows of x go to out (the same buffer: in place); strides (row, head, layer) in
+    elements, 0 the dense one."""
+    return Rows(_ptr(x), _ptr(out), heads, *in_strides, *out_strides)
+
+
+def _byref(rows):
+    return None if rows is None else ctypes.byref(rows)
+
+
+def _flags(live, n):
+    return None if live is None else (ctypes.c_uint8 * n)(*[1 if x else 0 for x in live])
+
+
+class Rotary:
+    """One infs_rotary (a configuration of rotary positions)."""
+
+    def __init__(self, config: RotaryConfig):
+        h = ctypes.c_void_p()
+        _check(None, load().infs_rotary_create(ctypes.byref(config), ctypes.byref(h)))
+        self._h = h
+        self.config = config
+
+    def frequencies(self):
+        """(angle per position of every pair, amplitude)."""
+        n = self.config.rotary_dim // 2
+        f, amp = np.zeros(n), ctypes.c_double()
+        _check(None, load().infs_rotary_frequencies(self._h, f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), n,
+                                                    ctypes.byref(amp)))
+        return f, amp.value
+
+    def rotate_rows(self, dtype, tokens, q=None, k=None, positions=None, first_position=0, inverse=False, stream=None):
+        """infs_rotate_rows; q and k are rotary_rows(...)."""
+        _check(None, load().infs_rotate_rows(self._h, _stream(stream), dtype, tokens, _byref(q), _byref(k),
+                                             _ptr(positions), first_position, 1 if inverse else 0))
+
+    def __del__(self):
+        try:
+            if self._h:
+                load().infs_rotary_destroy(self._h)
+                self._h = None
+        except Exception:
+            pass
 
 
 class Context:
@@ -270,6 +346,15 @@ class Context:
             buf = (ctypes.c_uint8 * n)(*[1 if x else 0 for x in live])
         self._call(load().infs_probe_step_layers, prompt, first_sample, n, buf, _ptr(q), _ptr(k_new), _ptr(v_new),
                    _ptr(o), q_layer_stride, kv_layer_stride, o_layer_stride)
+
+    def rotate_step(self, rotary, q=None, k=None, num_layers=1):
+        """Rotate a running step's rows before it is decoded; q and k are rotary_rows(...)."""
+        self._call(load().infs_rotate_step, rotary._h, num_layers, _byref(q), _byref(k))
+
+    def rotate_probe(self, rotary, prompt, first_sample, n, live, q=None, k=None, num_layers=1):
+        """Rotate a probe step's rows before it is decoded."""
+        self._call(load().infs_rotate_probe, rotary._h, prompt, first_sample, n, _flags(live, n), num_layers,
+                   _byref(q), _byref(k))
 
     def end_probe_step(self):
         self._call(load().infs_end_probe_step)
