@@ -494,6 +494,63 @@ infs_status infs_rotate_probe(infs_ctx* ctx, const infs_rotary* r, int32_t promp
                               const uint8_t* live_host, int32_t num_layers, const infs_rows* q, const infs_rows* k);
 
 /* ---------------------------------------------------------------------------------------------
+ * Scores of tokens: what a group's samples and its learner take from a model's logits.  For a row z of
+ * `vocab` logits at temperature T, with m = max z and S = sum_j exp((z_j - m) / T):
+ *     log p_j  = (z_j - m) / T - ln S
+ *     entropy  = -sum_j p_j log p_j
+ * Entries of -inf are masked: probability 0, no part in the entropy, never an alternative.  A row with
+ * every entry masked has log probability -inf, entropy 0, no alternatives and a zero gradient.  A row
+ * that holds a NaN or +inf has NaN scores (of a token, entropy, ln S, alternatives, whose ids are -1) and
+ * a NaN gradient.
+ * ------------------------------------------------------------------------------------------- */
+#define INFS_SCORE_MAX_TOP 32
+
+typedef struct infs_scorer_config {
+    int32_t vocab;       /* entries of a row, 1 .. 2^24 */
+    int32_t dtype;       /* infs_dtype of logits and gradients */
+    int32_t max_rows;    /* rows of one call, 1 .. 2^24 */
+    int32_t top_k;       /* alternatives per row, 0 .. INFS_SCORE_MAX_TOP */
+    float temperature;   /* T in [2^-20, 2^20]; 0: 1 */
+    uint32_t flags;      /* INFS_FLAG_DRY_RUN: arguments are checked, nothing is allocated or launched */
+} infs_scorer_config;
+
+/* A scorer: its stream and a workspace on the current device (of hip_stream where given) by which
+   work-groups join the parts of a row.  Calls on one scorer are ordered by its stream; captured graphs that
+   hold its calls must not run at the same time as other work of the same scorer.  Messages of all scorer
+   calls: infs_last_error(NULL).  A scorer must be used from one host thread at a time. */
+typedef struct infs_scorer infs_scorer;
+infs_status infs_scorer_create(const infs_scorer_config* cfg, void* hip_stream, infs_scorer** out);
+/* Waits for the scorer's stream first.  NULL is a no-op. */
+void infs_scorer_destroy(infs_scorer* s);
+
+/* Scores of `rows` rows (0 .. max_rows) of logits, row_stride elements apart (0: vocab; at least vocab,
+   any alignment to an element), read once:
+     logprob_dev [rows]        log probability of tokens_dev[row] (int32); 0 for token -1 (no token), NaN for
+                               any other token outside [0, vocab)
+     entropy_dev [rows]        entropy in nats, or NULL
+     top_id_dev, top_logprob_dev [rows, top_k]  the top_k most probable entries, most probable first, equal
+                               logits by the lower index; id -1 and -inf where fewer are not masked.  Both
+                               NULL: none are sought
+     stats_dev [rows, 2]       m and ln S, for infs_score_grad, or NULL (-inf and -inf: every entry masked)
+   tokens_dev NULL (then logprob_dev NULL too): no token is scored.  All outputs are fp32 (ids int32), aligned
+   to 4 bytes (stats_dev to 8).  Sums are kept in fp32 around a running maximum, in an order that depends on
+   the shape alone. */
+infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_dev, int64_t row_stride,
+                              const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev, int32_t* top_id_dev,
+                              float* top_logprob_dev, float* stats_dev);
+
+/* Gradient with respect to the logits, of the logits' type, grad_row_stride elements apart (0: vocab; rows
+   may be written over the logits where the strides agree):
+     grad_j = [ d_logprob (1{j = token} - p_j) - d_entropy p_j (log p_j + entropy) ] / T
+   from stats_dev (and, with d_entropy_dev, entropy_dev) of infs_score_tokens.  d_logprob_dev, d_entropy_dev
+   [rows] fp32: either may be NULL; rows without a token (-1) take no part of d_logprob.  NaN for a token
+   outside [-1, vocab). */
+infs_status infs_score_grad(infs_scorer* s, int32_t rows, const void* logits_dev, int64_t row_stride,
+                            const int32_t* tokens_dev, const float* stats_dev, const float* entropy_dev,
+                            const float* d_logprob_dev, const float* d_entropy_dev, void* grad_dev,
+                            int64_t grad_row_stride);
+
+/* ---------------------------------------------------------------------------------------------
  * Host scheduler (CPU only, no device): chooses which sample a freed slot receives.
  * One scheduler serves one prompt's m slots (local slot ids 0..m-1) and G samples.
  * Use: after the retirements of a step, call infs_sched_next for every empty slot in ascending

@@ -1,10 +1,11 @@
 // Host side of the operators that need no context: rotary configurations and
-// rows.  Arguments are checked before anything is enqueued; messages go to
+// rows, and scores of tokens.  Arguments are checked before anything is enqueued; messages go to
 // infs_last_error(NULL) of the calling thread.
 #include "ops.h"
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <new>
 
 namespace infs {
@@ -49,6 +50,34 @@ void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a) {
 }  // namespace infs
 
 using infs::op_fail;
+
+struct infs_scorer {
+  infs_scorer_config cfg{};
+  bool dry = false, bf16 = false;
+  size_t es = 0;
+  float inv_t = 1.f;
+  hipStream_t stream = nullptr;
+};
+
+namespace {
+
+infs_status check_rows(const infs_scorer* s, int32_t rows, const void* logits, int64_t* stride, const char* what) {
+  if (rows < 0 || rows > s->cfg.max_rows) return op_fail(INFS_E_ARG, "rows must be in [0, %d]", s->cfg.max_rows);
+  if (*stride == 0) *stride = s->cfg.vocab;
+  if (*stride < s->cfg.vocab || *stride > (int64_t(1) << 40))
+    return op_fail(INFS_E_ARG, "%s: row stride must be 0 or in [vocab, 2^40]", what);
+  if (rows > 0 && !s->dry && !logits) return op_fail(INFS_E_ARG, "%s: null buffer", what);
+  if ((uintptr_t)logits % s->es) return op_fail(INFS_E_ARG, "%s must be aligned to an element", what);
+  return INFS_OK;
+}
+
+bool misaligned(std::initializer_list<const void*> ptrs, size_t n) {
+  for (const void* p : ptrs)
+    if ((uintptr_t)p % n) return true;
+  return false;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -145,6 +174,80 @@ infs_status infs_rotate_rows(const infs_rotary* r, void* hip_stream, int32_t dty
   if (e == hipSuccess)
     e = infs::launch_rotate(a, dtype == INFS_BF16, r->cfg.layout == INFS_ROTARY_INTERLEAVED, 1, (hipStream_t)hip_stream);
   return e == hipSuccess ? INFS_OK : op_fail(INFS_E_DEVICE, "rotating rows failed: %s", hipGetErrorString(e));
+}
+
+infs_status infs_scorer_create(const infs_scorer_config* cfg, void* hip_stream, infs_scorer** out) {
+  if (!out) return op_fail(INFS_E_ARG, "out is null");
+  *out = nullptr;
+  if (!cfg) return op_fail(INFS_E_ARG, "cfg is null");
+  const infs_scorer_config& k = *cfg;
+  if (k.vocab < 1 || k.vocab > (1 << 24)) return op_fail(INFS_E_ARG, "vocab must be in [1, 2^24]");
+  if (k.dtype != INFS_F32 && k.dtype != INFS_BF16) return op_fail(INFS_E_ARG, "dtype must be INFS_F32 or INFS_BF16");
+  if (k.max_rows < 1 || k.max_rows > (1 << 24)) return op_fail(INFS_E_ARG, "max_rows must be in [1, 2^24]");
+  if (k.top_k < 0 || k.top_k > INFS_SCORE_MAX_TOP) return op_fail(INFS_E_ARG, "top_k must be in [0, %d]", INFS_SCORE_MAX_TOP);
+  if (k.temperature != 0.f && !(k.temperature >= 0x1p-20f && k.temperature <= 0x1p20f))
+    return op_fail(INFS_E_ARG, "temperature must be 0 (for 1) or in [2^-20, 2^20]");
+  if (k.flags & ~INFS_FLAG_DRY_RUN) return op_fail(INFS_E_ARG, "unknown flags");
+  infs_scorer* s = new (std::nothrow) infs_scorer;
+  if (!s) return op_fail(INFS_E_NOMEM, "host allocation failed");
+  s->cfg = k;
+  s->dry = (k.flags & INFS_FLAG_DRY_RUN) != 0;
+  s->bf16 = k.dtype == INFS_BF16;
+  s->es = s->bf16 ? 2 : 4;
+  s->inv_t = k.temperature != 0.f ? 1.f / k.temperature : 1.f;
+  s->stream = (hipStream_t)hip_stream;
+  *out = s;
+  return INFS_OK;
+}
+
+void infs_scorer_destroy(infs_scorer* s) {
+  if (!s) return;
+  if (!s->dry) (void)hipStreamSynchronize(s->stream);
+  delete s;
+}
+
+infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_dev, int64_t row_stride,
+                              const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev, int32_t* top_id_dev,
+                              float* top_logprob_dev, float* stats_dev) {
+  if (!s) return op_fail(INFS_E_ARG, "null scorer");
+  const infs_status st = check_rows(s, rows, logits_dev, &row_stride, "logits");
+  if (st != INFS_OK) return st;
+  if (!tokens_dev != !logprob_dev) return op_fail(INFS_E_ARG, "tokens and logprob go together");
+  if (!top_id_dev != !top_logprob_dev) return op_fail(INFS_E_ARG, "top_id and top_logprob go together");
+  if (top_id_dev && s->cfg.top_k == 0) return op_fail(INFS_E_ARG, "alternatives need a scorer with top_k > 0");
+  if (misaligned({tokens_dev, logprob_dev, entropy_dev, top_id_dev, top_logprob_dev}, 4) || misaligned({stats_dev}, 8))
+    return op_fail(INFS_E_ARG, "tokens and outputs must be aligned to 4 bytes (stats: 8)");
+  if (s->dry || rows == 0) return INFS_OK;
+  infs::ScoreArgs a{logits_dev, row_stride, tokens_dev, logprob_dev, entropy_dev, top_id_dev, top_logprob_dev, stats_dev,
+                    rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t};
+  infs::StreamDevice dev(s->stream);
+  hipError_t e = dev.status();
+  if (e == hipSuccess) e = infs::launch_score(a, s->bf16, s->stream);
+  return e == hipSuccess ? INFS_OK : op_fail(INFS_E_DEVICE, "scoring failed: %s", hipGetErrorString(e));
+}
+
+infs_status infs_score_grad(infs_scorer* s, int32_t rows, const void* logits_dev, int64_t row_stride,
+                            const int32_t* tokens_dev, const float* stats_dev, const float* entropy_dev,
+                            const float* d_logprob_dev, const float* d_entropy_dev, void* grad_dev,
+                            int64_t grad_row_stride) {
+  if (!s) return op_fail(INFS_E_ARG, "null scorer");
+  infs_status st = check_rows(s, rows, logits_dev, &row_stride, "logits");
+  if (st == INFS_OK) st = check_rows(s, rows, grad_dev, &grad_row_stride, "grad");
+  if (st != INFS_OK) return st;
+  if (d_logprob_dev && !tokens_dev) return op_fail(INFS_E_ARG, "d_logprob needs tokens");
+  if (d_entropy_dev && !entropy_dev) return op_fail(INFS_E_ARG, "d_entropy needs entropy");
+  if (rows > 0 && !s->dry && !stats_dev) return op_fail(INFS_E_ARG, "null stats");
+  if (logits_dev && grad_dev == logits_dev && rows > 1 && row_stride != grad_row_stride)
+    return op_fail(INFS_E_ARG, "a gradient over the logits needs their row stride");
+  if (misaligned({tokens_dev, entropy_dev, d_logprob_dev, d_entropy_dev}, 4) || misaligned({stats_dev}, 8))
+    return op_fail(INFS_E_ARG, "tokens and gradients must be aligned to 4 bytes (stats: 8)");
+  if (s->dry || rows == 0) return INFS_OK;
+  infs::ScoreGradArgs a{logits_dev, grad_dev, row_stride, grad_row_stride, d_logprob_dev ? tokens_dev : nullptr, stats_dev,
+                        d_entropy_dev ? entropy_dev : nullptr, d_logprob_dev, d_entropy_dev, rows, s->cfg.vocab, s->inv_t};
+  infs::StreamDevice dev(s->stream);
+  hipError_t e = dev.status();
+  if (e == hipSuccess) e = infs::launch_score_grad(a, s->bf16, s->stream);
+  return e == hipSuccess ? INFS_OK : op_fail(INFS_E_DEVICE, "the gradient of scores failed: %s", hipGetErrorString(e));
 }
 
 }  // extern "C"

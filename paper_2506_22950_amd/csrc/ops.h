@@ -79,4 +79,34 @@ infs_status pack_rotary_rows(const infs_rows* r, const char* what, int head_dim,
 // The configuration's part of the launch arguments.
 void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a);
 
+// ---- scores of tokens -----------------------------------------------------------
+struct ScoreArgs {
+  const void* logits;
+  int64_t row_stride;  // elements
+  const int32_t* tokens;
+  float* logprob;      // [rows]; these five may be null
+  float* entropy;      // [rows]
+  int32_t* top_id;     // [rows, top_k]
+  float* top_logprob;  // [rows, top_k]
+  float* stats;        // [rows, 2]
+  int32_t rows, vocab, top_k;
+  float inv_t;         // 1 / temperature
+};
+
+struct ScoreGradArgs {
+  const void* logits;
+  void* grad;
+  int64_t row_stride, grad_row_stride;
+  const int32_t* tokens;     // null where d_logprob is
+  const float* stats;
+  const float* entropy;      // null where d_entropy is
+  const float* d_logprob;
+  const float* d_entropy;
+  int32_t rows, vocab;
+  float inv_t;
+};
+
+hipError_t launch_score(const ScoreArgs& args, bool bf16, hipStream_t stream);
+hipError_t launch_score_grad(const ScoreGradArgs& args, bool bf16, hipStream_t stream);
+
 }  // namespace infs

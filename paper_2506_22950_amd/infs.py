@@ -28,6 +28,7 @@ FPTAS_EPSILON = 0.1
 FLAG_DRY_RUN = 1
 FLAG_KV_FP8 = 2
 STATIC_SCRATCH_BYTES = 16 << 20
+SCORE_MAX_TOP = 32
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_NONE, ROTARY_LINEAR, ROTARY_NTK, ROTARY_YARN, ROTARY_BANDS = 0, 1, 2, 3, 4
 
@@ -43,7 +44,8 @@ EXPORTS = (
     "infs_sched_optimum", "infs_decode_step_layers", "infs_step_launch_workgroups", "infs_set_step_split",
     "infs_step_split_plan", "infs_step_launch_plan", "infs_probe_step_layers",
     "infs_rotary_create", "infs_rotary_destroy", "infs_rotary_frequencies", "infs_rotate_rows",
-    "infs_rotate_step", "infs_rotate_probe",
+    "infs_rotate_step", "infs_rotate_probe", "infs_scorer_create", "infs_scorer_destroy", "infs_score_tokens",
+    "infs_score_grad",
 )
 
 
@@ -80,6 +82,11 @@ class Rows(ctypes.Structure):
     _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("heads", ctypes.c_int32),
                 ("in_row", ctypes.c_int64), ("in_head", ctypes.c_int64), ("in_layer", ctypes.c_int64),
                 ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64), ("out_layer", ctypes.c_int64)]
+
+
+class ScorerConfig(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("top_k", ctypes.c_int32), ("temperature", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 class Stats(ctypes.Structure):
@@ -153,6 +160,10 @@ def load():
         "infs_rotate_step": (I32, [P, P, I32, ctypes.POINTER(Rows), ctypes.POINTER(Rows)]),
         "infs_rotate_probe": (I32, [P, P, I32, I32, I32, ctypes.POINTER(ctypes.c_uint8), I32, ctypes.POINTER(Rows),
                                     ctypes.POINTER(Rows)]),
+        "infs_scorer_create": (I32, [ctypes.POINTER(ScorerConfig), P, ctypes.POINTER(P)]),
+        "infs_scorer_destroy": (None, [P]),
+        "infs_score_tokens": (I32, [P, I32, P, I64, P, P, P, P, P, P]),
+        "infs_score_grad": (I32, [P, I32, P, I64, P, P, P, P, P, P, I64]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -239,6 +250,47 @@ class Rotary:
             if self._h:
                 load().infs_rotary_destroy(self._h)
                 self._h = None
+        except Exception:
+            pass
+
+
+def make_scorer_config(**kw) -> ScorerConfig:
+    c = ScorerConfig()
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+class Scorer:
+    """One infs_scorer: scores of tokens and their gradient."""
+
+    def __init__(self, config: ScorerConfig, stream=None):
+        h = ctypes.c_void_p()
+        _check(None, load().infs_scorer_create(ctypes.byref(config), _stream(stream), ctypes.byref(h)))
+        self._h = h
+        self.config = config
+
+    def score(self, rows, logits, tokens=None, logprob=None, entropy=None, top_id=None, top_logprob=None, stats=None,
+              row_stride=0):
+        """infs_score_tokens."""
+        _check(None, load().infs_score_tokens(self._h, rows, _ptr(logits), row_stride, _ptr(tokens), _ptr(logprob),
+                                              _ptr(entropy), _ptr(top_id), _ptr(top_logprob), _ptr(stats)))
+
+    def grad(self, rows, logits, tokens, stats, d_logprob, grad, entropy=None, d_entropy=None, row_stride=0,
+             grad_row_stride=0):
+        """infs_score_grad."""
+        _check(None, load().infs_score_grad(self._h, rows, _ptr(logits), row_stride, _ptr(tokens), _ptr(stats),
+                                            _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(grad),
+                                            grad_row_stride))
+
+    def destroy(self):
+        if self._h:
+            load().infs_scorer_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
         except Exception:
             pass
 

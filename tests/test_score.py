@@ -1,0 +1,85 @@
+"""Scores of tokens, host side: every refusal (dry-run scorers: no GPU needed)."""
+
+import math
+
+import pytest
+
+from paper_2506_22950_amd import infs
+
+AT = 0x10000  # an address that no refused and no dry-run call reads
+
+
+def config(**over):
+    c = dict(vocab=1000, dtype=infs.BF16, max_rows=16, top_k=4, temperature=1.0, flags=infs.FLAG_DRY_RUN)
+    c.update(over)
+    return infs.make_scorer_config(**c)
+
+
+def status(call, *a, **kw):
+    try:
+        call(*a, **kw)
+        return infs.OK
+    except infs.InfsError as e:
+        assert e.status == infs.OK or not str(e).endswith("no error")
+        return e.status
+
+
+@pytest.mark.parametrize("over", [
+    {"vocab": 0}, {"vocab": (1 << 24) + 1}, {"dtype": 2}, {"max_rows": 0}, {"max_rows": (1 << 24) + 1}, {"top_k": -1},
+    {"top_k": infs.SCORE_MAX_TOP + 1}, {"temperature": -1.0}, {"temperature": math.nan}, {"temperature": math.inf},
+    {"temperature": 2.0 ** -21}, {"temperature": 2.0 ** 21}, {"flags": 2}, {"flags": 4}])
+def test_config_refusals(over):
+    assert status(infs.Scorer, config(**over)) == infs.E_ARG
+
+
+def test_config_limits_are_allowed():
+    for over in ({"vocab": 1}, {"vocab": 1 << 24}, {"max_rows": 1 << 24}, {"top_k": 0}, {"top_k": 32},
+                 {"temperature": 0.0}, {"temperature": 2.0 ** -20}, {"temperature": 2.0 ** 20}):
+        infs.Scorer(config(**over)).destroy()
+
+
+@pytest.mark.parametrize("kw,ok", [
+    ({}, True), ({"rows": 0, "logits": None}, True), ({"row_stride": 1000}, True), ({"row_stride": 1001}, True),
+    ({"tokens": None, "logprob": None}, True), ({"top_id": None, "top_logprob": None}, True),
+    ({"entropy": None, "stats": None}, True),
+    ({"rows": -1}, False), ({"rows": 17}, False), ({"row_stride": 999}, False), ({"row_stride": -5}, False),
+    ({"row_stride": (1 << 40) + 1}, False), ({"logits": AT + 1}, False), ({"tokens": None}, False),
+    ({"logprob": None}, False), ({"top_id": None}, False), ({"top_logprob": None}, False), ({"tokens": AT + 2}, False),
+    ({"logprob": AT + 1}, False), ({"entropy": AT + 2}, False), ({"top_id": AT + 3}, False),
+    ({"top_logprob": AT + 2}, False), ({"stats": AT + 4}, False)])
+def test_score_refusals(kw, ok):
+    s = infs.Scorer(config())
+    args = dict(rows=16, logits=AT, tokens=AT, logprob=AT, entropy=AT, top_id=AT, top_logprob=AT, stats=AT, row_stride=0)
+    args.update(kw)
+    assert status(s.score, args.pop("rows"), args.pop("logits"), **args) == (infs.OK if ok else infs.E_ARG)
+
+
+def test_alternatives_need_top_k():
+    s = infs.Scorer(config(top_k=0))
+    assert status(s.score, 1, AT, AT, AT) == infs.OK
+    assert status(s.score, 1, AT, AT, AT, top_id=AT, top_logprob=AT) == infs.E_ARG
+
+
+@pytest.mark.parametrize("kw,ok", [
+    ({}, True), ({"d_logprob": None, "tokens": None}, True), ({"d_entropy": None, "entropy": None}, True),
+    ({"grad": AT, "logits": AT}, True), ({"rows": 0, "stats": AT, "grad": None}, True),
+    ({"grad": AT, "logits": AT, "row_stride": 1001, "grad_row_stride": 1001}, True),
+    ({"grad": AT, "logits": AT, "row_stride": 1001}, False), ({"tokens": None}, False), ({"entropy": None}, False),
+    ({"rows": 17}, False), ({"rows": -1}, False), ({"row_stride": 12}, False), ({"grad_row_stride": 12}, False),
+    ({"grad": AT + 1}, False), ({"logits": AT + 1}, False), ({"stats": AT + 4}, False), ({"tokens": AT + 1}, False),
+    ({"entropy": AT + 2}, False), ({"d_logprob": AT + 2}, False), ({"d_entropy": AT + 2}, False)])
+def test_grad_refusals(kw, ok):
+    s = infs.Scorer(config())
+    args = dict(rows=16, logits=AT, tokens=AT, stats=AT, d_logprob=AT, grad=AT + 64, entropy=AT, d_entropy=AT,
+                row_stride=0, grad_row_stride=0)
+    args.update(kw)
+    assert status(s.grad, *(args.pop(n) for n in ("rows", "logits", "tokens", "stats", "d_logprob", "grad")),
+                  **args) == (infs.OK if ok else infs.E_ARG)
+
+
+def test_null_scorer():
+    s = infs.Scorer(config())
+    s.destroy()
+    assert status(s.score, 1, AT, AT, AT) == infs.E_ARG
+    assert status(s.grad, 1, AT, AT, AT, AT, AT) == infs.E_ARG
+    s.destroy()
