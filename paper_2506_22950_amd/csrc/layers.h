@@ -192,6 +192,11 @@ __device__ __forceinline__ void wave_compute(const Addr& ad, int t0, int t1, con
           s[x][r] = ok ? y : NEG_INF;
         }
       }
+      if (base + (b + 1) * SB * TPI > t1) {  // the range ends inside: clear V (0 * whatever is there must be 0)
+#pragma unroll
+        for (int u = b * SB; u < b * SB + SB; ++u)
+          if (base + u * TPI + ts >= t1) R.vv[u] = u32x4{0, 0, 0, 0};
+      }
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         float mb = s[0][r];
