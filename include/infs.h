@@ -413,6 +413,37 @@ infs_status infs_timing_end(infs_ctx* ctx, double* kernel_ms, double* region_ms,
 const char* infs_last_error(const infs_ctx* ctx);
 
 /* ---------------------------------------------------------------------------------------------
+ * Responses' pages as a whole: fork, hand out, take in (next to infs_refill_slot and infs_retire_slot; the
+ * sample-level cache life cycle of Section 3.2).  All layers in one call, up to 64 responses at once, on the
+ * context's stream; nothing is allocated.  Dense rows of a response are [len, Hkv, head_dim] per layer in the
+ * context dtype, as infs_prefill_shared takes a prompt's; layer l at + l * layer_stride bytes (0: the rows of
+ * that response; else a multiple of 16, at least the longest response's rows; responses of one call share it).
+ * E_ARG: n outside [0, 64], null or misaligned arrays and buffers, slots or samples out of range or twice in one
+ * call.  E_STATE: a step is open, a source slot is empty, a slot to fill is live, or the sample has probe tokens.
+ * E_DUP: the sample was already dispatched.  E_CAPACITY: too few free pages, or a len above max_suffix_len.
+ * An error changes nothing.  Tokens taken in or shared are not counted by infs_sample_tokens.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Branches of live samples: empty slot dst_slots[i] becomes live with sample_ids[i] (of its prompt, which must be
+   that of src_slots[i]) and the first lens[i] response tokens of src_slots[i] (0 .. its length; lens NULL: all).
+   Full pages are shared and return to the pool with their last holder; a part of a page is copied.  Each goes on
+   at its own next token.  A source may appear several times. */
+infs_status infs_fork_slots(infs_ctx* ctx, int32_t n, const int32_t* src_slots, const int32_t* dst_slots,
+                            const int64_t* sample_ids, const int32_t* lens);
+
+/* Write the response K/V of live slots as dense rows to k_dev[i], v_dev[i] (device pointers, 16-byte aligned),
+   widened exactly where the cache is E4M3: on the device what infs_read_response is on the host. */
+infs_status infs_export_responses(infs_ctx* ctx, int32_t n, const int32_t* slots, void* const* k_dev,
+                                  void* const* v_dev, int64_t layer_stride);
+
+/* Empty slot slots[i] becomes live with sample_ids[i] of its prompt and a response of lens[i] tokens (0 ..
+   max_suffix_len) given as dense rows: a partial response of an earlier iteration, or of another context.  An E4M3
+   cache rounds them as infs_decode_step does.  The sample decodes its next token at the next step. */
+infs_status infs_import_responses(infs_ctx* ctx, int32_t n, const int32_t* slots, const int64_t* sample_ids,
+                                  const int32_t* lens, const void* const* k_dev, const void* const* v_dev,
+                                  int64_t layer_stride);
+
+/* ---------------------------------------------------------------------------------------------
  * Rotary positions on rows of Q and K: what a model applies between its projections and
  * infs_prefill_shared / infs_decode_step / infs_probe_step, which take rows as they are to be attended.
  * A pair (a, b) of elements of a head at position p turns by the angle t = p * f_j of its pair j:

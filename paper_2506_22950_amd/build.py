@@ -24,7 +24,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 # (inst_*.hip) that compile in parallel; the device code is in decode.h.
 SOURCES = ["kernels.hip", "inst_wave_f32_d64.hip", "inst_wave_f32_d128.hip", "inst_wave_bf16_d64.hip",
            "inst_wave_bf16_d128.hip", "inst_mfma_d64.hip", "inst_mfma_d128a.hip", "inst_mfma_d128b.hip",
-           "inst_kv8a.hip", "inst_kv8b.hip", "scratch.hip", "rotary.hip", "score.hip", "runtime.cpp", "sched.cpp", "ops.cpp"]
+           "inst_kv8a.hip", "inst_kv8b.hip", "scratch.hip", "rotary.hip", "score.hip", "pages.hip", "runtime.cpp", "sched.cpp", "ops.cpp"]
 CALIB_SOURCES = ["calib.hip"]
 
 

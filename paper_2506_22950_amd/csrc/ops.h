@@ -1,4 +1,5 @@
-// Launch entry points of the row and page operators (rotary.hip), and the
+// Launch entry points of the row and page operators (rotary.hip, score.hip,
+// pages.hip), and the
 // error and device helpers their host code shares.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -108,5 +109,55 @@ struct ScoreGradArgs {
 
 hipError_t launch_score(const ScoreArgs& args, bool bf16, hipStream_t stream);
 hipError_t launch_score_grad(const ScoreGradArgs& args, bool bf16, hipStream_t stream);
+
+// ---- responses' pages -----------------------------------------------------------
+struct ForkArgs {
+  char* pool;
+  int64_t layer_bytes, page_bytes;  // of the pool's layers, of a page (all KV heads, K and V)
+  int32_t* page_table;
+  int32_t pages_per_slot, n;
+  struct Fork {
+    int32_t src_seq, dst_seq;  // page-table rows
+    int32_t full;              // pages shared
+    int32_t src_page, dst_page;  // a part of a page is copied (dst_page >= 0)
+  } fork[kMaxSlots];
+};
+static_assert(sizeof(ForkArgs) <= 4096, "kernel argument block must fit 4 KiB");
+
+// Runs of pages to write into the page table.
+constexpr int kRunsPerLaunch = 300;
+struct PageRuns {
+  int32_t* page_table;
+  int32_t n;
+  struct Run {
+    int32_t at, page, count;  // entries at .. at+count-1 become page, page+1, ...
+  } run[kRunsPerLaunch];
+};
+static_assert(sizeof(PageRuns) <= 4096, "kernel argument block must fit 4 KiB");
+
+// Dense rows <-> pages of several responses.
+struct MoveArgs {
+  char* pool;
+  int64_t layer_bytes, layer_stride;  // layer_stride 0: a response's own rows
+  const int32_t* page_table;
+  int32_t pages_per_slot, hkv, n;
+  struct Response {
+    char *k, *v;
+    int32_t seq, len;
+    int32_t first_block, pad_;  // first work-group of the response in a layer
+  } r[kMaxSlots];
+};
+static_assert(sizeof(MoveArgs) <= 4096, "kernel argument block must fit 4 KiB");
+
+// How responses lie in pages (KernelKey's bf16 and kv8, head_dim).
+struct PageFormat {
+  int bf16, kv8, head_dim;
+};
+
+hipError_t launch_fork(const ForkArgs& args, int layers, hipStream_t stream);
+hipError_t launch_page_runs(const PageRuns& args, hipStream_t stream);
+// Fills in first_block.
+hipError_t launch_export(const PageFormat& f, MoveArgs& args, int layers, hipStream_t stream);
+hipError_t launch_import(const PageFormat& f, MoveArgs& args, int layers, hipStream_t stream);
 
 }  // namespace infs

@@ -84,6 +84,7 @@ struct infs_ctx {
   std::vector<int32_t> slot_handle;                // -1: empty slot
   std::vector<std::vector<int32_t>> seq_pages;     // host copy of each handle's page list
   std::priority_queue<int32_t, std::vector<int32_t>, std::greater<int32_t>> free_pages;
+  std::vector<int32_t> page_refs;                  // responses that hold a page (forks share full pages)
   std::vector<std::vector<uint8_t>> dispatched;    // [prompt][G]
   // Arrivals each slot's device counter has been sent so far (the same for
   // every KV head): its response chunks and its prompt's prefix chunks.
@@ -173,6 +174,17 @@ infs_status device_fail(infs_ctx* c, hipError_t e, const char* what) {
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// A page out of the pool, and a holder's return of one.
+int32_t take_page(infs_ctx* c) {
+  const int32_t pg = c->free_pages.top();
+  c->free_pages.pop();
+  c->page_refs[pg] = 1;
+  return pg;
+}
+void drop_page(infs_ctx* c, int32_t pg) {
+  if (--c->page_refs[pg] == 0) c->free_pages.push(pg);
+}
+
 void free_device(infs_ctx* c) {
   if (c->dry) return;
   (void)hipFree(c->prefix);
@@ -228,6 +240,7 @@ void reset_host(infs_ctx* c) {
   c->seq_pages.assign(c->H, {});
   c->free_pages = {};
   for (int i = 0; i < c->num_pages; ++i) c->free_pages.push(i);
+  c->page_refs.assign(c->num_pages, 0);
   c->dispatched.assign(c->NP, std::vector<uint8_t>(c->G, 0));
   c->slot_arrivals.assign(c->S, 0);
   c->merged_arrivals.assign(c->NP, 0);
@@ -310,8 +323,7 @@ infs_status open_step(infs_ctx* c) {
     const int pos = len - 1;
     const int h = c->slot_handle[s];
     if (pos % infs::kPageTokens == 0) {
-      c->seq_pages[h].push_back(c->free_pages.top());
-      c->free_pages.pop();
+      c->seq_pages[h].push_back(take_page(c));
     }
     a.live_slot[lives++] = (int8_t)s;
     sp.len = len;
@@ -392,8 +404,7 @@ infs_status open_probe(infs_ctx* c, int p, int first, int n, const uint8_t* live
     const int i = first + j, h = p * c->G + i;
     const int len = c->probe_len[p][i] + 1, pos = len - 1;
     if (pos % infs::kPageTokens == 0) {
-      c->seq_pages[h].push_back(c->free_pages.top());
-      c->free_pages.pop();
+      c->seq_pages[h].push_back(take_page(c));
     }
     a.live_slot[lives++] = (int8_t)j;
     sp.len = len;
@@ -835,7 +846,7 @@ infs_status infs_retire_slot(infs_ctx* c, int32_t slot) {
   if (c->step_open) return fail(c, INFS_E_STATE, "retire while a step is open");
   if (c->slot_sample[slot] < 0) return fail(c, INFS_E_STATE, "slot %d is empty", slot);
   std::vector<int32_t>& pages = c->seq_pages[c->slot_handle[slot]];
-  for (int32_t pg : pages) c->free_pages.push(pg);
+  for (int32_t pg : pages) drop_page(c, pg);
   pages.clear();
   c->slot_sample[slot] = -1;
   c->slot_len[slot] = 0;
@@ -855,7 +866,7 @@ infs_status infs_release_sample(infs_ctx* c, int32_t prompt, int64_t sample_id) 
                 prompt);
   c->dispatched[prompt][sample_id] = 1;
   std::vector<int32_t>& pages = c->seq_pages[prompt * c->G + (int32_t)sample_id];
-  for (int32_t pg : pages) c->free_pages.push(pg);
+  for (int32_t pg : pages) drop_page(c, pg);
   pages.clear();
   return INFS_OK;
 }
@@ -1601,6 +1612,211 @@ infs_status infs_rotate_probe(infs_ctx* c, const infs_rotary* r, int32_t prompt,
     pos[j] = c->plen[prompt] + c->probe_len[prompt][first_sample + j];
   }
   return rotate_slots(c, r, num_layers, q, k, n, live, pos);
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int kMaxMoved = infs::kMaxSlots;  // responses of one call
+
+// Checks of the calls that work on several responses: n and its arrays, no step open.
+infs_status check_many(infs_ctx* c, int n, bool arrays) {
+  if (n < 0 || n > kMaxMoved) return fail(c, INFS_E_ARG, "n must be in [0, %d]", kMaxMoved);
+  if (n > 0 && !arrays) return fail(c, INFS_E_ARG, "null array");
+  if (c->step_open || c->probe_open) return fail(c, INFS_E_STATE, "responses are moved between steps");
+  return INFS_OK;
+}
+
+// The slots to fill and their samples: distinct, empty, not dispatched, without probe tokens.
+infs_status check_targets(infs_ctx* c, int n, const int32_t* slots, const int64_t* samples) {
+  for (int i = 0; i < n; ++i) {
+    const int s = slots[i];
+    if (s < 0 || s >= c->S) return fail(c, INFS_E_ARG, "slot %d out of range [0, %d)", s, c->S);
+    if (samples[i] < 0 || samples[i] >= c->G)
+      return fail(c, INFS_E_ARG, "sample_id %lld out of range [0, %d)", (long long)samples[i], c->G);
+    for (int j = 0; j < i; ++j) {
+      if (slots[j] == s) return fail(c, INFS_E_ARG, "slot %d twice in one call", s);
+      if (slots[j] / c->m == s / c->m && samples[j] == samples[i])
+        return fail(c, INFS_E_ARG, "sample %lld twice in one call", (long long)samples[i]);
+    }
+    const int p = s / c->m;
+    if (c->slot_sample[s] >= 0) return fail(c, INFS_E_STATE, "slot %d is live", s);
+    if (c->dispatched[p][samples[i]])
+      return fail(c, INFS_E_DUP, "sample %lld of prompt %d was already dispatched", (long long)samples[i], p);
+    if (c->probe_k > 0 && c->probe_len[p][samples[i]] > 0)
+      return fail(c, INFS_E_STATE, "sample %lld of prompt %d has probe tokens", (long long)samples[i], p);
+  }
+  return INFS_OK;
+}
+
+// The page-table row of a sample about to fill a slot.
+int handle_of(const infs_ctx* c, int slot, int64_t sample) {
+  return c->probe_k > 0 ? slot / c->m * c->G + (int)sample : slot;
+}
+
+void fill_slot(infs_ctx* c, int slot, int64_t sample, int len) {
+  c->dispatched[slot / c->m][sample] = 1;
+  c->slot_sample[slot] = sample;
+  c->slot_handle[slot] = handle_of(c, slot, sample);
+  c->slot_len[slot] = len;
+}
+
+// Dense rows of n responses of len[i] tokens: pointers, alignment, layer stride.
+infs_status check_dense(infs_ctx* c, int n, const int32_t* len, const void* const* k, const void* const* v, int64_t stride) {
+  const int64_t row = (int64_t)c->Hkv * c->D * (int64_t)c->es;
+  if (stride < 0 || stride % 16) return fail(c, INFS_E_ARG, "layer_stride must be 0 or a positive multiple of 16 bytes");
+  for (int i = 0; i < n; ++i) {
+    if (len[i] == 0) continue;
+    if (stride && c->L > 1 && stride < len[i] * row)
+      return fail(c, INFS_E_ARG, "layer_stride below the %lld bytes of a response of %d tokens", (long long)(len[i] * row), len[i]);
+    if (c->dry) continue;
+    if (!k[i] || !v[i]) return fail(c, INFS_E_ARG, "null K/V pointer");
+    if (((uintptr_t)k[i] | (uintptr_t)v[i]) & 15) return fail(c, INFS_E_ARG, "K/V must be 16-byte aligned");
+  }
+  return INFS_OK;
+}
+
+infs::MoveArgs move_args(const infs_ctx* c, int n, const int32_t* slots, const int32_t* len, const void* const* k,
+                         const void* const* v, int64_t stride) {
+  infs::MoveArgs a{};
+  a.pool = c->pool;
+  a.layer_bytes = (int64_t)c->pool_layer_bytes;
+  a.layer_stride = stride;
+  a.page_table = c->page_table;
+  a.pages_per_slot = c->pages_per_slot;
+  a.hkv = c->Hkv;
+  a.n = n;
+  for (int i = 0; i < n; ++i)
+    a.r[i] = {const_cast<char*>((const char*)k[i]), const_cast<char*>((const char*)v[i]), c->slot_handle[slots[i]], len[i],
+              0, 0};
+  return a;
+}
+
+infs::PageFormat page_format(const infs_ctx* c) { return {c->key.bf16, c->key.kv8, c->D}; }
+
+}  // namespace
+
+extern "C" {
+
+infs_status infs_fork_slots(infs_ctx* c, int32_t n, const int32_t* src_slots, const int32_t* dst_slots,
+                            const int64_t* sample_ids, const int32_t* lens) {
+  CHECK_CTX(c);
+  infs_status st = check_many(c, n, src_slots && dst_slots && sample_ids);
+  if (st == INFS_OK) st = check_targets(c, n, dst_slots, sample_ids);
+  if (st != INFS_OK) return st;
+  size_t need = 0;
+  int32_t keep[kMaxMoved];
+  for (int i = 0; i < n; ++i) {
+    const int s = src_slots[i];
+    if (s < 0 || s >= c->S) return fail(c, INFS_E_ARG, "slot %d out of range [0, %d)", s, c->S);
+    if (s / c->m != dst_slots[i] / c->m)
+      return fail(c, INFS_E_ARG, "slots %d and %d serve different prompts", s, dst_slots[i]);
+    if (c->slot_sample[s] < 0) return fail(c, INFS_E_STATE, "slot %d is empty", s);
+    keep[i] = lens ? lens[i] : c->slot_len[s];
+    if (keep[i] < 0 || keep[i] > c->slot_len[s])
+      return fail(c, INFS_E_ARG, "len %d out of range [0, %d] of slot %d", keep[i], c->slot_len[s], s);
+    need += keep[i] % infs::kPageTokens != 0;
+  }
+  if (need > c->free_pages.size())
+    return fail(c, INFS_E_CAPACITY, "page pool exhausted: need %zu pages, %zu free", need, c->free_pages.size());
+  try {
+    for (int i = 0; i < n; ++i)
+      c->seq_pages[handle_of(c, dst_slots[i], sample_ids[i])].reserve(ceil_div(keep[i], infs::kPageTokens));
+  } catch (const std::bad_alloc&) {
+    return fail(c, INFS_E_NOMEM, "host allocation failed");
+  }
+  infs::ForkArgs a{};
+  a.pool = c->pool;
+  a.layer_bytes = (int64_t)c->pool_layer_bytes;
+  a.page_bytes = (int64_t)c->Hkv * 2 * infs::kPageTokens * c->D * (int64_t)c->kv_es;
+  a.page_table = c->page_table;
+  a.pages_per_slot = c->pages_per_slot;
+  for (int i = 0; i < n; ++i) {
+    const int src = c->slot_handle[src_slots[i]], dst = handle_of(c, dst_slots[i], sample_ids[i]);
+    const int full = keep[i] / infs::kPageTokens;
+    const std::vector<int32_t>& from = c->seq_pages[src];
+    std::vector<int32_t>& to = c->seq_pages[dst];
+    for (int j = 0; j < full; ++j) {
+      ++c->page_refs[from[j]];
+      to.push_back(from[j]);
+    }
+    int32_t part = -1;
+    if (keep[i] % infs::kPageTokens) to.push_back(part = take_page(c));
+    fill_slot(c, dst_slots[i], sample_ids[i], keep[i]);
+    if (keep[i] > 0) a.fork[a.n++] = {src, dst, full, part >= 0 ? from[full] : 0, part};
+  }
+  if (!c->dry) HIP_TRY(c, infs::launch_fork(a, c->L, c->stream));
+  return INFS_OK;
+}
+
+infs_status infs_export_responses(infs_ctx* c, int32_t n, const int32_t* slots, void* const* k_dev, void* const* v_dev,
+                                  int64_t layer_stride) {
+  CHECK_CTX(c);
+  infs_status st = check_many(c, n, slots && k_dev && v_dev);
+  if (st != INFS_OK) return st;
+  int32_t len[kMaxMoved];
+  for (int i = 0; i < n; ++i) {
+    if (slots[i] < 0 || slots[i] >= c->S) return fail(c, INFS_E_ARG, "slot %d out of range [0, %d)", slots[i], c->S);
+    if (c->slot_sample[slots[i]] < 0) return fail(c, INFS_E_STATE, "slot %d is empty", slots[i]);
+    len[i] = c->slot_len[slots[i]];
+  }
+  st = check_dense(c, n, len, k_dev, v_dev, layer_stride);
+  if (st != INFS_OK || c->dry) return st;
+  infs::MoveArgs a = move_args(c, n, slots, len, k_dev, v_dev, layer_stride);
+  HIP_TRY(c, infs::launch_export(page_format(c), a, c->L, c->stream));
+  return INFS_OK;
+}
+
+infs_status infs_import_responses(infs_ctx* c, int32_t n, const int32_t* slots, const int64_t* sample_ids,
+                                  const int32_t* lens, const void* const* k_dev, const void* const* v_dev,
+                                  int64_t layer_stride) {
+  CHECK_CTX(c);
+  infs_status st = check_many(c, n, slots && sample_ids && lens && k_dev && v_dev);
+  if (st == INFS_OK) st = check_targets(c, n, slots, sample_ids);
+  if (st != INFS_OK) return st;
+  size_t need = 0;
+  for (int i = 0; i < n; ++i) {
+    if (lens[i] < 0) return fail(c, INFS_E_ARG, "negative len");
+    if (lens[i] > c->cfg.max_suffix_len)
+      return fail(c, INFS_E_CAPACITY, "a response of %d tokens exceeds max_suffix_len=%d", lens[i], c->cfg.max_suffix_len);
+    need += ceil_div(lens[i], infs::kPageTokens);
+  }
+  st = check_dense(c, n, lens, k_dev, v_dev, layer_stride);
+  if (st != INFS_OK) return st;
+  if (need > c->free_pages.size())
+    return fail(c, INFS_E_CAPACITY, "page pool exhausted: need %zu pages, %zu free", need, c->free_pages.size());
+  try {
+    for (int i = 0; i < n; ++i)
+      c->seq_pages[handle_of(c, slots[i], sample_ids[i])].reserve(ceil_div(lens[i], infs::kPageTokens));
+  } catch (const std::bad_alloc&) {
+    return fail(c, INFS_E_NOMEM, "host allocation failed");
+  }
+  infs::PageRuns runs;
+  runs.page_table = c->page_table;
+  runs.n = 0;
+  for (int i = 0; i < n; ++i) {
+    const int h = handle_of(c, slots[i], sample_ids[i]);
+    std::vector<int32_t>& pages = c->seq_pages[h];
+    for (int j = 0; j < ceil_div(lens[i], infs::kPageTokens); ++j) {
+      pages.push_back(take_page(c));
+      if (j > 0 && runs.n > 0 && pages[j] == pages[j - 1] + 1) {
+        ++runs.run[runs.n - 1].count;
+        continue;
+      }
+      if (runs.n == infs::kRunsPerLaunch) {
+        if (!c->dry) HIP_TRY(c, infs::launch_page_runs(runs, c->stream));
+        runs.n = 0;
+      }
+      runs.run[runs.n++] = {h * c->pages_per_slot + j, pages[j], 1};
+    }
+    fill_slot(c, slots[i], sample_ids[i], lens[i]);
+  }
+  if (c->dry) return INFS_OK;
+  HIP_TRY(c, infs::launch_page_runs(runs, c->stream));
+  infs::MoveArgs a = move_args(c, n, slots, lens, k_dev, v_dev, layer_stride);
+  HIP_TRY(c, infs::launch_import(page_format(c), a, c->L, c->stream));
+  return INFS_OK;
 }
 
 }  // extern "C"

@@ -45,7 +45,7 @@ EXPORTS = (
     "infs_step_split_plan", "infs_step_launch_plan", "infs_probe_step_layers",
     "infs_rotary_create", "infs_rotary_destroy", "infs_rotary_frequencies", "infs_rotate_rows",
     "infs_rotate_step", "infs_rotate_probe", "infs_scorer_create", "infs_scorer_destroy", "infs_score_tokens",
-    "infs_score_grad",
+    "infs_score_grad", "infs_fork_slots", "infs_export_responses", "infs_import_responses",
 )
 
 
@@ -163,6 +163,11 @@ def load():
         "infs_scorer_create": (I32, [ctypes.POINTER(ScorerConfig), P, ctypes.POINTER(P)]),
         "infs_scorer_destroy": (None, [P]),
         "infs_score_tokens": (I32, [P, I32, P, I64, P, P, P, P, P, P]),
+        "infs_fork_slots": (I32, [P, I32, ctypes.POINTER(I32), ctypes.POINTER(I32), ctypes.POINTER(I64),
+                                  ctypes.POINTER(I32)]),
+        "infs_export_responses": (I32, [P, I32, ctypes.POINTER(I32), ctypes.POINTER(P), ctypes.POINTER(P), I64]),
+        "infs_import_responses": (I32, [P, I32, ctypes.POINTER(I32), ctypes.POINTER(I64), ctypes.POINTER(I32),
+                                        ctypes.POINTER(P), ctypes.POINTER(P), I64]),
         "infs_score_grad": (I32, [P, I32, P, I64, P, P, P, P, P, P, I64]),
     }
     for name, (res, args) in sig.items():
@@ -330,6 +335,33 @@ class Context:
 
     def retire_slot(self, slot):
         self._call(load().infs_retire_slot, slot)
+
+    def fork_slots(self, src_slots, dst_slots, sample_ids, lens=None):
+        """Branches: dst slot i takes sample_ids[i] with the first lens[i] tokens (None: all) of src slot i."""
+        n = len(src_slots)
+        if not (len(dst_slots) == len(sample_ids) == n and (lens is None or len(lens) == n)):
+            raise ValueError("one destination, sample (and length) per source")
+        I32, I64 = ctypes.c_int32, ctypes.c_int64
+        self._call(load().infs_fork_slots, n, (I32 * n)(*src_slots), (I32 * n)(*dst_slots), (I64 * n)(*sample_ids),
+                   None if lens is None else (I32 * n)(*lens))
+
+    def export_responses(self, slots, k, v, layer_stride=0):
+        """Dense response rows of live slots: k[i], v[i] receive [layers, len, Hkv, d]."""
+        n = len(slots)
+        if not len(k) == len(v) == n:
+            raise ValueError("one K and one V buffer per slot")
+        P = ctypes.c_void_p
+        self._call(load().infs_export_responses, n, (ctypes.c_int32 * n)(*slots), (P * n)(*map(_ptr, k)),
+                   (P * n)(*map(_ptr, v)), layer_stride)
+
+    def import_responses(self, slots, sample_ids, lens, k, v, layer_stride=0):
+        """Empty slots take samples with responses of lens[i] tokens given as dense rows k[i], v[i]."""
+        n = len(slots)
+        if not len(sample_ids) == len(lens) == len(k) == len(v) == n:
+            raise ValueError("one sample, length, K and V buffer per slot")
+        I32, I64, P = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+        self._call(load().infs_import_responses, n, (I32 * n)(*slots), (I64 * n)(*sample_ids), (I32 * n)(*lens),
+                   (P * n)(*map(_ptr, k)), (P * n)(*map(_ptr, v)), layer_stride)
 
     def decode_step(self, layer, q, k_new, v_new, o):
         self._call(load().infs_decode_step, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o))
