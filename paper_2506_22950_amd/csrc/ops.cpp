@@ -57,6 +57,9 @@ struct infs_scorer {
   size_t es = 0;
   float inv_t = 1.f;
   hipStream_t stream = nullptr;
+  int device = 0;
+  // One allocation: arrived [kScoreMaxRecords], part [kScoreMaxRecords][3], keys [kScoreMaxRecords][top_k].
+  char* workspace = nullptr;
 };
 
 namespace {
@@ -69,6 +72,10 @@ infs_status check_rows(const infs_scorer* s, int32_t rows, const void* logits, i
   if (rows > 0 && !s->dry && !logits) return op_fail(INFS_E_ARG, "%s: null buffer", what);
   if ((uintptr_t)logits % s->es) return op_fail(INFS_E_ARG, "%s must be aligned to an element", what);
   return INFS_OK;
+}
+
+size_t workspace_bytes(const infs_scorer& s) {
+  return (sizeof(int32_t) + 3 * sizeof(float) + sizeof(unsigned long long) * s.cfg.top_k) * infs::kScoreMaxRecords;
 }
 
 bool misaligned(std::initializer_list<const void*> ptrs, size_t n) {
@@ -196,13 +203,30 @@ infs_status infs_scorer_create(const infs_scorer_config* cfg, void* hip_stream, 
   s->es = s->bf16 ? 2 : 4;
   s->inv_t = k.temperature != 0.f ? 1.f / k.temperature : 1.f;
   s->stream = (hipStream_t)hip_stream;
+  if (!s->dry) {
+    infs::StreamDevice dev(s->stream);
+    hipError_t e = dev.status();
+    if (e == hipSuccess) e = hipGetDevice(&s->device);
+    if (e == hipSuccess) e = hipMalloc((void**)&s->workspace, workspace_bytes(*s));
+    if (e == hipSuccess) e = hipMemset(s->workspace, 0, workspace_bytes(*s));
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);  // the stream need not wait for the null stream
+    if (e != hipSuccess) {
+      if (s->workspace) (void)hipFree(s->workspace);
+      delete s;
+      return op_fail(e == hipErrorOutOfMemory ? INFS_E_NOMEM : INFS_E_DEVICE, "a scorer's workspace: %s", hipGetErrorString(e));
+    }
+  }
   *out = s;
   return INFS_OK;
 }
 
 void infs_scorer_destroy(infs_scorer* s) {
   if (!s) return;
-  if (!s->dry) (void)hipStreamSynchronize(s->stream);
+  if (!s->dry) {
+    infs::StreamDevice dev(s->stream, s->device);
+    (void)hipStreamSynchronize(s->stream);
+    (void)hipFree(s->workspace);
+  }
   delete s;
 }
 
@@ -219,8 +243,12 @@ infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_d
     return op_fail(INFS_E_ARG, "tokens and outputs must be aligned to 4 bytes (stats: 8)");
   if (s->dry || rows == 0) return INFS_OK;
   infs::ScoreArgs a{logits_dev, row_stride, tokens_dev, logprob_dev, entropy_dev, top_id_dev, top_logprob_dev, stats_dev,
-                    rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t};
-  infs::StreamDevice dev(s->stream);
+                    rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t, 0, 0, nullptr, nullptr, nullptr};
+  char* ws = s->workspace;
+  a.arrived = (int32_t*)ws;
+  a.part = (float*)(ws + sizeof(int32_t) * infs::kScoreMaxRecords);
+  a.keys = (unsigned long long*)(ws + (sizeof(int32_t) + 3 * sizeof(float)) * infs::kScoreMaxRecords);
+  infs::StreamDevice dev(s->stream, s->device);
   hipError_t e = dev.status();
   if (e == hipSuccess) e = infs::launch_score(a, s->bf16, s->stream);
   return e == hipSuccess ? INFS_OK : op_fail(INFS_E_DEVICE, "scoring failed: %s", hipGetErrorString(e));
@@ -244,7 +272,7 @@ infs_status infs_score_grad(infs_scorer* s, int32_t rows, const void* logits_dev
   if (s->dry || rows == 0) return INFS_OK;
   infs::ScoreGradArgs a{logits_dev, grad_dev, row_stride, grad_row_stride, d_logprob_dev ? tokens_dev : nullptr, stats_dev,
                         d_entropy_dev ? entropy_dev : nullptr, d_logprob_dev, d_entropy_dev, rows, s->cfg.vocab, s->inv_t};
-  infs::StreamDevice dev(s->stream);
+  infs::StreamDevice dev(s->stream, s->device);
   hipError_t e = dev.status();
   if (e == hipSuccess) e = infs::launch_score_grad(a, s->bf16, s->stream);
   return e == hipSuccess ? INFS_OK : op_fail(INFS_E_DEVICE, "the gradient of scores failed: %s", hipGetErrorString(e));

@@ -21,14 +21,15 @@ namespace infs {
 // Records the message infs_last_error(NULL) gives on this thread; returns st.
 infs_status op_fail(infs_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 
-// Makes the device of `stream` current for its lifetime (the null stream: the current one stays).
+// Makes the device of `stream` current for its lifetime (the null stream: device `fallback`, or
+// the current one where that is -1).
 class StreamDevice {
  public:
-  explicit StreamDevice(hipStream_t stream) {
-    if (!stream) return;
-    int dev = 0;
+  explicit StreamDevice(hipStream_t stream, int fallback = -1) {
+    int dev = fallback;
+    if (!stream && dev < 0) return;
     status_ = hipGetDevice(&before_);
-    if (status_ == hipSuccess) status_ = hipStreamGetDevice(stream, &dev);
+    if (status_ == hipSuccess && stream) status_ = hipStreamGetDevice(stream, &dev);
     if (status_ == hipSuccess && dev != before_) {
       status_ = hipSetDevice(dev);
       changed_ = status_ == hipSuccess;
@@ -81,6 +82,9 @@ infs_status pack_rotary_rows(const infs_rows* r, const char* what, int head_dim,
 void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a);
 
 // ---- scores of tokens -----------------------------------------------------------
+constexpr int kScoreMaxPieces = 32;      // pieces of a row
+constexpr int kScoreWorkGroups = 1024;   // work-groups that the rows of a call are cut for
+
 struct ScoreArgs {
   const void* logits;
   int64_t row_stride;  // elements
@@ -92,7 +96,15 @@ struct ScoreArgs {
   float* stats;        // [rows, 2]
   int32_t rows, vocab, top_k;
   float inv_t;         // 1 / temperature
+  int32_t pieces, batches;  // pieces of a row, batches of a piece (plan_score)
+  // Where rows are cut (pieces > 1), per record row * pieces + piece: the part of a piece [3] and
+  // its best keys [top_k]; and the pieces of a row that have arrived (0 between launches).
+  float* part;
+  unsigned long long* keys;
+  int32_t* arrived;
 };
+// Rows are cut only where that leaves at most this many records.
+constexpr int kScoreMaxRecords = 2 * kScoreWorkGroups;
 
 struct ScoreGradArgs {
   const void* logits;
@@ -107,7 +119,8 @@ struct ScoreGradArgs {
   float inv_t;
 };
 
-hipError_t launch_score(const ScoreArgs& args, bool bf16, hipStream_t stream);
+// Fills in pieces and batches.
+hipError_t launch_score(ScoreArgs& args, bool bf16, hipStream_t stream);
 hipError_t launch_score_grad(const ScoreGradArgs& args, bool bf16, hipStream_t stream);
 
 // ---- responses' pages -----------------------------------------------------------

@@ -14,8 +14,12 @@
 
 #include <float.h>
 
+#include <algorithm>
+
 namespace infs {
 namespace {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int kThreads = 256;
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -60,39 +64,336 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
   return __uint_as_float((o >> 31) ? o & 0x7fffffffu : ~o);
 }
 
-// One work-group a row; every alternative is a pass of its own over the row.
+// ---- the forward pass ----------------------------------------------------------
+//
+// A row is read once, 16 bytes a lane and load.  Loads go by aligned vectors of
+// N elements: vector v covers elements v N - lead .. of the row, lead the elements
+// by which the row's start lies behind a 16-byte boundary; the first and the last
+// vector of a row may be in part outside it and are then read by elements, what is
+// outside counting as masked.  A work-group takes batches of kBatch vectors, kUnroll a
+// lane, every lane around its own running maximum.
+//
+// Few rows are cut into pieces of whole batches, a work-group each; the pieces of a
+// row are joined by the work-group that finishes last (see join_pieces), always in
+// the order of the pieces.
+constexpr int kUnroll = 4;
+constexpr int kBatch = kThreads * kUnroll;  // vectors
+constexpr int kMaxPieces = kScoreMaxPieces;
+constexpr int kWaveKeys = INFS_SCORE_MAX_TOP + 64 * 8;  // candidates a wavefront holds: one vector a lane beside the best
+constexpr int kKeptKeys = 64;                           // most it hands on
+constexpr int kFewLanes = 8;  // lanes with candidates in a batch that do not move the bound
+static_assert(INFS_SCORE_MAX_TOP <= kKeptKeys, "candidate buffers");
+static_assert(kMaxPieces <= 64 && kMaxPieces * INFS_SCORE_MAX_TOP <= kThreads / 64 * kWaveKeys, "joining pieces");
+
 template <bool BF>
-__global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
-  const int64_t row = blockIdx.x;
-  const char* z = (const char*)a.logits + row * a.row_stride * (BF ? 2 : 4);
-  const float c = a.inv_t * kLog2E;
-  Part p = empty_part();
-  for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-    const float x = load1<BF>(z, i), m = fmaxf(p.m, x);
-    const float y = (x - m) * c, d = fmaxf((p.m - m) * c, kFar), e = __builtin_amdgcn_exp2f(y), f = __builtin_amdgcn_exp2f(d);
-    p.w = (p.w + p.s * d) * f + e * fmaxf(y, kFar);
-    p.s = p.s * f + e;
-    p.m = m;
+struct Vec {
+  static constexpr int N = BF ? 8 : 4, ES = BF ? 2 : 4;
+  static __device__ __forceinline__ float get(const u32x4& v, int i) {
+    if constexpr (BF) {
+      const uint32_t w = v[i >> 1];
+      return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
+    } else {
+      return __uint_as_float(v[i]);
+    }
   }
-  __shared__ Part parts[kThreads];
-  __shared__ unsigned long long best[kThreads];
-  parts[threadIdx.x] = p;
+  static constexpr uint32_t kMasked = BF ? 0xff80ff80u : 0xff800000u;
+};
+
+// One row's vectors.
+template <bool BF>
+struct RowReader {
+  using V = Vec<BF>;
+  const char* at;     // vector 0
+  const char* row;    // element 0
+  int lead, vocab, count;  // elements before the row in vector 0; elements; vectors
+  int lo, hi;         // vectors wholly inside the row
+  __device__ RowReader(const void* logits, int64_t offset, int n) : vocab(n) {
+    row = (const char*)logits + offset * V::ES;
+    lead = (int)((uintptr_t)row / V::ES % V::N);
+    at = row - lead * V::ES;
+    count = (lead + n + V::N - 1) / V::N;
+    lo = lead > 0;
+    hi = (lead + n) / V::N;
+  }
+  // Vectors first + 256 u + thread of [first, end): all loads at once, each inside the row.
+  __device__ __forceinline__ void load(int first, int end, u32x4 (&x)[kUnroll]) const {
+    const int v0 = first + (int)threadIdx.x;
+    if (first >= lo && first + kBatch <= min(end, hi)) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) x[u] = *(const u32x4*)(at + (int64_t)(v0 + u * kThreads) * 16);
+      return;
+    }
+    if (lo < hi) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) x[u] = *(const u32x4*)(at + (int64_t)min(max(v0 + u * kThreads, lo), hi - 1) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int v = v0 + u * kThreads;
+      if (v >= lo && v < min(end, hi)) continue;
+      x[u] = u32x4{V::kMasked, V::kMasked, V::kMasked, V::kMasked};
+      if (v >= end) continue;
+      const int e0 = v * V::N - lead;
+      for (int e = max(e0, 0); e < min(e0 + V::N, vocab); ++e) {
+        if constexpr (BF) {
+          const uint32_t b = ((const uint16_t*)row)[e];
+          const int i = e - e0;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            if (w == i >> 1) x[u][w] = (i & 1) ? (x[u][w] & 0xffffu) | (b << 16) : (x[u][w] & 0xffff0000u) | b;
+        } else {
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            if (w == e - e0) x[u][w] = ((const uint32_t*)row)[e];
+        }
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ Part shuffle(const Part& p, int mask) {
+  return Part{__shfl_xor(p.m, mask), __shfl_xor(p.s, mask), __shfl_xor(p.w, mask)};
+}
+__device__ __forceinline__ Part wave_join(Part p, float c) {
+#pragma unroll
+  for (int mask = 1; mask < 64; mask <<= 1) p = join(p, shuffle(p, mask), c);
+  return p;
+}
+
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return (b >> 31) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float((o >> 31) ? o & 0x7fffffffu : ~o); }
+
+// The most probable entries a wavefront has seen, as a superset: every element not
+// below `bound`.  base is a value that at least k of the elements seen so far reach: the
+// k-th largest of the lanes' running maxima (its upper 16 bits are taken, which can only
+// lower it), or the k-th best when a full buffer was cut.  It rises as the wavefront
+// reads on, so that few elements reach it, and a vector costs one comparison.  An
+// element of a later batch has a higher index than all those and must exceed base.
+struct Candidates {
+  unsigned long long* keys;  // kWaveKeys in LDS
+  int n, k;
+  float base, bound;
+  // Before the elements of a batch, whose largest in this lane is `largest` (of all so far: lane_max).
+  __device__ __forceinline__ void next_batch(float largest, float lane_max, bool first) {
+    if (!first) bound = fmaxf(bound, above(base));
+    if (__popcll(__ballot(largest >= bound)) <= kFewLanes) return;
+    const uint32_t o = order_of(lane_max);
+    uint32_t t = 0;
+    for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+      if (__popcll(__ballot(o >= (t | bit))) >= k) t |= bit;
+    base = fmaxf(base, value_of(t));  // NaN, below every number, drops out
+    bound = fmaxf(bound, base);
+  }
+  // The next larger number.
+  static __device__ __forceinline__ float above(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return x == 0.f ? __uint_as_float(1u) : __uint_as_float((b >> 31) ? b - 1 : b + 1);
+  }
+  // Cut to the k best, in order.
+  __device__ __forceinline__ void cut() {
+    constexpr int R = (kWaveKeys + 63) / 64;
+    const int lane = threadIdx.x & 63;
+    unsigned long long mine[R], kth = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) mine[i] = i * 64 + lane < n ? keys[i * 64 + lane] : 0;
+    for (int r = 0; r < k; ++r) {
+      unsigned long long best = mine[0];
+#pragma unroll
+      for (int i = 1; i < R; ++i) best = max(best, mine[i]);
+#pragma unroll
+      for (int mask = 1; mask < 64; mask <<= 1) best = max(best, (unsigned long long)__shfl_xor((long long)best, mask));
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (mine[i] == best) mine[i] = 0;
+      if (lane == 0) keys[r] = best;
+      kth = best;
+    }
+    n = min(n, k);
+    if (kth != 0) {
+      base = fmaxf(base, key_value(kth));
+      bound = fmaxf(bound, base);
+    }
+  }
+  // Room for `more` (at most kWaveKeys - k).
+  __device__ __forceinline__ void reserve(int more) {
+    if (n + more > kWaveKeys) cut();
+  }
+  // The lanes' elements x of index i that reach the bound.
+  __device__ __forceinline__ void add(float x, int i) {
+    const bool hit = x >= bound;
+    const unsigned long long mask = __ballot(hit);
+    if (mask == 0) return;
+    const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+    if (hit) keys[at] = key_of(x, i);
+    n += __popcll(mask);
+  }
+};
+
+// Ranks by counting: the k largest of n keys to out, largest first; 0 where fewer.
+__device__ __forceinline__ void rank_keys(const unsigned long long* keys, int n, int k, unsigned long long* out) {
+  for (int i = threadIdx.x; i < k; i += kThreads)
+    if (i >= n) out[i] = 0;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const unsigned long long key = keys[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += keys[j] > key;
+    if (rank < k) out[rank] = key;
+  }
+}
+
+__device__ __forceinline__ void publish(float* p, float x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float collect(const float* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <bool BF, bool TOP>
+__global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
+  using V = Vec<BF>;
+  constexpr int kWaves = kThreads / 64;
+  __shared__ Part parts[kWaves];
+  __shared__ unsigned long long wave_keys[TOP ? kWaves : 1][TOP ? kWaveKeys : 1];
+  __shared__ unsigned long long keys[TOP ? kWaves * kKeptKeys : 1];
+  __shared__ unsigned long long best[TOP ? INFS_SCORE_MAX_TOP : 1];
+  __shared__ int counts[kWaves], last;
+  const int piece = (int)(blockIdx.x % (unsigned)a.pieces), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t row = blockIdx.x / (unsigned)a.pieces;
+  const RowReader<BF> in(a.logits, row * a.row_stride, a.vocab);
+  const float c = a.inv_t * kLog2E;
+  // the given token's logit, for whoever finishes the row
+  const int token = a.logprob ? a.tokens[row] : -1;
+  const bool known = token >= 0 && token < a.vocab;
+  const float given = known ? load1<BF>(in.row, token) : 0.f;
+
+  Part p = empty_part();
+  Candidates top{wave_keys[TOP ? wave : 0], 0, a.top_k, -FLT_MAX, -FLT_MAX};  // masked entries are below
+  const int begin = piece * a.batches * kBatch, end = min(begin + a.batches * kBatch, in.count);
+  for (int first = begin; first < end; first += kBatch) {
+    u32x4 x[kUnroll];
+    in.load(first, end, x);
+    float vm[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      vm[u] = V::get(x[u], 0);
+#pragma unroll
+      for (int i = 1; i < V::N; ++i) vm[u] = fmaxf(vm[u], V::get(x[u], i));
+    }
+    const float m = fmaxf(p.m, fmaxf(fmaxf(vm[0], vm[1]), fmaxf(vm[2], vm[3])));
+    const float d = fmaxf((p.m - m) * c, kFar), f = __builtin_amdgcn_exp2f(d);
+    p.w = (p.w + p.s * d) * f;
+    p.s *= f;
+    p.m = m;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int i = 0; i < V::N; ++i) {
+        const float y = (V::get(x[u], i) - m) * c, e = __builtin_amdgcn_exp2f(y);
+        p.s += e;
+        p.w = fmaf(e, fmaxf(y, kFar), p.w);
+      }
+    if constexpr (TOP) {
+      top.next_batch(fmaxf(fmaxf(vm[0], vm[1]), fmaxf(vm[2], vm[3])), m, first == begin);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (__ballot(vm[u] >= top.bound) == 0) continue;
+        top.reserve(64 * V::N);
+        const int e0 = (first + u * kThreads + (int)threadIdx.x) * V::N - in.lead;
+#pragma unroll
+        for (int i = 0; i < V::N; ++i) top.add(V::get(x[u], i), e0 + i);
+      }
+    }
+  }
+
+  // the work-group's part
+  p = wave_join(p, c);
+  if (lane == 0) parts[wave] = p;
+  if constexpr (TOP) {
+    if (top.n > kKeptKeys) top.cut();
+    if (lane == 0) counts[wave] = top.n;
+  }
   __syncthreads();
-  for (int n = kThreads / 2; n > 0; n >>= 1) {
-    if ((int)threadIdx.x < n) parts[threadIdx.x] = join(parts[threadIdx.x], parts[threadIdx.x + n], c);
+  p = join(join(parts[0], parts[1], c), join(parts[2], parts[3], c), c);
+  if constexpr (TOP) {
+    int at = 0, n = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) at += counts[w];
+      n += counts[w];
+    }
+    if (lane < counts[wave]) keys[at + lane] = wave_keys[wave][lane];
+    __syncthreads();
+    rank_keys(keys, n, a.top_k, best);
     __syncthreads();
   }
-  p = parts[0];
+
+  if (a.pieces > 1) {
+    // hand the part over; the last work-group of the row joins them
+    const int64_t rec = row * a.pieces + piece;
+    if (threadIdx.x == 0) {
+      publish(a.part + 3 * rec, p.m);
+      publish(a.part + 3 * rec + 1, p.s);
+      publish(a.part + 3 * rec + 2, p.w);
+    }
+    if constexpr (TOP) {
+      if ((int)threadIdx.x < a.top_k)
+        __hip_atomic_store(a.keys + rec * a.top_k + threadIdx.x, best[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have reached the coherence point
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      last = __hip_atomic_fetch_add(a.arrived + row, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
+      if (last) __hip_atomic_store(a.arrived + row, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+    }
+    __syncthreads();
+    if (!last) return;
+    if (wave == 0) {
+      Part q = empty_part();
+      if (lane < a.pieces) {
+        const float* r = a.part + 3 * (row * a.pieces + lane);
+        q = Part{collect(r), collect(r + 1), collect(r + 2)};
+      }
+      q = wave_join(q, c);
+      if (lane == 0) parts[0] = q;
+    }
+    if constexpr (TOP) {
+      // The pieces' lists are sorted: with j = ceil(k / pieces) - 1, at least k keys reach the
+      // least of the lists' entries j, and only those can be among the k best.
+      const int n = a.pieces * a.top_k, j = (a.top_k + a.pieces - 1) / a.pieces - 1;
+      unsigned long long* all = wave_keys[0];  // of all wavefronts
+      if (threadIdx.x == 0) counts[0] = 0;
+      if (wave == 0) {
+        unsigned long long least = ~0ull;
+        if (lane < a.pieces)
+          least = __hip_atomic_load(a.keys + (row * a.pieces + lane) * a.top_k + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int mask = 1; mask < 64; mask <<= 1) least = min(least, (unsigned long long)__shfl_xor((long long)least, mask));
+        if (lane == 0) keys[0] = least;
+      }
+      __syncthreads();
+      const unsigned long long least = keys[0];
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const unsigned long long key =
+            __hip_atomic_load(a.keys + row * n + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (key != 0 && key >= least) all[atomicAdd(&counts[0], 1)] = key;
+      }
+      __syncthreads();
+      rank_keys(all, counts[0], a.top_k, best);
+    }
+    __syncthreads();
+    p = parts[0];
+  }
+
   const bool none = p.s == 0.f;  // every entry masked
   const float log2_s = log2f(p.s), ln_s = none ? -__builtin_huge_valf() : log2_s * kLn2;
   if (threadIdx.x == 0) {
     if (a.logprob) {
-      const int t = a.tokens[row];
-      float lp = __builtin_nanf("");
-      if (t == -1)
-        lp = 0.f;
-      else if (t >= 0 && t < a.vocab)
-        lp = none ? -__builtin_huge_valf() : (load1<BF>(z, t) - p.m) * a.inv_t - ln_s;
+      float lp = token == -1 ? 0.f : __builtin_nanf("");
+      if (known) lp = none ? -__builtin_huge_valf() : (given - p.m) * a.inv_t - ln_s;
       a.logprob[row] = lp;
     }
     if (a.entropy) a.entropy[row] = none ? 0.f : kLn2 * (log2_s - p.w / p.s);
@@ -101,27 +402,13 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
       a.stats[2 * row + 1] = ln_s;
     }
   }
-  if (!a.top_id) return;
-  unsigned long long last = ~0ull;
-  for (int k = 0; k < a.top_k; ++k) {
-    unsigned long long b = 0;
-    for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
-      const unsigned long long key = key_of(load1<BF>(z, i), i);
-      if (key < last && key > b) b = key;
-    }
-    __syncthreads();
-    best[threadIdx.x] = b;
-    __syncthreads();
-    for (int n = kThreads / 2; n > 0; n >>= 1) {
-      if ((int)threadIdx.x < n && best[threadIdx.x + n] > best[threadIdx.x]) best[threadIdx.x] = best[threadIdx.x + n];
-      __syncthreads();
-    }
-    last = best[0];
-    if (threadIdx.x == 0) {
+  if constexpr (TOP) {
+    if ((int)threadIdx.x < a.top_k) {
+      const unsigned long long key = best[threadIdx.x];
       const bool bad = !(p.s == p.s);
-      a.top_id[row * a.top_k + k] = last == 0 || bad ? -1 : key_id(last);
-      a.top_logprob[row * a.top_k + k] =
-          bad ? __builtin_nanf("") : last == 0 ? -__builtin_huge_valf() : (key_value(last) - p.m) * a.inv_t - ln_s;
+      a.top_id[row * a.top_k + threadIdx.x] = key == 0 || bad ? -1 : key_id(key);
+      a.top_logprob[row * a.top_k + threadIdx.x] =
+          bad ? __builtin_nanf("") : key == 0 ? -__builtin_huge_valf() : (key_value(key) - p.m) * a.inv_t - ln_s;
     }
   }
 }
@@ -152,9 +439,27 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
 
 }  // namespace
 
-hipError_t launch_score(const ScoreArgs& a, bool bf16, hipStream_t stream) {
+// Pieces of a row and batches of a piece: whole rows where they are many, else pieces
+// so that about kScoreWorkGroups work-groups share the batches of all rows.
+void plan_score(ScoreArgs& a, bool bf16) {
+  const int n = bf16 ? 8 : 4;
+  const int64_t all = (a.vocab + (n - 1) + n - 1) / n;  // vectors of a row, whatever its alignment
+  const int64_t batches = (all + kBatch - 1) / kBatch;
+  int64_t per = std::max<int64_t>(1, batches * a.rows / kScoreWorkGroups);
+  per = std::max(per, (batches + kMaxPieces - 1) / kMaxPieces);
+  while ((batches + per - 1) / per > 1 && (batches + per - 1) / per * a.rows > kScoreMaxRecords) ++per;
+  const int64_t pieces = (batches + per - 1) / per;
+  a.batches = (int)((batches + pieces - 1) / pieces);
+  a.pieces = (int)((batches + a.batches - 1) / a.batches);
+}
+
+hipError_t launch_score(ScoreArgs& a, bool bf16, hipStream_t stream) {
   if (a.rows == 0) return hipSuccess;
-  hipLaunchKernelGGL(bf16 ? score_kernel<true> : score_kernel<false>, dim3(a.rows), dim3(kThreads), 0, stream, a);
+  plan_score(a, bf16);
+  void (*const kernels[2][2])(const ScoreArgs) = {{score_kernel<false, false>, score_kernel<false, true>},
+                                                  {score_kernel<true, false>, score_kernel<true, true>}};
+  hipLaunchKernelGGL(kernels[bf16][a.top_id != nullptr], dim3((unsigned)(a.rows * (int64_t)a.pieces)), dim3(kThreads), 0,
+                     stream, a);
   return hipGetLastError();
 }
 
