@@ -271,7 +271,7 @@ infs_status infs_score_grad(infs_scorer* s, int32_t rows, const void* logits_dev
     return op_fail(INFS_E_ARG, "tokens and gradients must be aligned to 4 bytes (stats: 8)");
   if (s->dry || rows == 0) return INFS_OK;
   infs::ScoreGradArgs a{logits_dev, grad_dev, row_stride, grad_row_stride, d_logprob_dev ? tokens_dev : nullptr, stats_dev,
-                        d_entropy_dev ? entropy_dev : nullptr, d_logprob_dev, d_entropy_dev, rows, s->cfg.vocab, s->inv_t};
+                        d_entropy_dev ? entropy_dev : nullptr, d_logprob_dev, d_entropy_dev, rows, s->cfg.vocab, s->inv_t, 0};
   infs::StreamDevice dev(s->stream, s->device);
   hipError_t e = dev.status();
   if (e == hipSuccess) e = infs::launch_score_grad(a, s->bf16, s->stream);

@@ -117,11 +117,12 @@ struct ScoreGradArgs {
   const float* d_entropy;
   int32_t rows, vocab;
   float inv_t;
+  int32_t batches;           // of a row (launch_score_grad)
 };
 
 // Fills in pieces and batches.
 hipError_t launch_score(ScoreArgs& args, bool bf16, hipStream_t stream);
-hipError_t launch_score_grad(const ScoreGradArgs& args, bool bf16, hipStream_t stream);
+hipError_t launch_score_grad(ScoreGradArgs& args, bool bf16, hipStream_t stream);
 
 // ---- responses' pages -----------------------------------------------------------
 struct ForkArgs {

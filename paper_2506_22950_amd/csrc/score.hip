@@ -413,26 +413,59 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
   }
 }
 
+// ---- the gradient ---------------------------------------------------------------
+//
 // grad_j = p_j (A + B log p_j) + [j = token] C with A = -(g_lp + g_h H) / T, B = -g_h / T,
-// C = g_lp / T.  Rows from rows on are no work: a work-group strides over them.
-template <bool BF>
+// C = g_lp / T: elements alone, a batch of a row a work-group.
+template <bool BF, bool ENTROPY>
 __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArgs a) {
-  const float c = a.inv_t * kLog2E;
-  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const char* z = (const char*)a.logits + row * a.row_stride * (BF ? 2 : 4);
-    char* g = (char*)a.grad + row * a.grad_row_stride * (BF ? 2 : 4);
-    const float m = a.stats[2 * row], ls2 = a.stats[2 * row + 1] * kLog2E;
-    const int t = a.d_logprob ? a.tokens[row] : -1;
-    float g_lp = a.d_logprob && t != -1 ? a.d_logprob[row] : 0.f;
-    if (t < -1 || t >= a.vocab) g_lp = __builtin_nanf("");
-    const float g_h = a.d_entropy ? a.d_entropy[row] : 0.f, h = a.d_entropy ? a.entropy[row] : 0.f;
-    const float ca = -(g_lp + g_h * h) * a.inv_t, cb = -g_h * a.inv_t * kLn2, cc = g_lp * a.inv_t;
-    const bool none = m == -__builtin_huge_valf();
-    for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.vocab; i += gridDim.x * kThreads) {
-      const float y = (load1<BF>(z, i) - m) * c - ls2, p = __builtin_amdgcn_exp2f(y);
-      float r = p * (ca + cb * fmaxf(y, kFar));
-      if (i == t) r += cc;
-      store1<BF>(g, i, none ? 0.f : r);
+  using V = Vec<BF>;
+  const int64_t row = blockIdx.x / (unsigned)a.batches;
+  const int first = (int)(blockIdx.x % (unsigned)a.batches) * kBatch;
+  const RowReader<BF> in(a.logits, row * a.row_stride, a.vocab);
+  u32x4 x[kUnroll];
+  in.load(first, in.count, x);
+  char* g = (char*)a.grad + row * a.grad_row_stride * V::ES;
+  const bool same = (int)((uintptr_t)g / V::ES % V::N) == in.lead;  // vectors of the two rows coincide
+  const float m = a.stats[2 * row], ls2 = a.stats[2 * row + 1] * kLog2E, c = a.inv_t * kLog2E;
+  const int token = a.d_logprob ? a.tokens[row] : -1;
+  float g_lp = a.d_logprob && token != -1 ? a.d_logprob[row] : 0.f;
+  if (token < -1 || token >= a.vocab) g_lp = __builtin_nanf("");
+  const float g_h = ENTROPY ? a.d_entropy[row] : 0.f;
+  const float ca = -(g_lp + (ENTROPY ? g_h * a.entropy[row] : 0.f)) * a.inv_t, cb = -g_h * a.inv_t * kLn2, cc = g_lp * a.inv_t;
+  const bool none = m == -__builtin_huge_valf();  // every entry masked
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int v = first + u * kThreads + (int)threadIdx.x;
+    if (v >= in.count) break;
+    const int e0 = v * V::N - in.lead;
+    float r[V::N];
+#pragma unroll
+    for (int i = 0; i < V::N; ++i) {
+      const float y = (V::get(x[u], i) - m) * c - ls2, p = __builtin_amdgcn_exp2f(y);
+      r[i] = ENTROPY ? p * fmaf(cb, fmaxf(y, kFar), ca) : p * ca;
+      if (none) r[i] = 0.f;
+    }
+    if (token >= e0 && token < e0 + V::N && !none) {
+#pragma unroll
+      for (int i = 0; i < V::N; ++i)
+        if (e0 + i == token) r[i] += cc;
+    }
+    if (same && v >= in.lo && v < in.hi) {
+      u32x4 w;
+      if constexpr (BF) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = __builtin_bit_cast(uint16_t, (__bf16)r[2 * i]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)r[2 * i + 1]) << 16;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(r[i]);
+      }
+      *(u32x4*)(g + (int64_t)e0 * V::ES) = w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < V::N; ++i)
+        if (e0 + i >= 0 && e0 + i < a.vocab) store1<BF>(g, e0 + i, r[i]);
     }
   }
 }
@@ -463,12 +496,28 @@ hipError_t launch_score(ScoreArgs& a, bool bf16, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_score_grad(const ScoreGradArgs& a, bool bf16, hipStream_t stream) {
+hipError_t launch_score_grad(ScoreGradArgs& a, bool bf16, hipStream_t stream) {
   if (a.rows == 0) return hipSuccess;
-  const unsigned x = (unsigned)((a.vocab + kThreads - 1) / kThreads), y = (unsigned)(a.rows < 32768 ? a.rows : 32768);
-  hipLaunchKernelGGL(bf16 ? score_grad_kernel<true> : score_grad_kernel<false>, dim3(x < 64 ? x : 64, y), dim3(kThreads), 0,
-                     stream, a);
-  return hipGetLastError();
+  const int n = bf16 ? 8 : 4;
+  a.batches = (int)(((a.vocab + 2 * (n - 1)) / n + kBatch - 1) / kBatch);
+  const int64_t most = INT32_MAX / a.batches;  // rows of a launch
+  void (*const kernels[2][2])(const ScoreGradArgs) = {{score_grad_kernel<false, false>, score_grad_kernel<false, true>},
+                                                      {score_grad_kernel<true, false>, score_grad_kernel<true, true>}};
+  const ScoreGradArgs all = a;
+  for (int64_t r0 = 0; r0 < all.rows; r0 += most) {
+    a.rows = (int32_t)std::min(most, all.rows - r0);
+    a.logits = (const char*)all.logits + r0 * all.row_stride * (bf16 ? 2 : 4);
+    a.grad = (char*)all.grad + r0 * all.grad_row_stride * (bf16 ? 2 : 4);
+    a.tokens = all.tokens ? all.tokens + r0 : nullptr;
+    a.stats = all.stats + 2 * r0;
+    a.entropy = all.entropy ? all.entropy + r0 : nullptr;
+    a.d_logprob = all.d_logprob ? all.d_logprob + r0 : nullptr;
+    a.d_entropy = all.d_entropy ? all.d_entropy + r0 : nullptr;
+    hipLaunchKernelGGL(kernels[bf16][a.d_entropy != nullptr], dim3((unsigned)(a.rows * a.batches)), dim3(kThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace infs
