@@ -83,7 +83,8 @@ constexpr int kWaveKeys = INFS_SCORE_MAX_TOP + 64 * 8;  // candidates a wavefron
 constexpr int kKeptKeys = 64;                           // most it hands on
 constexpr int kFewLanes = 8;  // lanes with candidates in a batch that do not move the bound
 static_assert(INFS_SCORE_MAX_TOP <= kKeptKeys, "candidate buffers");
-static_assert(kMaxPieces <= 64 && kMaxPieces * INFS_SCORE_MAX_TOP <= kThreads / 64 * kWaveKeys, "joining pieces");
+static_assert(kMaxPieces <= 64 && kMaxPieces * INFS_SCORE_MAX_TOP + 8 <= kThreads / 64 * kWaveKeys, "joining pieces");
+static_assert(kMaxPieces * INFS_SCORE_MAX_TOP <= 4 * kThreads, "a lane's keys of a join");
 
 template <bool BF>
 struct Vec {
@@ -176,16 +177,35 @@ struct Candidates {
   unsigned long long* keys;  // kWaveKeys in LDS
   int n, k;
   float base, bound;
-  // Before the elements of a batch, whose largest in this lane is `largest` (of all so far: lane_max).
-  __device__ __forceinline__ void next_batch(float largest, float lane_max, bool first) {
-    if (!first) bound = fmaxf(bound, above(base));
-    if (__popcll(__ballot(largest >= bound)) <= kFewLanes) return;
-    const uint32_t o = order_of(lane_max);
+  // base to the k-th largest of R values a lane, given by the upper halves of their orders.
+  template <int R>
+  __device__ __forceinline__ void raise(const uint32_t (&o)[R]) {
     uint32_t t = 0;
-    for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
-      if (__popcll(__ballot(o >= (t | bit))) >= k) t |= bit;
-    base = fmaxf(base, value_of(t));  // NaN, below every number, drops out
+#pragma unroll
+    for (uint32_t bit = 0x8000u; bit > 0; bit >>= 1) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) n += __popcll(__ballot(o[i] >= (t | bit)));
+      if (n >= k) t |= bit;
+    }
+    base = fmaxf(base, value_of(t << 16));  // NaN, below every number, drops out
     bound = fmaxf(bound, base);
+  }
+  // Before the first batch's elements: the lanes' maxima of all wavefronts together.
+  __device__ __forceinline__ void first_batch(float lane_max, uint32_t (&shared)[kThreads]) {
+    shared[threadIdx.x] = order_of(lane_max) >> 16;
+    __syncthreads();
+    uint32_t o[kThreads / 64];
+#pragma unroll
+    for (int i = 0; i < kThreads / 64; ++i) o[i] = shared[i * 64 + (threadIdx.x & 63)];
+    raise(o);
+  }
+  // Before the elements of a later batch, whose largest in this lane is `largest` (of all so far: lane_max).
+  __device__ __forceinline__ void next_batch(float largest, float lane_max) {
+    bound = fmaxf(bound, above(base));
+    if (__popcll(__ballot(largest >= bound)) <= kFewLanes) return;
+    const uint32_t o[1] = {order_of(lane_max) >> 16};
+    raise(o);
   }
   // The next larger number.
   static __device__ __forceinline__ float above(float x) {
@@ -232,14 +252,24 @@ struct Candidates {
   }
 };
 
-// Ranks by counting: the k largest of n keys to out, largest first; 0 where fewer.
-__device__ __forceinline__ void rank_keys(const unsigned long long* keys, int n, int k, unsigned long long* out) {
-  for (int i = threadIdx.x; i < k; i += kThreads)
-    if (i >= n) out[i] = 0;
+// Ranks by counting: the k largest of n keys to out, largest first; 0 where fewer.  keys is
+// kRankStep keys longer than n and aligned to 16 bytes: the reads go by whole steps, so that they
+// overlap (n counted one by one took 4 us of a call).
+constexpr int kRankStep = 8;
+__device__ __forceinline__ void rank_keys(unsigned long long* keys, int n, int k, unsigned long long* out) {
+  if ((int)threadIdx.x < kRankStep) keys[n + threadIdx.x] = 0;
+  if ((int)threadIdx.x < k && (int)threadIdx.x >= n) out[threadIdx.x] = 0;
+  __syncthreads();
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const unsigned long long key = keys[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += keys[j] > key;
+    for (int j = 0; j < n; j += kRankStep) {
+      unsigned long long x[kRankStep];
+#pragma unroll
+      for (int q = 0; q < kRankStep; ++q) x[q] = keys[j + q];
+#pragma unroll
+      for (int q = 0; q < kRankStep; ++q) rank += x[q] > key;
+    }
     if (rank < k) out[rank] = key;
   }
 }
@@ -256,9 +286,10 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
   using V = Vec<BF>;
   constexpr int kWaves = kThreads / 64;
   __shared__ Part parts[kWaves];
-  __shared__ unsigned long long wave_keys[TOP ? kWaves : 1][TOP ? kWaveKeys : 1];
-  __shared__ unsigned long long keys[TOP ? kWaves * kKeptKeys : 1];
+  __shared__ __attribute__((aligned(16))) unsigned long long wave_keys[TOP ? kWaves : 1][TOP ? kWaveKeys : 1];
+  __shared__ __attribute__((aligned(16))) unsigned long long keys[TOP ? kWaves * kKeptKeys + kRankStep : 1];
   __shared__ unsigned long long best[TOP ? INFS_SCORE_MAX_TOP : 1];
+  __shared__ uint32_t maxima[TOP ? kThreads : 1];
   __shared__ int counts[kWaves], last;
   const int piece = (int)(blockIdx.x % (unsigned)a.pieces), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t row = blockIdx.x / (unsigned)a.pieces;
@@ -296,7 +327,10 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
         p.w = fmaf(e, fmaxf(y, kFar), p.w);
       }
     if constexpr (TOP) {
-      top.next_batch(fmaxf(fmaxf(vm[0], vm[1]), fmaxf(vm[2], vm[3])), m, first == begin);
+      if (first == begin)
+        top.first_batch(m, maxima);
+      else
+        top.next_batch(fmaxf(fmaxf(vm[0], vm[1]), fmaxf(vm[2], vm[3])), m);
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         if (__ballot(vm[u] >= top.bound) == 0) continue;
@@ -325,7 +359,6 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
       n += counts[w];
     }
     if (lane < counts[wave]) keys[at + lane] = wave_keys[wave][lane];
-    __syncthreads();
     rank_keys(keys, n, a.top_k, best);
     __syncthreads();
   }
@@ -365,24 +398,26 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
       // least of the lists' entries j, and only those can be among the k best.
       const int n = a.pieces * a.top_k, j = (a.top_k + a.pieces - 1) / a.pieces - 1;
       unsigned long long* all = wave_keys[0];  // of all wavefronts
-      if (threadIdx.x == 0) counts[0] = 0;
-      if (wave == 0) {
-        unsigned long long least = ~0ull;
-        if (lane < a.pieces)
-          least = __hip_atomic_load(a.keys + (row * a.pieces + lane) * a.top_k + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      unsigned long long mine[4];
 #pragma unroll
-        for (int mask = 1; mask < 64; mask <<= 1) least = min(least, (unsigned long long)__shfl_xor((long long)least, mask));
-        if (lane == 0) keys[0] = least;
+      for (int i = 0; i < 4; ++i) {
+        const int at = i * kThreads + (int)threadIdx.x;
+        mine[i] = at < n ? __hip_atomic_load(a.keys + row * n + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+        if (at < n && at % a.top_k == j) keys[at / a.top_k] = mine[i];
       }
+      if (threadIdx.x == 0) counts[0] = 0;
       __syncthreads();
-      const unsigned long long least = keys[0];
-      for (int i = threadIdx.x; i < n; i += kThreads) {
-        const unsigned long long key =
-            __hip_atomic_load(a.keys + row * n + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (key != 0 && key >= least) all[atomicAdd(&counts[0], 1)] = key;
-      }
+      unsigned long long least = lane < a.pieces ? keys[lane] : ~0ull;
+#pragma unroll
+      for (int mask = 1; mask < kMaxPieces; mask <<= 1) least = min(least, (unsigned long long)__shfl_xor((long long)least, mask));
+      least = max(least, 1ull);
+      least = __shfl((long long)least, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (mine[i] >= least) all[atomicAdd(&counts[0], 1)] = mine[i];
       __syncthreads();
-      rank_keys(all, counts[0], a.top_k, best);
+      const int kept = counts[0];
+      rank_keys(all, kept, a.top_k, best);
     }
     __syncthreads();
     p = parts[0];
