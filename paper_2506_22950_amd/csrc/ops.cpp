@@ -58,7 +58,8 @@ struct infs_scorer {
   float inv_t = 1.f;
   hipStream_t stream = nullptr;
   int device = 0;
-  // One allocation: arrived [kScoreMaxRecords], part [kScoreMaxRecords][3], keys [kScoreMaxRecords][top_k].
+  // One allocation: arrived [kScoreMaxRecords], part [kScoreMaxRecords][3], keys
+  // [kScoreMaxRecords][kScorePieceKeys] (top_k > 0).
   char* workspace = nullptr;
 };
 
@@ -75,7 +76,8 @@ infs_status check_rows(const infs_scorer* s, int32_t rows, const void* logits, i
 }
 
 size_t workspace_bytes(const infs_scorer& s) {
-  return (sizeof(int32_t) + 3 * sizeof(float) + sizeof(unsigned long long) * s.cfg.top_k) * infs::kScoreMaxRecords;
+  const size_t keys = s.cfg.top_k > 0 ? sizeof(unsigned long long) * infs::kScorePieceKeys : 0;
+  return (sizeof(int32_t) + 3 * sizeof(float) + keys) * infs::kScoreMaxRecords;
 }
 
 bool misaligned(std::initializer_list<const void*> ptrs, size_t n) {

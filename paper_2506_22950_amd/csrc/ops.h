@@ -83,6 +83,7 @@ void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a);
 
 // ---- scores of tokens -----------------------------------------------------------
 constexpr int kScoreMaxPieces = 32;      // pieces of a row
+constexpr int kScorePieceKeys = 64;      // candidates that a piece hands over
 constexpr int kScoreWorkGroups = 1024;   // work-groups that the rows of a call are cut for
 
 struct ScoreArgs {
@@ -98,7 +99,7 @@ struct ScoreArgs {
   float inv_t;         // 1 / temperature
   int32_t pieces, batches;  // pieces of a row, batches of a piece (plan_score)
   // Where rows are cut (pieces > 1), per record row * pieces + piece: the part of a piece [3] and
-  // its best keys [top_k]; and the pieces of a row that have arrived (0 between launches).
+  // its candidates [kScorePieceKeys]; and the pieces of a row that have arrived (0 between launches).
   float* part;
   unsigned long long* keys;
   int32_t* arrived;

@@ -44,13 +44,6 @@ struct Part {
   float m, s, w;
 };
 __device__ __forceinline__ Part empty_part() { return Part{-FLT_MAX, 0.f, 0.f}; }
-__device__ __forceinline__ Part join(const Part& a, const Part& b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  const float da = fmaxf((a.m - m) * c, kFar), db = fmaxf((b.m - m) * c, kFar);
-  const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
-  return Part{m, a.s * ea + b.s * eb, (a.w + a.s * da) * ea + (b.w + b.s * db) * eb};
-}
-
 // Order of alternatives as one number: by value, then by the lower index; 0: none.
 __device__ __forceinline__ unsigned long long key_of(float x, int i) {
   if (!(x > -__builtin_huge_valf())) return 0;
@@ -83,8 +76,11 @@ constexpr int kWaveKeys = INFS_SCORE_MAX_TOP + 64 * 8;  // candidates a wavefron
 constexpr int kKeptKeys = 64;                           // most it hands on
 constexpr int kFewLanes = 8;  // lanes with candidates in a batch that do not move the bound
 static_assert(INFS_SCORE_MAX_TOP <= kKeptKeys, "candidate buffers");
-static_assert(kMaxPieces <= 64 && kMaxPieces * INFS_SCORE_MAX_TOP + 8 <= kThreads / 64 * kWaveKeys, "joining pieces");
-static_assert(kMaxPieces * INFS_SCORE_MAX_TOP <= 4 * kThreads, "a lane's keys of a join");
+constexpr int kPieceKeys = kScorePieceKeys;
+static_assert(kMaxPieces <= 64, "a lane a piece");
+static_assert(kPieceKeys >= INFS_SCORE_MAX_TOP && kPieceKeys <= kThreads && kMaxPieces * kPieceKeys % kThreads == 0 &&
+                  kMaxPieces * kPieceKeys + 8 <= kThreads / 64 * kWaveKeys,
+              "joining pieces");
 
 template <bool BF>
 struct Vec {
@@ -152,13 +148,41 @@ struct RowReader {
   }
 };
 
-__device__ __forceinline__ Part shuffle(const Part& p, int mask) {
-  return Part{__shfl_xor(p.m, mask), __shfl_xor(p.s, mask), __shfl_xor(p.w, mask)};
+// Reductions over a wavefront without LDS: within rows of 16 lanes by lane permutations, then
+// each row's total to the next row and the lower half's to the upper; lane 63 ends with all of it.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float lanes(float old, float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL, ROWS, 0xF, false));
 }
-__device__ __forceinline__ Part wave_join(Part p, float c) {
-#pragma unroll
-  for (int mask = 1; mask < 64; mask <<= 1) p = join(p, shuffle(p, mask), c);
-  return p;
+__device__ __forceinline__ float last_lane(float x) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, lanes<0xB1, 0xF>(x, x));   // quad_perm [1,0,3,2]
+  x = fmaxf(x, lanes<0x4E, 0xF>(x, x));   // quad_perm [2,3,0,1]
+  x = fmaxf(x, lanes<0x141, 0xF>(x, x));  // row_half_mirror
+  x = fmaxf(x, lanes<0x140, 0xF>(x, x));  // row_mirror
+  x = fmaxf(x, lanes<0x142, 0xA>(x, x));  // row_bcast:15 into rows 1 and 3
+  x = fmaxf(x, lanes<0x143, 0xC>(x, x));  // row_bcast:31 into rows 2 and 3
+  return last_lane(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x += lanes<0xB1, 0xF>(0.f, x);
+  x += lanes<0x4E, 0xF>(0.f, x);
+  x += lanes<0x141, 0xF>(0.f, x);
+  x += lanes<0x140, 0xF>(0.f, x);
+  x += lanes<0x142, 0xA>(0.f, x);
+  x += lanes<0x143, 0xC>(0.f, x);
+  return last_lane(x);
+}
+// A part around another maximum (m >= p.m).
+__device__ __forceinline__ Part around(const Part& p, float m, float c) {
+  const float d = fmaxf((p.m - m) * c, kFar), f = __builtin_amdgcn_exp2f(d);
+  return Part{m, p.s * f, (p.w + p.s * d) * f};
+}
+__device__ __forceinline__ Part wave_join(const Part& p, float c) {
+  const Part q = around(p, wave_max(p.m), c);
+  return Part{q.m, wave_sum(q.s), wave_sum(q.w)};
 }
 
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -166,6 +190,23 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return (b >> 31) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float((o >> 31) ? o & 0x7fffffffu : ~o); }
+
+// The k-th largest of the lanes' 16-bit values: bit by bit, by counting lanes.
+__device__ __forceinline__ uint32_t kth_largest(uint32_t o, int k) {
+  uint32_t t = 0;
+#pragma unroll
+  for (uint32_t bit = 0x8000u; bit > 0; bit >>= 1)
+    if (__popcll(__ballot(o >= (t | bit))) >= k) t |= bit;
+  return t;
+}
+// The largest of a lane's values in the four wavefronts: 64 groups of the work-group's threads.
+// (The k-th largest group maximum lets few more elements through than the k-th of all threads.)
+__device__ __forceinline__ uint32_t columns(uint32_t o, uint32_t (&shared)[kThreads]) {
+  shared[threadIdx.x] = o;
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  return max(max(shared[lane], shared[64 + lane]), max(shared[128 + lane], shared[192 + lane]));
+}
 
 // The most probable entries a wavefront has seen, as a superset: every element not
 // below `bound`.  base is a value that at least k of the elements seen so far reach: the
@@ -177,35 +218,19 @@ struct Candidates {
   unsigned long long* keys;  // kWaveKeys in LDS
   int n, k;
   float base, bound;
-  // base to the k-th largest of R values a lane, given by the upper halves of their orders.
-  template <int R>
-  __device__ __forceinline__ void raise(const uint32_t (&o)[R]) {
-    uint32_t t = 0;
-#pragma unroll
-    for (uint32_t bit = 0x8000u; bit > 0; bit >>= 1) {
-      int n = 0;
-#pragma unroll
-      for (int i = 0; i < R; ++i) n += __popcll(__ballot(o[i] >= (t | bit)));
-      if (n >= k) t |= bit;
-    }
-    base = fmaxf(base, value_of(t << 16));  // NaN, below every number, drops out
+  // base to the k-th largest of the lanes' values, given by the upper halves of their orders.
+  __device__ __forceinline__ void raise(uint32_t o) {
+    base = fmaxf(base, value_of(kth_largest(o, k) << 16));  // NaN, below every number, drops out
     bound = fmaxf(bound, base);
   }
   // Before the first batch's elements: the lanes' maxima of all wavefronts together.
   __device__ __forceinline__ void first_batch(float lane_max, uint32_t (&shared)[kThreads]) {
-    shared[threadIdx.x] = order_of(lane_max) >> 16;
-    __syncthreads();
-    uint32_t o[kThreads / 64];
-#pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) o[i] = shared[i * 64 + (threadIdx.x & 63)];
-    raise(o);
+    raise(columns(order_of(lane_max) >> 16, shared));
   }
   // Before the elements of a later batch, whose largest in this lane is `largest` (of all so far: lane_max).
   __device__ __forceinline__ void next_batch(float largest, float lane_max) {
     bound = fmaxf(bound, above(base));
-    if (__popcll(__ballot(largest >= bound)) <= kFewLanes) return;
-    const uint32_t o[1] = {order_of(lane_max) >> 16};
-    raise(o);
+    if (__popcll(__ballot(largest >= bound)) > kFewLanes) raise(order_of(lane_max) >> 16);
   }
   // The next larger number.
   static __device__ __forceinline__ float above(float x) {
@@ -241,14 +266,22 @@ struct Candidates {
   __device__ __forceinline__ void reserve(int more) {
     if (n + more > kWaveKeys) cut();
   }
-  // The lanes' elements x of index i that reach the bound.
-  __device__ __forceinline__ void add(float x, int i) {
-    const bool hit = x >= bound;
-    const unsigned long long mask = __ballot(hit);
-    if (mask == 0) return;
-    const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-    if (hit) keys[at] = key_of(x, i);
-    n += __popcll(mask);
+  // The lanes' elements of vector x that reach the bound, the first of them of index e0.
+  template <bool BF>
+  __device__ __forceinline__ void add(const u32x4& x, int e0) {
+    using V = Vec<BF>;
+    reserve(64 * V::N);
+    unsigned long long masks[V::N];  // all comparisons first: no branch waits for each
+#pragma unroll
+    for (int i = 0; i < V::N; ++i) masks[i] = __ballot(V::get(x, i) >= bound);
+#pragma unroll
+    for (int i = 0; i < V::N; ++i) {
+      if (masks[i] == 0) continue;
+      const uint32_t lo = (uint32_t)masks[i], hi = (uint32_t)(masks[i] >> 32);
+      const int at = n + __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+      if (V::get(x, i) >= bound) keys[at] = key_of(V::get(x, i), e0 + i);
+      n += __popcll(masks[i]);
+    }
   }
 };
 
@@ -277,7 +310,11 @@ __device__ __forceinline__ void rank_keys(unsigned long long* keys, int n, int k
 __device__ __forceinline__ void publish(float* p, float x) {
   __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ float collect(const float* p) {
+__device__ __forceinline__ void publish(unsigned long long* p, unsigned long long x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class T>
+__device__ __forceinline__ T collect(const T* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
@@ -334,10 +371,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         if (__ballot(vm[u] >= top.bound) == 0) continue;
-        top.reserve(64 * V::N);
-        const int e0 = (first + u * kThreads + (int)threadIdx.x) * V::N - in.lead;
-#pragma unroll
-        for (int i = 0; i < V::N; ++i) top.add(V::get(x[u], i), e0 + i);
+        top.template add<BF>(x[u], (first + u * kThreads + (int)threadIdx.x) * V::N - in.lead);
       }
     }
   }
@@ -350,21 +384,33 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
     if (lane == 0) counts[wave] = top.n;
   }
   __syncthreads();
-  p = join(join(parts[0], parts[1], c), join(parts[2], parts[3], c), c);
+  {
+    Part q[kWaves];
+    float m = parts[0].m;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, parts[w].m);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) q[w] = around(parts[w], m, c);
+    p = Part{m, (q[0].s + q[1].s) + (q[2].s + q[3].s), (q[0].w + q[1].w) + (q[2].w + q[3].w)};
+  }
+  unsigned long long* all = wave_keys[0];  // the candidates of all wavefronts, as one array
+  int before = 0, found = 0;               // candidates of the wavefronts before this one, and of all
   if constexpr (TOP) {
-    int at = 0, n = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) at += counts[w];
-      n += counts[w];
+      if (w < wave) before += counts[w];
+      found += counts[w];
     }
-    if (lane < counts[wave]) keys[at + lane] = wave_keys[wave][lane];
-    rank_keys(keys, n, a.top_k, best);
-    __syncthreads();
+    if (a.pieces == 1 || found > kPieceKeys) {
+      if (lane < counts[wave]) keys[before + lane] = wave_keys[wave][lane];
+      rank_keys(keys, found, a.top_k, best);
+      __syncthreads();
+    }
   }
 
   if (a.pieces > 1) {
-    // hand the part over; the last work-group of the row joins them
+    // Hand the part over, and the candidates (more than kPieceKeys: the best); the last work-group
+    // of the row joins them.
     const int64_t rec = row * a.pieces + piece;
     if (threadIdx.x == 0) {
       publish(a.part + 3 * rec, p.m);
@@ -372,8 +418,13 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
       publish(a.part + 3 * rec + 2, p.w);
     }
     if constexpr (TOP) {
-      if ((int)threadIdx.x < a.top_k)
-        __hip_atomic_store(a.keys + rec * a.top_k + threadIdx.x, best[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      unsigned long long* to = a.keys + rec * kPieceKeys;
+      if (found > kPieceKeys) {
+        if ((int)threadIdx.x < kPieceKeys) publish(to + threadIdx.x, (int)threadIdx.x < a.top_k ? best[threadIdx.x] : 0);
+      } else {
+        if (lane < counts[wave]) publish(to + before + lane, wave_keys[wave][lane]);
+        if ((int)threadIdx.x >= found && (int)threadIdx.x < kPieceKeys) publish(to + threadIdx.x, 0);
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have reached the coherence point
@@ -381,9 +432,19 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
     if (threadIdx.x == 0) {
       last = __hip_atomic_fetch_add(a.arrived + row, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
       if (last) __hip_atomic_store(a.arrived + row, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+      counts[0] = 0;
     }
     __syncthreads();
     if (!last) return;
+    constexpr int kMine = TOP ? kMaxPieces * kPieceKeys / kThreads : 1;
+    unsigned long long mine[kMine];
+    if constexpr (TOP) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int at = i * kThreads + (int)threadIdx.x;
+        mine[i] = at < a.pieces * kPieceKeys ? collect(a.keys + row * a.pieces * kPieceKeys + at) : 0;
+      }
+    }
     if (wave == 0) {
       Part q = empty_part();
       if (lane < a.pieces) {
@@ -394,27 +455,14 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
       if (lane == 0) parts[0] = q;
     }
     if constexpr (TOP) {
-      // The pieces' lists are sorted: with j = ceil(k / pieces) - 1, at least k keys reach the
-      // least of the lists' entries j, and only those can be among the k best.
-      const int n = a.pieces * a.top_k, j = (a.top_k + a.pieces - 1) / a.pieces - 1;
-      unsigned long long* all = wave_keys[0];  // of all wavefronts
-      unsigned long long mine[4];
+      // the best of them, again by a bound that at least k reach
+      unsigned long long largest = mine[0];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = i * kThreads + (int)threadIdx.x;
-        mine[i] = at < n ? __hip_atomic_load(a.keys + row * n + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
-        if (at < n && at % a.top_k == j) keys[at / a.top_k] = mine[i];
-      }
-      if (threadIdx.x == 0) counts[0] = 0;
-      __syncthreads();
-      unsigned long long least = lane < a.pieces ? keys[lane] : ~0ull;
+      for (int i = 1; i < kMine; ++i) largest = max(largest, mine[i]);
+      const uint32_t least = kth_largest(columns((uint32_t)(largest >> 48), maxima), a.top_k);
 #pragma unroll
-      for (int mask = 1; mask < kMaxPieces; mask <<= 1) least = min(least, (unsigned long long)__shfl_xor((long long)least, mask));
-      least = max(least, 1ull);
-      least = __shfl((long long)least, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (mine[i] >= least) all[atomicAdd(&counts[0], 1)] = mine[i];
+      for (int i = 0; i < kMine; ++i)
+        if (mine[i] != 0 && (uint32_t)(mine[i] >> 48) >= least) all[atomicAdd(&counts[0], 1)] = mine[i];
       __syncthreads();
       const int kept = counts[0];
       rank_keys(all, kept, a.top_k, best);
@@ -511,7 +559,8 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
 // so that about kScoreWorkGroups work-groups share the batches of all rows.
 void plan_score(ScoreArgs& a, bool bf16) {
   const int n = bf16 ? 8 : 4;
-  const int64_t all = (a.vocab + (n - 1) + n - 1) / n;  // vectors of a row, whatever its alignment
+  const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.row_stride % n == 0;  // every row is
+  const int64_t all = (a.vocab + (aligned ? 0 : n - 1) + n - 1) / n;            // most vectors of a row
   const int64_t batches = (all + kBatch - 1) / kBatch;
   int64_t per = std::max<int64_t>(1, batches * a.rows / kScoreWorkGroups);
   per = std::max(per, (batches + kMaxPieces - 1) / kMaxPieces);
