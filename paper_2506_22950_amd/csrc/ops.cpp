@@ -58,8 +58,7 @@ struct infs_scorer {
   float inv_t = 1.f;
   hipStream_t stream = nullptr;
   int device = 0;
-  // One allocation: arrived [kScoreMaxRecords], part [kScoreMaxRecords][3], keys
-  // [kScoreMaxRecords][kScorePieceKeys] (top_k > 0).
+  // Arrivals, parts and candidates of the pieces of rows (see ScoreArgs), zero before the first launch.
   char* workspace = nullptr;
 };
 
@@ -76,8 +75,7 @@ infs_status check_rows(const infs_scorer* s, int32_t rows, const void* logits, i
 }
 
 size_t workspace_bytes(const infs_scorer& s) {
-  const size_t keys = s.cfg.top_k > 0 ? sizeof(unsigned long long) * infs::kScorePieceKeys : 0;
-  return (sizeof(int32_t) + 3 * sizeof(float) + keys) * infs::kScoreMaxRecords;
+  return infs::kScoreArrivedBytes + infs::kScorePartBytes + (s.cfg.top_k > 0 ? infs::kScoreKeyBytes : 0);
 }
 
 bool misaligned(std::initializer_list<const void*> ptrs, size_t n) {
@@ -248,8 +246,8 @@ infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_d
                     rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t, 0, 0, nullptr, nullptr, nullptr};
   char* ws = s->workspace;
   a.arrived = (int32_t*)ws;
-  a.part = (float*)(ws + sizeof(int32_t) * infs::kScoreMaxRecords);
-  a.keys = (unsigned long long*)(ws + (sizeof(int32_t) + 3 * sizeof(float)) * infs::kScoreMaxRecords);
+  a.part = (float*)(ws + infs::kScoreArrivedBytes);
+  a.keys = (unsigned long long*)(ws + infs::kScoreArrivedBytes + infs::kScorePartBytes);
   infs::StreamDevice dev(s->stream, s->device);
   hipError_t e = dev.status();
   if (e == hipSuccess) e = infs::launch_score(a, s->bf16, s->stream);

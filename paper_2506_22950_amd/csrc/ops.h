@@ -84,6 +84,7 @@ void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a);
 // ---- scores of tokens -----------------------------------------------------------
 constexpr int kScoreMaxPieces = 32;      // pieces of a row
 constexpr int kScorePieceKeys = 64;      // candidates that a piece hands over
+constexpr int kScorePartStride = 32;     // floats: no two work-groups write one 128-byte line
 constexpr int kScoreWorkGroups = 1024;   // work-groups that the rows of a call are cut for
 
 struct ScoreArgs {
@@ -98,8 +99,9 @@ struct ScoreArgs {
   int32_t rows, vocab, top_k;
   float inv_t;         // 1 / temperature
   int32_t pieces, batches;  // pieces of a row, batches of a piece (plan_score)
-  // Where rows are cut (pieces > 1), per record row * pieces + piece: the part of a piece [3] and
-  // its candidates [kScorePieceKeys]; and the pieces of a row that have arrived (0 between launches).
+  // Where rows are cut (pieces > 1), per record row * pieces + piece: the part of a piece (3 floats,
+  // kScorePartStride apart) and its candidates [kScorePieceKeys]; and, kCounterStride apart, the pieces
+  // of a row that have arrived (0 between launches).
   float* part;
   unsigned long long* keys;
   int32_t* arrived;
@@ -123,6 +125,10 @@ struct ScoreGradArgs {
 
 // Fills in pieces and batches.
 hipError_t launch_score(ScoreArgs& args, bool bf16, hipStream_t stream);
+// The workspace of a scorer: arrived, part, then (top) keys.
+constexpr size_t kScoreArrivedBytes = sizeof(int32_t) * kCounterStride * kScoreMaxRecords;
+constexpr size_t kScorePartBytes = sizeof(float) * kScorePartStride * kScoreMaxRecords;
+constexpr size_t kScoreKeyBytes = sizeof(unsigned long long) * kScorePieceKeys * kScoreMaxRecords;
 hipError_t launch_score_grad(ScoreGradArgs& args, bool bf16, hipStream_t stream);
 
 // ---- responses' pages -----------------------------------------------------------

@@ -413,9 +413,10 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
     // of the row joins them.
     const int64_t rec = row * a.pieces + piece;
     if (threadIdx.x == 0) {
-      publish(a.part + 3 * rec, p.m);
-      publish(a.part + 3 * rec + 1, p.s);
-      publish(a.part + 3 * rec + 2, p.w);
+      float* to = a.part + kScorePartStride * rec;
+      publish(to, p.m);
+      publish(to + 1, p.s);
+      publish(to + 2, p.w);
     }
     if constexpr (TOP) {
       unsigned long long* to = a.keys + rec * kPieceKeys;
@@ -430,8 +431,8 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
     __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have reached the coherence point
     __syncthreads();
     if (threadIdx.x == 0) {
-      last = __hip_atomic_fetch_add(a.arrived + row, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
-      if (last) __hip_atomic_store(a.arrived + row, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+      last = __hip_atomic_fetch_add(a.arrived + row * kCounterStride, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
+      if (last) __hip_atomic_store(a.arrived + row * kCounterStride, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
       counts[0] = 0;
     }
     __syncthreads();
@@ -448,7 +449,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
     if (wave == 0) {
       Part q = empty_part();
       if (lane < a.pieces) {
-        const float* r = a.part + 3 * (row * a.pieces + lane);
+        const float* r = a.part + kScorePartStride * (row * a.pieces + lane);
         q = Part{collect(r), collect(r + 1), collect(r + 2)};
       }
       q = wave_join(q, c);
