@@ -243,7 +243,7 @@ infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_d
     return op_fail(INFS_E_ARG, "tokens and outputs must be aligned to 4 bytes (stats: 8)");
   if (s->dry || rows == 0) return INFS_OK;
   infs::ScoreArgs a{logits_dev, row_stride, tokens_dev, logprob_dev, entropy_dev, top_id_dev, top_logprob_dev, stats_dev,
-                    rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t, 0, 0, nullptr, nullptr, nullptr};
+                    rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t, 0, 0, 0, nullptr, nullptr, nullptr};
   char* ws = s->workspace;
   a.arrived = (int32_t*)ws;
   a.part = (float*)(ws + infs::kScoreArrivedBytes);

@@ -86,6 +86,8 @@ constexpr int kScoreMaxPieces = 32;      // pieces of a row
 constexpr int kScorePieceKeys = 64;      // candidates that a piece hands over
 constexpr int kScorePartStride = 32;     // floats: no two work-groups write one 128-byte line
 constexpr int kScoreWorkGroups = 1024;   // work-groups that the rows of a call are cut for
+constexpr int kScoreWaveRows = 2048;     // rows from which ..
+constexpr int kScoreWaveVectors = 1024;  // .. rows of so many 16-byte vectors go a wavefront each
 
 struct ScoreArgs {
   const void* logits;
@@ -98,7 +100,8 @@ struct ScoreArgs {
   float* stats;        // [rows, 2]
   int32_t rows, vocab, top_k;
   float inv_t;         // 1 / temperature
-  int32_t pieces, batches;  // pieces of a row, batches of a piece (plan_score)
+  int32_t wave_rows;        // 1: a wavefront a row (plan_score); else
+  int32_t pieces, batches;  // pieces of a row, batches of a piece
   // Where rows are cut (pieces > 1), per record row * pieces + piece: the part of a piece (3 floats,
   // kScorePartStride apart) and its candidates [kScorePieceKeys]; and, kCounterStride apart, the pieces
   // of a row that have arrived (0 between launches).

@@ -21,7 +21,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kBlockThreads;
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kFar = -1000.f;  // 2^kFar is 0
 
@@ -63,23 +63,23 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 // N elements: vector v covers elements v N - lead .. of the row, lead the elements
 // by which the row's start lies behind a 16-byte boundary; the first and the last
 // vector of a row may be in part outside it and are then read by elements, what is
-// outside counting as masked.  A work-group takes batches of kBatch vectors, kUnroll a
-// lane, every lane around its own running maximum.
+// outside counting as masked.  W wavefronts take a row (a work-group, or one of its
+// wavefronts where rows are many and short) in batches of kUnroll vectors a lane,
+// every lane around its own running maximum.
 //
 // Few rows are cut into pieces of whole batches, a work-group each; the pieces of a
-// row are joined by the work-group that finishes last (see join_pieces), always in
-// the order of the pieces.
+// row are joined by the work-group that finishes last, always in the same order.
 constexpr int kUnroll = 4;
-constexpr int kBatch = kThreads * kUnroll;  // vectors
+constexpr int kBatch = kThreads * kUnroll;  // vectors of a batch of a work-group
 constexpr int kMaxPieces = kScoreMaxPieces;
-constexpr int kWaveKeys = INFS_SCORE_MAX_TOP + 64 * 8;  // candidates a wavefront holds: one vector a lane beside the best
+constexpr int kWaveKeys = INFS_SCORE_MAX_TOP + 64 * 8;  // candidates a wavefront holds: a vector a lane beside the best
 constexpr int kKeptKeys = 64;                           // most it hands on
-constexpr int kFewLanes = 8;  // lanes with candidates in a batch that do not move the bound
+constexpr int kFewLanes = 8;  // lanes with candidates in a batch that do not move a wavefront's bound
 static_assert(INFS_SCORE_MAX_TOP <= kKeptKeys, "candidate buffers");
 constexpr int kPieceKeys = kScorePieceKeys;
 static_assert(kMaxPieces <= 64, "a lane a piece");
 static_assert(kPieceKeys >= INFS_SCORE_MAX_TOP && kPieceKeys <= kThreads && kMaxPieces * kPieceKeys % kThreads == 0 &&
-                  kMaxPieces * kPieceKeys + 8 <= kThreads / 64 * kWaveKeys,
+                  kMaxPieces * kPieceKeys + 8 <= kWaves * kWaveKeys,
               "joining pieces");
 
 template <bool BF>
@@ -112,21 +112,22 @@ struct RowReader {
     lo = lead > 0;
     hi = (lead + n) / V::N;
   }
-  // Vectors first + 256 u + thread of [first, end): all loads at once, each inside the row.
+  // Vectors first + L u + lane of [first, end), L lanes: all loads at once, each inside the row.
+  template <int L>
   __device__ __forceinline__ void load(int first, int end, u32x4 (&x)[kUnroll]) const {
-    const int v0 = first + (int)threadIdx.x;
-    if (first >= lo && first + kBatch <= min(end, hi)) {
+    const int v0 = first + (int)threadIdx.x % L;
+    if (first >= lo && first + L * kUnroll <= min(end, hi)) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) x[u] = *(const u32x4*)(at + (int64_t)(v0 + u * kThreads) * 16);
+      for (int u = 0; u < kUnroll; ++u) x[u] = *(const u32x4*)(at + (int64_t)(v0 + u * L) * 16);
       return;
     }
     if (lo < hi) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) x[u] = *(const u32x4*)(at + (int64_t)min(max(v0 + u * kThreads, lo), hi - 1) * 16);
+      for (int u = 0; u < kUnroll; ++u) x[u] = *(const u32x4*)(at + (int64_t)min(max(v0 + u * L, lo), hi - 1) * 16);
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int v = v0 + u * kThreads;
+      const int v = v0 + u * L;
       if (v >= lo && v < min(end, hi)) continue;
       x[u] = u32x4{V::kMasked, V::kMasked, V::kMasked, V::kMasked};
       if (v >= end) continue;
@@ -201,7 +202,8 @@ __device__ __forceinline__ uint32_t kth_largest(uint32_t o, int k) {
 }
 // The largest of a lane's values in the four wavefronts: 64 groups of the work-group's threads.
 // (The k-th largest group maximum lets few more elements through than the k-th of all threads.)
-__device__ __forceinline__ uint32_t columns(uint32_t o, uint32_t (&shared)[kThreads]) {
+// Two calls in a row need two buffers.
+__device__ __forceinline__ uint32_t columns(uint32_t o, uint32_t* shared) {
   shared[threadIdx.x] = o;
   __syncthreads();
   const int lane = threadIdx.x & 63;
@@ -223,44 +225,37 @@ struct Candidates {
     base = fmaxf(base, value_of(kth_largest(o, k) << 16));  // NaN, below every number, drops out
     bound = fmaxf(bound, base);
   }
-  // Before the first batch's elements: the lanes' maxima of all wavefronts together.
-  __device__ __forceinline__ void first_batch(float lane_max, uint32_t (&shared)[kThreads]) {
-    raise(columns(order_of(lane_max) >> 16, shared));
-  }
-  // Before the elements of a later batch, whose largest in this lane is `largest` (of all so far: lane_max).
+  // Before the elements of a later batch of a wavefront, whose largest in this lane is `largest` (of all
+  // so far: lane_max).
   __device__ __forceinline__ void next_batch(float largest, float lane_max) {
-    bound = fmaxf(bound, above(base));
     if (__popcll(__ballot(largest >= bound)) > kFewLanes) raise(order_of(lane_max) >> 16);
   }
+  // An element of a later batch must exceed base.
+  __device__ __forceinline__ void end_batch() { bound = fmaxf(bound, above(base)); }
   // The next larger number.
   static __device__ __forceinline__ float above(float x) {
     const uint32_t b = __float_as_uint(x);
     return x == 0.f ? __uint_as_float(1u) : __uint_as_float((b >> 31) ? b - 1 : b + 1);
   }
-  // Cut to the k best, in order.
+  // Cut to the k best, in order: the largest below the one before, k times.
   __device__ __forceinline__ void cut() {
-    constexpr int R = (kWaveKeys + 63) / 64;
     const int lane = threadIdx.x & 63;
-    unsigned long long mine[R], kth = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) mine[i] = i * 64 + lane < n ? keys[i * 64 + lane] : 0;
-    for (int r = 0; r < k; ++r) {
-      unsigned long long best = mine[0];
-#pragma unroll
-      for (int i = 1; i < R; ++i) best = max(best, mine[i]);
+    unsigned long long kth = ~0ull, kept = 0;
+    for (int r = 0; r < min(n, k); ++r) {
+      unsigned long long best = 0;
+      for (int i = lane; i < n; i += 64)
+        if (keys[i] < kth) best = max(best, keys[i]);
 #pragma unroll
       for (int mask = 1; mask < 64; mask <<= 1) best = max(best, (unsigned long long)__shfl_xor((long long)best, mask));
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-        if (mine[i] == best) mine[i] = 0;
-      if (lane == 0) keys[r] = best;
       kth = best;
+      if (lane == r) kept = best;
     }
-    n = min(n, k);
-    if (kth != 0) {
+    if (lane < min(n, k)) keys[lane] = kept;
+    if (n >= k) {
       base = fmaxf(base, key_value(kth));
       bound = fmaxf(bound, base);
     }
+    n = min(n, k);
   }
   // Room for `more` (at most kWaveKeys - k).
   __device__ __forceinline__ void reserve(int more) {
@@ -285,15 +280,27 @@ struct Candidates {
   }
 };
 
-// Ranks by counting: the k largest of n keys to out, largest first; 0 where fewer.  keys is
-// kRankStep keys longer than n and aligned to 16 bytes: the reads go by whole steps, so that they
-// overlap (n counted one by one took 4 us of a call).
+template <int W>
+__device__ __forceinline__ void row_sync() {
+  if constexpr (W > 1) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Ranks by counting, by the threads of W wavefronts: the k largest of n keys to out, largest first; 0
+// where fewer.  keys is kRankStep keys longer than n and aligned to 16 bytes: the reads go by whole
+// steps, so that they overlap.
 constexpr int kRankStep = 8;
+template <int W>
 __device__ __forceinline__ void rank_keys(unsigned long long* keys, int n, int k, unsigned long long* out) {
-  if ((int)threadIdx.x < kRankStep) keys[n + threadIdx.x] = 0;
-  if ((int)threadIdx.x < k && (int)threadIdx.x >= n) out[threadIdx.x] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kThreads) {
+  const int t = threadIdx.x % (64 * W);
+  if (t < kRankStep) keys[n + t] = 0;
+  if (t < k && t >= n) out[t] = 0;
+  row_sync<W>();
+  for (int i = t; i < n; i += 64 * W) {
     const unsigned long long key = keys[i];
     int rank = 0;
     for (int j = 0; j < n; j += kRankStep) {
@@ -305,6 +312,7 @@ __device__ __forceinline__ void rank_keys(unsigned long long* keys, int n, int k
     }
     if (rank < k) out[rank] = key;
   }
+  row_sync<W>();
 }
 
 __device__ __forceinline__ void publish(float* p, float x) {
@@ -318,18 +326,21 @@ __device__ __forceinline__ T collect(const T* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <bool BF, bool TOP>
+template <bool BF, bool TOP, int W>
 __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
   using V = Vec<BF>;
-  constexpr int kWaves = kThreads / 64;
+  constexpr int L = 64 * W;  // lanes of a row
+  constexpr int kRows = kWaves / W;
   __shared__ Part parts[kWaves];
-  __shared__ __attribute__((aligned(16))) unsigned long long wave_keys[TOP ? kWaves : 1][TOP ? kWaveKeys : 1];
-  __shared__ __attribute__((aligned(16))) unsigned long long keys[TOP ? kWaves * kKeptKeys + kRankStep : 1];
-  __shared__ unsigned long long best[TOP ? INFS_SCORE_MAX_TOP : 1];
-  __shared__ uint32_t maxima[TOP ? kThreads : 1];
+  __shared__ __attribute__((aligned(16))) unsigned long long wave_keys[TOP ? kWaves : 1][TOP ? kWaveKeys + kRankStep : 1];
+  __shared__ __attribute__((aligned(16))) unsigned long long keys[TOP && W > 1 ? kWaves * kKeptKeys + kRankStep : 1];
+  __shared__ unsigned long long bests[TOP ? kRows : 1][TOP ? INFS_SCORE_MAX_TOP : 1];
+  __shared__ uint32_t maxima[2][TOP && W > 1 ? kThreads : 1];
   __shared__ int counts[kWaves], last;
-  const int piece = (int)(blockIdx.x % (unsigned)a.pieces), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t row = blockIdx.x / (unsigned)a.pieces;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, thread = threadIdx.x % L;
+  const int piece = W > 1 ? (int)(blockIdx.x % (unsigned)a.pieces) : 0;
+  const int64_t row = W > 1 ? blockIdx.x / (unsigned)a.pieces : (int64_t)blockIdx.x * kRows + wave;
+  if (W == 1 && row >= a.rows) return;  // nothing waits for this wavefront
   const RowReader<BF> in(a.logits, row * a.row_stride, a.vocab);
   const float c = a.inv_t * kLog2E;
   // the given token's logit, for whoever finishes the row
@@ -339,10 +350,11 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
 
   Part p = empty_part();
   Candidates top{wave_keys[TOP ? wave : 0], 0, a.top_k, -FLT_MAX, -FLT_MAX};  // masked entries are below
-  const int begin = piece * a.batches * kBatch, end = min(begin + a.batches * kBatch, in.count);
-  for (int first = begin; first < end; first += kBatch) {
+  constexpr int kStep = L * kUnroll;
+  const int begin = W > 1 ? piece * a.batches * kStep : 0, end = W > 1 ? min(begin + a.batches * kStep, in.count) : in.count;
+  for (int first = begin, b = 0, raised = 0; first < end; first += kStep, ++b) {
     u32x4 x[kUnroll];
-    in.load(first, end, x);
+    in.template load<L>(first, end, x);
     float vm[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -350,41 +362,43 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
 #pragma unroll
       for (int i = 1; i < V::N; ++i) vm[u] = fmaxf(vm[u], V::get(x[u], i));
     }
-    const float m = fmaxf(p.m, fmaxf(fmaxf(vm[0], vm[1]), fmaxf(vm[2], vm[3])));
-    const float d = fmaxf((p.m - m) * c, kFar), f = __builtin_amdgcn_exp2f(d);
-    p.w = (p.w + p.s * d) * f;
-    p.s *= f;
-    p.m = m;
+    const float largest = fmaxf(fmaxf(vm[0], vm[1]), fmaxf(vm[2], vm[3]));
+    p = around(p, fmaxf(p.m, largest), c);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
       for (int i = 0; i < V::N; ++i) {
-        const float y = (V::get(x[u], i) - m) * c, e = __builtin_amdgcn_exp2f(y);
+        const float y = (V::get(x[u], i) - p.m) * c, e = __builtin_amdgcn_exp2f(y);
         p.s += e;
         p.w = fmaf(e, fmaxf(y, kFar), p.w);
       }
     if constexpr (TOP) {
-      if (first == begin)
-        top.first_batch(m, maxima);
+      // the bound: from all lanes of the row at batches 0, 1, 2, 4, 8 .., else from the wavefront's
+      if (W > 1 && (b & (b - 1)) == 0)
+        top.raise(columns(order_of(p.m) >> 16, maxima[raised++ & 1]));
       else
-        top.next_batch(fmaxf(fmaxf(vm[0], vm[1]), fmaxf(vm[2], vm[3])), m);
+        top.next_batch(largest, p.m);
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        if (__ballot(vm[u] >= top.bound) == 0) continue;
-        top.template add<BF>(x[u], (first + u * kThreads + (int)threadIdx.x) * V::N - in.lead);
-      }
+      for (int u = 0; u < kUnroll; ++u)
+        if (__ballot(vm[u] >= top.bound) != 0) top.template add<BF>(x[u], (first + u * L + thread) * V::N - in.lead);
+      top.end_batch();
     }
   }
 
-  // the work-group's part
+  // the part of the row's wavefronts
   p = wave_join(p, c);
-  if (lane == 0) parts[wave] = p;
+  if constexpr (W > 1) {
+    if (lane == 0) parts[wave] = p;
+  }
   if constexpr (TOP) {
     if (top.n > kKeptKeys) top.cut();
-    if (lane == 0) counts[wave] = top.n;
+    if (W > 1 && lane == 0) counts[wave] = top.n;
   }
-  __syncthreads();
-  {
+  unsigned long long* best = bests[TOP && W == 1 ? wave : 0];
+  if constexpr (W == 1) {
+    if constexpr (TOP) rank_keys<1>(wave_keys[wave], top.n, a.top_k, best);
+  } else {
+    __syncthreads();
     Part q[kWaves];
     float m = parts[0].m;
 #pragma unroll
@@ -392,89 +406,88 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) q[w] = around(parts[w], m, c);
     p = Part{m, (q[0].s + q[1].s) + (q[2].s + q[3].s), (q[0].w + q[1].w) + (q[2].w + q[3].w)};
-  }
-  unsigned long long* all = wave_keys[0];  // the candidates of all wavefronts, as one array
-  int before = 0, found = 0;               // candidates of the wavefronts before this one, and of all
-  if constexpr (TOP) {
+    int before = 0, found = 0;  // candidates of the wavefronts before this one, and of all
+    if constexpr (TOP) {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) before += counts[w];
-      found += counts[w];
+      for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) before += counts[w];
+        found += counts[w];
+      }
+      if (a.pieces == 1 || found > kPieceKeys) {
+        if (lane < counts[wave]) keys[before + lane] = wave_keys[wave][lane];
+        rank_keys<W>(keys, found, a.top_k, best);
+      }
     }
-    if (a.pieces == 1 || found > kPieceKeys) {
-      if (lane < counts[wave]) keys[before + lane] = wave_keys[wave][lane];
-      rank_keys(keys, found, a.top_k, best);
+    if (a.pieces > 1) {
+      // Hand the part over, and the candidates (more than kPieceKeys: the best); the last work-group
+      // of the row joins them.
+      const int64_t rec = row * a.pieces + piece;
+      if (threadIdx.x == 0) {
+        float* to = a.part + kScorePartStride * rec;
+        publish(to, p.m);
+        publish(to + 1, p.s);
+        publish(to + 2, p.w);
+      }
+      if constexpr (TOP) {
+        unsigned long long* to = a.keys + rec * kPieceKeys;
+        if (found > kPieceKeys) {
+          if ((int)threadIdx.x < kPieceKeys) publish(to + threadIdx.x, (int)threadIdx.x < a.top_k ? best[threadIdx.x] : 0);
+        } else {
+          if (lane < counts[wave]) publish(to + before + lane, wave_keys[wave][lane]);
+          if ((int)threadIdx.x >= found && (int)threadIdx.x < kPieceKeys) publish(to + threadIdx.x, 0);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have reached the coherence point
       __syncthreads();
-    }
-  }
-
-  if (a.pieces > 1) {
-    // Hand the part over, and the candidates (more than kPieceKeys: the best); the last work-group
-    // of the row joins them.
-    const int64_t rec = row * a.pieces + piece;
-    if (threadIdx.x == 0) {
-      float* to = a.part + kScorePartStride * rec;
-      publish(to, p.m);
-      publish(to + 1, p.s);
-      publish(to + 2, p.w);
-    }
-    if constexpr (TOP) {
-      unsigned long long* to = a.keys + rec * kPieceKeys;
-      if (found > kPieceKeys) {
-        if ((int)threadIdx.x < kPieceKeys) publish(to + threadIdx.x, (int)threadIdx.x < a.top_k ? best[threadIdx.x] : 0);
-      } else {
-        if (lane < counts[wave]) publish(to + before + lane, wave_keys[wave][lane]);
-        if ((int)threadIdx.x >= found && (int)threadIdx.x < kPieceKeys) publish(to + threadIdx.x, 0);
+      if (threadIdx.x == 0) {
+        int32_t* arrived = a.arrived + row * kCounterStride;
+        last = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
+        if (last) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+        counts[0] = 0;
       }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-    __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have reached the coherence point
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      last = __hip_atomic_fetch_add(a.arrived + row * kCounterStride, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
-      if (last) __hip_atomic_store(a.arrived + row * kCounterStride, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
-      counts[0] = 0;
-    }
-    __syncthreads();
-    if (!last) return;
-    constexpr int kMine = TOP ? kMaxPieces * kPieceKeys / kThreads : 1;
-    unsigned long long mine[kMine];
-    if constexpr (TOP) {
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const int at = i * kThreads + (int)threadIdx.x;
-        mine[i] = at < a.pieces * kPieceKeys ? collect(a.keys + row * a.pieces * kPieceKeys + at) : 0;
-      }
-    }
-    if (wave == 0) {
-      Part q = empty_part();
-      if (lane < a.pieces) {
-        const float* r = a.part + kScorePartStride * (row * a.pieces + lane);
-        q = Part{collect(r), collect(r + 1), collect(r + 2)};
-      }
-      q = wave_join(q, c);
-      if (lane == 0) parts[0] = q;
-    }
-    if constexpr (TOP) {
-      // the best of them, again by a bound that at least k reach
-      unsigned long long largest = mine[0];
-#pragma unroll
-      for (int i = 1; i < kMine; ++i) largest = max(largest, mine[i]);
-      const uint32_t least = kth_largest(columns((uint32_t)(largest >> 48), maxima), a.top_k);
-#pragma unroll
-      for (int i = 0; i < kMine; ++i)
-        if (mine[i] != 0 && (uint32_t)(mine[i] >> 48) >= least) all[atomicAdd(&counts[0], 1)] = mine[i];
       __syncthreads();
-      const int kept = counts[0];
-      rank_keys(all, kept, a.top_k, best);
+      if (!last) return;
+      constexpr int kMine = TOP ? kMaxPieces * kPieceKeys / kThreads : 1;
+      unsigned long long mine[kMine];
+      if constexpr (TOP) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+          const int at = i * kThreads + (int)threadIdx.x;
+          mine[i] = at < a.pieces * kPieceKeys ? collect(a.keys + row * a.pieces * kPieceKeys + at) : 0;
+        }
+      }
+      if (wave == 0) {
+        Part t = empty_part();
+        if (lane < a.pieces) {
+          const float* r = a.part + kScorePartStride * (row * a.pieces + lane);
+          t = Part{collect(r), collect(r + 1), collect(r + 2)};
+        }
+        t = wave_join(t, c);
+        if (lane == 0) parts[0] = t;
+      }
+      if constexpr (TOP) {
+        // the best of them, again by a bound that at least k reach
+        unsigned long long* all = wave_keys[0];  // of all wavefronts, as one array
+        unsigned long long largest = mine[0];
+#pragma unroll
+        for (int i = 1; i < kMine; ++i) largest = max(largest, mine[i]);
+        const uint32_t least = kth_largest(columns((uint32_t)(largest >> 48), maxima[0]), a.top_k);
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+          if (mine[i] != 0 && (uint32_t)(mine[i] >> 48) >= least) all[atomicAdd(&counts[0], 1)] = mine[i];
+        __syncthreads();
+        const int kept = counts[0];
+        rank_keys<W>(all, kept, a.top_k, best);
+      }
+      __syncthreads();
+      p = parts[0];
     }
-    __syncthreads();
-    p = parts[0];
   }
 
   const bool none = p.s == 0.f;  // every entry masked
   const float log2_s = log2f(p.s), ln_s = none ? -__builtin_huge_valf() : log2_s * kLn2;
-  if (threadIdx.x == 0) {
+  if (thread == 0) {
     if (a.logprob) {
       float lp = token == -1 ? 0.f : __builtin_nanf("");
       if (known) lp = none ? -__builtin_huge_valf() : (given - p.m) * a.inv_t - ln_s;
@@ -487,11 +500,11 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a) {
     }
   }
   if constexpr (TOP) {
-    if ((int)threadIdx.x < a.top_k) {
-      const unsigned long long key = best[threadIdx.x];
+    if (thread < a.top_k) {
+      const unsigned long long key = best[thread];
       const bool bad = !(p.s == p.s);
-      a.top_id[row * a.top_k + threadIdx.x] = key == 0 || bad ? -1 : key_id(key);
-      a.top_logprob[row * a.top_k + threadIdx.x] =
+      a.top_id[row * a.top_k + thread] = key == 0 || bad ? -1 : key_id(key);
+      a.top_logprob[row * a.top_k + thread] =
           bad ? __builtin_nanf("") : key == 0 ? -__builtin_huge_valf() : (key_value(key) - p.m) * a.inv_t - ln_s;
     }
   }
@@ -508,7 +521,7 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
   const int first = (int)(blockIdx.x % (unsigned)a.batches) * kBatch;
   const RowReader<BF> in(a.logits, row * a.row_stride, a.vocab);
   u32x4 x[kUnroll];
-  in.load(first, in.count, x);
+  in.template load<kThreads>(first, in.count, x);
   char* g = (char*)a.grad + row * a.grad_row_stride * V::ES;
   const bool same = (int)((uintptr_t)g / V::ES % V::N) == in.lead;  // vectors of the two rows coincide
   const float m = a.stats[2 * row], ls2 = a.stats[2 * row + 1] * kLog2E, c = a.inv_t * kLog2E;
@@ -563,6 +576,7 @@ void plan_score(ScoreArgs& a, bool bf16) {
   const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.row_stride % n == 0;  // every row is
   const int64_t all = (a.vocab + (aligned ? 0 : n - 1) + n - 1) / n;            // most vectors of a row
   const int64_t batches = (all + kBatch - 1) / kBatch;
+  a.wave_rows = a.rows >= kScoreWaveRows && all <= kScoreWaveVectors;
   int64_t per = std::max<int64_t>(1, batches * a.rows / kScoreWorkGroups);
   per = std::max(per, (batches + kMaxPieces - 1) / kMaxPieces);
   while ((batches + per - 1) / per > 1 && (batches + per - 1) / per * a.rows > kScoreMaxRecords) ++per;
@@ -574,10 +588,13 @@ void plan_score(ScoreArgs& a, bool bf16) {
 hipError_t launch_score(ScoreArgs& a, bool bf16, hipStream_t stream) {
   if (a.rows == 0) return hipSuccess;
   plan_score(a, bf16);
-  void (*const kernels[2][2])(const ScoreArgs) = {{score_kernel<false, false>, score_kernel<false, true>},
-                                                  {score_kernel<true, false>, score_kernel<true, true>}};
-  hipLaunchKernelGGL(kernels[bf16][a.top_id != nullptr], dim3((unsigned)(a.rows * (int64_t)a.pieces)), dim3(kThreads), 0,
-                     stream, a);
+  void (*const kernels[2][2][2])(const ScoreArgs) = {
+      {{score_kernel<false, false, kWaves>, score_kernel<false, false, 1>},
+       {score_kernel<false, true, kWaves>, score_kernel<false, true, 1>}},
+      {{score_kernel<true, false, kWaves>, score_kernel<true, false, 1>},
+       {score_kernel<true, true, kWaves>, score_kernel<true, true, 1>}}};
+  const int64_t blocks = a.wave_rows ? (a.rows + kWaves - 1) / kWaves : a.rows * (int64_t)a.pieces;
+  hipLaunchKernelGGL(kernels[bf16][a.top_id != nullptr][a.wave_rows], dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
