@@ -179,11 +179,9 @@ def load():
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
-    return int(x.data_ptr())
+    return int(x) if isinstance(x, int) else x.data_ptr()
 
 
 def _stream(s):
@@ -247,8 +245,10 @@ class Rotary:
 
     def rotate_rows(self, dtype, tokens, q=None, k=None, positions=None, first_position=0, inverse=False, stream=None):
         """infs_rotate_rows; q and k are rotary_rows(...)."""
-        _check(None, load().infs_rotate_rows(self._h, _stream(stream), dtype, tokens, _byref(q), _byref(k),
-                                             _ptr(positions), first_position, 1 if inverse else 0))
+        st = _lib.infs_rotate_rows(self._h, _stream(stream), dtype, tokens, _byref(q), _byref(k), _ptr(positions),
+                                   first_position, 1 if inverse else 0)
+        if st != OK:
+            _check(None, st)
 
     def __del__(self):
         try:
@@ -278,15 +278,18 @@ class Scorer:
     def score(self, rows, logits, tokens=None, logprob=None, entropy=None, top_id=None, top_logprob=None, stats=None,
               row_stride=0):
         """infs_score_tokens."""
-        _check(None, load().infs_score_tokens(self._h, rows, _ptr(logits), row_stride, _ptr(tokens), _ptr(logprob),
-                                              _ptr(entropy), _ptr(top_id), _ptr(top_logprob), _ptr(stats)))
+        st = _lib.infs_score_tokens(self._h, rows, _ptr(logits), row_stride, _ptr(tokens), _ptr(logprob), _ptr(entropy),
+                                    _ptr(top_id), _ptr(top_logprob), _ptr(stats))
+        if st != OK:
+            _check(None, st)
 
     def grad(self, rows, logits, tokens, stats, d_logprob, grad, entropy=None, d_entropy=None, row_stride=0,
              grad_row_stride=0):
         """infs_score_grad."""
-        _check(None, load().infs_score_grad(self._h, rows, _ptr(logits), row_stride, _ptr(tokens), _ptr(stats),
-                                            _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(grad),
-                                            grad_row_stride))
+        st = _lib.infs_score_grad(self._h, rows, _ptr(logits), row_stride, _ptr(tokens), _ptr(stats), _ptr(entropy),
+                                  _ptr(d_logprob), _ptr(d_entropy), _ptr(grad), grad_row_stride)
+        if st != OK:
+            _check(None, st)
 
     def destroy(self):
         if self._h:
@@ -322,7 +325,9 @@ class Context:
             pass
 
     def _call(self, fn, *args):
-        _check(self._h, fn(self._h, *args))
+        st = fn(self._h, *args)
+        if st != OK:
+            _check(self._h, st)
 
     def reset(self):
         self._call(load().infs_reset)
@@ -433,7 +438,9 @@ class Context:
 
     def rotate_step(self, rotary, q=None, k=None, num_layers=1):
         """Rotate a running step's rows before it is decoded; q and k are rotary_rows(...)."""
-        self._call(load().infs_rotate_step, rotary._h, num_layers, _byref(q), _byref(k))
+        st = _lib.infs_rotate_step(self._h, rotary._h, num_layers, _byref(q), _byref(k))
+        if st != OK:
+            _check(self._h, st)
 
     def rotate_probe(self, rotary, prompt, first_sample, n, live, q=None, k=None, num_layers=1):
         """Rotate a probe step's rows before it is decoded."""
