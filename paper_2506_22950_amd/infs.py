@@ -10,6 +10,7 @@ there is no fallback.
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -163,11 +164,10 @@ def load():
         "infs_scorer_create": (I32, [ctypes.POINTER(ScorerConfig), P, ctypes.POINTER(P)]),
         "infs_scorer_destroy": (None, [P]),
         "infs_score_tokens": (I32, [P, I32, P, I64, P, P, P, P, P, P]),
-        "infs_fork_slots": (I32, [P, I32, ctypes.POINTER(I32), ctypes.POINTER(I32), ctypes.POINTER(I64),
-                                  ctypes.POINTER(I32)]),
-        "infs_export_responses": (I32, [P, I32, ctypes.POINTER(I32), ctypes.POINTER(P), ctypes.POINTER(P), I64]),
-        "infs_import_responses": (I32, [P, I32, ctypes.POINTER(I32), ctypes.POINTER(I64), ctypes.POINTER(I32),
-                                        ctypes.POINTER(P), ctypes.POINTER(P), I64]),
+        # arrays as packed bytes (_i32s, _i64s, _ptrs)
+        "infs_fork_slots": (I32, [P, I32, P, P, P, P]),
+        "infs_export_responses": (I32, [P, I32, P, P, P, I64]),
+        "infs_import_responses": (I32, [P, I32, P, P, P, P, P, I64]),
         "infs_score_grad": (I32, [P, I32, P, I64, P, P, P, P, P, P, I64]),
     }
     for name, (res, args) in sig.items():
@@ -182,6 +182,18 @@ def _ptr(x):
     if x is None or type(x) is int:
         return x
     return int(x) if isinstance(x, int) else x.data_ptr()
+
+
+def _i32s(x):
+    return struct.pack(f"{len(x)}i", *x)
+
+
+def _i64s(x):
+    return struct.pack(f"{len(x)}q", *x)
+
+
+def _ptrs(x):
+    return struct.pack(f"{len(x)}Q", *[_ptr(y) or 0 for y in x])
 
 
 def _stream(s):
@@ -346,27 +358,23 @@ class Context:
         n = len(src_slots)
         if not (len(dst_slots) == len(sample_ids) == n and (lens is None or len(lens) == n)):
             raise ValueError("one destination, sample (and length) per source")
-        I32, I64 = ctypes.c_int32, ctypes.c_int64
-        self._call(load().infs_fork_slots, n, (I32 * n)(*src_slots), (I32 * n)(*dst_slots), (I64 * n)(*sample_ids),
-                   None if lens is None else (I32 * n)(*lens))
+        self._call(_lib.infs_fork_slots, n, _i32s(src_slots), _i32s(dst_slots), _i64s(sample_ids),
+                   None if lens is None else _i32s(lens))
 
     def export_responses(self, slots, k, v, layer_stride=0):
         """Dense response rows of live slots: k[i], v[i] receive [layers, len, Hkv, d]."""
         n = len(slots)
         if not len(k) == len(v) == n:
             raise ValueError("one K and one V buffer per slot")
-        P = ctypes.c_void_p
-        self._call(load().infs_export_responses, n, (ctypes.c_int32 * n)(*slots), (P * n)(*map(_ptr, k)),
-                   (P * n)(*map(_ptr, v)), layer_stride)
+        self._call(_lib.infs_export_responses, n, _i32s(slots), _ptrs(k), _ptrs(v), layer_stride)
 
     def import_responses(self, slots, sample_ids, lens, k, v, layer_stride=0):
         """Empty slots take samples with responses of lens[i] tokens given as dense rows k[i], v[i]."""
         n = len(slots)
         if not len(sample_ids) == len(lens) == len(k) == len(v) == n:
             raise ValueError("one sample, length, K and V buffer per slot")
-        I32, I64, P = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
-        self._call(load().infs_import_responses, n, (I32 * n)(*slots), (I64 * n)(*sample_ids), (I32 * n)(*lens),
-                   (P * n)(*map(_ptr, k)), (P * n)(*map(_ptr, v)), layer_stride)
+        self._call(_lib.infs_import_responses, n, _i32s(slots), _i64s(sample_ids), _i32s(lens), _ptrs(k), _ptrs(v),
+                   layer_stride)
 
     def decode_step(self, layer, q, k_new, v_new, o):
         self._call(load().infs_decode_step, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o))
