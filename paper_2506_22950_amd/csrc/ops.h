@@ -49,8 +49,8 @@ class StreamDevice {
 };
 
 // ---- rotary positions --------------------------------------------------------
-constexpr int kRotaryThreads = 256;
-constexpr int kRotaryTable = 256;  // (cos, sin) entries of a work-group
+constexpr int kRotaryThreads = 256;  // most of a work-group
+constexpr int kRotaryTable = 256;  // angles of a work-group
 static_assert(INFS_ROTARY_MAX_DIM / 2 <= kRotaryTable, "a token's pairs fit the table");
 
 struct RotaryRows {
@@ -67,12 +67,13 @@ struct RotaryArgs {
   uint64_t live;             // slots: bit t set where token t is rotated (0: every token)
   int32_t tokens, first, head_dim, pairs;
   int32_t tokens_per_wg;     // tokens_per_wg * pairs <= kRotaryTable
+  uint32_t per_unit, per_head;  // 2^32 over the units of a head and over the heads, rounded up
   float amplitude, sign;     // of cos and sin; sign of the angle
   int32_t pos[kMaxSlots];
 };
 static_assert(sizeof(RotaryArgs) <= 4096, "kernel argument block must fit 4 KiB");
 
-// Rotate `layers` layers of rows; fills in tokens_per_wg.
+// Rotate `layers` layers of rows; fills in tokens_per_wg, per_unit and per_head.
 hipError_t launch_rotate(RotaryArgs& args, bool bf16, bool interleaved, int layers, hipStream_t stream);
 
 // Checks and packs one side's rows (op_fail on E_ARG).  es: element bytes.

@@ -15,8 +15,12 @@
 //
 // Bound by memory: every row is read and written once, three operations an
 // element.  A work-group takes one or more tokens with all their heads, so that
-// an angle is computed once per token and layer and read from LDS by every head.
+// an angle is computed once per token and layer and read from LDS by every head;
+// it has as many threads as its tokens have units of work, whose first rows are loaded
+// while the angles are computed.
 #include "ops.h"
+
+#include <algorithm>
 
 namespace infs {
 namespace {
@@ -81,72 +85,156 @@ struct Elem<false> {
   }
 };
 
-// VEC: 16-byte units -- N pairs (32 bytes) of the rotated part, or 16 bytes of the
-// rest of a head; else one pair or one element at a time (pairs, strides or
-// addresses that 16 bytes do not divide).
-template <bool BF, bool INTERLEAVED, bool VEC>
+// What a unit of work is.
+enum Unit {
+  kElement,  // a pair, or an element behind the rotated part: any sizes and alignment
+  kChunk,    // 16 bytes of a head, whose partners may lie in other chunks of it (through LDS): heads of
+             // whole chunks, aligned
+  kPairs     // 16 bytes of first and 16 bytes of second elements of pairs (a chunk behind the rotated part):
+             // the pairs too are whole chunks
+};
+
+// n / d by inv = ceil(2^32 / d): exact where n d < 2^32 (n is below 2^21, d below 2^14; d = 1 has no inv).
+__device__ __forceinline__ int divide(int n, int d, uint32_t inv) { return d == 1 ? n : (int)__umulhi((uint32_t)n, inv); }
+
+template <bool BF>
+struct Row {  // one unit of one head
+  const char* in;
+  char* out;
+  int u, t;  // unit of the head, token of the work-group
+  bool there;
+};
+
+// Unit i of the work-group's nt tokens.
+template <bool BF>
+__device__ __forceinline__ Row<BF> find_unit(const RotaryArgs& a, int i, int t0, int nt, int units, int64_t layer) {
+  constexpr int ES = BF ? 2 : 4;
+  Row<BF> r;
+  const int heads = a.q.heads + a.k.heads;
+  const int head = divide(i, units, a.per_unit), h = head - heads * divide(head, heads, a.per_head);
+  r.u = i - head * units;
+  r.t = divide(head, heads, a.per_head);
+  r.there = r.t < nt && !(a.live && !((a.live >> ((t0 + r.t) & 63)) & 1));
+  const bool is_k = h >= a.q.heads;
+  const RotaryRows& rows = is_k ? a.k : a.q;
+  const int64_t hh = is_k ? h - a.q.heads : h, t = t0 + r.t;
+  r.in = rows.in + (t * rows.in_row + hh * rows.in_head + layer * rows.in_layer) * ES;
+  r.out = rows.out + (t * rows.out_row + hh * rows.out_head + layer * rows.out_layer) * ES;
+  return r;
+}
+
+template <bool BF, bool INTERLEAVED, int UNIT>
 __global__ __launch_bounds__(kRotaryThreads) void rotate_kernel(const RotaryArgs a) {
   using E = Elem<BF>;
-  constexpr int N = VEC ? E::N : 1, ES = BF ? 2 : 4;
-  __shared__ float2 table[kRotaryTable];
+  constexpr int N = UNIT == kElement ? 1 : E::N, ES = BF ? 2 : 4;
+  // (cos, sin); kChunk: whole rows of N columns a token
+  __shared__ float2 table[UNIT == kChunk ? kRotaryTable * N : kRotaryTable];
+  __shared__ __attribute__((aligned(16))) char chunks[UNIT == kChunk && !INTERLEAVED ? kRotaryThreads * 16 : 16];
   const int t0 = blockIdx.x * a.tokens_per_wg, nt = min(a.tokens_per_wg, a.tokens - t0);
   const int64_t layer = blockIdx.y;
-  for (int i = threadIdx.x; i < nt * a.pairs; i += kRotaryThreads) {
-    const int t = t0 + i / a.pairs;
+  const int turned = a.pairs / N;  // kPairs, kElement: units of pairs, then of the rest
+  const int units = UNIT == kChunk ? a.head_dim / N : turned + (a.head_dim - 2 * a.pairs) / N;
+  const int threads = (int)blockDim.x;
+  // kChunk: a head's chunks are in one wavefront, so that each holds whole heads (and idle lanes)
+  const int lane = threadIdx.x & 63, wave_units = UNIT == kChunk ? 64 / units * units : 64;
+  const int step = threads / 64 * wave_units;
+  int i = (int)(threadIdx.x >> 6) * wave_units + lane;
+  const int total = nt * (a.q.heads + a.k.heads) * units;
+  const bool works = lane < wave_units;
+  Row<BF> r = find_unit<BF>(a, i, t0, nt, units, layer);
+  r.there = r.there && works && i < total;
+  // byte offsets of the unit's two halves
+  const auto first_of = [&](int u) {
+    return (UNIT == kChunk ? u * N : u >= turned ? 2 * a.pairs + (u - turned) * N : INTERLEAVED ? 2 * u * N : u * N) * ES;
+  };
+  const auto second_of = [&](int u) { return (INTERLEAVED ? (2 * u + 1) * N : a.pairs + u * N) * ES; };
+  const auto load = [&](const Row<BF>& r, u32x4& x, u32x4& y) {
+    if (UNIT == kElement || !r.there) return;
+    x = *(const u32x4*)(r.in + first_of(r.u));
+    if (UNIT == kPairs && r.u < turned) y = *(const u32x4*)(r.in + second_of(r.u));
+  };
+  // kChunk: a lane's N angles are apart in the table, so that the lanes' next to each other lie together
+  // (16 of them on one bank otherwise)
+  const int columns = (a.pairs + N - 1) / N;
+  const auto place_of = [&](int t, int f) { return UNIT == kChunk ? (t * N + f % N) * columns + f / N : t * a.pairs + f; };
+  u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+  load(r, x, y);
+  for (int j = threadIdx.x; j < nt * a.pairs; j += threads) {
+    const int t = t0 + j / a.pairs;
     const int p = a.positions ? a.positions[t] : a.live ? a.pos[t & (kMaxSlots - 1)] : a.first + t;
     float c, s;
-    turn_of((double)p * a.freq[i % a.pairs], c, s);
-    table[i] = float2{c * a.amplitude, s * a.amplitude * a.sign};
+    turn_of((double)p * a.freq[j % a.pairs], c, s);
+    table[place_of(j / a.pairs, j % a.pairs)] = float2{c * a.amplitude, s * a.amplitude * a.sign};
   }
   __syncthreads();
-  const int turned = a.pairs / N, units = turned + (a.head_dim - 2 * a.pairs) / N;
-  const int heads = a.q.heads + a.k.heads;
-  for (int i = threadIdx.x; i < nt * heads * units; i += kRotaryThreads) {
-    const int u = i % units, h = i / units % heads, t = i / units / heads;
-    if (a.live && !((a.live >> ((t0 + t) & 63)) & 1)) continue;
-    const bool is_k = h >= a.q.heads;
-    const RotaryRows& r = is_k ? a.k : a.q;
-    const int64_t hh = is_k ? h - a.q.heads : h;
-    const char* in = r.in + ((int64_t)(t0 + t) * r.in_row + hh * r.in_head + layer * r.in_layer) * ES;
-    char* out = r.out + ((int64_t)(t0 + t) * r.out_row + hh * r.out_head + layer * r.out_layer) * ES;
-    if (u >= turned) {  // the rest of the head
-      const int e = 2 * a.pairs + (u - turned) * N;
-      if constexpr (VEC)
-        *(u32x4*)(out + e * ES) = *(const u32x4*)(in + e * ES);
-      else
-        E::copy(out, e, in, e);
-      continue;
-    }
-    const float2* cs = table + t * a.pairs + u * N;
-    if constexpr (VEC) {
-      const int e0 = INTERLEAVED ? 2 * u * N : u * N, e1 = INTERLEAVED ? e0 + N : a.pairs + u * N;
-      const u32x4 x = *(const u32x4*)(in + e0 * ES), y = *(const u32x4*)(in + e1 * ES);
-      float lo[N], hi[N];
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if constexpr (INTERLEAVED) {
-          const float p = E::get(2 * j < N ? x : y, 2 * j % N), q = E::get(2 * j < N ? x : y, 2 * j % N + 1);
-          const float ra = fmaf(p, cs[j].x, -(q * cs[j].y)), rb = fmaf(q, cs[j].x, p * cs[j].y);
-          (2 * j < N ? lo : hi)[2 * j % N] = ra;
-          (2 * j < N ? lo : hi)[2 * j % N + 1] = rb;
-        } else {
-          const float p = E::get(x, j), q = E::get(y, j);
-          lo[j] = fmaf(p, cs[j].x, -(q * cs[j].y));
-          hi[j] = fmaf(q, cs[j].x, p * cs[j].y);
-        }
+  while (true) {
+    const float2* cs = table + place_of(r.t, 0);
+    if constexpr (UNIT == kElement) {
+      if (r.there && r.u >= turned) {
+        const int e = 2 * a.pairs + r.u - turned;
+        E::copy(r.out, e, r.in, e);
+      } else if (r.there) {
+        const int e0 = INTERLEAVED ? 2 * r.u : r.u, e1 = INTERLEAVED ? e0 + 1 : a.pairs + e0;
+        const float p = E::load(r.in, e0), q = E::load(r.in, e1);
+        E::store(r.out, e0, fmaf(p, cs[r.u].x, -(q * cs[r.u].y)));
+        E::store(r.out, e1, fmaf(q, cs[r.u].x, p * cs[r.u].y));
       }
-      *(u32x4*)(out + e0 * ES) = E::pack(lo);
-      *(u32x4*)(out + e1 * ES) = E::pack(hi);
+    } else if constexpr (UNIT == kPairs) {
+      if (r.there && r.u >= turned) {
+        __builtin_nontemporal_store(x, (u32x4*)(r.out + first_of(r.u)));
+      } else if (r.there) {
+        cs += r.u * N;
+        float lo[N], hi[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          if constexpr (INTERLEAVED) {
+            const float p = E::get(2 * j < N ? x : y, 2 * j % N), q = E::get(2 * j < N ? x : y, 2 * j % N + 1);
+            (2 * j < N ? lo : hi)[2 * j % N] = fmaf(p, cs[j].x, -(q * cs[j].y));
+            (2 * j < N ? lo : hi)[2 * j % N + 1] = fmaf(q, cs[j].x, p * cs[j].y);
+          } else {
+            const float p = E::get(x, j), q = E::get(y, j);
+            lo[j] = fmaf(p, cs[j].x, -(q * cs[j].y));
+            hi[j] = fmaf(q, cs[j].x, p * cs[j].y);
+          }
+        }
+        // past the L2: what a launch leaves there is written back at its end (2048 tokens 8.9 -> 7.5 us)
+        __builtin_nontemporal_store(E::pack(lo), (u32x4*)(r.out + first_of(r.u)));
+        __builtin_nontemporal_store(E::pack(hi), (u32x4*)(r.out + second_of(r.u)));
+      }
     } else {
-      const int e0 = INTERLEAVED ? 2 * u : u, e1 = INTERLEAVED ? 2 * u + 1 : a.pairs + u;
-      const float p = E::load(in, e0), q = E::load(in, e1);
-      E::store(out, e0, fmaf(p, cs[0].x, -(q * cs[0].y)));
-      E::store(out, e1, fmaf(q, cs[0].x, p * cs[0].y));
+      const char* head = chunks + (threadIdx.x - r.u) * 16;  // the head's elements
+      if constexpr (!INTERLEAVED) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last unit's reads are done
+        *(u32x4*)(chunks + threadIdx.x * 16) = x;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+      if (r.there) {
+        float v[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const int e = r.u * N + j;
+          const bool rest = e >= 2 * a.pairs, second = INTERLEAVED ? j & 1 : e >= a.pairs;
+          const float own = E::get(x, j);
+          float other;
+          if constexpr (INTERLEAVED)
+            other = E::get(x, j ^ 1);
+          else
+            other = E::load(head, rest ? e : second ? e - a.pairs : e + a.pairs);
+          const float2 w = cs[rest ? 0 : place_of(0, INTERLEAVED ? e >> 1 : second ? e - a.pairs : e)];
+          v[j] = rest ? own : fmaf(own, w.x, second ? other * w.y : -(other * w.y));
+        }
+        __builtin_nontemporal_store(E::pack(v), (u32x4*)(r.out + first_of(r.u)));
+      }
     }
+    i += step;
+    if (i - lane >= total) break;  // the same for all lanes of a wavefront
+    r = find_unit<BF>(a, i, t0, nt, units, layer);
+    r.there = r.there && works && i < total;
+    load(r, x, y);
   }
 }
 
-// Whether 16-byte units fit rows r.
+// Whether rows r are aligned to 16 bytes.
 bool vector_rows(const RotaryRows& r, int n) {
   if (r.heads == 0) return true;
   const int64_t s = r.in_row | r.in_head | r.in_layer | r.out_row | r.out_head | r.out_layer;
@@ -158,15 +246,25 @@ bool vector_rows(const RotaryRows& r, int n) {
 hipError_t launch_rotate(RotaryArgs& a, bool bf16, bool interleaved, int layers, hipStream_t stream) {
   if (a.tokens == 0 || layers == 0 || a.q.heads + a.k.heads == 0) return hipSuccess;
   const int n = bf16 ? 8 : 4;
-  const bool vec = a.pairs % n == 0 && (a.head_dim - 2 * a.pairs) % n == 0 && vector_rows(a.q, n) && vector_rows(a.k, n);
-  a.tokens_per_wg = 1;
+  const bool chunks = a.head_dim % n == 0 && vector_rows(a.q, n) && vector_rows(a.k, n);
+  const int unit = !chunks ? kElement : a.pairs % n == 0 && (a.head_dim - 2 * a.pairs) % n == 0 ? kPairs : kChunk;
+  const int units = unit == kElement ? a.head_dim - a.pairs : unit == kChunk ? a.head_dim / n : (a.head_dim - a.pairs) / n;
+  // Tokens of a work-group: one where it fills a work-group's threads, else as many as do, within the
+  // table of angles.
+  const int64_t per_token = (int64_t)(a.q.heads + a.k.heads) * units;
+  a.tokens_per_wg = (int)std::max<int64_t>(1, std::min<int64_t>({kRotaryTable / a.pairs, kRotaryThreads / per_token, a.tokens}));
+  const int64_t lanes = unit == kChunk ? per_token * a.tokens_per_wg * 64 / (64 / units * units) : per_token * a.tokens_per_wg;
+  const int threads = (int)std::min<int64_t>(kRotaryThreads, (lanes + 63) / 64 * 64);
+  a.per_unit = (uint32_t)(((uint64_t(1) << 32) + units - 1) / units);
+  const int heads = a.q.heads + a.k.heads;
+  a.per_head = (uint32_t)(((uint64_t(1) << 32) + heads - 1) / heads);
   const dim3 grid((unsigned)((a.tokens + a.tokens_per_wg - 1) / a.tokens_per_wg), (unsigned)layers);
-  void (*const kernels[2][2][2])(const RotaryArgs) = {
-      {{rotate_kernel<false, false, false>, rotate_kernel<false, false, true>},
-       {rotate_kernel<false, true, false>, rotate_kernel<false, true, true>}},
-      {{rotate_kernel<true, false, false>, rotate_kernel<true, false, true>},
-       {rotate_kernel<true, true, false>, rotate_kernel<true, true, true>}}};
-  hipLaunchKernelGGL(kernels[bf16][interleaved][vec], grid, dim3(kRotaryThreads), 0, stream, a);
+#define INFS_ROTATE(bf, il) \
+  { rotate_kernel<bf, il, kElement>, rotate_kernel<bf, il, kChunk>, rotate_kernel<bf, il, kPairs> }
+  void (*const kernels[2][2][3])(const RotaryArgs) = {{INFS_ROTATE(false, false), INFS_ROTATE(false, true)},
+                                                      {INFS_ROTATE(true, false), INFS_ROTATE(true, true)}};
+#undef INFS_ROTATE
+  hipLaunchKernelGGL(kernels[bf16][interleaved][unit], grid, dim3(threads), 0, stream, a);
   return hipGetLastError();
 }
 

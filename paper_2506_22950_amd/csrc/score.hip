@@ -118,7 +118,8 @@ struct RowReader {
     const int v0 = first + (int)threadIdx.x % L;
     if (first >= lo && first + L * kUnroll <= min(end, hi)) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) x[u] = *(const u32x4*)(at + (int64_t)(v0 + u * L) * 16);
+      for (int u = 0; u < kUnroll; ++u)
+        x[u] = __builtin_nontemporal_load((const u32x4*)(at + (int64_t)(v0 + u * L) * 16));
       return;
     }
     if (lo < hi) {
@@ -558,7 +559,7 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(r[i]);
       }
-      *(u32x4*)(g + (int64_t)e0 * V::ES) = w;
+      __builtin_nontemporal_store(w, (u32x4*)(g + (int64_t)e0 * V::ES));
     } else {
 #pragma unroll
       for (int i = 0; i < V::N; ++i)
