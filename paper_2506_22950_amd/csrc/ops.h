@@ -49,7 +49,8 @@ class StreamDevice {
 };
 
 // ---- rotary positions --------------------------------------------------------
-constexpr int kRotaryThreads = 256;  // most of a work-group
+constexpr int kRotaryThreads = 256;    // most of a work-group (see launch_rotate)
+constexpr int kRotaryFewBlocks = 256;
 constexpr int kRotaryTable = 256;  // angles of a work-group
 static_assert(INFS_ROTARY_MAX_DIM / 2 <= kRotaryTable, "a token's pairs fit the table");
 

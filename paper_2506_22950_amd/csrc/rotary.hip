@@ -88,10 +88,10 @@ struct Elem<false> {
 // What a unit of work is.
 enum Unit {
   kElement,  // a pair, or an element behind the rotated part: any sizes and alignment
-  kChunk,    // 16 bytes of a head, whose partners may lie in other chunks of it (through LDS): heads of
-             // whole chunks, aligned
-  kPairs     // 16 bytes of first and 16 bytes of second elements of pairs (a chunk behind the rotated part):
-             // the pairs too are whole chunks
+  kChunk,    // 16 bytes of a head of whole, aligned chunks; halves: its partners, in other chunks, come
+             // through LDS
+  kPairs     // halves: 16 bytes of first and 16 bytes of second elements (a chunk behind the rotated part),
+             // where the pairs too are whole chunks
 };
 
 // n / d by inv = ceil(2^32 / d): exact where n d < 2^32 (n is below 2^21, d below 2^14; d = 1 has no inv).
@@ -124,10 +124,10 @@ __device__ __forceinline__ Row<BF> find_unit(const RotaryArgs& a, int i, int t0,
 }
 
 template <bool BF, bool INTERLEAVED, int UNIT>
-__global__ __launch_bounds__(kRotaryThreads) void rotate_kernel(const RotaryArgs a) {
+__global__ __launch_bounds__(INTERLEAVED ? 2 * kRotaryThreads : kRotaryThreads) void rotate_kernel(const RotaryArgs a) {
   using E = Elem<BF>;
   constexpr int N = UNIT == kElement ? 1 : E::N, ES = BF ? 2 : 4;
-  // (cos, sin); kChunk: whole rows of N columns a token
+  // (cos, sin); kChunk: up to N whole columns a token
   __shared__ float2 table[UNIT == kChunk ? kRotaryTable * N : kRotaryTable];
   __shared__ __attribute__((aligned(16))) char chunks[UNIT == kChunk && !INTERLEAVED ? kRotaryThreads * 16 : 16];
   const int t0 = blockIdx.x * a.tokens_per_wg, nt = min(a.tokens_per_wg, a.tokens - t0);
@@ -145,18 +145,19 @@ __global__ __launch_bounds__(kRotaryThreads) void rotate_kernel(const RotaryArgs
   r.there = r.there && works && i < total;
   // byte offsets of the unit's two halves
   const auto first_of = [&](int u) {
-    return (UNIT == kChunk ? u * N : u >= turned ? 2 * a.pairs + (u - turned) * N : INTERLEAVED ? 2 * u * N : u * N) * ES;
+    return (UNIT == kChunk || u < turned ? u * N : 2 * a.pairs + (u - turned) * N) * ES;
   };
-  const auto second_of = [&](int u) { return (INTERLEAVED ? (2 * u + 1) * N : a.pairs + u * N) * ES; };
+  const auto second_of = [&](int u) { return (a.pairs + u * N) * ES; };
   const auto load = [&](const Row<BF>& r, u32x4& x, u32x4& y) {
     if (UNIT == kElement || !r.there) return;
-    x = *(const u32x4*)(r.in + first_of(r.u));
-    if (UNIT == kPairs && r.u < turned) y = *(const u32x4*)(r.in + second_of(r.u));
+    x = __builtin_nontemporal_load((const u32x4*)(r.in + first_of(r.u)));
+    if (UNIT == kPairs && r.u < turned) y = __builtin_nontemporal_load((const u32x4*)(r.in + second_of(r.u)));
   };
-  // kChunk: a lane's N angles are apart in the table, so that the lanes' next to each other lie together
-  // (16 of them on one bank otherwise)
-  const int columns = (a.pairs + N - 1) / N;
-  const auto place_of = [&](int t, int f) { return UNIT == kChunk ? (t * N + f % N) * columns + f / N : t * a.pairs + f; };
+  // kChunk: the angles of a chunk are apart in the table, so that those of lanes next to each other lie
+  // together (16 lanes read one bank otherwise)
+  constexpr int kApart = UNIT != kChunk ? 1 : INTERLEAVED ? N / 2 : N;
+  const int columns = (a.pairs + kApart - 1) / kApart;
+  const auto place_of = [&](int t, int f) { return (t * kApart + f % kApart) * columns + f / kApart; };
   u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
   load(r, x, y);
   for (int j = threadIdx.x; j < nt * a.pairs; j += threads) {
@@ -187,15 +188,9 @@ __global__ __launch_bounds__(kRotaryThreads) void rotate_kernel(const RotaryArgs
         float lo[N], hi[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          if constexpr (INTERLEAVED) {
-            const float p = E::get(2 * j < N ? x : y, 2 * j % N), q = E::get(2 * j < N ? x : y, 2 * j % N + 1);
-            (2 * j < N ? lo : hi)[2 * j % N] = fmaf(p, cs[j].x, -(q * cs[j].y));
-            (2 * j < N ? lo : hi)[2 * j % N + 1] = fmaf(q, cs[j].x, p * cs[j].y);
-          } else {
-            const float p = E::get(x, j), q = E::get(y, j);
-            lo[j] = fmaf(p, cs[j].x, -(q * cs[j].y));
-            hi[j] = fmaf(q, cs[j].x, p * cs[j].y);
-          }
+          const float p = E::get(x, j), q = E::get(y, j);
+          lo[j] = fmaf(p, cs[j].x, -(q * cs[j].y));
+          hi[j] = fmaf(q, cs[j].x, p * cs[j].y);
         }
         // past the L2: what a launch leaves there is written back at its end (2048 tokens 8.9 -> 7.5 us)
         __builtin_nontemporal_store(E::pack(lo), (u32x4*)(r.out + first_of(r.u)));
@@ -247,20 +242,25 @@ hipError_t launch_rotate(RotaryArgs& a, bool bf16, bool interleaved, int layers,
   if (a.tokens == 0 || layers == 0 || a.q.heads + a.k.heads == 0) return hipSuccess;
   const int n = bf16 ? 8 : 4;
   const bool chunks = a.head_dim % n == 0 && vector_rows(a.q, n) && vector_rows(a.k, n);
-  const int unit = !chunks ? kElement : a.pairs % n == 0 && (a.head_dim - 2 * a.pairs) % n == 0 ? kPairs : kChunk;
+  const int unit = !chunks ? kElement : !interleaved && a.pairs % n == 0 ? kPairs : kChunk;
   const int units = unit == kElement ? a.head_dim - a.pairs : unit == kChunk ? a.head_dim / n : (a.head_dim - a.pairs) / n;
   // Tokens of a work-group: one where it fills a work-group's threads, else as many as do, within the
   // table of angles.
   const int64_t per_token = (int64_t)(a.q.heads + a.k.heads) * units;
   a.tokens_per_wg = (int)std::max<int64_t>(1, std::min<int64_t>({kRotaryTable / a.pairs, kRotaryThreads / per_token, a.tokens}));
   const int64_t lanes = unit == kChunk ? per_token * a.tokens_per_wg * 64 / (64 / units * units) : per_token * a.tokens_per_wg;
-  const int threads = (int)std::min<int64_t>(kRotaryThreads, (lanes + 63) / 64 * 64);
+  // Twice the threads where a compute unit has one work-group at most and a head's units are 16 bytes
+  // each (interleaved): 16 tokens of 24 heads of 128 take 3.1 us so, 4.2 us in two turns; 7424 tokens of 40
+  // heads 45.7 us so and 37.5 us with 256 threads.
+  const int64_t blocks = (a.tokens + a.tokens_per_wg - 1) / a.tokens_per_wg * (int64_t)layers;
+  const int most = interleaved && blocks <= kRotaryFewBlocks ? 2 * kRotaryThreads : kRotaryThreads;
+  const int threads = (int)std::min<int64_t>(most, (lanes + 63) / 64 * 64);
   a.per_unit = (uint32_t)(((uint64_t(1) << 32) + units - 1) / units);
   const int heads = a.q.heads + a.k.heads;
   a.per_head = (uint32_t)(((uint64_t(1) << 32) + heads - 1) / heads);
   const dim3 grid((unsigned)((a.tokens + a.tokens_per_wg - 1) / a.tokens_per_wg), (unsigned)layers);
 #define INFS_ROTATE(bf, il) \
-  { rotate_kernel<bf, il, kElement>, rotate_kernel<bf, il, kChunk>, rotate_kernel<bf, il, kPairs> }
+  { rotate_kernel<bf, il, kElement>, rotate_kernel<bf, il, kChunk>, il ? nullptr : rotate_kernel<bf, false, kPairs> }
   void (*const kernels[2][2][3])(const RotaryArgs) = {{INFS_ROTATE(false, false), INFS_ROTATE(false, true)},
                                                       {INFS_ROTATE(true, false), INFS_ROTATE(true, true)}};
 #undef INFS_ROTATE
