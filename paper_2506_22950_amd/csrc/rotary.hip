@@ -150,8 +150,8 @@ __global__ __launch_bounds__(INTERLEAVED ? 2 * kRotaryThreads : kRotaryThreads) 
   const auto second_of = [&](int u) { return (a.pairs + u * N) * ES; };
   const auto load = [&](const Row<BF>& r, u32x4& x, u32x4& y) {
     if (UNIT == kElement || !r.there) return;
-    x = __builtin_nontemporal_load((const u32x4*)(r.in + first_of(r.u)));
-    if (UNIT == kPairs && r.u < turned) y = __builtin_nontemporal_load((const u32x4*)(r.in + second_of(r.u)));
+    x = *(const u32x4*)(r.in + first_of(r.u));
+    if (UNIT == kPairs && r.u < turned) y = *(const u32x4*)(r.in + second_of(r.u));
   };
   // kChunk: the angles of a chunk are apart in the table, so that those of lanes next to each other lie
   // together (16 lanes read one bank otherwise)
@@ -192,7 +192,9 @@ __global__ __launch_bounds__(INTERLEAVED ? 2 * kRotaryThreads : kRotaryThreads) 
           lo[j] = fmaf(p, cs[j].x, -(q * cs[j].y));
           hi[j] = fmaf(q, cs[j].x, p * cs[j].y);
         }
-        // past the L2: what a launch leaves there is written back at its end (2048 tokens 8.9 -> 7.5 us)
+        // Past the L2: what a launch leaves there is written back at its end.  Rows that a projection has
+        // just written are loaded through the caches: 7424 tokens 25.4 us so, 27.9 us past them (rows from
+        // memory: 30.3 and 28.8); both through the caches 30.6 us.
         __builtin_nontemporal_store(E::pack(lo), (u32x4*)(r.out + first_of(r.u)));
         __builtin_nontemporal_store(E::pack(hi), (u32x4*)(r.out + second_of(r.u)));
       }
