@@ -150,28 +150,34 @@ struct ForkArgs {
 };
 static_assert(sizeof(ForkArgs) <= 4096, "kernel argument block must fit 4 KiB");
 
-// Runs of pages to write into the page table.
+// Pages that follow each other: entries at .. at+count-1 of a list are page, page+1, ...
+struct PageRun {
+  int32_t at, page, count;
+};
+
+// Runs to write into the page table (at: its entries).
 constexpr int kRunsPerLaunch = 300;
 struct PageRuns {
   int32_t* page_table;
   int32_t n;
-  struct Run {
-    int32_t at, page, count;  // entries at .. at+count-1 become page, page+1, ...
-  } run[kRunsPerLaunch];
+  PageRun run[kRunsPerLaunch];
 };
 static_assert(sizeof(PageRuns) <= 4096, "kernel argument block must fit 4 KiB");
 
 // Dense rows <-> pages of several responses.
+constexpr int kRunsInline = 96;
 struct MoveArgs {
   char* pool;
   int64_t layer_bytes, layer_stride;  // layer_stride 0: a response's own rows
-  const int32_t* page_table;
+  int32_t* page_table;
   int32_t pages_per_slot, hkv, n;
   struct Response {
     char *k, *v;
     int32_t seq, len;
-    int32_t first_block, pad_;  // first work-group of the response in a layer
+    int32_t first_block;       // first work-group of the response in a layer
+    int16_t first_run, runs;   // its runs (at: its pages); 0 runs: its pages are in the page table
   } r[kMaxSlots];
+  PageRun run[kRunsInline];    // import: pages taken in this call, which it writes into the page table
 };
 static_assert(sizeof(MoveArgs) <= 4096, "kernel argument block must fit 4 KiB");
 

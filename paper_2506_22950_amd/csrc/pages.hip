@@ -180,7 +180,17 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(const MoveArgs a) {
   const int64_t layer = blockIdx.y, pitch = (int64_t)a.hkv * D * P::ES;
   const int64_t stride = a.layer_stride ? a.layer_stride : r.len * pitch;
   const int64_t row = layer * stride + (int64_t)page * kPageTokens * pitch + head * (D * P::ES);
-  const int64_t pg = a.page_table[(int64_t)r.seq * a.pages_per_slot + page];
+  int32_t* entry = a.page_table + (int64_t)r.seq * a.pages_per_slot + page;
+  int64_t pg = 0;
+  if (r.runs > 0) {
+    for (int j = r.first_run; j < r.first_run + r.runs; ++j) {
+      const int d = page - a.run[j].at;
+      if (d >= 0 && d < a.run[j].count) pg = a.run[j].page + d;
+    }
+    if (layer == 0 && head == 0 && threadIdx.x % P::LANES == 0) *entry = (int32_t)pg;
+  } else {
+    pg = *entry;
+  }
   char* at = a.pool + layer * a.layer_bytes + (pg * a.hkv + head) * (2 * P::HALF);
   const int n = min(kPageTokens, r.len - page * kPageTokens), lane = (int)threadIdx.x % P::LANES;
   if constexpr (OUT)
@@ -217,7 +227,7 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(const ForkArgs a) {
 }
 
 __global__ __launch_bounds__(64) void page_runs_kernel(const PageRuns a) {
-  const PageRuns::Run& r = a.run[blockIdx.x];
+  const PageRun& r = a.run[blockIdx.x];
   for (int i = threadIdx.x; i < r.count; i += 64) a.page_table[r.at + i] = r.page + i;
 }
 

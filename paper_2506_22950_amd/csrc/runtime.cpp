@@ -1689,7 +1689,7 @@ infs::MoveArgs move_args(const infs_ctx* c, int n, const int32_t* slots, const i
   a.n = n;
   for (int i = 0; i < n; ++i)
     a.r[i] = {const_cast<char*>((const char*)k[i]), const_cast<char*>((const char*)v[i]), c->slot_handle[slots[i]], len[i],
-              0, 0};
+              0, 0, 0};
   return a;
 }
 
@@ -1786,35 +1786,49 @@ infs_status infs_import_responses(infs_ctx* c, int32_t n, const int32_t* slots, 
   if (st != INFS_OK) return st;
   if (need > c->free_pages.size())
     return fail(c, INFS_E_CAPACITY, "page pool exhausted: need %zu pages, %zu free", need, c->free_pages.size());
+  std::vector<infs::PageRun> runs;  // of every response after the other, in pages of the response
+  int32_t ends[kMaxMoved];
   try {
+    runs.reserve(need);
     for (int i = 0; i < n; ++i)
       c->seq_pages[handle_of(c, slots[i], sample_ids[i])].reserve(ceil_div(lens[i], infs::kPageTokens));
   } catch (const std::bad_alloc&) {
     return fail(c, INFS_E_NOMEM, "host allocation failed");
   }
-  infs::PageRuns runs;
-  runs.page_table = c->page_table;
-  runs.n = 0;
   for (int i = 0; i < n; ++i) {
-    const int h = handle_of(c, slots[i], sample_ids[i]);
-    std::vector<int32_t>& pages = c->seq_pages[h];
+    std::vector<int32_t>& pages = c->seq_pages[handle_of(c, slots[i], sample_ids[i])];
     for (int j = 0; j < ceil_div(lens[i], infs::kPageTokens); ++j) {
       pages.push_back(take_page(c));
-      if (j > 0 && runs.n > 0 && pages[j] == pages[j - 1] + 1) {
-        ++runs.run[runs.n - 1].count;
-        continue;
-      }
-      if (runs.n == infs::kRunsPerLaunch) {
-        if (!c->dry) HIP_TRY(c, infs::launch_page_runs(runs, c->stream));
-        runs.n = 0;
-      }
-      runs.run[runs.n++] = {h * c->pages_per_slot + j, pages[j], 1};
+      if (j > 0 && pages[j] == pages[j - 1] + 1)
+        ++runs.back().count;
+      else
+        runs.push_back({j, pages[j], 1});
     }
+    ends[i] = (int32_t)runs.size();
     fill_slot(c, slots[i], sample_ids[i], lens[i]);
   }
   if (c->dry) return INFS_OK;
-  HIP_TRY(c, infs::launch_page_runs(runs, c->stream));
   infs::MoveArgs a = move_args(c, n, slots, lens, k_dev, v_dev, layer_stride);
+  if (runs.size() <= infs::kRunsInline) {
+    std::copy(runs.begin(), runs.end(), a.run);
+    for (int i = 0; i < n; ++i) {
+      a.r[i].first_run = (int16_t)(i > 0 ? ends[i - 1] : 0);
+      a.r[i].runs = (int16_t)(ends[i] - a.r[i].first_run);
+    }
+  } else {  // the page table first
+    infs::PageRuns part;
+    part.page_table = c->page_table;
+    part.n = 0;
+    for (int i = 0, j = 0; i < n; ++i)
+      for (; j < ends[i]; ++j) {
+        part.run[part.n] = runs[j];
+        part.run[part.n++].at += a.r[i].seq * c->pages_per_slot;
+        if (part.n < infs::kRunsPerLaunch) continue;
+        HIP_TRY(c, infs::launch_page_runs(part, c->stream));
+        part.n = 0;
+      }
+    HIP_TRY(c, infs::launch_page_runs(part, c->stream));
+  }
   HIP_TRY(c, infs::launch_import(page_format(c), a, c->L, c->stream));
   return INFS_OK;
 }
