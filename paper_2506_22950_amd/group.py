@@ -38,7 +38,8 @@ def schedulers_for(cfg, policy: str, pred=None) -> List[infs.Sched]:
 
 
 def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Callable,
-                log: Optional[list] = None, after_step: Optional[Callable] = None, entry: str = "probe_step") -> int:
+                log: Optional[list] = None, after_step: Optional[Callable] = None, entry: str = "probe_step",
+                rotary: Optional[infs.Rotary] = None) -> int:
     """Probe phase of prefix reuse (Section 4): every sample decodes its first
     min(L_i, k) tokens against the shared prompt, in batches of up to
     ctx.probe_batch samples of one prompt; samples that finish within their
@@ -52,7 +53,15 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
     entry: "probe_step" (one launch per layer) or "probe_step_layers" (every
     layer of a probe step in one launch; the layer strides are read off the
     pointers provide returns for layers 0 and 1).
+    rotary: the rows of q and k_new are rotated in place to their positions
+    before each call (one layer at a time).
     """
+    c = ctx.config
+
+    def rotate(p, first, n, live, rows):
+        ctx.rotate_probe(rotary, p, first, n, live, infs.rotary_rows(rows[0], rows[0], c.num_q_heads),
+                         infs.rotary_rows(rows[1], rows[1], c.num_kv_heads))
+
     nb = ctx.probe_batch
     steps = 0
     for t in range(1, k + 1):
@@ -71,10 +80,16 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
                         strides = [b1[0] - b0[0], b1[1] - b0[1], b1[3] - b0[3]]
                         if b1[2] - b0[2] != strides[1]:
                             raise ValueError("k_new and v_new need the same layer stride")
+                    if rotary is not None:
+                        for layer in range(num_layers):
+                            rotate(p, first, n, live, provide(steps, p, first, n, layer))
                     ctx.probe_step_layers(p, first, n, live, *b0, *strides)
                 else:
                     for layer in range(num_layers):
-                        ctx.probe_step(layer, p, first, n, live, *provide(steps, p, first, n, layer))
+                        rows = provide(steps, p, first, n, layer)
+                        if rotary is not None:
+                            rotate(p, first, n, live, rows)
+                        ctx.probe_step(layer, p, first, n, live, *rows)
                 ctx.end_probe_step()
                 if after_step is not None:
                     after_step(steps)
@@ -91,7 +106,10 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
 def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_layers: int,
                  provide: Callable, after_step: Optional[Callable] = None,
                  log: Optional[list] = None, stop_after: Optional[int] = None,
-                 accepted: Optional[list] = None, reuse: int = 0, entry: str = "decode_step") -> int:
+                 accepted: Optional[list] = None, reuse: int = 0, entry: str = "decode_step",
+                 rotary: Optional[infs.Rotary] = None, scorer: Optional[infs.Scorer] = None,
+                 logits: Optional[Callable] = None, carried: Optional[dict] = None,
+                 unfinished: Optional[Callable] = None) -> int:
     """Decode every sample of every prompt; returns the number of running steps.
 
     lengths[p][i]: true length of sample i of prompt p.
@@ -113,6 +131,17 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
     pointers provide(step, 0) returns, whose layers must be laid out densely
     ([L, S, H, d] for Q, the new K/V rows and O).  A function of the step
     number picks the entry step by step.
+    rotary: the rows of q and k_new are rotated in place to their positions
+    before they are decoded.
+    scorer: scores every step's tokens; logits(step) -> (logits, tokens, outputs)
+    with a row per slot, outputs the keyword arguments of Scorer.score that
+    take the results (logprob=..., entropy=..., ...).
+    carried: {(prompt, sample): (tokens, k, v)}: partial responses of an earlier
+    iteration as dense rows; such a sample resumes after them when it is
+    dispatched (Context.import_responses).
+    unfinished(list of (slot, prompt, sample, tokens)) is called before the
+    samples that a stopped prompt was still decoding are discarded: what it
+    exports (Context.export_responses) can be carried into the next iteration.
     """
     entries = {"decode_step": ctx.decode_step, "decode_step_static": ctx.decode_step_static,
                "decode_step_layers": None}
@@ -125,8 +154,15 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
     Ls = [[int(x) for x in row] for row in lengths]
     done = [[] for _ in range(NP)]
     stopped = [False] * NP
+    c = ctx.config
+    carried = carried or {}
+
+    def rotate(layers, rows):
+        ctx.rotate_step(rotary, infs.rotary_rows(rows[0], rows[0], c.num_q_heads),
+                        infs.rotary_rows(rows[1], rows[1], c.num_kv_heads), num_layers=layers)
 
     def fill():
+        taken = []
         for p in range(NP):
             if stopped[p]:
                 continue
@@ -140,9 +176,19 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
                     if reuse and Ls[p][i] <= reuse:  # finished within its probe tokens
                         sch.done(ls)
                         continue
-                    ctx.refill_slot(s, p, i)
                     slot_sample[s] = i
+                    if (p, i) in carried:
+                        slot_len[s] = carried[p, i][0]
+                        if not slot_len[s] < Ls[p][i]:
+                            raise ValueError(f"sample {i} of prompt {p} was carried over finished")
+                        taken.append(s)
+                        continue
+                    ctx.refill_slot(s, p, i)
                     slot_len[s] = reuse
+        if taken:
+            part = [carried[s // m, slot_sample[s]] for s in taken]
+            ctx.import_responses(taken, [slot_sample[s] for s in taken], [x[0] for x in part], [x[1] for x in part],
+                                 [x[2] for x in part])
 
     fill()
     step = 0
@@ -152,10 +198,19 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
                              for s in range(S)))
         decode = entries[entry_of(step)]
         if decode is None:
-            ctx.decode_step_layers(*provide(step, 0))
+            rows = provide(step, 0)
+            if rotary is not None:
+                rotate(num_layers, rows)
+            ctx.decode_step_layers(*rows)
         else:
             for layer in range(num_layers):
-                decode(layer, *provide(step, layer))
+                rows = provide(step, layer)
+                if rotary is not None:
+                    rotate(1, rows)
+                decode(layer, *rows)
+        if scorer is not None:
+            z, tokens, outputs = logits(step)
+            scorer.score(S, z, tokens, **outputs)
         ctx.end_step()
         if after_step is not None:
             after_step(step)
@@ -175,6 +230,9 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
                     stopped[p] = stop_after is not None and len(done[p]) >= stop_after
         for p in range(NP):
             if stopped[p]:
+                left = [(s, p, slot_sample[s], slot_len[s]) for s in range(p * m, (p + 1) * m) if slot_sample[s] >= 0]
+                if unfinished is not None and left:
+                    unfinished(left)
                 for s in range(p * m, (p + 1) * m):
                     if slot_sample[s] >= 0:
                         ctx.retire_slot(s)

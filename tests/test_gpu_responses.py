@@ -288,3 +288,31 @@ def test_two_contexts_and_another_stream():
         assert np.array_equal(stored(fmt, x), y)
     a.destroy()
     b.destroy()
+
+
+def test_import_into_hundreds_of_runs():
+    # two responses grow by turns, one goes: every second page is free, each a run of its own, more than
+    # one launch names
+    import torch
+
+    fmt, L, n = ("f32", 64, 1, 1, 4), 1, 16 * 330
+    ctx = context(fmt, L=L, cap=n, pages=2 * 330 + 40)
+    ctx.refill_slot(0, 0, 0)
+    ctx.refill_slot(1, 0, 1)
+    q = torch.zeros(4, 1, 64, device="cuda")
+    k, v = rows(fmt, 4, L, 6)
+    o = torch.empty(4, 1, 64, device="cuda")
+    for _ in range(n):
+        ctx.decode_step(0, q, k[0], v[0], o)
+        ctx.end_step()
+    ctx.retire_slot(0)
+    nk, nv = rows(fmt, n, L, 7)
+    part = 16 * 120 + 5  # more runs than a launch carries along
+    ctx.import_responses([2, 3], [5, 6], [part, n - part], [nk[:, :part].contiguous(), nk[:, part:].contiguous()],
+                         [nv[:, :part].contiguous(), nv[:, part:].contiguous()])
+    got = export(ctx, fmt, [2, 3, 1], L)
+    for x, i in ((nk, 0), (nv, 1)):
+        assert np.array_equal(np.concatenate([got[0][i], got[1][i]], 1), x.double().cpu().numpy())
+    assert np.array_equal(got[2][0], np.repeat(k[:, 1:2].double().cpu().numpy(), n, axis=1))
+    ctx.sync()
+    ctx.destroy()
