@@ -419,7 +419,7 @@ const char* infs_last_error(const infs_ctx* ctx);
  * context dtype, as infs_prefill_shared takes a prompt's; layer l at + l * layer_stride bytes (0: the rows of
  * that response; else a multiple of 16, at least the longest response's rows; responses of one call share it).
  * E_ARG: n outside [0, 64], null or misaligned arrays and buffers, slots or samples out of range or twice in one
- * call.  E_STATE: a step is open, a source slot is empty, a slot to fill is live, or the sample has probe tokens.
+ * call, more than 2^24 pages times KV heads to hand out or take in.  E_STATE: a step is open, a source slot is empty, a slot to fill is live, or the sample has probe tokens.
  * E_DUP: the sample was already dispatched.  E_CAPACITY: too few free pages, or a len above max_suffix_len.
  * An error changes nothing.  Tokens taken in or shared are not counted by infs_sample_tokens.
  * ------------------------------------------------------------------------------------------- */
@@ -539,7 +539,7 @@ infs_status infs_rotate_probe(infs_ctx* ctx, const infs_rotary* r, int32_t promp
 typedef struct infs_scorer_config {
     int32_t vocab;       /* entries of a row, 1 .. 2^24 */
     int32_t dtype;       /* infs_dtype of logits and gradients */
-    int32_t max_rows;    /* rows of one call, 1 .. 2^24 */
+    int32_t max_rows;    /* rows of one call, 1 .. 2^23 */
     int32_t top_k;       /* alternatives per row, 0 .. INFS_SCORE_MAX_TOP */
     float temperature;   /* T in [2^-20, 2^20]; 0: 1 */
     uint32_t flags;      /* INFS_FLAG_DRY_RUN: arguments are checked, nothing is allocated or launched */

@@ -190,7 +190,7 @@ infs_status infs_scorer_create(const infs_scorer_config* cfg, void* hip_stream, 
   const infs_scorer_config& k = *cfg;
   if (k.vocab < 1 || k.vocab > (1 << 24)) return op_fail(INFS_E_ARG, "vocab must be in [1, 2^24]");
   if (k.dtype != INFS_F32 && k.dtype != INFS_BF16) return op_fail(INFS_E_ARG, "dtype must be INFS_F32 or INFS_BF16");
-  if (k.max_rows < 1 || k.max_rows > (1 << 24)) return op_fail(INFS_E_ARG, "max_rows must be in [1, 2^24]");
+  if (k.max_rows < 1 || k.max_rows > infs::kScoreMaxRows) return op_fail(INFS_E_ARG, "max_rows must be in [1, 2^23]");
   if (k.top_k < 0 || k.top_k > INFS_SCORE_MAX_TOP) return op_fail(INFS_E_ARG, "top_k must be in [0, %d]", INFS_SCORE_MAX_TOP);
   if (k.temperature != 0.f && !(k.temperature >= 0x1p-20f && k.temperature <= 0x1p20f))
     return op_fail(INFS_E_ARG, "temperature must be 0 (for 1) or in [2^-20, 2^20]");

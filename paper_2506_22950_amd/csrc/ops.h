@@ -48,6 +48,9 @@ class StreamDevice {
   hipError_t status_ = hipSuccess;
 };
 
+// Work-groups of 256 threads of one launch: a grid's threads along an axis are counted in 32 bits.
+constexpr int64_t kMostBlocks = int64_t(1) << 23;
+
 // ---- rotary positions --------------------------------------------------------
 constexpr int kRotaryThreads = 256;    // most of a work-group (see launch_rotate)
 constexpr int kRotaryFewBlocks = 256;
@@ -84,6 +87,8 @@ infs_status pack_rotary_rows(const infs_rows* r, const char* what, int head_dim,
 void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a);
 
 // ---- scores of tokens -----------------------------------------------------------
+constexpr int kScoreMaxRows = 1 << 23;
+static_assert(kScoreMaxRows <= kMostBlocks, "a work-group a row");
 constexpr int kScoreMaxPieces = 32;      // pieces of a row
 constexpr int kScorePieceKeys = 64;      // candidates that a piece hands over
 constexpr int kScorePartStride = 32;     // floats: no two work-groups write one 128-byte line

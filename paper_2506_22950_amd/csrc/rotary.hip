@@ -260,14 +260,26 @@ hipError_t launch_rotate(RotaryArgs& a, bool bf16, bool interleaved, int layers,
   a.per_unit = (uint32_t)(((uint64_t(1) << 32) + units - 1) / units);
   const int heads = a.q.heads + a.k.heads;
   a.per_head = (uint32_t)(((uint64_t(1) << 32) + heads - 1) / heads);
-  const dim3 grid((unsigned)((a.tokens + a.tokens_per_wg - 1) / a.tokens_per_wg), (unsigned)layers);
 #define INFS_ROTATE(bf, il) \
   { rotate_kernel<bf, il, kElement>, rotate_kernel<bf, il, kChunk>, il ? nullptr : rotate_kernel<bf, false, kPairs> }
   void (*const kernels[2][2][3])(const RotaryArgs) = {{INFS_ROTATE(false, false), INFS_ROTATE(false, true)},
                                                       {INFS_ROTATE(true, false), INFS_ROTATE(true, true)}};
 #undef INFS_ROTATE
-  hipLaunchKernelGGL(kernels[bf16][interleaved][unit], grid, dim3(threads), 0, stream, a);
-  return hipGetLastError();
+  const int64_t per_launch = kMostBlocks / 2 * a.tokens_per_wg;  // tokens of a launch
+  for (int64_t left = a.tokens; left > 0; left -= per_launch) {
+    a.tokens = (int32_t)std::min(per_launch, left);
+    const dim3 grid((unsigned)((a.tokens + a.tokens_per_wg - 1) / a.tokens_per_wg), (unsigned)layers);
+    hipLaunchKernelGGL(kernels[bf16][interleaved][unit], grid, dim3(threads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    for (RotaryRows* r : {&a.q, &a.k}) {
+      r->in += per_launch * r->in_row * (bf16 ? 2 : 4);
+      r->out += per_launch * r->out_row * (bf16 ? 2 : 4);
+    }
+    if (a.positions) a.positions += per_launch;
+    if (left > per_launch) a.first += (int32_t)per_launch;
+  }
+  return hipSuccess;
 }
 
 }  // namespace infs

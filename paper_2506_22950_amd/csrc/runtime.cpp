@@ -1666,6 +1666,10 @@ void fill_slot(infs_ctx* c, int slot, int64_t sample, int len) {
 infs_status check_dense(infs_ctx* c, int n, const int32_t* len, const void* const* k, const void* const* v, int64_t stride) {
   const int64_t row = (int64_t)c->Hkv * c->D * (int64_t)c->es;
   if (stride < 0 || stride % 16) return fail(c, INFS_E_ARG, "layer_stride must be 0 or a positive multiple of 16 bytes");
+  int64_t units = 0;
+  for (int i = 0; i < n; ++i) units += (int64_t)ceil_div(len[i], infs::kPageTokens) * c->Hkv;
+  if (units > 2 * infs::kMostBlocks)
+    return fail(c, INFS_E_ARG, "%lld pages times KV heads in one call (limit %lld)", (long long)units, (long long)(2 * infs::kMostBlocks));
   for (int i = 0; i < n; ++i) {
     if (len[i] == 0) continue;
     if (stride && c->L > 1 && stride < len[i] * row)

@@ -612,7 +612,7 @@ hipError_t launch_score_grad(ScoreGradArgs& a, bool bf16, hipStream_t stream) {
   // work-groups; longer ones do not (4096 x 5003 in more batches 22.1 us, 20.0 us with work-groups).
   const bool wave_rows = a.rows >= kScoreWorkGroups && vectors <= 64 * kUnroll;
   a.batches = (int)((vectors + kBatch - 1) / kBatch);
-  const int64_t most = INT32_MAX / a.batches;  // rows of a launch
+  const int64_t most = kMostBlocks / a.batches;  // rows of a launch
 #define INFS_GRAD(bf, h) \
   { score_grad_kernel<bf, h, kWaves>, score_grad_kernel<bf, h, 1> }
   void (*const kernels[2][2][2])(const ScoreGradArgs) = {{INFS_GRAD(false, false), INFS_GRAD(false, true)},

@@ -257,3 +257,23 @@ def test_step_and_probe_positions(bf16):
             length[s] += 1
     ctx.sync()
     ctx.destroy()
+
+
+def test_more_tokens_than_a_launch():
+    # two tokens a work-group (256 angles): over 2^23 tokens go in two launches, in place
+    import torch
+
+    T, d = (1 << 23) + 5, 256
+    r = infs.Rotary(config(head_dim=d, rotary_dim=d))
+    f, amp = r.frequencies()
+    x = torch.ones(T, 1, d, dtype=torch.bfloat16, device="cuda")
+    at = [0, 1, (1 << 22) + 3, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, T - 1]
+    y, yn = make((len(at), 1, d), True, 51)
+    x[at] = y
+    for positions in (None, torch.arange(T, dtype=torch.int32, device="cuda") + 7):
+        z = x.clone()
+        r.rotate_rows(infs.BF16, T, k=infs.rotary_rows(z, z, 1), positions=positions, first_position=7,
+                      stream=torch.cuda.current_stream())
+        check(z[at], *rotated(yn, 7 + np.array(at), f, amp, infs.ROTARY_HALF, d), True, far=2.0 ** -24)
+        same, _ = rotated(np.ones((2, 1, d)), [7 + 5, 7 + T - 3], f, amp, infs.ROTARY_HALF, d)
+        assert np.abs(z[[5, T - 3]].double().cpu().numpy() - same).max() < 2 ** -7

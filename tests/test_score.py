@@ -25,7 +25,7 @@ def status(call, *a, **kw):
 
 
 @pytest.mark.parametrize("over", [
-    {"vocab": 0}, {"vocab": (1 << 24) + 1}, {"dtype": 2}, {"max_rows": 0}, {"max_rows": (1 << 24) + 1}, {"top_k": -1},
+    {"vocab": 0}, {"vocab": (1 << 24) + 1}, {"dtype": 2}, {"max_rows": 0}, {"max_rows": (1 << 23) + 1}, {"top_k": -1},
     {"top_k": infs.SCORE_MAX_TOP + 1}, {"temperature": -1.0}, {"temperature": math.nan}, {"temperature": math.inf},
     {"temperature": 2.0 ** -21}, {"temperature": 2.0 ** 21}, {"flags": 2}, {"flags": 4}])
 def test_config_refusals(over):
@@ -33,7 +33,7 @@ def test_config_refusals(over):
 
 
 def test_config_limits_are_allowed():
-    for over in ({"vocab": 1}, {"vocab": 1 << 24}, {"max_rows": 1 << 24}, {"top_k": 0}, {"top_k": 32},
+    for over in ({"vocab": 1}, {"vocab": 1 << 24}, {"max_rows": 1 << 23}, {"top_k": 0}, {"top_k": 32},
                  {"temperature": 0.0}, {"temperature": 2.0 ** -20}, {"temperature": 2.0 ** 20}):
         infs.Scorer(config(**over)).destroy()
 
