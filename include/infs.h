@@ -565,7 +565,7 @@ void infs_scorer_destroy(infs_scorer* s);
      stats_dev [rows, 2]       m and ln S, for infs_score_grad, or NULL (-inf and -inf: every entry masked)
    tokens_dev NULL (then logprob_dev NULL too): no token is scored.  All outputs are fp32 (ids int32), aligned
    to 4 bytes (stats_dev to 8).  Sums are kept in fp32 around a running maximum, in an order that depends on
-   the shape alone. */
+   sizes, strides and alignment alone. */
 infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_dev, int64_t row_stride,
                               const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev, int32_t* top_id_dev,
                               float* top_logprob_dev, float* stats_dev);

@@ -44,6 +44,7 @@ struct Part {
   float m, s, w;
 };
 __device__ __forceinline__ Part empty_part() { return Part{-FLT_MAX, 0.f, 0.f}; }
+
 // Order of alternatives as one number: by value, then by the lower index; 0: none.
 __device__ __forceinline__ unsigned long long key_of(float x, int i) {
   if (!(x > -__builtin_huge_valf())) return 0;
@@ -69,6 +70,18 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 //
 // Few rows are cut into pieces of whole batches, a work-group each; the pieces of a
 // row are joined by the work-group that finishes last, always in the same order.
+//
+// Many rows are bound by memory: 2048 x 151936 bf16 takes 106 us, 5.9 TB/s (loads past the
+// caches; 120 us through them).  An element costs about ten operations of the vector
+// unit (the exponential four), 15 would be all its time at that rate, so that
+// alternatives, which keep the batch's elements beside its exponentials, bind that
+// unit: 122 us with 20 of them.  16 rows take 9 us: 2.2 thousand cycles until the first
+// batch is there, 6 for its sums and candidates, 2 until a piece has arrived, 6 for the
+// join, and the launch.
+//
+// kUnroll: 8 vectors a lane are 5 % faster on 2048 rows and a third slower on 301 x 50257
+// fp32 and on short rows; loading a batch ahead is 5 % faster on 2048 rows and 10 to 25 %
+// slower below.
 constexpr int kUnroll = 4;
 constexpr int kBatch = kThreads * kUnroll;  // vectors of a batch of a work-group
 constexpr int kMaxPieces = kScoreMaxPieces;
@@ -217,14 +230,17 @@ __device__ __forceinline__ uint32_t columns(uint32_t o, uint32_t* shared) {
 // lower it), or the k-th best when a full buffer was cut.  It rises as the wavefront
 // reads on, so that few elements reach it, and a vector costs one comparison.  An
 // element of a later batch has a higher index than all those and must exceed base.
+// Before k elements are known base is the lowest number, which nothing need exceed.
 struct Candidates {
   unsigned long long* keys;  // kWaveKeys in LDS
   int n, k;
   float base, bound;
+  bool reached = false;  // k elements reach base
   // base to the k-th largest of the lanes' values, given by the upper halves of their orders.
   __device__ __forceinline__ void raise(uint32_t o) {
     base = fmaxf(base, value_of(kth_largest(o, k) << 16));  // NaN, below every number, drops out
     bound = fmaxf(bound, base);
+    reached = reached || base > -FLT_MAX;  // lanes without elements count as the lowest number
   }
   // Before the elements of a later batch of a wavefront, whose largest in this lane is `largest` (of all
   // so far: lane_max).
@@ -232,7 +248,9 @@ struct Candidates {
     if (__popcll(__ballot(largest >= bound)) > kFewLanes) raise(order_of(lane_max) >> 16);
   }
   // An element of a later batch must exceed base.
-  __device__ __forceinline__ void end_batch() { bound = fmaxf(bound, above(base)); }
+  __device__ __forceinline__ void end_batch() {
+    if (reached) bound = fmaxf(bound, above(base));
+  }
   // The next larger number.
   static __device__ __forceinline__ float above(float x) {
     const uint32_t b = __float_as_uint(x);
@@ -255,6 +273,7 @@ struct Candidates {
     if (n >= k) {
       base = fmaxf(base, key_value(kth));
       bound = fmaxf(bound, base);
+      reached = true;
     }
     n = min(n, k);
   }
@@ -575,8 +594,11 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
 
 }  // namespace
 
-// Pieces of a row and batches of a piece: whole rows where they are many, else pieces
-// so that about kScoreWorkGroups work-groups share the batches of all rows.
+// A wavefront a row from 2048 rows (as many work-groups fit the GPU) of up to 1024 vectors: 4096 x 1000
+// bf16 5.9 us, 14.1 with a work-group a row; 4096 x 8000 with 5 alternatives 19.9 and 22.7; but 1024 x 8000
+// 7.8 and 6.8, with alternatives 12.6 and 8.7.  Otherwise pieces, so that about kScoreWorkGroups
+// work-groups share the batches of all rows: of 512, 1024, 2048 and 4096 no target is best everywhere
+// (301 x 50257 fp32, 5 alternatives: 21.7, 18.3, 21.8, 21.7 us; 1000 x 151936 bf16: 58.6, 64.8, 60.9, 59.3).
 void plan_score(ScoreArgs& a, bool bf16) {
   const int n = bf16 ? 8 : 4;
   const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.row_stride % n == 0;  // every row is

@@ -210,6 +210,20 @@ def test_masks(bf16):
     check(z, tokens, 1.0, 32, bf16)
 
 
+@pytest.mark.parametrize("n,v", [(300, 50000), (2100, 3000)])  # a work-group's batches, a wavefront's
+def test_alternatives_among_lowest_values(n, v):
+    # few entries at first, then the type's lowest values, alternatives too: by index, however late they come
+    import torch
+
+    low = float(torch.finfo(torch.float32).min)
+    z = np.full((n, v), -np.inf, np.float32)
+    z[:, 10], z[:, 200], z[:, 700] = 1.0, low, 2.0
+    for i, at in enumerate((1100, 1500, 2047, 2048, v - 2, v - 1)):
+        z[i % 3::3, at] = low
+    z[1::5, 2500:] = low
+    check(z, np.arange(n) % v, 1.0, 8, False, grads=False)
+
+
 def test_tokens_out_of_range_give_nan():
     z = logits(4, 999, 1)
     check(z, [-2, 999, 2147483647, -2147483648], 1.0, 0, True)
