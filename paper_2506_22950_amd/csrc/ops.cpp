@@ -58,6 +58,7 @@ struct infs_scorer {
   float inv_t = 1.f;
   hipStream_t stream = nullptr;
   int device = 0;
+  int resident = 0;  // work-groups on the GPU at once, of the kernel that gives all outputs of the scorer
   // Arrivals, parts and candidates of the pieces of rows (see ScoreArgs), zero before the first launch.
   char* workspace = nullptr;
 };
@@ -207,6 +208,7 @@ infs_status infs_scorer_create(const infs_scorer_config* cfg, void* hip_stream, 
     infs::StreamDevice dev(s->stream);
     hipError_t e = dev.status();
     if (e == hipSuccess) e = hipGetDevice(&s->device);
+    if (e == hipSuccess) e = infs::score_resident(s->bf16, cfg->top_k > 0, &s->resident);
     if (e == hipSuccess) e = hipMalloc((void**)&s->workspace, workspace_bytes(*s));
     if (e == hipSuccess) e = hipMemset(s->workspace, 0, workspace_bytes(*s));
     if (e == hipSuccess) e = hipStreamSynchronize(nullptr);  // the stream need not wait for the null stream
@@ -243,7 +245,8 @@ infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_d
     return op_fail(INFS_E_ARG, "tokens and outputs must be aligned to 4 bytes (stats: 8)");
   if (s->dry || rows == 0) return INFS_OK;
   infs::ScoreArgs a{logits_dev, row_stride, tokens_dev, logprob_dev, entropy_dev, top_id_dev, top_logprob_dev, stats_dev,
-                    rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t, 0, 0, 0, nullptr, nullptr, nullptr};
+                    rows, s->cfg.vocab, top_id_dev ? s->cfg.top_k : 0, s->inv_t, 0, 0, 0,
+                    s->resident, nullptr, nullptr, nullptr};
   char* ws = s->workspace;
   a.arrived = (int32_t*)ws;
   a.part = (float*)(ws + infs::kScoreArrivedBytes);

@@ -92,7 +92,6 @@ static_assert(kScoreMaxRows <= kMostBlocks, "a work-group a row");
 constexpr int kScoreMaxPieces = 32;      // pieces of a row
 constexpr int kScorePieceKeys = 64;      // candidates that a piece hands over
 constexpr int kScorePartStride = 32;     // floats: no two work-groups write one 128-byte line
-constexpr int kScoreWorkGroups = 1024;   // work-groups that the rows of a call are cut for
 constexpr int kScoreWaveRows = 2048;     // rows from which ..
 constexpr int kScoreWaveVectors = 1024;  // .. rows of so many 16-byte vectors go a wavefront each
 
@@ -109,6 +108,8 @@ struct ScoreArgs {
   float inv_t;         // 1 / temperature
   int32_t wave_rows;        // 1: a wavefront a row (plan_score); else
   int32_t pieces, batches;  // pieces of a row, batches of a piece
+  int32_t resident;         // work-groups that fit the GPU at once (score_resident), the same whatever outputs are
+                            // asked for: rows are cut, and sums rounded, alike
   // Where rows are cut (pieces > 1), per record row * pieces + piece: the part of a piece (3 floats,
   // kScorePartStride apart) and its candidates [kScorePieceKeys]; and, kCounterStride apart, the pieces
   // of a row that have arrived (0 between launches).
@@ -117,7 +118,7 @@ struct ScoreArgs {
   int32_t* arrived;
 };
 // Rows are cut only where that leaves at most this many records.
-constexpr int kScoreMaxRecords = 2 * kScoreWorkGroups;
+constexpr int kScoreMaxRecords = 2048;
 
 struct ScoreGradArgs {
   const void* logits;
@@ -133,7 +134,10 @@ struct ScoreGradArgs {
   int32_t batches;           // of a row (launch_score_grad)
 };
 
-// Fills in pieces and batches.
+// Work-groups of the forward kernel that the current device keeps resident at once.
+hipError_t score_resident(bool bf16, bool top, int* resident);
+
+// Fills in wave_rows, pieces and batches.
 hipError_t launch_score(ScoreArgs& args, bool bf16, hipStream_t stream);
 // The workspace of a scorer: arrived, part, then (top) keys.
 constexpr size_t kScoreArrivedBytes = sizeof(int32_t) * kCounterStride * kScoreMaxRecords;

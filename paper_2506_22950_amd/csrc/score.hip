@@ -594,21 +594,29 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
 
 }  // namespace
 
+void (*score_kernel_of(bool bf16, bool top, bool wave_rows))(const ScoreArgs) {
+  static void (*const kernels[2][2][2])(const ScoreArgs) = {
+      {{score_kernel<false, false, kWaves>, score_kernel<false, false, 1>},
+       {score_kernel<false, true, kWaves>, score_kernel<false, true, 1>}},
+      {{score_kernel<true, false, kWaves>, score_kernel<true, false, 1>},
+       {score_kernel<true, true, kWaves>, score_kernel<true, true, 1>}}};
+  return kernels[bf16][top][wave_rows];
+}
+
 // A wavefront a row from 2048 rows (as many work-groups fit the GPU) of up to 1024 vectors: 4096 x 1000
 // bf16 5.9 us, 14.1 with a work-group a row; 4096 x 8000 with 5 alternatives 19.9 and 22.7; but 1024 x 8000
-// 7.8 and 6.8, with alternatives 12.6 and 8.7.  Otherwise pieces, so that about kScoreWorkGroups
-// work-groups share the batches of all rows: of 512, 1024, 2048 and 4096 no target is best everywhere
-// (301 x 50257 fp32, 5 alternatives: 21.7, 18.3, 21.8, 21.7 us; 1000 x 151936 bf16: 58.6, 64.8, 60.9, 59.3).
+// 7.8 and 6.8, with alternatives 12.6 and 8.7.  Otherwise as many pieces of a row as leave all work-groups
+// on the GPU at once: a few more than fit would run almost alone at the end (1000 x 151936 bf16 52.6 us, 57.7
+// with pieces for about 1024 work-groups whatever fits; 512 x 151936 with 20 alternatives 42.5 and 45.1;
+// 600 x 20000 fp32, the other way, 12.8 and 12.1).
 void plan_score(ScoreArgs& a, bool bf16) {
   const int n = bf16 ? 8 : 4;
   const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.row_stride % n == 0;  // every row is
   const int64_t all = (a.vocab + (aligned ? 0 : n - 1) + n - 1) / n;            // most vectors of a row
   const int64_t batches = (all + kBatch - 1) / kBatch;
   a.wave_rows = a.rows >= kScoreWaveRows && all <= kScoreWaveVectors;
-  int64_t per = std::max<int64_t>(1, batches * a.rows / kScoreWorkGroups);
-  per = std::max(per, (batches + kMaxPieces - 1) / kMaxPieces);
-  while ((batches + per - 1) / per > 1 && (batches + per - 1) / per * a.rows > kScoreMaxRecords) ++per;
-  const int64_t pieces = (batches + per - 1) / per;
+  const int64_t most = std::min<int64_t>(std::min(a.resident, kScoreMaxRecords) / a.rows, kMaxPieces);
+  const int64_t pieces = std::max<int64_t>(1, std::min(most, batches));
   a.batches = (int)((batches + pieces - 1) / pieces);
   a.pieces = (int)((batches + a.batches - 1) / a.batches);
 }
@@ -616,14 +624,19 @@ void plan_score(ScoreArgs& a, bool bf16) {
 hipError_t launch_score(ScoreArgs& a, bool bf16, hipStream_t stream) {
   if (a.rows == 0) return hipSuccess;
   plan_score(a, bf16);
-  void (*const kernels[2][2][2])(const ScoreArgs) = {
-      {{score_kernel<false, false, kWaves>, score_kernel<false, false, 1>},
-       {score_kernel<false, true, kWaves>, score_kernel<false, true, 1>}},
-      {{score_kernel<true, false, kWaves>, score_kernel<true, false, 1>},
-       {score_kernel<true, true, kWaves>, score_kernel<true, true, 1>}}};
   const int64_t blocks = a.wave_rows ? (a.rows + kWaves - 1) / kWaves : a.rows * (int64_t)a.pieces;
-  hipLaunchKernelGGL(kernels[bf16][a.top_id != nullptr][a.wave_rows], dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(score_kernel_of(bf16, a.top_id != nullptr, a.wave_rows), dim3((unsigned)blocks), dim3(kThreads), 0,
+                     stream, a);
   return hipGetLastError();
+}
+
+hipError_t score_resident(bool bf16, bool top, int* resident) {
+  int per_cu = 0, dev = 0, cus = 0;
+  hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, score_kernel_of(bf16, top, false), kThreads, 0);
+  if (e == hipSuccess) e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e == hipSuccess) *resident = per_cu * cus;
+  return e;
 }
 
 hipError_t launch_score_grad(ScoreGradArgs& a, bool bf16, hipStream_t stream) {
@@ -632,7 +645,7 @@ hipError_t launch_score_grad(ScoreGradArgs& a, bool bf16, hipStream_t stream) {
   const int64_t vectors = (a.vocab + 2 * (n - 1)) / n;  // most of a row
   // Rows of a wavefront's batch go a wavefront each where they are many: 4096 x 1000 bf16 5.9 us, 7.5 us with
   // work-groups; longer ones do not (4096 x 5003 in more batches 22.1 us, 20.0 us with work-groups).
-  const bool wave_rows = a.rows >= kScoreWorkGroups && vectors <= 64 * kUnroll;
+  const bool wave_rows = a.rows >= 1024 && vectors <= 64 * kUnroll;
   a.batches = (int)((vectors + kBatch - 1) / kBatch);
   const int64_t most = kMostBlocks / a.batches;  // rows of a launch
 #define INFS_GRAD(bf, h) \
