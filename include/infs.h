@@ -419,8 +419,9 @@ const char* infs_last_error(const infs_ctx* ctx);
  * context dtype, as infs_prefill_shared takes a prompt's; layer l at + l * layer_stride bytes (0: the rows of
  * that response; else a multiple of 16, at least the longest response's rows; responses of one call share it).
  * E_ARG: n outside [0, 64], null or misaligned arrays and buffers, slots or samples out of range or twice in one
- * call, more than 2^24 pages times KV heads to hand out or take in.  E_STATE: a step is open, a source slot is empty, a slot to fill is live, or the sample has probe tokens.
- * E_DUP: the sample was already dispatched.  E_CAPACITY: too few free pages, or a len above max_suffix_len.
+ * call, more than 2^24 pages times KV heads to hand out or take in.  E_STATE: a step is open, a source slot is
+ * empty, a slot to fill is live, or the sample has probe tokens.  E_DUP: the sample was already dispatched.
+ * E_CAPACITY: too few free pages, or a len above max_suffix_len.
  * An error changes nothing.  Tokens taken in or shared are not counted by infs_sample_tokens.
  * ------------------------------------------------------------------------------------------- */
 

@@ -1,6 +1,6 @@
 // Host side of the operators that need no context: rotary configurations and
-// rows, and scores of tokens.  Arguments are checked before anything is enqueued; messages go to
-// infs_last_error(NULL) of the calling thread.
+// rows, and scores of tokens.  Arguments are checked before anything is
+// enqueued; messages go to infs_last_error(NULL) of the calling thread.
 #include "ops.h"
 
 #include <algorithm>

@@ -1,6 +1,5 @@
 // Launch entry points of the row and page operators (rotary.hip, score.hip,
-// pages.hip), and the
-// error and device helpers their host code shares.
+// pages.hip), and the error and device helpers their host code shares.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

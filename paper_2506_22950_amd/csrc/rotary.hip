@@ -94,7 +94,8 @@ enum Unit {
              // where the pairs too are whole chunks
 };
 
-// n / d by inv = ceil(2^32 / d): exact where n d < 2^32 (n is below 2^21, d below 2^14; d = 1 has no inv).
+// n / d by inv = ceil(2^32 / d): exact where n d < 2^32 (a work-group has fewer than 2^21 units, at most
+// 2^8 to a head, of at most 2^13 heads of one token or 2^8 of several; d = 1 has no inv).
 __device__ __forceinline__ int divide(int n, int d, uint32_t inv) { return d == 1 ? n : (int)__umulhi((uint32_t)n, inv); }
 
 template <bool BF>
@@ -266,20 +267,19 @@ hipError_t launch_rotate(RotaryArgs& a, bool bf16, bool interleaved, int layers,
                                                       {INFS_ROTATE(true, false), INFS_ROTATE(true, true)}};
 #undef INFS_ROTATE
   const int64_t per_launch = kMostBlocks / 2 * a.tokens_per_wg;  // tokens of a launch
-  for (int64_t left = a.tokens; left > 0; left -= per_launch) {
+  for (int64_t left = a.tokens;; left -= per_launch) {
     a.tokens = (int32_t)std::min(per_launch, left);
     const dim3 grid((unsigned)((a.tokens + a.tokens_per_wg - 1) / a.tokens_per_wg), (unsigned)layers);
     hipLaunchKernelGGL(kernels[bf16][interleaved][unit], grid, dim3(threads), 0, stream, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || left <= per_launch) return e;
     for (RotaryRows* r : {&a.q, &a.k}) {
       r->in += per_launch * r->in_row * (bf16 ? 2 : 4);
       r->out += per_launch * r->out_row * (bf16 ? 2 : 4);
     }
     if (a.positions) a.positions += per_launch;
-    if (left > per_launch) a.first += (int32_t)per_launch;
+    a.first += (int32_t)per_launch;
   }
-  return hipSuccess;
 }
 
 }  // namespace infs
