@@ -324,9 +324,10 @@ infs_status infs_set_merge_wait(infs_ctx* ctx, int32_t max_polls);
            work-groups run.
    mode 1: through the L2 of the XCD that runs a KV head's work-groups (fewer trips to the
            coherence point).  Available when infs_create saw, in a probe launch, work-group b run on
-           XCD b % n for the device's n XCDs and num_kv_heads is a multiple of n; then it is the
-           default.  Every work-group checks its XCD again; a mismatch makes the next synchronising
-           call return E_DEVICE (outputs of that launch are invalid).
+           XCD (start + b) % n for the device's n XCDs and num_kv_heads is a multiple of n; then it is the
+           default.  Every work-group checks its XCD again against the first one's (the start may change
+           from launch to launch: it depends on the hardware queue that serves the stream); a mismatch
+           makes the next synchronising call return E_DEVICE (outputs of that launch are invalid).
    mode 2: mode 1 with every work-group's check made to fail, so the error path can be tested.
    E_STATE while a step is open or when mode 1/2 is unavailable (always on dry-run contexts). */
 infs_status infs_set_exchange(infs_ctx* ctx, int32_t mode);

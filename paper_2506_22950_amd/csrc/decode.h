@@ -172,9 +172,9 @@ struct Shape {
 //    producer of that line has arrived, so the L1 never returns an older
 //    copy within one launch that writes each record once.  Valid when every
 //    work-group of a KV head runs on one XCD: work-group b on XCD
-//    b % l2_xcds with Hkv a multiple of l2_xcds, which the host verified
-//    when it created the context and which every work-group checks again (a
-//    mismatch sets the status word).
+//    (start + b) % l2_xcds with Hkv a multiple of l2_xcds, which the host
+//    verified when it created the context and which every work-group checks
+//    again (check_xcd; a mismatch sets the status word).
 // Neither needs an agent-scope fence (on this chip one writes back the whole
 // L2).  Raw buffer resources over the workspace let a lane's 16 bytes leave
 // as one write; offsets are in bytes and below ws_o_bytes / ws_ml_bytes.  The
@@ -187,6 +187,30 @@ constexpr int kLoadCoherent = 16;  // sc1
 constexpr int kStoreL2 = 0;
 constexpr int kLoadL2 = 1;         // sc0: coherent at work-group scope: may hit the CU's L1 (clean at a launch's start), else the XCD's L2
 constexpr int kXccIdReg = 20 | (3 << 11);  // s_getreg operand: HW_REG_XCC_ID bits 3:0
+
+// One thread of every work-group, at its end: the XCD it runs on.  The first work-group's
+// XCD (the start) is a matter of the hardware queue, and a stream that has been idle may
+// go on in another one.  So a work-group that does not find the start seen last waits for
+// the first work-group's, which is dispatched before all others and says so at its own
+// end; the host takes that start over with the next launch.
+__device__ __forceinline__ void check_xcd(const StepArgs& a) {
+  const uint32_t xcd = __builtin_amdgcn_s_getreg(kXccIdReg) & 15, n = (uint32_t)a.l2_xcds;
+  if (__builtin_expect(xcd == (blockIdx.x + (uint32_t)a.l2_start) % n, 1)) return;
+  if (a.l2_seq > 0) {
+    LaunchStatus* const words = (LaunchStatus*)a.status;
+    const int32_t start = (int32_t)((xcd + n - blockIdx.x % n) % n), seen = a.l2_seq * 16 + start;
+    if (blockIdx.x == 0) {
+      __hip_atomic_store(&words->seen, seen, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(words->start, start, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+      return;
+    }
+    for (int i = 0; i < kMergeSpins; ++i) {
+      if (__hip_atomic_load(&words->seen, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == seen) return;
+      __builtin_amdgcn_s_sleep(2);
+    }
+  }
+  __hip_atomic_store(a.status, 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 // MISS_L1: loads miss the CU's L1 also in the XCD-local exchange (sc0 loads
 // are coherent only at work-group scope and may hit a line the L1 kept from
@@ -1781,9 +1805,6 @@ template <class SH, bool L2, bool WAVES>
 __device__ __forceinline__ void decode_block(const StepArgs& a, float* smem, unsigned long long* flagp) {
   const int item = blockIdx.x / a.Hkv;
   const int g = blockIdx.x - item * a.Hkv;
-  if (L2 && threadIdx.x == 0 &&
-      (__builtin_amdgcn_s_getreg(kXccIdReg) & 15) != (int)((blockIdx.x + a.l2_check_shift) % a.l2_xcds))
-    __hip_atomic_store(a.status, 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   if (item < a.n_prefix_items) {
     int p = 0;
     while (p < a.num_prompts - 1 && !(a.prompt[p].nchunks > 0 && item < a.prompt[p].item_begin + a.prompt[p].nchunks))
@@ -1855,6 +1876,7 @@ __global__ __launch_bounds__(kBlockThreads, SH::MIN_WAVES) void decode_kernel(co
     __hip_atomic_fetch_min(a.clock_start + cs, (unsigned long long)__builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED,
                            __HIP_MEMORY_SCOPE_AGENT);
   decode_block<SH, L2, WAVES>(a, smem, &flag);
+  if (L2 && threadIdx.x == 0) check_xcd(a);
   if (a.clock_start) {
     __syncthreads();
     if (threadIdx.x == 0)

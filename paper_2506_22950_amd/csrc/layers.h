@@ -917,9 +917,6 @@ __global__ __launch_bounds__(kBlockThreads, SH::MIN_WAVES) void layers_kernel(co
     __hip_atomic_fetch_min(a.clock_start + cs, (unsigned long long)__builtin_amdgcn_s_memrealtime(), __ATOMIC_RELAXED,
                            __HIP_MEMORY_SCOPE_AGENT);
   if (threadIdx.x == 0) __hip_atomic_store(peer_line(a, blockIdx.x) + 4, cu_id() + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  if (L2 && threadIdx.x == 0 &&
-      (__builtin_amdgcn_s_getreg(kXccIdReg) & 15) != (int)((blockIdx.x + a.l2_check_shift) % a.l2_xcds))
-    __hip_atomic_store(a.status, 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   const int g = blockIdx.x % a.Hkv, j = blockIdx.x / a.Hkv;
   int idx;
   const int role = wg_role(a, j, idx);
@@ -934,6 +931,7 @@ __global__ __launch_bounds__(kBlockThreads, SH::MIN_WAVES) void layers_kernel(co
     }
   } else
     merge_loop<SH, L2>(a, g, idx);
+  if (L2 && threadIdx.x == 0) check_xcd(a);
   if (a.clock_start) {
     __syncthreads();
     if (threadIdx.x == 0)

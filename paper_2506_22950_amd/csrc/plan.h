@@ -21,6 +21,7 @@ constexpr int kMaxPartials = 128;  // prefix + response chunks merged for one sl
 constexpr int kMaxSplit = 4096;    // split-K chunk length limit (a wavefront covers <= 64 pages)
 
 constexpr int kMergeSpins = 1 << 20;   // bound on a merge block's wait for its producers
+constexpr int kMostLaunches = (1 << 27) - 1;  // StepArgs::l2_seq
 constexpr int kCounterStride = 32;     // int32 per arrival counter: each counter has a 128-byte line of its own
 constexpr int kRecordsPerLine = 16;   // (max, sum) records of 8 bytes per 128-byte line
 constexpr int kClockSlots = 16;        // timing slots per launch (see StepArgs::clock_start)
@@ -63,6 +64,13 @@ struct PromptPlan {
   int32_t pad_;
 };
 
+// Device words of a context's launches.
+struct LaunchStatus {
+  int32_t status;  // 0, or why a launch's outputs are invalid
+  int32_t seen;    // l2_seq * 16 + start of the last launch that started on another XCD than l2_start
+  int32_t* start;  // its start, in host memory
+};
+
 struct StepArgs {
   // caller buffers
   const void* q;       // [S, Hq, d]
@@ -100,9 +108,9 @@ struct StepArgs {
   float scale_log2;           // softmax scale * log2(e)
   uint32_t ws_o_bytes;        // size of ws_o (below 2^31)
   uint32_t ws_ml_bytes;       // size of ws_ml
-  int32_t l2_xcds;            // > 0: partials exchanged through the XCD's L2; work-group b runs on XCD
-                              // b % l2_xcds (0: written through to the device coherence point)
-  int32_t l2_check_shift;     // 0; 1 makes every work-group's XCD check fail (error-path tests)
+  int32_t l2_xcds;            // > 0: partials exchanged through the XCD's L2; work-group b runs on XCD (start + b) %
+                              // l2_xcds (0: written through to the device coherence point)
+  int32_t l2_start;           // the start seen last (one more with l2_seq 0: every check fails, for error-path tests)
   int32_t merge_polls;        // bound on a merge block's polls of its counters (kMergeSpins; < 0: none)
   // Step launch through every layer (infs_decode_step_layers); unused by per-layer launches.
   // Layer l reads q + l * q_layer_stride (knew, vnew alike) and writes o + l * o_layer_stride; the
@@ -132,6 +140,7 @@ struct StepArgs {
   int32_t peer_base;                   // progress value before this launch (grows by num_layers a launch)
   // this step
   int32_t n_prefix_items, n_suffix_items, n_zero_items, n_merge_items;
+  int32_t l2_seq;  // number of this launch, 1 .. kMostLaunches, or 0 (see l2_start)
   int32_t num_prompts;
   PromptPlan prompt[kMaxPrompts];
   SlotPlan slot[kMaxSlots];

@@ -53,7 +53,7 @@ struct infs_ctx {
   KernelKey key{};
   int S = 0, m = 0, G = 0, hpk = 0, D = 0, Hkv = 0, Hq = 0, L = 0, NP = 0;
   int pmax_pad = 0, split = 0, prefix_split = 0, pages_per_slot = 0, num_pages = 0, pcmax = 0, scmax = 0;
-  int l2_xcds = 0;    // > 0: work-group b was seen on XCD b % l2_xcds and Hkv is a multiple of it
+  int l2_xcds = 0;    // > 0: work-group b was seen on XCD (start + b) % l2_xcds and Hkv is a multiple of it
   size_t es = 0;      // bytes per Q / K / V element handed over the ABI
   size_t kv_es = 0;   // bytes per stored K / V element (prefix store and pages)
   size_t prefix_layer_bytes = 0, pool_layer_bytes = 0;
@@ -66,7 +66,10 @@ struct infs_ctx {
   float* ws_ml = nullptr;
   int32_t* counters = nullptr;
   int32_t* tokens = nullptr;
-  int32_t* status = nullptr;
+  int32_t* status = nullptr;         // the status word, first of a LaunchStatus
+  int32_t* l2_start_host = nullptr;  // pinned, with l2_xcds > 0
+  bool xcd_check_fails = false;      // exchange mode 2
+  int32_t launches = 0;              // modulo kMostLaunches (StepArgs::l2_seq)
   void* scratch = nullptr;  // this device's static scratch array (infs_decode_step_static)
   int layers_resident = 0;  // work-groups of the step-launch kernel resident at once (0: no step launch)
   int players_resident = 0; // the same for the probe kernel's step launch (0: none)
@@ -195,6 +198,7 @@ void free_device(infs_ctx* c) {
   (void)hipFree(c->counters);
   (void)hipFree(c->tokens);
   (void)hipFree(c->status);
+  if (c->l2_start_host) (void)hipHostFree(c->l2_start_host);
 }
 
 // Counters: one per (slot, KV head) for decode launches [S][Hkv], then the
@@ -509,6 +513,11 @@ infs_status timed_launch(infs_ctx* c, const KernelKey& key, StepArgs& a, int gri
     a.clock_end = t.clocks + ((size_t)t.capacity + t.used) * kClockWords;
     ++t.used;
   }
+  if (c->l2_xcds > 0) {
+    a.l2_start = __atomic_load_n(c->l2_start_host, __ATOMIC_RELAXED) + (c->xcd_check_fails ? 1 : 0);
+    c->launches = c->launches % infs::kMostLaunches + 1;
+    a.l2_seq = c->xcd_check_fails ? 0 : c->launches;
+  }
   HIP_TRY(c, layers ? infs::launch_layers(key, a, grid, c->stream) : infs::launch_decode(key, a, grid, c->stream));
   return INFS_OK;
 }
@@ -534,9 +543,9 @@ StaticLayout static_layout(const infs_ctx* c) {
 }
 
 // Where work-groups run: a probe launch of kProbeBlocks work-groups records
-// each one's XCD.  If work-group b ran on XCD b % n for n distinct XCDs and Hkv
-// is a multiple of n, every KV head's work-groups share one XCD (item * Hkv + g
-// is g modulo n), and partials can be exchanged through that XCD's L2.
+// each one's XCD.  If work-group b ran on XCD (start + b) % n for n distinct XCDs
+// and Hkv is a multiple of n, every KV head's work-groups share one XCD (item *
+// Hkv + g is g modulo n), and partials can be exchanged through that XCD's L2.
 infs_status probe_xcds(infs_ctx* c) {
   constexpr int kProbeBlocks = 4096;
   c->l2_xcds = 0;
@@ -551,8 +560,14 @@ infs_status probe_xcds(infs_ctx* c) {
   if (e != hipSuccess) return device_fail(nullptr, e, "XCD probe");
   const int n = *std::max_element(h.begin(), h.end()) + 1;
   bool ok = n >= 1 && c->Hkv % n == 0;
-  for (int b = 0; ok && b < kProbeBlocks; ++b) ok = h[b] == b % n;
-  if (ok) c->l2_xcds = n;
+  for (int b = 0; ok && b < kProbeBlocks; ++b) ok = h[b] == (h[0] + b) % n;
+  if (!ok) return INFS_OK;
+  e = hipHostMalloc((void**)&c->l2_start_host, sizeof(int32_t), hipHostMallocDefault);
+  if (e != hipSuccess) return device_fail(nullptr, e, "hipHostMalloc(XCD start)");
+  *c->l2_start_host = h[0];
+  e = hipMemcpy(&((infs::LaunchStatus*)c->status)->start, &c->l2_start_host, sizeof c->l2_start_host, hipMemcpyHostToDevice);
+  if (e != hipSuccess) return device_fail(nullptr, e, "hipMemcpy(XCD start)");
+  c->l2_xcds = n;
   return INFS_OK;
 }
 
@@ -743,7 +758,7 @@ infs_status infs_create(const infs_config* cfg, void* hip_stream, infs_ctx** out
     if (st == INFS_OK) st = alloc((void**)&c->ws_ml, sizeof(float) * c->ws_records * 2, "workspace");
     if (st == INFS_OK) st = alloc((void**)&c->counters, counter_bytes(c), "counters");
     if (st == INFS_OK) st = alloc((void**)&c->tokens, sizeof(int32_t) * c->NP * c->G, "token counters");
-    if (st == INFS_OK) st = alloc((void**)&c->status, sizeof(int32_t), "status word");
+    if (st == INFS_OK) st = alloc((void**)&c->status, sizeof(infs::LaunchStatus), "status words");
     if (st != INFS_OK) {
       free_device(c);
       delete c;
@@ -1291,7 +1306,7 @@ infs_status infs_set_exchange(infs_ctx* c, int32_t mode) {
     return fail(c, INFS_E_STATE, "no XCD-local exchange: %s",
                 c->dry ? "dry-run context" : "work-groups of one KV head do not share an XCD on this device");
   c->plan.l2_xcds = mode > 0 ? c->l2_xcds : 0;
-  c->plan.l2_check_shift = mode == 2 ? 1 : 0;
+  c->xcd_check_fails = mode == 2;
   return INFS_OK;
 }
 
@@ -1357,7 +1372,7 @@ infs_status infs_set_step_split(infs_ctx* c, int32_t mode) {
 
 int32_t infs_exchange_mode(const infs_ctx* c) {
   if (!c) return -1;
-  return c->plan.l2_xcds == 0 ? 0 : c->plan.l2_check_shift ? 2 : 1;
+  return c->plan.l2_xcds == 0 ? 0 : c->xcd_check_fails ? 2 : 1;
 }
 
 infs_status infs_probe_state(const infs_ctx* c, int32_t prompt, int64_t sample_id, int32_t* probe_len) {
