@@ -366,3 +366,59 @@ def test_captured_and_replayed(n):
         torch.cuda.synchronize()
         for a, b in zip(e, (lp, h, ids, tl, st, out)):
             assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_lowest_values_at_small_temperatures(bf16):
+    # (z - m) / T passes the type's range: probability 0, no part in any sum
+    import torch
+
+    v = 5003
+    z = logits(3, v, 21)
+    z[0, 100:] = z[1, :4000] = z[2, 1::2] = float(torch.finfo(torch.bfloat16 if bf16 else torch.float32).min)
+    check(z, [7, 4500, 0], 2.0 ** -10, 0, bf16)
+
+
+@pytest.mark.parametrize("n,v", [(5, 9001), (3000, 501), (64, 4096)])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_gradient_over_the_logits(n, v, bf16):
+    import torch
+
+    s, z, tok, lp, h, st = check(logits(n, v, 31), np.arange(n) % v, 1.0, 0, bf16, grads=False)
+    z = z.contiguous()
+    g, gh = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    out = torch.empty_like(z)
+    s.grad(n, z, tok, st, g, out, entropy=h, d_entropy=gh)
+    s.grad(n, z, tok, st, g, z, entropy=h, d_entropy=gh)
+    assert torch.equal(z, out)
+
+
+def test_two_scorers_at_once():
+    # scorers on streams of their own, calls of both in flight; each gives what it gives alone
+    import torch
+
+    n, v, top = 16, 100003, 20
+    z = [torch.from_numpy(logits(n, v, 41 + i)).cuda().to(torch.bfloat16) for i in range(2)]
+    tok = torch.arange(n, dtype=torch.int32, device="cuda")
+
+    def outputs():
+        return (torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, top, dtype=torch.int32, device="cuda"),
+                torch.empty(n, top, device="cuda"), torch.empty(n, 2, device="cuda"))
+
+    def call(s, z, o):
+        s.score(n, z, tok, o[0], entropy=o[1], top_id=o[2], top_logprob=o[3], stats=o[4])
+
+    alone, s = [outputs() for _ in range(2)], scorer(vocab=v, max_rows=n, top_k=top)
+    for i in range(2):
+        call(s, z[i], alone[i])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    scorers = [infs.Scorer(infs.make_scorer_config(vocab=v, dtype=infs.BF16, max_rows=n, top_k=top), stream=x) for x in streams]
+    got = [[outputs() for _ in range(20)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for j in range(20):
+        for i in range(2):
+            call(scorers[i], z[(i + j) % 2], got[i][j])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for j in range(20):
+            assert all(torch.equal(a, b) for a, b in zip(got[i][j], alone[(i + j) % 2])), (i, j)
