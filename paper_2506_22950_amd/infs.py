@@ -224,14 +224,13 @@ def make_rotary_config(**kw) -> RotaryConfig:
     return c
 
 
+_pack_rows = struct.Struct("@PPiqqqqqq").pack  # a Rows
+
+
 def rotary_rows(x, out, heads, in_strides=(0, 0, 0), out_strides=(0, 0, 0)) -> Rows:
     """infs_rows: rows of x go to out (the same buffer: in place); strides (row, head, layer) in
     elements, 0 the dense one."""
-    return Rows(_ptr(x), _ptr(out), heads, *in_strides, *out_strides)
-
-
-def _byref(rows):
-    return None if rows is None else ctypes.byref(rows)
+    return Rows.from_buffer_copy(_pack_rows(_ptr(x) or 0, _ptr(out) or 0, heads, *in_strides, *out_strides))
 
 
 def _flags(live, n):
@@ -257,8 +256,8 @@ class Rotary:
 
     def rotate_rows(self, dtype, tokens, q=None, k=None, positions=None, first_position=0, inverse=False, stream=None):
         """infs_rotate_rows; q and k are rotary_rows(...)."""
-        st = _lib.infs_rotate_rows(self._h, _stream(stream), dtype, tokens, _byref(q), _byref(k), _ptr(positions),
-                                   first_position, 1 if inverse else 0)
+        st = _lib.infs_rotate_rows(self._h, _stream(stream), dtype, tokens, q, k, _ptr(positions), first_position,
+                                   1 if inverse else 0)
         if st != OK:
             _check(None, st)
 
@@ -446,14 +445,13 @@ class Context:
 
     def rotate_step(self, rotary, q=None, k=None, num_layers=1):
         """Rotate a running step's rows before it is decoded; q and k are rotary_rows(...)."""
-        st = _lib.infs_rotate_step(self._h, rotary._h, num_layers, _byref(q), _byref(k))
+        st = _lib.infs_rotate_step(self._h, rotary._h, num_layers, q, k)
         if st != OK:
             _check(self._h, st)
 
     def rotate_probe(self, rotary, prompt, first_sample, n, live, q=None, k=None, num_layers=1):
         """Rotate a probe step's rows before it is decoded."""
-        self._call(load().infs_rotate_probe, rotary._h, prompt, first_sample, n, _flags(live, n), num_layers,
-                   _byref(q), _byref(k))
+        self._call(load().infs_rotate_probe, rotary._h, prompt, first_sample, n, _flags(live, n), num_layers, q, k)
 
     def end_probe_step(self):
         self._call(load().infs_end_probe_step)
