@@ -316,3 +316,28 @@ def test_import_into_hundreds_of_runs():
     assert np.array_equal(got[2][0], np.repeat(k[:, 1:2].double().cpu().numpy(), n, axis=1))
     ctx.sync()
     ctx.destroy()
+
+
+def test_pages_beyond_32_bit_offsets():
+    # 43 responses of 32000 tokens in a layer's pool of 5.6 GB: the last ones' pages lie beyond 4 GiB
+    import torch
+
+    fmt, n, m = ("bf16", 128, 16, 8, 48), 32000, 43
+    ctx = context(fmt, L=1, cap=n, pages=m * 2000 + 8)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    k, v = (torch.randint(-30000, 30000, (n, 8, 128), dtype=torch.int16, device="cuda", generator=g) for _ in range(2))
+    slots = list(range(m))
+    for i in slots:
+        ctx.import_responses([i], [i], [n], [k if i % 2 else v], [v if i % 2 else k])
+    last = m - 1
+    ctx.retire_slot(0)
+    ctx.fork_slots([last, last], [m, m + 1], [m, m + 1], [n, n - 11])
+    bk, bv = torch.zeros_like(k), torch.zeros_like(v)
+    for slot, t in ((1, n), (last - 1, n), (last, n), (m, n), (m + 1, n - 11)):
+        bk.zero_(), bv.zero_()
+        ctx.export_responses([slot], [bk], [bv])
+        odd = slot % 2 if slot < m else last % 2
+        for x, y in ((k if odd else v, bk), (v if odd else k, bv)):
+            assert torch.equal(x[:t], y[:t]) and not bool(y[t:].any()), slot
+    ctx.sync()
+    ctx.destroy()
