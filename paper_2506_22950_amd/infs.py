@@ -164,7 +164,7 @@ def load():
         "infs_scorer_create": (I32, [ctypes.POINTER(ScorerConfig), P, ctypes.POINTER(P)]),
         "infs_scorer_destroy": (None, [P]),
         "infs_score_tokens": (I32, [P, I32, P, I64, P, P, P, P, P, P]),
-        # arrays as packed bytes (_i32s, _i64s, _ptrs)
+        # arrays as packed bytes (_I32, _I64, _ptrs)
         "infs_fork_slots": (I32, [P, I32, P, P, P, P]),
         "infs_export_responses": (I32, [P, I32, P, P, P, I64]),
         "infs_import_responses": (I32, [P, I32, P, P, P, P, P, I64]),
@@ -184,16 +184,23 @@ def _ptr(x):
     return int(x) if isinstance(x, int) else x.data_ptr()
 
 
-def _i32s(x):
-    return struct.pack(f"{len(x)}i", *x)
+class _Packers(dict):
+    """n: what packs n numbers of a type into bytes (an array of slots, samples, lengths or buffers)."""
+
+    def __init__(self, code):
+        self.code = code
+
+    def __missing__(self, n):
+        self[n] = struct.Struct(f"{n}{self.code}").pack
+        return self[n]
 
 
-def _i64s(x):
-    return struct.pack(f"{len(x)}q", *x)
+_I32, _I64, _U64 = _Packers("i"), _Packers("q"), _Packers("Q")
+_NO_TENSOR = frozenset((int, type(None)))
 
 
-def _ptrs(x):
-    return struct.pack(f"{len(x)}Q", *[_ptr(y) or 0 for y in x])
+def _ptrs(n, x):
+    return _U64[n](*[(y or 0) if type(y) in _NO_TENSOR else y.data_ptr() for y in x])
 
 
 def _stream(s):
@@ -350,30 +357,30 @@ class Context:
         self._call(load().infs_refill_slot, slot, prompt, sample_id)
 
     def retire_slot(self, slot):
-        self._call(load().infs_retire_slot, slot)
+        self._call(_lib.infs_retire_slot, slot)
 
     def fork_slots(self, src_slots, dst_slots, sample_ids, lens=None):
         """Branches: dst slot i takes sample_ids[i] with the first lens[i] tokens (None: all) of src slot i."""
         n = len(src_slots)
         if not (len(dst_slots) == len(sample_ids) == n and (lens is None or len(lens) == n)):
             raise ValueError("one destination, sample (and length) per source")
-        self._call(_lib.infs_fork_slots, n, _i32s(src_slots), _i32s(dst_slots), _i64s(sample_ids),
-                   None if lens is None else _i32s(lens))
+        self._call(_lib.infs_fork_slots, n, _I32[n](*src_slots), _I32[n](*dst_slots), _I64[n](*sample_ids),
+                   None if lens is None else _I32[n](*lens))
 
     def export_responses(self, slots, k, v, layer_stride=0):
         """Dense response rows of live slots: k[i], v[i] receive [layers, len, Hkv, d]."""
         n = len(slots)
         if not len(k) == len(v) == n:
             raise ValueError("one K and one V buffer per slot")
-        self._call(_lib.infs_export_responses, n, _i32s(slots), _ptrs(k), _ptrs(v), layer_stride)
+        self._call(_lib.infs_export_responses, n, _I32[n](*slots), _ptrs(n, k), _ptrs(n, v), layer_stride)
 
     def import_responses(self, slots, sample_ids, lens, k, v, layer_stride=0):
         """Empty slots take samples with responses of lens[i] tokens given as dense rows k[i], v[i]."""
         n = len(slots)
         if not len(sample_ids) == len(lens) == len(k) == len(v) == n:
             raise ValueError("one sample, length, K and V buffer per slot")
-        self._call(_lib.infs_import_responses, n, _i32s(slots), _i64s(sample_ids), _i32s(lens), _ptrs(k), _ptrs(v),
-                   layer_stride)
+        self._call(_lib.infs_import_responses, n, _I32[n](*slots), _I64[n](*sample_ids), _I32[n](*lens), _ptrs(n, k),
+                   _ptrs(n, v), layer_stride)
 
     def decode_step(self, layer, q, k_new, v_new, o):
         self._call(load().infs_decode_step, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o))
