@@ -325,9 +325,9 @@ infs_status infs_set_merge_wait(infs_ctx* ctx, int32_t max_polls);
    mode 1: through the L2 of the XCD that runs a KV head's work-groups (fewer trips to the
            coherence point).  Available when infs_create saw, in a probe launch, work-group b run on
            XCD (start + b) % n for the device's n XCDs and num_kv_heads is a multiple of n; then it is the
-           default.  Every work-group checks its XCD again against the first one's (the start may change
-           from launch to launch: it depends on the hardware queue that serves the stream); a mismatch
-           makes the next synchronising call return E_DEVICE (outputs of that launch are invalid).
+           default.  Every work-group checks its XCD again.  The start may change from launch to launch (it
+           depends on the hardware queue that serves the stream); a launch whose work-groups do not agree
+           on one makes the next synchronising call return E_DEVICE (its outputs are invalid).
    mode 2: mode 1 with every work-group's check made to fail, so the error path can be tested.
    E_STATE while a step is open or when mode 1/2 is unavailable (always on dry-run contexts). */
 infs_status infs_set_exchange(infs_ctx* ctx, int32_t mode);
@@ -384,6 +384,13 @@ infs_status infs_step_launch_plan(const infs_ctx* ctx, int32_t nj, const int32_t
 
 /* The current exchange mode (0, 1 or 2); -1 for a NULL context. */
 int32_t infs_exchange_mode(const infs_ctx* ctx);
+
+/* The start of a context's launches in mode 1 as it was seen last: the XCD of the first work-group (-1 for a
+   NULL context or where mode 1 is unavailable), and another value in its place, in [0, n).  Launches enqueued
+   from then on find a changed start until one of them has run, which costs them some microseconds: a way to
+   exercise that path from the host.  E_STATE where mode 1 is unavailable. */
+int32_t infs_exchange_start(const infs_ctx* ctx);
+infs_status infs_set_exchange_start(infs_ctx* ctx, int32_t start);
 
 infs_status infs_get_stats(const infs_ctx* ctx, infs_stats* out);
 

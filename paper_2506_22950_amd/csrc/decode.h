@@ -174,7 +174,7 @@ struct Shape {
 //    work-group of a KV head runs on one XCD: work-group b on XCD
 //    (start + b) % l2_xcds with Hkv a multiple of l2_xcds, which the host
 //    verified when it created the context and which every work-group checks
-//    again (check_xcd; a mismatch sets the status word).
+//    again (check_xcd; launches whose work-groups do not agree are reported).
 // Neither needs an agent-scope fence (on this chip one writes back the whole
 // L2).  Raw buffer resources over the workspace let a lane's 16 bytes leave
 // as one write; offsets are in bytes and below ws_o_bytes / ws_ml_bytes.  The
@@ -190,26 +190,19 @@ constexpr int kXccIdReg = 20 | (3 << 11);  // s_getreg operand: HW_REG_XCC_ID bi
 
 // One thread of every work-group, at its end: the XCD it runs on.  The first work-group's
 // XCD (the start) is a matter of the hardware queue, and a stream that has been idle may
-// go on in another one.  So a work-group that does not find the start seen last waits for
-// the first work-group's, which is dispatched before all others and says so at its own
-// end; the host takes that start over with the next launch.
+// go on in another one.  A work-group that does not find the start seen last adds its term
+// to a sum that is 0 again only if all work-groups of the launch found the same other start
+// (moved_term); the host looks at it where it looks at the status word, and takes the start
+// that the first work-group reports over with the next launch.  Nothing waits.
 __device__ __forceinline__ void check_xcd(const StepArgs& a) {
   const uint32_t xcd = __builtin_amdgcn_s_getreg(kXccIdReg) & 15, n = (uint32_t)a.l2_xcds;
-  if (__builtin_expect(xcd == (blockIdx.x + (uint32_t)a.l2_start) % n, 1)) return;
-  if (a.l2_seq > 0) {
-    LaunchStatus* const words = (LaunchStatus*)a.status;
-    const int32_t start = (int32_t)((xcd + n - blockIdx.x % n) % n), seen = a.l2_seq * 16 + start;
-    if (blockIdx.x == 0) {
-      __hip_atomic_store(&words->seen, seen, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(words->start, start, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-      return;
-    }
-    for (int i = 0; i < kMergeSpins; ++i) {
-      if (__hip_atomic_load(&words->seen, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == seen) return;
-      __builtin_amdgcn_s_sleep(2);
-    }
-  }
-  __hip_atomic_store(a.status, 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (__builtin_expect(a.l2_seq > 0 && xcd == (blockIdx.x + (uint32_t)a.l2_start) % n, 1)) return;
+  LaunchStatus* const words = (LaunchStatus*)a.status;
+  const uint32_t start = start_of(xcd, blockIdx.x, n);
+  if (blockIdx.x == 0) __hip_atomic_store(words->start, (int32_t)start, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  __hip_atomic_fetch_add(&words->moved, moved_term(a.l2_seq, a.l2_seq > 0 ? start : start + blockIdx.x, blockIdx.x,
+                                                   (uint32_t)a.l2_blocks),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // MISS_L1: loads miss the CU's L1 also in the XCD-local exchange (sc0 loads

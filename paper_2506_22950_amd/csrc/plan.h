@@ -21,7 +21,6 @@ constexpr int kMaxPartials = 128;  // prefix + response chunks merged for one sl
 constexpr int kMaxSplit = 4096;    // split-K chunk length limit (a wavefront covers <= 64 pages)
 
 constexpr int kMergeSpins = 1 << 20;   // bound on a merge block's wait for its producers
-constexpr int kMostLaunches = (1 << 27) - 1;  // StepArgs::l2_seq
 constexpr int kCounterStride = 32;     // int32 per arrival counter: each counter has a 128-byte line of its own
 constexpr int kRecordsPerLine = 16;   // (max, sum) records of 8 bytes per 128-byte line
 constexpr int kClockSlots = 16;        // timing slots per launch (see StepArgs::clock_start)
@@ -67,9 +66,28 @@ struct PromptPlan {
 // Device words of a context's launches.
 struct LaunchStatus {
   int32_t status;  // 0, or why a launch's outputs are invalid
-  int32_t seen;    // l2_seq * 16 + start of the last launch that started on another XCD than l2_start
-  int32_t* start;  // its start, in host memory
+  int32_t pad_;
+  uint64_t moved;  // sum of the moved_term()s of all launches: 0 where each one's work-groups agree on its start
+  int32_t* start;  // start of the last launch that started on another XCD than l2_start, in host memory
 };
+
+// The XCD of a launch's first work-group, by work-group b on XCD `xcd` of n under the round robin.
+constexpr uint32_t start_of(uint32_t xcd, uint32_t b, uint32_t n) { return (xcd + n - b % n) % n; }
+
+// What work-group b of `blocks` adds to LaunchStatus::moved where it found another start than
+// StepArgs::l2_start.  All but the first add a weight of the launch and the start, the first takes away
+// blocks - 1 times its own.  So a launch adds nothing if none of them or all of them found one and the
+// same other start; anything else leaves a multiple of an odd number that is not 0 modulo 2^64, or, with
+// several starts, sums of weights that are as good as random (as are those of different launches).
+constexpr uint64_t moved_term(int32_t seq, uint32_t start, uint32_t b, uint32_t blocks) {
+  uint64_t w = ((uint64_t)(uint32_t)seq << 32 | start) + 1;
+  for (int i = 0; i < 3; ++i) {
+    w *= 0x9e3779b97f4a7c15u;  // 2^64 over the golden ratio
+    w ^= w >> 32;
+  }
+  w |= 1;
+  return b > 0 ? w : 0 - (uint64_t)(blocks - 1) * w;
+}
 
 struct StepArgs {
   // caller buffers
@@ -88,8 +106,7 @@ struct StepArgs {
                        // (wrapping); each launch carries the values they reach once its producers
                        // have all arrived.
   int32_t* tokens;     // [num_prompts, G] per-sample token counters
-  int32_t* status;     // device status word: 1 after a merge wait hit its bound, 2 after a work-group
-                       // of an XCD-local exchange ran on another XCD than planned
+  int32_t* status;     // device status word, first of a LaunchStatus: 1 after a merge wait hit its bound
   // Timing mode (else null): kClockSlots start/end slots of this launch,
   // kClockStride apart; block b folds its start into the minimum of slot
   // b % kClockSlots and its end into the maximum of that slot (spread over
@@ -110,7 +127,7 @@ struct StepArgs {
   uint32_t ws_ml_bytes;       // size of ws_ml
   int32_t l2_xcds;            // > 0: partials exchanged through the XCD's L2; work-group b runs on XCD (start + b) %
                               // l2_xcds (0: written through to the device coherence point)
-  int32_t l2_start;           // the start seen last (one more with l2_seq 0: every check fails, for error-path tests)
+  int32_t l2_start;           // the start seen last
   int32_t merge_polls;        // bound on a merge block's polls of its counters (kMergeSpins; < 0: none)
   // Step launch through every layer (infs_decode_step_layers); unused by per-layer launches.
   // Layer l reads q + l * q_layer_stride (knew, vnew alike) and writes o + l * o_layer_stride; the
@@ -140,7 +157,9 @@ struct StepArgs {
   int32_t peer_base;                   // progress value before this launch (grows by num_layers a launch)
   // this step
   int32_t n_prefix_items, n_suffix_items, n_zero_items, n_merge_items;
-  int32_t l2_seq;  // number of this launch, 1 .. kMostLaunches, or 0 (see l2_start)
+  int32_t l2_seq;     // number of this launch, above 0; below: every work-group reports a start of its own, so that
+                      // the check fails (error-path tests)
+  int32_t l2_blocks;  // work-groups of this launch
   int32_t num_prompts;
   PromptPlan prompt[kMaxPrompts];
   SlotPlan slot[kMaxSlots];

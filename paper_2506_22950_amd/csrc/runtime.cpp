@@ -69,7 +69,7 @@ struct infs_ctx {
   int32_t* status = nullptr;         // the status word, first of a LaunchStatus
   int32_t* l2_start_host = nullptr;  // pinned, with l2_xcds > 0
   bool xcd_check_fails = false;      // exchange mode 2
-  int32_t launches = 0;              // modulo kMostLaunches (StepArgs::l2_seq)
+  int32_t launches = 0;              // 1 .. INT32_MAX, then 1 again (StepArgs::l2_seq)
   void* scratch = nullptr;  // this device's static scratch array (infs_decode_step_static)
   int layers_resident = 0;  // work-groups of the step-launch kernel resident at once (0: no step launch)
   int players_resident = 0; // the same for the probe kernel's step launch (0: none)
@@ -473,12 +473,12 @@ infs_status harvest_clocks(infs_ctx* c) {
   return arm_clocks(c);
 }
 
-// After a synchronisation: report a merge block that stopped waiting.
+// After a synchronisation: report a merge block that stopped waiting, or work-groups that ran elsewhere.
 infs_status check_status(infs_ctx* c) {
-  int32_t st = 0;
+  infs::LaunchStatus st{};
   HIP_TRY(c, hipMemcpy(&st, c->status, sizeof st, hipMemcpyDeviceToHost));
-  if (st != 0) {
-    fail(c, INFS_E_DEVICE, st == 2 ? "a work-group ran on another XCD than the XCD-local exchange of partials "
+  if (st.status != 0 || st.moved != 0) {
+    fail(c, INFS_E_DEVICE, st.status == 0 ? "a work-group ran on another XCD than the XCD-local exchange of partials "
                                      "assumes; outputs are invalid (infs_set_exchange(ctx, 0) avoids it)"
                                    : "a decode launch gave up waiting (a merge for its producers, or a layer of a "
                                      "step launch for the previous layer); outputs are invalid");
@@ -514,9 +514,10 @@ infs_status timed_launch(infs_ctx* c, const KernelKey& key, StepArgs& a, int gri
     ++t.used;
   }
   if (c->l2_xcds > 0) {
-    a.l2_start = __atomic_load_n(c->l2_start_host, __ATOMIC_RELAXED) + (c->xcd_check_fails ? 1 : 0);
-    c->launches = c->launches % infs::kMostLaunches + 1;
-    a.l2_seq = c->xcd_check_fails ? 0 : c->launches;
+    a.l2_start = __atomic_load_n(c->l2_start_host, __ATOMIC_RELAXED);
+    c->launches = c->launches % INT32_MAX + 1;
+    a.l2_seq = c->xcd_check_fails ? -c->launches : c->launches;
+    a.l2_blocks = grid;
   }
   HIP_TRY(c, layers ? infs::launch_layers(key, a, grid, c->stream) : infs::launch_decode(key, a, grid, c->stream));
   return INFS_OK;
@@ -1368,6 +1369,19 @@ infs_status infs_set_step_split(infs_ctx* c, int32_t mode) {
   if (c->step_open || c->probe_open) return fail(c, INFS_E_STATE, "set_step_split while a step is open");
   c->step_split = mode;
   return INFS_OK;
+}
+
+infs_status infs_set_exchange_start(infs_ctx* c, int32_t start) {
+  CHECK_CTX(c);
+  if (start < 0) return fail(c, INFS_E_ARG, "negative start");
+  if (c->l2_xcds == 0) return fail(c, INFS_E_STATE, "no XCD-local exchange in this context");
+  if (start >= c->l2_xcds) return fail(c, INFS_E_ARG, "start must be in [0, %d)", c->l2_xcds);
+  __atomic_store_n(c->l2_start_host, start, __ATOMIC_RELAXED);
+  return INFS_OK;
+}
+
+int32_t infs_exchange_start(const infs_ctx* c) {
+  return c && c->l2_xcds > 0 ? __atomic_load_n(c->l2_start_host, __ATOMIC_RELAXED) : -1;
 }
 
 int32_t infs_exchange_mode(const infs_ctx* c) {

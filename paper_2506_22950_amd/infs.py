@@ -46,7 +46,8 @@ EXPORTS = (
     "infs_step_split_plan", "infs_step_launch_plan", "infs_probe_step_layers",
     "infs_rotary_create", "infs_rotary_destroy", "infs_rotary_frequencies", "infs_rotate_rows",
     "infs_rotate_step", "infs_rotate_probe", "infs_scorer_create", "infs_scorer_destroy", "infs_score_tokens",
-    "infs_score_grad", "infs_fork_slots", "infs_export_responses", "infs_import_responses",
+    "infs_score_grad", "infs_fork_slots", "infs_export_responses", "infs_import_responses", "infs_exchange_start",
+    "infs_set_exchange_start",
 )
 
 
@@ -126,6 +127,8 @@ def load():
         "infs_get_stats": (I32, [P, ctypes.POINTER(Stats)]),
         "infs_get_kernel_info": (I32, [P, ctypes.POINTER(KernelInfo)]),
         "infs_set_exchange": (I32, [P, I32]),
+        "infs_exchange_start": (I32, [P]),
+        "infs_set_exchange_start": (I32, [P, I32]),
         "infs_exchange_mode": (I32, [P]),
         "infs_set_step_split": (I32, [P, I32]),
         "infs_step_split_plan": (I32, [I32, I32, I32, I32, ctypes.POINTER(I32), I32, I32, I32, ctypes.POINTER(I32),
@@ -507,6 +510,14 @@ class Context:
 
     def exchange_mode(self) -> int:
         return load().infs_exchange_mode(self._h)
+
+    def exchange_start(self) -> int:
+        """XCD of the first work-group of the launches in mode 1, as seen last (-1: no mode 1)."""
+        return load().infs_exchange_start(self._h)
+
+    def set_exchange_start(self, start: int):
+        """Another start in its place: launches find a changed one until one of them has run."""
+        self._call(load().infs_set_exchange_start, start)
 
     def set_step_split(self, mode: int):
         """Work split of step launches: 1 near-equal response pieces (default), 0 the
