@@ -8,7 +8,7 @@ next step on.  The host knows each sample's length (synthetic workloads), so it
 never waits on the GPU inside the loop.
 """
 
-from typing import Callable, List, Optional, Sequence
+from typing import Callable, Collection, List, Optional, Sequence
 
 from . import infs
 
@@ -39,7 +39,7 @@ def schedulers_for(cfg, policy: str, pred=None) -> List[infs.Sched]:
 
 def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Callable,
                 log: Optional[list] = None, after_step: Optional[Callable] = None, entry: str = "probe_step",
-                rotary: Optional[infs.Rotary] = None) -> int:
+                rotary: Optional[infs.Rotary] = None, carried: Collection = ()) -> int:
     """Probe phase of prefix reuse (Section 4): every sample decodes its first
     min(L_i, k) tokens against the shared prompt, in batches of up to
     ctx.probe_batch samples of one prompt; samples that finish within their
@@ -55,6 +55,8 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
     pointers provide returns for layers 0 and 1).
     rotary: the rows of q and k_new are rotated in place to their positions
     before each call (one layer at a time).
+    carried: the (prompt, sample) pairs that decode_group will take in as carried;
+    they have tokens already and are neither probed nor released.
     """
     c = ctx.config
 
@@ -69,7 +71,7 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
             G = len(row)
             for first in range(0, G, nb):
                 n = min(nb, G - first)
-                live = [int(row[first + j]) >= t for j in range(n)]
+                live = [int(row[first + j]) >= t and (p, first + j) not in carried for j in range(n)]
                 if not any(live):
                     continue
                 if entry == "probe_step_layers":
@@ -98,7 +100,7 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
                 steps += 1
     for p, row in enumerate(lengths):
         for i, x in enumerate(row):
-            if int(x) <= k:
+            if int(x) <= k and (p, i) not in carried:
                 ctx.release_sample(p, i)
     return steps
 
@@ -138,7 +140,9 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
     take the results (logprob=..., entropy=..., ...).
     carried: {(prompt, sample): (tokens, k, v)}: partial responses of an earlier
     iteration as dense rows; such a sample resumes after them when it is
-    dispatched (Context.import_responses).
+    dispatched (Context.import_responses).  ValueError, before anything is done,
+    where one is finished or has probe tokens (with reuse, hand carried to
+    probe_group too).
     unfinished(list of (slot, prompt, sample, tokens)) is called before the
     samples that a stopped prompt was still decoding are discarded: what it
     exports (Context.export_responses) can be carried into the next iteration.
@@ -156,6 +160,14 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
     stopped = [False] * NP
     c = ctx.config
     carried = carried or {}
+    for p in range(NP):
+        for i, length in enumerate(Ls[p]):
+            if (p, i) not in carried:
+                continue
+            if not 0 <= carried[p, i][0] < length:
+                raise ValueError(f"sample {i} of prompt {p} was carried over finished")
+            if ctx.probe_state(p, i) > 0:
+                raise ValueError(f"sample {i} of prompt {p} was carried over and probed")
 
     def rotate(layers, rows):
         ctx.rotate_step(rotary, infs.rotary_rows(rows[0], rows[0], c.num_q_heads),
@@ -173,14 +185,12 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
                     i = sch.next(ls)
                     if i < 0:
                         break
-                    if reuse and Ls[p][i] <= reuse:  # finished within its probe tokens
+                    if reuse and Ls[p][i] <= reuse and (p, i) not in carried:  # finished within its probe tokens
                         sch.done(ls)
                         continue
                     slot_sample[s] = i
                     if (p, i) in carried:
                         slot_len[s] = carried[p, i][0]
-                        if not slot_len[s] < Ls[p][i]:
-                            raise ValueError(f"sample {i} of prompt {p} was carried over finished")
                         taken.append(s)
                         continue
                     ctx.refill_slot(s, p, i)
