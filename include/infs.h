@@ -583,8 +583,8 @@ infs_status infs_score_tokens(infs_scorer* s, int32_t rows, const void* logits_d
    may be written over the logits where the strides agree):
      grad_j = [ d_logprob (1{j = token} - p_j) - d_entropy p_j (log p_j + entropy) ] / T
    from stats_dev (and, with d_entropy_dev, entropy_dev) of infs_score_tokens.  d_logprob_dev, d_entropy_dev
-   [rows] fp32: either may be NULL; rows without a token (-1) take no part of d_logprob.  NaN for a token
-   outside [-1, vocab). */
+   [rows] fp32: either may be NULL; rows without a token (-1) take no part of d_logprob.  With d_logprob, NaN
+   for a token outside [-1, vocab), also where every entry is masked. */
 infs_status infs_score_grad(infs_scorer* s, int32_t rows, const void* logits_dev, int64_t row_stride,
                             const int32_t* tokens_dev, const float* stats_dev, const float* entropy_dev,
                             const float* d_logprob_dev, const float* d_entropy_dev, void* grad_dev,

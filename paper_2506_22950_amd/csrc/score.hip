@@ -552,10 +552,12 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
   const float m = a.stats[2 * row], ls2 = a.stats[2 * row + 1] * kLog2E, c = a.inv_t * kLog2E;
   const int token = a.d_logprob ? a.tokens[row] : -1;
   float g_lp = a.d_logprob && token != -1 ? a.d_logprob[row] : 0.f;
-  if (token < -1 || token >= a.vocab) g_lp = __builtin_nanf("");
+  const bool outside = token < -1 || token >= a.vocab;
+  if (outside) g_lp = __builtin_nanf("");
   const float g_h = ENTROPY ? a.d_entropy[row] : 0.f;
   const float ca = -(g_lp + (ENTROPY ? g_h * a.entropy[row] : 0.f)) * a.inv_t, cb = -g_h * a.inv_t * kLn2, cc = g_lp * a.inv_t;
   const bool none = m == -__builtin_huge_valf();  // every entry masked
+  const float masked = outside ? g_lp : 0.f;      // the gradient then
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
     const int v = first + u * L + (int)threadIdx.x % L;
@@ -566,7 +568,7 @@ __global__ __launch_bounds__(kThreads) void score_grad_kernel(const ScoreGradArg
     for (int i = 0; i < V::N; ++i) {
       const float y = (V::get(x[u], i) - m) * c - ls2, p = __builtin_amdgcn_exp2f(y);
       r[i] = ENTROPY ? p * fmaf(cb, fmaxf(y, kFar), ca) : p * ca;
-      if (none) r[i] = 0.f;
+      if (none) r[i] = masked;
     }
     if (token >= e0 && token < e0 + V::N && !none) {
 #pragma unroll
