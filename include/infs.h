@@ -49,7 +49,8 @@
  *   - Element type of Q/K/V buffers is the context dtype (fp32, or bf16 as
  *     raw 16-bit patterns); O is always fp32.  Buffers handed to kernels are
  *     16-byte aligned.
- *   - A context must be used from one host thread at a time.
+ *   - A context must be used from one host thread at a time, with its device (the one current in
+ *     infs_create) current.
  */
 #ifndef INFS_H
 #define INFS_H
@@ -387,8 +388,8 @@ int32_t infs_exchange_mode(const infs_ctx* ctx);
 
 /* The start of a context's launches in mode 1 as it was seen last: the XCD of the first work-group (-1 for a
    NULL context or where mode 1 is unavailable), and another value in its place, in [0, n).  Launches enqueued
-   from then on find a changed start until one of them has run, which costs them some microseconds: a way to
-   exercise that path from the host.  E_STATE where mode 1 is unavailable. */
+   from then on find a changed start until one of them has run: a way to exercise that path from the host.
+   E_STATE where mode 1 is unavailable. */
 int32_t infs_exchange_start(const infs_ctx* ctx);
 infs_status infs_set_exchange_start(infs_ctx* ctx, int32_t start);
 
@@ -515,8 +516,8 @@ infs_status infs_rotary_frequencies(const infs_rotary* r, double* freq_out, int3
 /* Rotate `tokens` rows of Q and K (either may be NULL) on hip_stream: a prompt before its prefill, or a
    training batch.  Token t is at position positions_dev[t], or first_position + t without them (any sign;
    up to 2^31 - 1).  inverse != 0 turns the other way: the gradient of the rows with respect to the inputs.
-   dtype: infs_dtype.  One launch; nothing is allocated, so it may be captured.  Messages:
-   infs_last_error(NULL). */
+   dtype: infs_dtype.  One launch (one more for every further 2^22 work-groups of one or more tokens); nothing is
+   allocated, so it may be captured.  Messages: infs_last_error(NULL). */
 infs_status infs_rotate_rows(const infs_rotary* r, void* hip_stream, int32_t dtype, int64_t tokens, const infs_rows* q,
                              const infs_rows* k, const int32_t* positions_dev, int32_t first_position, int32_t inverse);
 

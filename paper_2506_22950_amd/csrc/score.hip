@@ -71,13 +71,14 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 // Few rows are cut into pieces of whole batches, a work-group each; the pieces of a
 // row are joined by the work-group that finishes last, always in the same order.
 //
-// Many rows are bound by memory: 2048 x 151936 bf16 takes 106 us, 5.9 TB/s (loads past the
-// caches; 120 us through them).  An element costs about ten operations of the vector
+// Many rows are bound by memory: 2048 x 151936 bf16 takes 111 us, 5.6 TB/s (loads past the
+// caches; 9 % more through them).  An element costs about ten operations of the vector
 // unit (the exponential four), 15 would be all its time at that rate, so that
 // alternatives, which keep the batch's elements beside its exponentials, bind that
-// unit: 122 us with 20 of them.  16 rows take 9 us: 2.2 thousand cycles until the first
-// batch is there, 6 for its sums and candidates, 2 until a piece has arrived, 6 for the
-// join, and the launch.
+// unit: 13 % more with 20 of them.  16 rows, each cut into 19 pieces of one batch, take 9 us:
+// 2.2 thousand cycles until the batch is there (behind the row's token and that token's
+// logit, which every piece loads first), 6 for its sums and candidates, 2 until a
+// piece has arrived, 6 for the join, and the launch.
 //
 // kUnroll: 8 vectors a lane are 5 % faster on 2048 rows and a third slower on 301 x 50257
 // fp32 and on short rows; loading a batch ahead is 5 % faster on 2048 rows and 10 to 25 %
@@ -605,8 +606,8 @@ void (*score_kernel_of(bool bf16, bool top, bool wave_rows))(const ScoreArgs) {
   return kernels[bf16][top][wave_rows];
 }
 
-// A wavefront a row from 2048 rows (as many work-groups fit the GPU) of up to 1024 vectors: 4096 x 1000
-// bf16 5.9 us, 14.1 with a work-group a row; 4096 x 8000 with 5 alternatives 19.9 and 22.7; but 1024 x 8000
+// A wavefront a row from 2048 rows (a work-group a row would be more than fit the GPU at once, 1280 to 1792
+// by the kernels' registers) of up to 1024 vectors: 4096 x 1000 bf16 5.9 us, 14.1 with a work-group a row; 4096 x 8000 with 5 alternatives 19.9 and 22.7; but 1024 x 8000
 // 7.8 and 6.8, with alternatives 12.6 and 8.7.  Otherwise as many pieces of a row as leave all work-groups
 // on the GPU at once: a few more than fit would run almost alone at the end (1000 x 151936 bf16 52.6 us, 57.7
 // with pieces for about 1024 work-groups whatever fits; 512 x 151936 with 20 alternatives 42.5 and 45.1;
