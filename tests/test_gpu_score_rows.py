@@ -1,5 +1,6 @@
 """GPU: scores and gradients of rows at the borders of what the calls take: tokens outside the vocabulary in
-masked rows, gradients that lie otherwise than the logits, rows as long as a wavefront takes alone."""
+masked rows, gradients that lie otherwise than the logits, rows as long as a wavefront takes alone, the most
+rows and the longest."""
 
 import numpy as np
 import pytest
@@ -105,3 +106,30 @@ def test_the_longest_rows_of_a_wavefront(bf16, n, v, top):
         assert np.array_equal(ids.cpu().numpy(), order)
         want = np.take_along_axis(ref.lp, order, 1)
         close(tl, want, (ref.s_err + more)[:, None] + 8 * U * (np.abs(want) + 2 * ref.ls[:, None]))
+
+
+@pytest.mark.parametrize("bf16,n,v,top", [(True, 1 << 23, 3, 2), (False, 1, 1 << 24, 32), (True, 2, 1 << 24, 5)])
+def test_the_most_rows_and_the_longest(bf16, n, v, top):
+    import torch
+
+    dt = torch.bfloat16 if bf16 else torch.float32
+    z = (torch.randn(n, v, generator=torch.Generator(device="cuda").manual_seed(81), device="cuda") * 3).to(dt)
+    tokens = np.random.default_rng(8).integers(-1, v, n)
+    tok = torch.from_numpy(tokens.astype(np.int32)).cuda()
+    s = infs.Scorer(infs.make_scorer_config(vocab=v, dtype=infs.BF16 if bf16 else infs.F32, max_rows=n, top_k=top),
+                    stream=torch.cuda.current_stream())
+    lp, h, st = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, 2, device="cuda")
+    ids, tl = torch.empty(n, top, dtype=torch.int32, device="cuda"), torch.empty(n, top, device="cuda")
+    s.score(n, z, tok, lp, entropy=h, stats=st, top_id=ids, top_logprob=tl)
+    g, out = torch.ones(n, device="cuda"), torch.full_like(z, 9.0)
+    s.grad(n, z, tok, st, g, out)
+    z64 = z.double().cpu().numpy()
+    ref = Ref(z64, tokens, 1.0)
+    close(lp, ref.lp_t, ref.lp_err)
+    close(h, ref.h, ref.h_err)
+    close(st[:, 1], ref.ls, ref.s_err + 2 * U * ref.ls)
+    assert np.array_equal(st[:, 0].double().cpu().numpy(), ref.m)
+    order = np.argsort(-z64, axis=1, kind="stable")[:, :top]
+    assert np.array_equal(ids.cpu().numpy(), order)
+    want, err = grad_ref(ref, tokens, 1.0, np.ones(n), np.zeros(n))
+    close(out, want, err + np.abs(want) * HALF[bf16])

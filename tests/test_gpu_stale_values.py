@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 # rows and over MFMA blocks
 SHAPES = [("f32", 128, 1, 1, 6), ("f32", 64, 2, 1, 6), ("f32", 128, 4, 1, 4), ("f32", 64, 8, 1, 2),
           ("f32", 128, 8, 2, 1), ("bf16", 64, 2, 2, 6), ("bf16", 128, 4, 4, 6), ("bf16", 64, 8, 2, 2), ("bf16", 128, 8, 1, 1),
-          ("bf16", 64, 4, 2, 20), ("bf16", 128, 8, 1, 8), ("bf16", 64, 8, 8, 40), ("bf16", 128, 16, 2, 16), ("e4m3", 128, 4, 4, 16),
+          ("bf16", 64, 4, 2, 20), ("bf16", 128, 8, 1, 8), ("bf16", 64, 8, 8, 32), ("bf16", 128, 16, 2, 16), ("e4m3", 128, 4, 4, 16),
           ("e4m3", 128, 8, 1, 8)]
 
 
@@ -21,8 +21,6 @@ def test_values_behind_the_ends(fmt, prompts):
     import torch
 
     L, m, S = 2, fmt[4], fmt[4] * prompts
-    if S > 64:
-        pytest.skip("more slots than a context has")
     cap, plen = 100, 64
     ctx = context(fmt, L=L, cap=cap, prompts=prompts, plen=plen)
     nan, inf = float("nan"), float("inf")
