@@ -389,7 +389,7 @@ int32_t infs_exchange_mode(const infs_ctx* ctx);
 /* The start of a context's launches in mode 1 as it was seen last: the XCD of the first work-group (-1 for a
    NULL context or where mode 1 is unavailable), and another value in its place, in [0, n).  Launches enqueued
    from then on find a changed start until one of them has run: a way to exercise that path from the host.
-   E_STATE where mode 1 is unavailable. */
+   E_STATE where mode 1 is unavailable, E_ARG for a start that is no XCD. */
 int32_t infs_exchange_start(const infs_ctx* ctx);
 infs_status infs_set_exchange_start(infs_ctx* ctx, int32_t start);
 

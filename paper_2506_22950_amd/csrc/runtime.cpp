@@ -478,10 +478,11 @@ infs_status check_status(infs_ctx* c) {
   infs::LaunchStatus st{};
   HIP_TRY(c, hipMemcpy(&st, c->status, sizeof st, hipMemcpyDeviceToHost));
   if (st.status != 0 || st.moved != 0) {
-    fail(c, INFS_E_DEVICE, st.status == 0 ? "a work-group ran on another XCD than the XCD-local exchange of partials "
-                                     "assumes; outputs are invalid (infs_set_exchange(ctx, 0) avoids it)"
-                                   : "a decode launch gave up waiting (a merge for its producers, or a layer of a "
-                                     "step launch for the previous layer); outputs are invalid");
+    fail(c, INFS_E_DEVICE,
+         st.status == 0 ? "a work-group ran on another XCD than the XCD-local exchange of partials assumes; outputs "
+                          "are invalid (infs_set_exchange(ctx, 0) avoids it)"
+                        : "a decode launch gave up waiting (a merge for its producers, or a layer of a step launch for "
+                          "the previous layer); outputs are invalid");
     c->dead = true;
     c->dead_msg = c->err;
     return INFS_E_DEVICE;

@@ -606,9 +606,10 @@ void (*score_kernel_of(bool bf16, bool top, bool wave_rows))(const ScoreArgs) {
   return kernels[bf16][top][wave_rows];
 }
 
-// A wavefront a row from 2048 rows (a work-group a row would be more than fit the GPU at once, 1280 to 1792
-// by the kernels' registers) of up to 1024 vectors: 4096 x 1000 bf16 5.9 us, 14.1 with a work-group a row; 4096 x 8000 with 5 alternatives 19.9 and 22.7; but 1024 x 8000
-// 7.8 and 6.8, with alternatives 12.6 and 8.7.  Otherwise as many pieces of a row as leave all work-groups
+// A wavefront a row from 2048 rows (a work-group each would be more than fit the GPU at once, 1280 to 1792
+// by the kernels' registers) of up to 1024 vectors: 4096 x 1000 bf16 5.9 us, 14.1 with a work-group a row;
+// 4096 x 8000 with 5 alternatives 19.9 and 22.7; but 1024 x 8000 7.8 and 6.8, with alternatives 12.6 and
+// 8.7.  Otherwise as many pieces of a row as leave all work-groups
 // on the GPU at once: a few more than fit would run almost alone at the end (1000 x 151936 bf16 52.6 us, 57.7
 // with pieces for about 1024 work-groups whatever fits; 512 x 151936 with 20 alternatives 42.5 and 45.1;
 // 600 x 20000 fp32, the other way, 12.8 and 12.1).
