@@ -535,6 +535,93 @@ infs_status infs_rotate_probe(infs_ctx* ctx, const infs_rotary* r, int32_t promp
                               const uint8_t* live_host, int32_t num_layers, const infs_rows* q, const infs_rows* k);
 
 /* ---------------------------------------------------------------------------------------------
+ * Norms of heads with the rotation in the same pass: what models whose queries and keys are normed head by
+ * head apply in the place of infs_rotate_*.  For a head x of d = head_dim elements with weights w:
+ *     n = sqrt(sum x_e^2 / d + eps),   z_e = w_e x_e / n,   out = the rotation of z
+ * Sums and products are held in fp32, outputs rounded once.  A head that holds an infinity or NaN is NaN
+ * wherever the formula is (an infinity makes n infinite); one of zeros stays zero.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct infs_norms {
+    const void* weight_q;   /* device, [head_dim] elements, a layer's at + layer * layer_stride; NULL: ones */
+    const void* weight_k;
+    int32_t dtype;          /* infs_dtype of the weights */
+    float eps;              /* finite, >= 0 */
+    int64_t layer_stride;   /* elements; 0: every layer has the same weights */
+} infs_norms;
+
+/* infs_rotate_rows, infs_rotate_step and infs_rotate_probe with the norm ahead of the rotation: the same
+   arguments, rules and errors.  Weights may have any alignment to an element. */
+infs_status infs_norm_rotate_rows(const infs_rotary* r, void* hip_stream, int32_t dtype, int64_t tokens,
+                                  const infs_norms* norms, const infs_rows* q, const infs_rows* k,
+                                  const int32_t* positions_dev, int32_t first_position);
+infs_status infs_norm_rotate_step(infs_ctx* ctx, const infs_rotary* r, const infs_norms* norms, int32_t num_layers,
+                                  const infs_rows* q, const infs_rows* k);
+infs_status infs_norm_rotate_probe(infs_ctx* ctx, const infs_rotary* r, const infs_norms* norms, int32_t prompt,
+                                   int32_t first_sample, int32_t n, const uint8_t* live_host, int32_t num_layers,
+                                   const infs_rows* q, const infs_rows* k);
+
+/* The gradient of infs_norm_rotate_rows.  q and k: in the rows it was given, out the gradients with respect to
+   them (the rows may be overwritten); dq and dk: in the gradients of its outputs (out is not used; they may be
+   overwritten too, where the strides agree).  With g the rotation of a gradient by the negative angle:
+       d_x_e = (w_e g_e - x_e sum_f(w_f g_f x_f) / (d n^2)) / n
+       d_w_e = sum of g_e x_e / n over tokens and heads (fp32, [head_dim], or NULL)
+   q and dq go together, and k and dk; one pair may be NULL.  With a d_weight, workspace_dev has
+   infs_norm_rotate_grad_workspace(tokens, head_dim) bytes, aligned to 16; calls that share it must not run at the
+   same time.  Sums are added in an order that depends on sizes, strides and alignment alone. */
+infs_status infs_norm_rotate_grad(const infs_rotary* r, void* hip_stream, int32_t dtype, int64_t tokens,
+                                  const infs_norms* norms, const infs_rows* q, const infs_rows* k, const infs_rows* dq,
+                                  const infs_rows* dk, float* d_weight_q_dev, float* d_weight_k_dev, void* workspace_dev,
+                                  const int32_t* positions_dev, int32_t first_position);
+int64_t infs_norm_rotate_grad_workspace(int64_t tokens, int32_t head_dim);
+
+/* ---------------------------------------------------------------------------------------------
+ * Attention of packed sequences: a prompt's own pass before infs_prefill_shared, and a learner's batch.
+ * Sequence i has queries q_offsets[i] .. q_offsets[i+1]-1 and keys k_offsets[i] .. k_offsets[i+1]-1 of the
+ * packed rows; its queries are its last tokens: of n queries and m keys, query t sees keys 0 .. t + m - n (none
+ * where that is negative, then o = 0 and lse = -inf).  Query head h goes with KV head h / (Hq / Hkv), and over the
+ * keys that a query sees
+ *     s_j = scale q.k_j,   lse = ln sum_j e^(s_j),   o = sum_j e^(s_j - lse) v_j
+ * Sums are held in fp32.  No output depends on a token that it does not see, whatever that holds.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct infs_attention_config {
+    int32_t num_q_heads;   /* Hq, a multiple of num_kv_heads, up to 4096 */
+    int32_t num_kv_heads;  /* Hkv */
+    int32_t head_dim;      /* 64 or 128 */
+    int32_t dtype;         /* infs_dtype of all rows */
+    float scale;           /* finite, > 0; 0: 1/sqrt(head_dim) */
+    int32_t max_tokens;    /* packed query rows of one call, >= 1; max_tokens * Hq / Hkv below 2^31 */
+    uint32_t flags;        /* INFS_FLAG_DRY_RUN: arguments are checked, nothing is allocated or launched */
+} infs_attention_config;
+
+/* An attention: its stream and a workspace on the current device (of hip_stream where given).  Calls on one
+   attention are ordered by its stream; captured graphs that hold its calls must not run at the same time as other
+   work of the same attention.  Messages: infs_last_error(NULL).  One host thread at a time. */
+typedef struct infs_attention infs_attention;
+infs_status infs_attention_create(const infs_attention_config* cfg, void* hip_stream, infs_attention** out);
+/* Waits for the attention's stream first.  NULL is a no-op. */
+void infs_attention_destroy(infs_attention* a);
+
+/* Attention of `sequences` sequences (0 .. 2^20) whose q_tokens (0 .. max_tokens) query rows and k_tokens (0 ..
+   2^31 - 1) key rows are packed; q_offsets_dev, k_offsets_dev: sequences + 1 ascending int32 within them (k_offsets_dev
+   NULL: the queries', then k_tokens is q_tokens).  Offsets are read by the launch: where they do not ascend or leave
+   [0, tokens] (they are taken into it), the outputs of their rows are undefined and nothing else is touched.  Rows
+   outside every sequence are neither read nor written.
+   q: in the queries, out their outputs o; k, v: in (out is not used).  lse_dev [q_tokens, Hq] fp32, or NULL.  Rows
+   are of one layer; addresses and strides are multiples of 16 bytes, and o may not overlap the inputs.
+   E_ARG also where a launch would have more than 2^22 work-groups. */
+infs_status infs_attend(infs_attention* a, int32_t sequences, int64_t q_tokens, const int32_t* q_offsets_dev,
+                        int64_t k_tokens, const int32_t* k_offsets_dev, const infs_rows* q, const infs_rows* k,
+                        const infs_rows* v, float* lse_dev);
+
+/* Its gradient: q, k, v: in as in infs_attend, out the gradients with respect to them; o, d_o: in the outputs and
+   their gradients; lse_dev as infs_attend wrote it.  dk and dv are sums over the queries of a group's heads,
+   added in an order that depends on sizes and offsets alone; keys that no query sees get zeros.  The gradients may
+   not overlap the inputs. */
+infs_status infs_attend_grad(infs_attention* a, int32_t sequences, int64_t q_tokens, const int32_t* q_offsets_dev,
+                             int64_t k_tokens, const int32_t* k_offsets_dev, const infs_rows* q, const infs_rows* k,
+                             const infs_rows* v, const infs_rows* o, const infs_rows* d_o, const float* lse_dev);
+
+/* ---------------------------------------------------------------------------------------------
  * Scores of tokens: what a group's samples and its learner take from a model's logits.  For a row z of
  * `vocab` logits at temperature T, with m = max z and S = sum_j exp((z_j - m) / T):
  *     log p_j  = (z_j - m) / T - ln S
@@ -590,6 +677,52 @@ infs_status infs_score_grad(infs_scorer* s, int32_t rows, const void* logits_dev
                             const int32_t* tokens_dev, const float* stats_dev, const float* entropy_dev,
                             const float* d_logprob_dev, const float* d_entropy_dev, void* grad_dev,
                             int64_t grad_row_stride);
+
+/* ---------------------------------------------------------------------------------------------
+ * The choice of the next tokens.  Of a row z of logits at temperature T the entries are ranked by z, equal ones by
+ * the lower index first, and weighed w_j = exp((z_j - max z) / T); entries of -inf are masked and never chosen.
+ * What is kept is the beginning of that ranking that all of these leave:
+ *     top_k   its first top_k entries
+ *     top_p   of those, each whose predecessors weigh less than top_p times what the first top_k weigh
+ *     min_p   the entries with w_j >= min_p
+ * and the token is the first kept entry by index at which the sum of the kept weights up to it is above u times
+ * their whole sum, u a given uniform number in [0, 1).
+ * ------------------------------------------------------------------------------------------- */
+typedef struct infs_sampling {
+    double temperature;  /* T in [2^-20, 2^20]; 0: 1 */
+    double top_p;        /* in (0, 1]; 0: 1 */
+    double min_p;        /* in [0, 1]; 0: none */
+    int32_t top_k;       /* >= 0; 0: all */
+    int32_t reserved;    /* 0 */
+} infs_sampling;
+
+typedef struct infs_sampler_config {
+    int32_t vocab;       /* entries of a row, 1 .. 2^24 */
+    int32_t dtype;       /* infs_dtype of logits */
+    int32_t max_rows;    /* rows of one call, 1 .. 2^22 */
+    uint32_t flags;      /* INFS_FLAG_DRY_RUN: arguments are checked, nothing is allocated or launched */
+} infs_sampler_config;
+
+/* A sampler: its stream and a workspace on the current device (of hip_stream where given).  Calls on one sampler are
+   ordered by its stream; captured graphs that hold its calls must not run at the same time as other work of the
+   same sampler.  Messages: infs_last_error(NULL).  One host thread at a time. */
+typedef struct infs_sampler infs_sampler;
+infs_status infs_sampler_create(const infs_sampler_config* cfg, void* hip_stream, infs_sampler** out);
+/* Waits for the sampler's stream first.  NULL is a no-op. */
+void infs_sampler_destroy(infs_sampler* s);
+
+/* A token for each of `rows` rows (0 .. max_rows) of logits, row_stride elements apart (0: vocab; at least vocab, any
+   alignment to an element), by the uniform numbers uniform_dev [rows] fp32.  All rows go by `all`, or row i by
+   each_dev[i] (device) where that is not NULL; `all` NULL: zeros.
+     token_dev [rows]    the token, int32; -1 where every entry is masked, where the row holds a NaN or +inf, where u is
+                         not in [0, 1) and where each_dev[i] is not allowed
+     logprob_dev [rows]  log of its weight's share of the kept weights, or NULL (NaN for token -1)
+     kept_dev [rows]     how many entries are kept, int32, or NULL (0 for token -1)
+   Weights are held in 64 bits as whole multiples of 2^-(62 - log2 vocab) of the largest (2^-50 at finest), so that
+   their sums are exact whatever the order. */
+infs_status infs_choose_tokens(infs_sampler* s, int32_t rows, const void* logits_dev, int64_t row_stride,
+                               const float* uniform_dev, const infs_sampling* all, const infs_sampling* each_dev,
+                               int32_t* token_dev, float* logprob_dev, int32_t* kept_dev);
 
 /* ---------------------------------------------------------------------------------------------
  * Host scheduler (CPU only, no device): chooses which sample a freed slot receives.

@@ -1,0 +1,718 @@
+// Causal attention of packed sequences with grouped heads, and its gradient.
+//
+// Token t of a sequence of n queries and m keys (its queries are its last
+// tokens) sees keys 0 .. t + m - n.  With s = scale q.k over the seen keys:
+//   lse = ln sum e^s,   o = sum e^(s - lse) v
+// and with up = d_o, D = up.o, p = e^(s - lse), ds = p (up.v - D):
+//   dq = scale sum ds k,   dk = scale sum ds q,   dv = sum p up
+// where the sums of dk and dv run over the queries of all heads of a group.
+//
+// Rows.  The queries of a KV head's group are one list of rows, row r being
+// token r / hpk of head r % hpk, so a tile of rows shares every key whatever
+// hpk is, and dk and dv add over the heads inside a work-group.
+//
+// Matrix products.  A wavefront owns 32 rows (in the kernel of dk and dv, 32
+// keys) as the columns of 32 x 32 products whose other side comes out of LDS:
+//   s^T = K q^T,  o^T += V^T p^T
+// A lane then holds one row's scores: its maximum and sum need one exchange
+// with the lane 32 further.  The result of the first product is the operand
+// of the second as it is: a lane's registers 8j .. 8j+7 are keys
+// {4h .. 4h+3, 8+4h .. 8+4h+3} of 16 (h: which half of the wavefront), and V^T is
+// read in that order (transposed out of LDS, 8 bytes of four keys a lane).
+// bf16 operands add up in fp32; p and ds are rounded to bf16 as operands
+// (2^-9 relative each, below the rounding of the outputs they add up to);
+// fp32 rows take fp32 products.
+//
+// Masked places.  A score that its row does not see is replaced, not added to,
+// and rows behind a sequence are zero in LDS.  Only a product over tokens of
+// one tile, some of them unseen, can meet 0 times an infinity or NaN: where
+// such a tile holds one (seen while it is staged), those elements are taken out
+// and added token by token, to the rows that see them.
+#include "ops.h"
+
+#include <algorithm>
+
+namespace infs {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The value of the lane 32 further (or back).
+__device__ __forceinline__ float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+template <bool BF>
+struct Type;
+template <>
+struct Type<true> {
+  static constexpr int kRegs = 8;  // accumulator registers that one operand takes
+  static __device__ __forceinline__ f32x16 mma(f32x16 c, u32x4 a, u32x4 b) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ u32x4 operand(const f32x16& s, int i) {
+    bf16x8 r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = (__bf16)s[i + j];
+    return __builtin_bit_cast(u32x4, r);
+  }
+  // slot j of 8 alone
+  static __device__ __forceinline__ u32x4 only(u32x4 x, int j, bool here) {
+    u32x4 r = {0, 0, 0, 0};
+    if (here) r[j >> 1] = x[j >> 1] & ((j & 1) ? 0xffff0000u : 0xffffu);
+    return r;
+  }
+  // the infinities and NaN alone
+  static __device__ __forceinline__ u32x4 odd_part(u32x4 x) {
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      r[j] = ((x[j] & 0x7f80u) == 0x7f80u ? x[j] & 0xffffu : 0u) | ((x[j] & 0x7f800000u) == 0x7f800000u ? x[j] & 0xffff0000u : 0u);
+    return r;
+  }
+  static __device__ __forceinline__ float dot(u32x4 x, u32x4 y) {
+    float r = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      r = fmaf(__uint_as_float(x[j] << 16), __uint_as_float(y[j] << 16), r);
+      r = fmaf(__uint_as_float(x[j] & 0xffff0000u), __uint_as_float(y[j] & 0xffff0000u), r);
+    }
+    return r;
+  }
+};
+template <>
+struct Type<false> {
+  static constexpr int kRegs = 4;
+  static __device__ __forceinline__ f32x16 mma(f32x16 c, u32x4 a, u32x4 b) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ u32x4 operand(const f32x16& s, int i) {
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = __float_as_uint(s[i + j]);
+    return r;
+  }
+  static __device__ __forceinline__ u32x4 only(u32x4 x, int j, bool here) {
+    u32x4 r = {0, 0, 0, 0};
+    if (here) r[j] = x[j];
+    return r;
+  }
+  static __device__ __forceinline__ u32x4 odd_part(u32x4 x) {
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = (x[j] & 0x7f800000u) == 0x7f800000u ? x[j] : 0u;
+    return r;
+  }
+  static __device__ __forceinline__ float dot(u32x4 x, u32x4 y) {
+    float r = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r = fmaf(__uint_as_float(x[j]), __uint_as_float(y[j]), r);
+    return r;
+  }
+};
+
+// Token (key or row) of accumulator register i, in its block of 32.
+__device__ __forceinline__ int token_of(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
+
+// A tile of rows of D elements in LDS.  Row r's chunk c of 16 bytes lies at chunk c ^ x(r), x from the low four
+// bits of r: the 8 rows (or 4 rows of 64 bytes) that a quarter of a wavefront reads at once lie in different banks.
+template <bool BF, int D>
+struct Tile {
+  static constexpr int kRow = D * (BF ? 2 : 4), kChunks = kRow / 16, kSteps = kChunks / 2, kBlocks = D / 32;
+  static __device__ __forceinline__ int turn(int r) {
+    return kChunks >= 16 ? ((r & 3) << 2 | ((r >> 2) & 3)) : (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
+  }
+  static __device__ __forceinline__ int place(int r, int c) { return r * kRow + ((c ^ turn(r)) << 4); }
+
+  int straight, across, across8;  // byte offsets of this lane
+  __device__ __forceinline__ Tile() {
+    const int l = threadIdx.x & 63, h = l >> 5;
+    straight = place(l & 31, h);
+    if constexpr (BF) {
+      const int a = l & 15, r = 4 * h + (a >> 2), c = 2 * ((l >> 4) & 1) + ((a & 3) >> 1);
+      across = place(r, c) + 8 * (a & 1);
+      across8 = place(r + 8, c) + 8 * (a & 1);
+    } else {
+      across = 4 * h * kRow + ((((l & 31) >> 2) ^ h) << 4) + 4 * (l & 3);
+    }
+  }
+  // Step s of the sum over a row's elements, rows row0 .. row0+31 (row0 a multiple of 32).
+  __device__ __forceinline__ u32x4 rows(const char* base, int row0, int s) const {
+    return *(const u32x4*)(base + row0 * kRow + (straight ^ (s << 5)));
+  }
+  // Elements 32 b .. 32 b + 31 of the tokens that an operand from kRegs accumulator registers on (from register
+  // i of the block of 32 tokens at token0) stands for, transposed.
+  __device__ __forceinline__ u32x4 columns(const char* base, int token0, int i, int b) const {
+    if constexpr (BF) {
+      const char* p = base + (token0 + 2 * i) * kRow;
+      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (across ^ (b << 6))));
+      const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (across8 ^ (b << 6))));
+      const u32x2 u = __builtin_bit_cast(u32x2, x), v = __builtin_bit_cast(u32x2, y);
+      return u32x4{u[0], u[1], v[0], v[1]};
+    } else {
+      u32x4 r;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        r[j] = *(const uint32_t*)(base + (token0 + 2 * i + j) * kRow +
+                                  (across ^ ((8 * b ^ (j << 2) ^ ((i >> 1) & 2)) << 4)));
+      return r;
+    }
+  }
+};
+
+// c += a b where a may hold infinities and NaN of tokens that a lane does not see: the others at once, so that their
+// sum is what it is without these; then these token by token, and the lane takes token t (of the 32 that the
+// registers from i on are part of) where lo <= t <= hi.
+template <bool BF>
+__device__ __forceinline__ void mma_seen(f32x16& c, u32x4 a, u32x4 b, int i, int lo, int hi) {
+  const int half = (threadIdx.x >> 5) & 1;
+  const u32x4 rest = Type<BF>::odd_part(a);
+  c = Type<BF>::mma(c, a ^ rest, b);
+#pragma unroll
+  for (int j = 0; j < Type<BF>::kRegs; ++j) {
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 one = Type<BF>::only(rest, j, half == h);
+      if (!__any(one[0] | one[1] | one[2] | one[3])) continue;
+      const f32x16 p = Type<BF>::mma(f32x16{}, one, Type<BF>::only(b, j, half == h));
+      const int t = token_of(i + j, h);
+      const bool seen = t >= lo && t <= hi;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) c[e] = seen ? c[e] + p[e] : c[e];
+    }
+  }
+}
+
+// Sequence whose tiles hold slot `slot`: the tiles (of 2^shift rows, per_token rows a token) of sequence i take
+// slots first(i) .. , first(i) = rows before it / tile + i, which leaves room for every tile and at most one
+// slot free.  Offsets are taken into [0, tokens], so that whatever they are nothing out of bounds is touched.
+struct Place {
+  int begin, end;  // tokens
+  int sequence, tile;
+};
+__device__ __forceinline__ int offset_of(const int32_t* offsets, int i, int tokens) {
+  return min(max(offsets[i], 0), tokens);
+}
+__device__ __forceinline__ Place find_place(const int32_t* offsets, int n, int tokens, int slot, int per_token, int shift) {
+  const int lane = threadIdx.x & 63;
+  const auto first = [&](int i) { return (int)(((int64_t)offset_of(offsets, i, tokens) * per_token >> shift) + i); };
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lane * step;
+    const unsigned long long m = __ballot(i < n && first(lo + min(i, n - 1)) <= slot);
+    const int j = m ? 63 - __builtin_clzll(m) : 0;
+    lo += j * step;
+    n = min(step, n - j * step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  Place p;
+  p.sequence = lo;
+  p.begin = offset_of(offsets, lo, tokens);
+  p.end = max(p.begin, offset_of(offsets, lo + 1, tokens));
+  p.tile = slot - (int)(((int64_t)p.begin * per_token >> shift) + lo);
+  return p;
+}
+
+// r / hpk by inv = ceil(2^32 / hpk) (at most one too large for r below 2^31).
+__device__ __forceinline__ int divide_rows(int r, int hpk, uint32_t inv) {
+  if (hpk == 1) return r;
+  const int t = (int)__umulhi((uint32_t)r, inv);
+  return t * hpk > r ? t - 1 : t;
+}
+
+// Rows of a tensor in registers between memory and LDS: `rows` of a tile, by `threads` threads.
+template <bool BF, int D, int ROWS, int THREADS>
+struct Stage {
+  using T = Tile<BF, D>;
+  static constexpr int kPer = ROWS * T::kChunks / THREADS, kStep = THREADS / T::kChunks;
+  static_assert(ROWS * T::kChunks % THREADS == 0 && THREADS % T::kChunks == 0, "whole chunks a thread");
+  u32x4 x[kPer];
+  static __device__ __forceinline__ int row(int i) { return (int)threadIdx.x / T::kChunks + i * kStep; }
+  static __device__ __forceinline__ int chunk() { return (int)threadIdx.x % T::kChunks; }
+  // Token rows first .. of `base` (stride bytes apart), zero from `end` on.
+  __device__ __forceinline__ void load(const char* base, int64_t stride, int first, int end) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int r = first + row(i);
+      x[i] = u32x4{0, 0, 0, 0};
+      if (r < end) x[i] = *(const u32x4*)(base + r * stride + chunk() * 16);
+    }
+  }
+  // Rows first .. of a group's heads.
+  __device__ __forceinline__ void load_rows(const char* base, int64_t stride, int64_t head, int first, int end, int hpk,
+                                            uint32_t inv) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int r = first + row(i);
+      x[i] = u32x4{0, 0, 0, 0};
+      if (r < end) {
+        const int t = divide_rows(r, hpk, inv);
+        x[i] = *(const u32x4*)(base + t * stride + (r - t * hpk) * head + chunk() * 16);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) *(u32x4*)(lds + T::place(row(i), chunk())) = x[i];
+  }
+  __device__ __forceinline__ bool odd() const {
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const u32x4 y = Type<BF>::odd_part(x[i]);
+      r |= y[0] | y[1] | y[2] | y[3];
+    }
+    return r != 0;
+  }
+};
+
+// Operands of a lane's own row (or key), straight from memory.
+template <int STEPS>
+__device__ __forceinline__ void load_operands(u32x4 (&f)[STEPS], const char* row, bool there) {
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    f[s] = u32x4{0, 0, 0, 0};
+    if (there) f[s] = *(const u32x4*)(row + (2 * s + half) * 16);
+  }
+}
+
+// A lane's row of results times `by`: acc[b] holds elements 32 b + token_of(i) of it.
+template <bool BF, int D>
+__device__ __forceinline__ void store_result(const f32x16 (&acc)[D / 32], float by, char* row, bool there) {
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b) {
+    if constexpr (BF) {
+#pragma unroll
+      for (int q = 0; q < 4; q += 2) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = 4 * q + 2 * k;
+          w[k] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)(acc[b][i] * by)) |
+                 (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)(acc[b][i + 1] * by)) << 16;
+        }
+        // two halves of 16 bytes each from two lanes: 8 elements from `half` on
+        const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        if (there) *(u32x4*)(row + 64 * b + 16 * q + 16 * half) = u32x4{x[0], y[0], x[1], y[1]};
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = acc[b][4 * q + k] * by;
+        if (there) *(f32x4*)(row + 128 * b + 32 * q + 16 * half) = v;
+      }
+    }
+  }
+}
+
+template <bool BF>
+constexpr int kTileKeys = BF ? 64 : 32;
+
+// ---- o and lse -----------------------------------------------------------------
+template <bool BF, int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attend_kernel(const AttendArgs a) {
+  using T = Tile<BF, D>;
+  constexpr int BM = NW * 32, BN = kTileKeys<BF>, NB = BN / 32, R = Type<BF>::kRegs;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][BN * T::kRow];  // K and V of two tiles
+  __shared__ int odd[2];  // the tile whose V holds an infinity or NaN
+  const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  const int slot = a.q_slots - 1 - (int)(blockIdx.x / (unsigned)a.kv_heads);  // the longest rows first
+  const Place p = find_place(a.q_offsets, a.sequences, a.q_tokens, slot, a.hpk, __builtin_ctz(BM));
+  const int rows = (p.end - p.begin) * a.hpk, row0 = p.tile * BM;
+  if (p.tile < 0 || row0 >= rows) return;
+  const int kb = offset_of(a.k_offsets, p.sequence, a.k_tokens);
+  const int keys = max(0, offset_of(a.k_offsets, p.sequence + 1, a.k_tokens) - kb);
+  const int shift = keys - (p.end - p.begin);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int wrow = row0 + wave * 32, row = wrow + (lane & 31);
+  const bool there = row < rows;
+  const int token = divide_rows(min(row, rows - 1), a.hpk, a.hpk_inv), head = g * a.hpk + min(row, rows - 1) - token * a.hpk;
+  const int last = there ? token + shift : -1;  // the last key that the row sees
+  // of the wavefront: the first row's, and the last row's
+  const int seen_all = wrow < rows ? divide_rows(wrow, a.hpk, a.hpk_inv) + shift : -1;
+  const int seen_any = wrow < rows ? divide_rows(min(wrow + 31, rows - 1), a.hpk, a.hpk_inv) + shift : -1;
+  const int seen_last = divide_rows(min(row0 + BM, rows) - 1, a.hpk, a.hpk_inv) + shift;
+  const int tiles = seen_last < 0 ? 0 : seen_last / BN + 1;
+
+  const char* kbase = a.k + kb * a.k_row + g * a.k_head;
+  const char* vbase = a.v + kb * a.v_row + g * a.v_head;
+  const int64_t q_token = p.begin + token;
+  u32x4 q[T::kSteps];
+  load_operands(q, a.q + q_token * a.q_row + head * a.q_head, there);
+
+  const T tile;
+  Stage<BF, D, BN, NW * 64> sk, sv;
+  f32x16 acc[T::kBlocks] = {};
+  float m = -INFINITY, sum = 0.f;
+  const float c = a.scale * kLog2e;
+  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+  if (tiles > 0) {
+    sk.load(kbase, a.k_row, 0, keys);
+    sv.load(vbase, a.v_row, 0, keys);
+    __syncthreads();
+    sk.store(lds[0][0]);
+    sv.store(lds[0][1]);
+    if (sv.odd()) odd[0] = 0;
+  }
+  __syncthreads();
+  for (int t = 0; t < tiles; ++t) {
+    if (t + 1 < tiles) {
+      sk.load(kbase, a.k_row, (t + 1) * BN, keys);
+      sv.load(vbase, a.v_row, (t + 1) * BN, keys);
+    }
+    const int key0 = t * BN;
+    if (key0 <= seen_any) {
+      const char *lk = lds[t & 1][0], *lv = lds[t & 1][1];
+      f32x16 s[NB] = {};
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 0; e < T::kSteps; ++e) s[n] = Type<BF>::mma(s[n], tile.rows(lk, 32 * n, e), q[e]);
+      const bool masked = key0 + BN - 1 > seen_all;
+      if (masked) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[n][i] = key0 + 32 * n + token_of(i, half) <= last ? s[n][i] : -INFINITY;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+      top = fmaxf(m, fmaxf(top, other_half(top)));
+      if (__any(top > m)) {
+        const float by = exp2_((m - (top == -INFINITY ? 0.f : top)) * c);
+        sum *= by;
+#pragma unroll
+        for (int b = 0; b < T::kBlocks; ++b) acc[b] *= by;
+        m = top;
+      }
+      const float off = m == -INFINITY ? 0.f : -m * c;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[n][i] = exp2_(fmaf(s[n][i], c, off));
+          sum += s[n][i];
+        }
+      const bool careful = masked && odd[t & 1] == t;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; i += R) {
+          const u32x4 w = Type<BF>::operand(s[n], i);
+#pragma unroll
+          for (int b = 0; b < T::kBlocks; ++b) {
+            const u32x4 v = tile.columns(lv, 32 * n, i, b);
+            if (careful)
+              mma_seen<BF>(acc[b], v, w, i, 0, last - key0 - 32 * n);
+            else
+              acc[b] = Type<BF>::mma(acc[b], v, w);
+          }
+        }
+    }
+    if (t + 1 < tiles) {
+      sk.store(lds[(t + 1) & 1][0]);
+      sv.store(lds[(t + 1) & 1][1]);
+      if (sv.odd()) odd[(t + 1) & 1] = t + 1;
+    }
+    __syncthreads();
+  }
+  sum += other_half(sum);
+  const float by = last < 0 ? 0.f : 1.f / sum;
+  store_result<BF, D>(acc, by, a.o + q_token * a.o_row + head * a.o_head, there);
+  if (there && half == 0 && a.lse)
+    a.lse[q_token * a.q_heads + head] = last < 0 ? -INFINITY : (m == -INFINITY ? 0.f : m * a.scale) + __log2f(sum) * kLn2;
+}
+
+// ---- dq (and D) ----------------------------------------------------------------
+// The loop of the forward kernel with the scores' exponentials from lse: s^T and (v up)^T of a tile, ds^T from
+// them, dq^T += K^T ds^T.  D = up.o of every row is left in a.delta for the kernel of dk and dv.
+template <bool BF, int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attend_dq_kernel(const AttendGradArgs a) {
+  using T = Tile<BF, D>;
+  constexpr int BM = NW * 32, BN = kTileKeys<BF>, NB = BN / 32, R = Type<BF>::kRegs;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][BN * T::kRow];
+  __shared__ int odd[2];  // the tile whose K holds an infinity or NaN
+  const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  const int slot = a.q_slots - 1 - (int)(blockIdx.x / (unsigned)a.kv_heads);
+  const Place p = find_place(a.q_offsets, a.sequences, a.q_tokens, slot, a.hpk, __builtin_ctz(BM));
+  const int rows = (p.end - p.begin) * a.hpk, row0 = p.tile * BM;
+  if (p.tile < 0 || row0 >= rows) return;
+  const int kb = offset_of(a.k_offsets, p.sequence, a.k_tokens);
+  const int keys = max(0, offset_of(a.k_offsets, p.sequence + 1, a.k_tokens) - kb);
+  const int shift = keys - (p.end - p.begin);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int wrow = row0 + wave * 32, row = wrow + (lane & 31);
+  const bool there = row < rows;
+  const int token = divide_rows(min(row, rows - 1), a.hpk, a.hpk_inv), head = g * a.hpk + min(row, rows - 1) - token * a.hpk;
+  const int last = there ? token + shift : -1;
+  const int seen_all = wrow < rows ? divide_rows(wrow, a.hpk, a.hpk_inv) + shift : -1;
+  const int seen_any = wrow < rows ? divide_rows(min(wrow + 31, rows - 1), a.hpk, a.hpk_inv) + shift : -1;
+  const int seen_last = divide_rows(min(row0 + BM, rows) - 1, a.hpk, a.hpk_inv) + shift;
+  const int tiles = seen_last < 0 ? 0 : seen_last / BN + 1;
+
+  const char* kbase = a.k + kb * a.k_row + g * a.k_head;
+  const char* vbase = a.v + kb * a.v_row + g * a.v_head;
+  const int64_t q_token = p.begin + token;
+  u32x4 q[T::kSteps], up[T::kSteps];
+  float delta = 0.f;
+  load_operands(q, a.o + q_token * a.o_row + head * a.o_head, there);
+  load_operands(up, a.d_o + q_token * a.do_row + head * a.do_head, there);
+#pragma unroll
+  for (int s = 0; s < T::kSteps; ++s) delta += Type<BF>::dot(q[s], up[s]);
+  delta += other_half(delta);
+  load_operands(q, a.q + q_token * a.q_row + head * a.q_head, there);
+  const int64_t at = q_token * a.q_heads + head;
+  if (there && half == 0) a.delta[at] = delta;
+  const float c = a.scale * kLog2e, off = there ? -a.lse[at] * kLog2e : 0.f;
+
+  const T tile;
+  Stage<BF, D, BN, NW * 64> sk, sv;
+  f32x16 acc[T::kBlocks] = {};
+  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+  if (tiles > 0) {
+    sk.load(kbase, a.k_row, 0, keys);
+    sv.load(vbase, a.v_row, 0, keys);
+    __syncthreads();
+    sk.store(lds[0][0]);
+    sv.store(lds[0][1]);
+    if (sk.odd()) odd[0] = 0;
+  }
+  __syncthreads();
+  for (int t = 0; t < tiles; ++t) {
+    if (t + 1 < tiles) {
+      sk.load(kbase, a.k_row, (t + 1) * BN, keys);
+      sv.load(vbase, a.v_row, (t + 1) * BN, keys);
+    }
+    const int key0 = t * BN;
+    if (key0 <= seen_any) {
+      const char *lk = lds[t & 1][0], *lv = lds[t & 1][1];
+      const bool masked = key0 + BN - 1 > seen_all, careful = masked && odd[t & 1] == t;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        f32x16 s = {}, ds = {};
+#pragma unroll
+        for (int e = 0; e < T::kSteps; ++e) {
+          s = Type<BF>::mma(s, tile.rows(lk, 32 * n, e), q[e]);
+          ds = Type<BF>::mma(ds, tile.rows(lv, 32 * n, e), up[e]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] = exp2_(fmaf(s[i], c, off)) * (ds[i] - delta);
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) ds[i] = key0 + 32 * n + token_of(i, half) <= last ? ds[i] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += R) {
+          const u32x4 w = Type<BF>::operand(ds, i);
+#pragma unroll
+          for (int b = 0; b < T::kBlocks; ++b) {
+            const u32x4 k = tile.columns(lk, 32 * n, i, b);
+            if (careful)
+              mma_seen<BF>(acc[b], k, w, i, 0, last - key0 - 32 * n);
+            else
+              acc[b] = Type<BF>::mma(acc[b], k, w);
+          }
+        }
+      }
+    }
+    if (t + 1 < tiles) {
+      sk.store(lds[(t + 1) & 1][0]);
+      sv.store(lds[(t + 1) & 1][1]);
+      if (sk.odd()) odd[(t + 1) & 1] = t + 1;
+    }
+    __syncthreads();
+  }
+  store_result<BF, D>(acc, a.scale, a.dq + q_token * a.dq_row + head * a.dq_head, there);
+}
+
+// ---- dk and dv -----------------------------------------------------------------
+// A wavefront's 32 keys are the columns: s = Q k^T and up v^T over a tile of rows, p and ds from them, then
+// dv^T += up^T p and dk^T += Q^T ds with the rows as the tokens of the sum.  A key is seen by the rows from
+// (key - shift) hpk on.
+template <bool BF, int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attend_dkv_kernel(const AttendGradArgs a) {
+  using T = Tile<BF, D>;
+  constexpr int BK = NW * 32, BR = BF && D == 64 ? 64 : 32, R = Type<BF>::kRegs;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][BR * T::kRow];  // Q and d_o of two tiles
+  __shared__ __attribute__((aligned(16))) float stats[2][2][BR];  // -lse log2(e) and D of their rows
+  __shared__ int odd[2];  // the tile that holds an infinity or NaN
+  const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  const int slot = (int)(blockIdx.x / (unsigned)a.kv_heads);
+  const Place p = find_place(a.k_offsets, a.sequences, a.k_tokens, slot, 1, __builtin_ctz(BK));
+  const int keys = p.end - p.begin, key0 = p.tile * BK;
+  if (p.tile < 0 || key0 >= keys) return;
+  const int qb = offset_of(a.q_offsets, p.sequence, a.q_tokens);
+  const int queries = max(0, offset_of(a.q_offsets, p.sequence + 1, a.q_tokens) - qb);
+  const int shift = keys - queries, rows = queries * a.hpk;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int wkey = key0 + wave * 32, key = wkey + (lane & 31);
+  const bool there = key < keys;
+  const auto first_row = [&](int k) { return max(0, k - shift) * a.hpk; };
+  const int first = there ? first_row(key) : INT32_MAX;       // the first row that sees the key
+  const int wfirst = wkey < keys ? first_row(wkey) : INT32_MAX;  // .. any, and all, of the wavefront's
+  const int wall = first_row(min(wkey + 31, keys - 1));
+  const int begin = first_row(key0), tiles = rows > begin ? (rows - begin + BR - 1) / BR : 0;
+
+  const int64_t k_token = p.begin + (there ? key : key0);
+  u32x4 k[T::kSteps], v[T::kSteps];
+  load_operands(k, a.k + k_token * a.k_row + g * a.k_head, there);
+  load_operands(v, a.v + k_token * a.v_row + g * a.v_head, there);
+  const char* qbase = a.q + qb * a.q_row + (int64_t)g * a.hpk * a.q_head;
+  const char* dobase = a.d_o + qb * a.do_row + (int64_t)g * a.hpk * a.do_head;
+  const float* stat = half ? a.delta : a.lse;
+  float st = 0.f;
+  // the first wavefronts: one of a row's two values a lane
+  const auto load_stats = [&](int r0) {
+    const int r = r0 + wave * 32 + (lane & 31);
+    st = 0.f;
+    if (wave < BR / 32 && r < rows) {
+      const int t = divide_rows(r, a.hpk, a.hpk_inv);
+      st = stat[(int64_t)(qb + t) * a.q_heads + g * a.hpk + r - t * a.hpk];
+    }
+  };
+  const auto store_stats = [&](int buf) {
+    if (wave < BR / 32) stats[buf][half][wave * 32 + (lane & 31)] = half ? st : -st * kLog2e;
+  };
+
+  const T tile;
+  Stage<BF, D, BR, NW * 64> sq, so;
+  f32x16 dk[T::kBlocks] = {}, dv[T::kBlocks] = {};
+  const float c = a.scale * kLog2e;
+  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+  if (tiles > 0) {
+    sq.load_rows(qbase, a.q_row, a.q_head, begin, rows, a.hpk, a.hpk_inv);
+    so.load_rows(dobase, a.do_row, a.do_head, begin, rows, a.hpk, a.hpk_inv);
+    load_stats(begin);
+    __syncthreads();
+    sq.store(lds[0][0]);
+    so.store(lds[0][1]);
+    store_stats(0);
+    if (sq.odd() || so.odd()) odd[0] = 0;
+  }
+  __syncthreads();
+  for (int t = 0; t < tiles; ++t) {
+    const int row0 = begin + t * BR;
+    if (t + 1 < tiles) {
+      sq.load_rows(qbase, a.q_row, a.q_head, row0 + BR, rows, a.hpk, a.hpk_inv);
+      so.load_rows(dobase, a.do_row, a.do_head, row0 + BR, rows, a.hpk, a.hpk_inv);
+      load_stats(row0 + BR);
+    }
+    if (row0 + BR > wfirst) {
+      const char *lq = lds[t & 1][0], *lo = lds[t & 1][1];
+      const bool masked = row0 < wall || row0 + BR > rows, careful = masked && odd[t & 1] == t;
+#pragma unroll
+      for (int n = 0; n < BR; n += 32) {
+        f32x16 s = {}, ds = {};
+#pragma unroll
+        for (int e = 0; e < T::kSteps; ++e) {
+          s = Type<BF>::mma(s, tile.rows(lq, n, e), k[e]);
+          ds = Type<BF>::mma(ds, tile.rows(lo, n, e), v[e]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 off = *(const f32x4*)&stats[t & 1][0][n + token_of(i, half)];
+          const f32x4 delta = *(const f32x4*)&stats[t & 1][1][n + token_of(i, half)];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            s[i + j] = exp2_(fmaf(s[i + j], c, off[j]));
+            ds[i + j] = s[i + j] * (ds[i + j] - delta[j]);
+          }
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int r = row0 + n + token_of(i, half);
+            const bool seen = r >= first && r < rows;
+            s[i] = seen ? s[i] : 0.f;
+            ds[i] = seen ? ds[i] : 0.f;
+          }
+        }
+        // rows of the block that see the key
+        const int from = first - row0 - n, to = rows - 1 - row0 - n;
+#pragma unroll
+        for (int i = 0; i < 16; i += R) {
+          const u32x4 w = Type<BF>::operand(s, i), dw = Type<BF>::operand(ds, i);
+#pragma unroll
+          for (int b = 0; b < T::kBlocks; ++b) {
+            const u32x4 o = tile.columns(lo, n, i, b), q = tile.columns(lq, n, i, b);
+            if (careful) {
+              mma_seen<BF>(dv[b], o, w, i, from, to);
+              mma_seen<BF>(dk[b], q, dw, i, from, to);
+            } else {
+              dv[b] = Type<BF>::mma(dv[b], o, w);
+              dk[b] = Type<BF>::mma(dk[b], q, dw);
+            }
+          }
+        }
+      }
+    }
+    if (t + 1 < tiles) {
+      sq.store(lds[(t + 1) & 1][0]);
+      so.store(lds[(t + 1) & 1][1]);
+      store_stats((t + 1) & 1);
+      if (sq.odd() || so.odd()) odd[(t + 1) & 1] = t + 1;
+    }
+    __syncthreads();
+  }
+  store_result<BF, D>(dk, a.scale, a.dk + k_token * a.dk_row + g * a.dk_head, there);
+  store_result<BF, D>(dv, 1.f, a.dv + k_token * a.dv_row + g * a.dv_head, there);
+}
+
+// Slots of the tiles of `tile` rows (per_token rows a token).
+int64_t slots_of(int64_t tokens, int per_token, int sequences, int tile) { return tokens * per_token / tile + sequences; }
+
+template <bool BF, int D>
+hipError_t attend(AttendArgs& a, hipStream_t stream) {
+  constexpr int NW = 8;
+  a.q_slots = (int32_t)slots_of(a.q_tokens, a.hpk, a.sequences, NW * 32);
+  hipLaunchKernelGGL((attend_kernel<BF, D, NW>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(NW * 64), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <bool BF, int D>
+hipError_t attend_grad(AttendGradArgs& a, hipStream_t stream) {
+  constexpr int NW = 8;
+  a.q_slots = (int32_t)slots_of(a.q_tokens, a.hpk, a.sequences, NW * 32);
+  a.k_slots = (int32_t)slots_of(a.k_tokens, 1, a.sequences, NW * 32);
+  hipLaunchKernelGGL((attend_dq_kernel<BF, D, NW>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(NW * 64), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attend_dkv_kernel<BF, D, NW>), dim3((unsigned)a.k_slots * a.kv_heads), dim3(NW * 64), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attend(AttendArgs& a, bool bf16, int head_dim, hipStream_t stream) {
+  return head_dim == 64 ? (bf16 ? attend<true, 64>(a, stream) : attend<false, 64>(a, stream))
+                        : (bf16 ? attend<true, 128>(a, stream) : attend<false, 128>(a, stream));
+}
+
+hipError_t launch_attend_grad(AttendGradArgs& a, bool bf16, int head_dim, hipStream_t stream) {
+  return head_dim == 64 ? (bf16 ? attend_grad<true, 64>(a, stream) : attend_grad<false, 64>(a, stream))
+                        : (bf16 ? attend_grad<true, 128>(a, stream) : attend_grad<false, 128>(a, stream));
+}
+
+}  // namespace infs

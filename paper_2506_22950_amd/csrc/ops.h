@@ -85,6 +85,36 @@ infs_status pack_rotary_rows(const infs_rows* r, const char* what, int head_dim,
 // The configuration's part of the launch arguments.
 void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a);
 
+// ---- norms with the rotation ----------------------------------------------------
+constexpr int kNormThreads = 512;      // most of a work-group
+constexpr int kNormGradParts = 512;    // work-groups a tensor whose sums of d_w are added by a second launch
+
+struct NormWeights {
+  const void* weight[2];  // of q and k, or null: ones
+  int64_t weight_layer;   // elements
+  float eps, inv_dim;     // inv_dim, group: launch_norm_rotate
+  int32_t weight_f32, group, group_log2;  // lanes that hold a head
+};
+struct NormArgs : NormWeights {
+  RotaryArgs r;
+};
+struct NormGradArgs : NormWeights {
+  RotaryArgs r;           // in: the rows, out: their gradients
+  RotaryRows dq, dk;      // in: gradients of the outputs
+  float* sums[2];         // d_w, or null
+  float* part;            // [2][parts][head_dim]
+  int32_t first, batch[2];  // first tensor; tokens of a batch
+  uint32_t per_head[2];
+};
+static_assert(sizeof(NormGradArgs) <= 4096, "kernel argument block must fit 4 KiB");
+
+inline int norm_grad_parts(int64_t tokens) { return (int)(tokens < kNormGradParts ? tokens : kNormGradParts); }
+// Fill in what the structs leave to them.
+hipError_t launch_norm_rotate(NormArgs& args, bool bf16, bool interleaved, int layers, hipStream_t stream);
+hipError_t launch_norm_rotate_grad(NormGradArgs& args, bool bf16, bool interleaved, hipStream_t stream);
+// E_ARG (op_fail), or the weights of `layers` layers.
+infs_status pack_norms(const infs_norms* n, int head_dim, int layers, NormWeights* out);
+
 // ---- scores of tokens -----------------------------------------------------------
 constexpr int kScoreMaxRows = 1 << 23;
 static_assert(kScoreMaxRows <= kMostBlocks, "a work-group a row");
@@ -199,5 +229,56 @@ hipError_t launch_page_runs(const PageRuns& args, hipStream_t stream);
 // Fills in first_block.
 hipError_t launch_export(const PageFormat& f, MoveArgs& args, int layers, hipStream_t stream);
 hipError_t launch_import(const PageFormat& f, MoveArgs& args, int layers, hipStream_t stream);
+
+// ---- the choice of tokens ---------------------------------------------------------
+using Sampling = infs_sampling;
+constexpr int kChooseMaxRows = 1 << 22;  // a work-group of up to 1024 threads a row
+
+struct ChooseArgs {
+  const void* logits;
+  int64_t row_stride;  // elements
+  const float* uniform;
+  const Sampling* each;  // or null: all
+  Sampling all;
+  int32_t* token;
+  float* logprob;  // these two may be null
+  int32_t* kept;
+  int32_t rows, vocab;
+  int32_t unit;  // a weight is a number of units of 2^-unit (launch_choose)
+};
+
+hipError_t launch_choose(ChooseArgs& args, bool bf16, hipStream_t stream);
+
+// ---- attention of packed sequences ------------------------------------------------
+// Work-groups of a launch: of at most 512 threads, so half as many as of 256.
+constexpr int64_t kAttendMostBlocks = kMostBlocks / 2;
+
+struct AttendShape {
+  const int32_t *q_offsets, *k_offsets;  // [sequences + 1]
+  int32_t sequences, q_tokens, k_tokens, q_heads, kv_heads, hpk;
+  uint32_t hpk_inv;                      // 2^32 / hpk, rounded up
+  float scale;
+};
+
+struct AttendArgs : AttendShape {
+  const char *q, *k, *v;
+  char* o;
+  float* lse;  // [q_tokens, q_heads], or null
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;  // bytes
+  int32_t q_slots;  // launch_attend
+};
+
+struct AttendGradArgs : AttendShape {
+  const char *q, *k, *v, *o, *d_o;
+  char *dq, *dk, *dv;
+  const float* lse;
+  float* delta;  // [q_tokens, q_heads]: d_o.o of every row
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, do_row, do_head, dq_row, dq_head, dk_row, dk_head,
+      dv_row, dv_head;           // bytes
+  int32_t q_slots, k_slots;      // launch_attend_grad
+};
+
+hipError_t launch_attend(AttendArgs& args, bool bf16, int head_dim, hipStream_t stream);
+hipError_t launch_attend_grad(AttendGradArgs& args, bool bf16, int head_dim, hipStream_t stream);
 
 }  // namespace infs

@@ -1579,14 +1579,20 @@ infs_status infs_timing_end(infs_ctx* c, double* kernel_ms, double* region_ms, i
 
 namespace {
 
-// Rotate the n rows of a running or probe step: row s at position pos[s] where bit s of live is set.
+// Rotate the n rows of a running or probe step: row s at position pos[s] where bit s of live is set.  normed: with
+// the norms ahead.
 infs_status rotate_slots(infs_ctx* c, const infs_rotary* r, int32_t num_layers, const infs_rows* q, const infs_rows* k,
-                         int n, uint64_t live, const int32_t* pos) {
+                         int n, uint64_t live, const int32_t* pos, bool normed, const infs_norms* norms) {
   if (!r) return fail(c, INFS_E_ARG, "null rotary configuration");
   if (num_layers < 1 || num_layers > c->L) return fail(c, INFS_E_ARG, "num_layers must be in [1, %d]", c->L);
   if (!q && !k) return fail(c, INFS_E_ARG, "no rows given");
   if (r->cfg.head_dim != c->D) return fail(c, INFS_E_ARG, "rotary head_dim %d is not the context's %d", r->cfg.head_dim, c->D);
-  infs::RotaryArgs a{};
+  infs::NormArgs na{};
+  infs::RotaryArgs& a = na.r;
+  if (normed) {
+    const infs_status st = infs::pack_norms(norms, c->D, num_layers, &na);
+    if (st != INFS_OK) return fail(c, st, "%s", g_thread_error.c_str());
+  }
   const infs_rows* rows[2] = {q, k};
   const int heads[2] = {c->Hq, c->Hkv};
   for (int i = 0; i < 2; ++i) {
@@ -1602,17 +1608,17 @@ infs_status rotate_slots(infs_ctx* c, const infs_rotary* r, int32_t num_layers, 
   a.live = live;
   a.tokens = n;
   std::copy(pos, pos + n, a.pos);
-  HIP_TRY(c, infs::launch_rotate(a, c->key.bf16 != 0, r->cfg.layout == INFS_ROTARY_INTERLEAVED, num_layers, c->stream));
+  const bool bf16 = c->key.bf16 != 0, interleaved = r->cfg.layout == INFS_ROTARY_INTERLEAVED;
+  if (normed)
+    HIP_TRY(c, infs::launch_norm_rotate(na, bf16, interleaved, num_layers, c->stream));
+  else
+    HIP_TRY(c, infs::launch_rotate(a, bf16, interleaved, num_layers, c->stream));
   return INFS_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-infs_status infs_rotate_step(infs_ctx* c, const infs_rotary* r, int32_t num_layers, const infs_rows* q,
-                             const infs_rows* k) {
-  CHECK_CTX(c);
+// Rows of a running step, and of a probe step.
+infs_status rotate_step(infs_ctx* c, const infs_rotary* r, int32_t num_layers, const infs_rows* q, const infs_rows* k,
+                        bool normed, const infs_norms* norms) {
   uint64_t live = 0;
   int32_t pos[infs::kMaxSlots] = {};
   for (int s = 0; s < c->S; ++s) {
@@ -1622,12 +1628,12 @@ infs_status infs_rotate_step(infs_ctx* c, const infs_rotary* r, int32_t num_laye
     live |= uint64_t(1) << s;
     pos[s] = c->plen[p] + c->slot_len[s];
   }
-  return rotate_slots(c, r, num_layers, q, k, c->S, live, pos);
+  return rotate_slots(c, r, num_layers, q, k, c->S, live, pos, normed, norms);
 }
 
-infs_status infs_rotate_probe(infs_ctx* c, const infs_rotary* r, int32_t prompt, int32_t first_sample, int32_t n,
-                              const uint8_t* live_host, int32_t num_layers, const infs_rows* q, const infs_rows* k) {
-  CHECK_CTX(c);
+infs_status rotate_probe(infs_ctx* c, const infs_rotary* r, int32_t prompt, int32_t first_sample, int32_t n,
+                         const uint8_t* live_host, int32_t num_layers, const infs_rows* q, const infs_rows* k, bool normed,
+                         const infs_norms* norms) {
   if (c->probe_k == 0) return fail(c, INFS_E_STATE, "rotate_probe needs a context with probe_tokens > 0");
   if (prompt < 0 || prompt >= c->NP) return fail(c, INFS_E_ARG, "prompt %d out of range [0, %d)", prompt, c->NP);
   if (n < 1 || n > c->probe_batch) return fail(c, INFS_E_ARG, "n=%d out of range [1, %d]", n, c->probe_batch);
@@ -1641,7 +1647,36 @@ infs_status infs_rotate_probe(infs_ctx* c, const infs_rotary* r, int32_t prompt,
     live |= uint64_t(1) << j;
     pos[j] = c->plen[prompt] + c->probe_len[prompt][first_sample + j];
   }
-  return rotate_slots(c, r, num_layers, q, k, n, live, pos);
+  return rotate_slots(c, r, num_layers, q, k, n, live, pos, normed, norms);
+}
+
+}  // namespace
+
+extern "C" {
+
+infs_status infs_rotate_step(infs_ctx* c, const infs_rotary* r, int32_t num_layers, const infs_rows* q,
+                             const infs_rows* k) {
+  CHECK_CTX(c);
+  return rotate_step(c, r, num_layers, q, k, false, nullptr);
+}
+
+infs_status infs_rotate_probe(infs_ctx* c, const infs_rotary* r, int32_t prompt, int32_t first_sample, int32_t n,
+                              const uint8_t* live_host, int32_t num_layers, const infs_rows* q, const infs_rows* k) {
+  CHECK_CTX(c);
+  return rotate_probe(c, r, prompt, first_sample, n, live_host, num_layers, q, k, false, nullptr);
+}
+
+infs_status infs_norm_rotate_step(infs_ctx* c, const infs_rotary* r, const infs_norms* norms, int32_t num_layers,
+                                  const infs_rows* q, const infs_rows* k) {
+  CHECK_CTX(c);
+  return rotate_step(c, r, num_layers, q, k, true, norms);
+}
+
+infs_status infs_norm_rotate_probe(infs_ctx* c, const infs_rotary* r, const infs_norms* norms, int32_t prompt,
+                                   int32_t first_sample, int32_t n, const uint8_t* live_host, int32_t num_layers,
+                                   const infs_rows* q, const infs_rows* k) {
+  CHECK_CTX(c);
+  return rotate_probe(c, r, prompt, first_sample, n, live_host, num_layers, q, k, true, norms);
 }
 
 }  // extern "C"

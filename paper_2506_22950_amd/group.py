@@ -37,9 +37,45 @@ def schedulers_for(cfg, policy: str, pred=None) -> List[infs.Sched]:
     return out
 
 
+def prefill_prompts(ctx: infs.Context, prompt_lens: Sequence[int], num_layers: int, provide: Callable,
+                    attention: infs.Attention, offsets, rotary: Optional[infs.Rotary] = None,
+                    norms: Optional[infs.Norms] = None, positions=None) -> None:
+    """The prompts' own pass through every layer, all prompts packed: their rows are rotated (rotary; norms: normed
+    ahead of it) in place, attend to one another (Attention.attend) and stay in the shared-prefix store.
+
+    provide(layer) -> (q, k, v, o) device buffers of the packed rows ([T, Hq, d], [T, Hkv, d] twice, and [T, Hq, d]
+    for the outputs, all dense and of the context's type), T the sum of prompt_lens; what a model does between
+    its layers happens in there, on the context's stream, which the attention's has to be too.
+    offsets: device int32 [prompts + 1], where each prompt begins in them; positions: device int32 [T], each
+    token's position in its prompt (with rotary).
+    """
+    if rotary is None and norms is not None:
+        raise ValueError("norms go with rotary positions")
+    if rotary is not None and positions is None:
+        raise ValueError("rotary positions need the tokens' positions")
+    c, tokens = ctx.config, sum(prompt_lens)
+    size = c.num_kv_heads * c.head_dim * (4 if c.dtype == infs.F32 else 2)  # bytes of a token's K or V
+    for layer in range(num_layers):
+        q, k, v, o = (infs._ptr(x) for x in provide(layer))
+        if rotary is not None:
+            rows = infs.rotary_rows(q, q, c.num_q_heads), infs.rotary_rows(k, k, c.num_kv_heads)
+            if norms is not None:
+                rotary.norm_rotate_rows(c.dtype, tokens, infs.layer_norms(norms, layer), *rows, positions=positions,
+                                        stream=ctx.stream)
+            else:
+                rotary.rotate_rows(c.dtype, tokens, *rows, positions=positions, stream=ctx.stream)
+        attention.attend(len(prompt_lens), tokens, offsets, infs.rotary_rows(q, o, c.num_q_heads),
+                         infs.rotary_rows(k, None, c.num_kv_heads), infs.rotary_rows(v, None, c.num_kv_heads))
+        first = 0
+        for p, n in enumerate(prompt_lens):
+            ctx.prefill_shared(p, layer, n, k + first * size, v + first * size)
+            first += n
+
+
 def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Callable,
                 log: Optional[list] = None, after_step: Optional[Callable] = None, entry: str = "probe_step",
-                rotary: Optional[infs.Rotary] = None, carried: Collection = ()) -> int:
+                rotary: Optional[infs.Rotary] = None, carried: Collection = (),
+                norms: Optional[infs.Norms] = None) -> int:
     """Probe phase of prefix reuse (Section 4): every sample decodes its first
     min(L_i, k) tokens against the shared prompt, in batches of up to
     ctx.probe_batch samples of one prompt; samples that finish within their
@@ -57,12 +93,19 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
     before each call (one layer at a time).
     carried: the (prompt, sample) pairs that decode_group will take in as carried;
     they have tokens already and are neither probed nor released.
+    norms (with rotary): the heads of q and k_new are normed ahead of the rotation,
+    by each layer's weights.
     """
     c = ctx.config
+    if rotary is None and norms is not None:
+        raise ValueError("norms go with rotary positions")
 
-    def rotate(p, first, n, live, rows):
-        ctx.rotate_probe(rotary, p, first, n, live, infs.rotary_rows(rows[0], rows[0], c.num_q_heads),
-                         infs.rotary_rows(rows[1], rows[1], c.num_kv_heads))
+    def rotate(p, first, n, live, rows, layer):
+        q, k = infs.rotary_rows(rows[0], rows[0], c.num_q_heads), infs.rotary_rows(rows[1], rows[1], c.num_kv_heads)
+        if norms is not None:
+            ctx.norm_rotate_probe(rotary, infs.layer_norms(norms, layer), p, first, n, live, q, k)
+        else:
+            ctx.rotate_probe(rotary, p, first, n, live, q, k)
 
     nb = ctx.probe_batch
     steps = 0
@@ -84,13 +127,13 @@ def probe_group(ctx: infs.Context, lengths, k: int, num_layers: int, provide: Ca
                             raise ValueError("k_new and v_new need the same layer stride")
                     if rotary is not None:
                         for layer in range(num_layers):
-                            rotate(p, first, n, live, provide(steps, p, first, n, layer))
+                            rotate(p, first, n, live, provide(steps, p, first, n, layer), layer)
                     ctx.probe_step_layers(p, first, n, live, *b0, *strides)
                 else:
                     for layer in range(num_layers):
                         rows = provide(steps, p, first, n, layer)
                         if rotary is not None:
-                            rotate(p, first, n, live, rows)
+                            rotate(p, first, n, live, rows, layer)
                         ctx.probe_step(layer, p, first, n, live, *rows)
                 ctx.end_probe_step()
                 if after_step is not None:
@@ -111,7 +154,8 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
                  accepted: Optional[list] = None, reuse: int = 0, entry: str = "decode_step",
                  rotary: Optional[infs.Rotary] = None, scorer: Optional[infs.Scorer] = None,
                  logits: Optional[Callable] = None, carried: Optional[dict] = None,
-                 unfinished: Optional[Callable] = None) -> int:
+                 unfinished: Optional[Callable] = None, norms: Optional[infs.Norms] = None,
+                 sampler: Optional[infs.Sampler] = None, draws: Optional[Callable] = None) -> int:
     """Decode every sample of every prompt; returns the number of running steps.
 
     lengths[p][i]: true length of sample i of prompt p.
@@ -138,6 +182,11 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
     scorer: scores every step's tokens; logits(step) -> (logits, tokens, outputs)
     with a row per slot, outputs the keyword arguments of Scorer.score that
     take the results (logprob=..., entropy=..., ...).
+    norms (with rotary): the heads of q and k_new are normed ahead of the rotation,
+    by each layer's weights.
+    sampler: chooses every step's tokens, before they are scored; draws(step) ->
+    (logits, uniform, outputs) with a row per slot, outputs the keyword arguments of
+    Sampler.sample that say how and take the results (token=..., sampling=..., ...).
     carried: {(prompt, sample): (tokens, k, v)}: partial responses of an earlier
     iteration as dense rows; such a sample resumes after them when it is
     dispatched (Context.import_responses).  ValueError, before anything is done,
@@ -160,6 +209,10 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
     stopped = [False] * NP
     c = ctx.config
     carried = carried or {}
+    if rotary is None and norms is not None:
+        raise ValueError("norms go with rotary positions")
+    if (sampler is None) != (draws is None):
+        raise ValueError("a sampler needs draws, and draws a sampler")
     for p in range(NP):
         for i, length in enumerate(Ls[p]):
             if (p, i) not in carried:
@@ -169,9 +222,12 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
             if ctx.probe_state(p, i) > 0:
                 raise ValueError(f"sample {i} of prompt {p} was carried over and probed")
 
-    def rotate(layers, rows):
-        ctx.rotate_step(rotary, infs.rotary_rows(rows[0], rows[0], c.num_q_heads),
-                        infs.rotary_rows(rows[1], rows[1], c.num_kv_heads), num_layers=layers)
+    def rotate(layers, rows, layer=0):
+        q, k = infs.rotary_rows(rows[0], rows[0], c.num_q_heads), infs.rotary_rows(rows[1], rows[1], c.num_kv_heads)
+        if norms is not None:
+            ctx.norm_rotate_step(rotary, infs.layer_norms(norms, layer), q, k, num_layers=layers)
+        else:
+            ctx.rotate_step(rotary, q, k, num_layers=layers)
 
     def fill():
         taken = []
@@ -216,8 +272,11 @@ def decode_group(ctx: infs.Context, scheds: Sequence[infs.Sched], lengths, num_l
             for layer in range(num_layers):
                 rows = provide(step, layer)
                 if rotary is not None:
-                    rotate(1, rows)
+                    rotate(1, rows, layer)
                 decode(layer, *rows)
+        if sampler is not None:
+            z, uniform, outputs = draws(step)
+            sampler.sample(S, z, uniform, **outputs)
         if scorer is not None:
             z, tokens, outputs = logits(step)
             scorer.score(S, z, tokens, **outputs)

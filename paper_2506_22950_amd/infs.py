@@ -47,7 +47,9 @@ EXPORTS = (
     "infs_rotary_create", "infs_rotary_destroy", "infs_rotary_frequencies", "infs_rotate_rows",
     "infs_rotate_step", "infs_rotate_probe", "infs_scorer_create", "infs_scorer_destroy", "infs_score_tokens",
     "infs_score_grad", "infs_fork_slots", "infs_export_responses", "infs_import_responses", "infs_exchange_start",
-    "infs_set_exchange_start",
+    "infs_set_exchange_start", "infs_norm_rotate_rows", "infs_norm_rotate_step", "infs_norm_rotate_probe",
+    "infs_norm_rotate_grad", "infs_norm_rotate_grad_workspace", "infs_attention_create", "infs_attention_destroy",
+    "infs_attend", "infs_attend_grad", "infs_sampler_create", "infs_sampler_destroy", "infs_choose_tokens",
 )
 
 
@@ -89,6 +91,27 @@ class Rows(ctypes.Structure):
 class ScorerConfig(ctypes.Structure):
     _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("max_rows", ctypes.c_int32),
                 ("top_k", ctypes.c_int32), ("temperature", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class Norms(ctypes.Structure):
+    _fields_ = [("weight_q", ctypes.c_void_p), ("weight_k", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("layer_stride", ctypes.c_int64)]
+
+
+class AttentionConfig(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("max_tokens", ctypes.c_int32),
+                ("flags", ctypes.c_uint32)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_double), ("top_p", ctypes.c_double), ("min_p", ctypes.c_double),
+                ("top_k", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class SamplerConfig(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("flags", ctypes.c_uint32)]
 
 
 class Stats(ctypes.Structure):
@@ -172,6 +195,22 @@ def load():
         "infs_export_responses": (I32, [P, I32, P, P, P, I64]),
         "infs_import_responses": (I32, [P, I32, P, P, P, P, P, I64]),
         "infs_score_grad": (I32, [P, I32, P, I64, P, P, P, P, P, P, I64]),
+        "infs_norm_rotate_rows": (I32, [P, P, I32, I64, ctypes.POINTER(Norms), ctypes.POINTER(Rows), ctypes.POINTER(Rows),
+                                        P, I32]),
+        "infs_norm_rotate_step": (I32, [P, P, ctypes.POINTER(Norms), I32, ctypes.POINTER(Rows), ctypes.POINTER(Rows)]),
+        "infs_norm_rotate_probe": (I32, [P, P, ctypes.POINTER(Norms), I32, I32, I32, ctypes.POINTER(ctypes.c_uint8), I32,
+                                         ctypes.POINTER(Rows), ctypes.POINTER(Rows)]),
+        "infs_norm_rotate_grad": (I32, [P, P, I32, I64, ctypes.POINTER(Norms), ctypes.POINTER(Rows), ctypes.POINTER(Rows),
+                                        ctypes.POINTER(Rows), ctypes.POINTER(Rows), P, P, P, P, I32]),
+        "infs_norm_rotate_grad_workspace": (I64, [I64, I32]),
+        "infs_attention_create": (I32, [ctypes.POINTER(AttentionConfig), P, ctypes.POINTER(P)]),
+        "infs_attention_destroy": (None, [P]),
+        "infs_attend": (I32, [P, I32, I64, P, I64, P, ctypes.POINTER(Rows), ctypes.POINTER(Rows), ctypes.POINTER(Rows), P]),
+        "infs_attend_grad": (I32, [P, I32, I64, P, I64, P, ctypes.POINTER(Rows), ctypes.POINTER(Rows), ctypes.POINTER(Rows),
+                                   ctypes.POINTER(Rows), ctypes.POINTER(Rows), P]),
+        "infs_sampler_create": (I32, [ctypes.POINTER(SamplerConfig), P, ctypes.POINTER(P)]),
+        "infs_sampler_destroy": (None, [P]),
+        "infs_choose_tokens": (I32, [P, I32, P, I64, P, ctypes.POINTER(Sampling), P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -271,11 +310,124 @@ class Rotary:
         if st != OK:
             _check(None, st)
 
+    def norm_rotate_rows(self, dtype, tokens, norms, q=None, k=None, positions=None, first_position=0, stream=None):
+        """infs_norm_rotate_rows; norms is make_norms(...), q and k are rotary_rows(...)."""
+        st = _lib.infs_norm_rotate_rows(self._h, _stream(stream), dtype, tokens, norms, q, k, _ptr(positions),
+                                        first_position)
+        if st != OK:
+            _check(None, st)
+
+    def norm_rotate_grad(self, dtype, tokens, norms, q=None, k=None, dq=None, dk=None, d_weight_q=None, d_weight_k=None,
+                         workspace=None, positions=None, first_position=0, stream=None):
+        """infs_norm_rotate_grad; q, k: rows and where their gradients go, dq, dk: gradients of the outputs."""
+        st = _lib.infs_norm_rotate_grad(self._h, _stream(stream), dtype, tokens, norms, q, k, dq, dk, _ptr(d_weight_q),
+                                        _ptr(d_weight_k), _ptr(workspace), _ptr(positions), first_position)
+        if st != OK:
+            _check(None, st)
+
     def __del__(self):
         try:
             if self._h:
                 load().infs_rotary_destroy(self._h)
                 self._h = None
+        except Exception:
+            pass
+
+
+def make_norms(weight_q=None, weight_k=None, dtype=BF16, eps=1e-6, layer_stride=0) -> Norms:
+    """infs_norms; the weights' buffers stay with the caller."""
+    return Norms(_ptr(weight_q), _ptr(weight_k), dtype, eps, layer_stride)
+
+
+def layer_norms(norms: Norms, layer: int) -> Norms:
+    """The norms of one layer of several: the same weights from that layer on."""
+    by = layer * norms.layer_stride * (4 if norms.dtype == F32 else 2)
+    return Norms(norms.weight_q and norms.weight_q + by, norms.weight_k and norms.weight_k + by, norms.dtype, norms.eps,
+                 norms.layer_stride)
+
+
+def norm_rotate_grad_workspace(tokens, head_dim):
+    """Bytes of the workspace of Rotary.norm_rotate_grad."""
+    return load().infs_norm_rotate_grad_workspace(tokens, head_dim)
+
+
+def make_attention_config(**kw) -> AttentionConfig:
+    c = AttentionConfig()
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+class Attention:
+    """One infs_attention: causal attention of packed sequences and its gradient."""
+
+    def __init__(self, config: AttentionConfig, stream=None):
+        h = ctypes.c_void_p()
+        _check(None, load().infs_attention_create(ctypes.byref(config), _stream(stream), ctypes.byref(h)))
+        self._h = h
+        self.config = config
+
+    def attend(self, sequences, q_tokens, q_offsets, q, k, v, lse=None, k_tokens=None, k_offsets=None):
+        """infs_attend; q (queries, and where their outputs go), k and v are rotary_rows(...)."""
+        st = _lib.infs_attend(self._h, sequences, q_tokens, _ptr(q_offsets), q_tokens if k_tokens is None else k_tokens,
+                              _ptr(k_offsets), q, k, v, _ptr(lse))
+        if st != OK:
+            _check(None, st)
+
+    def grad(self, sequences, q_tokens, q_offsets, q, k, v, o, d_o, lse, k_tokens=None, k_offsets=None):
+        """infs_attend_grad; q, k and v: rows and where their gradients go, o and d_o: outputs and their gradients."""
+        st = _lib.infs_attend_grad(self._h, sequences, q_tokens, _ptr(q_offsets),
+                                   q_tokens if k_tokens is None else k_tokens, _ptr(k_offsets), q, k, v, o, d_o, _ptr(lse))
+        if st != OK:
+            _check(None, st)
+
+    def destroy(self):
+        if self._h:
+            load().infs_attention_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def make_sampling(temperature=0.0, top_k=0, top_p=0.0, min_p=0.0) -> Sampling:
+    return Sampling(temperature, top_p, min_p, top_k, 0)
+
+
+def make_sampler_config(**kw) -> SamplerConfig:
+    c = SamplerConfig()
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+class Sampler:
+    """One infs_sampler: the choice of tokens by given uniform numbers."""
+
+    def __init__(self, config: SamplerConfig, stream=None):
+        h = ctypes.c_void_p()
+        _check(None, load().infs_sampler_create(ctypes.byref(config), _stream(stream), ctypes.byref(h)))
+        self._h = h
+        self.config = config
+
+    def sample(self, rows, logits, uniform, token, logprob=None, kept=None, sampling=None, each=None, row_stride=0):
+        """infs_choose_tokens; sampling is make_sampling(...) for all rows, each a device array of one per row."""
+        st = _lib.infs_choose_tokens(self._h, rows, _ptr(logits), row_stride, _ptr(uniform), sampling, _ptr(each),
+                                     _ptr(token), _ptr(logprob), _ptr(kept))
+        if st != OK:
+            _check(None, st)
+
+    def destroy(self):
+        if self._h:
+            load().infs_sampler_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
         except Exception:
             pass
 
@@ -330,7 +482,8 @@ class Context:
     def __init__(self, config: Config, stream=None):
         lib = load()
         h = ctypes.c_void_p()
-        _check(None, lib.infs_create(ctypes.byref(config), _stream(stream), ctypes.byref(h)))
+        self.stream = _stream(stream)
+        _check(None, lib.infs_create(ctypes.byref(config), self.stream, ctypes.byref(h)))
         self._h = h
         self.config = config
 
@@ -462,6 +615,17 @@ class Context:
     def rotate_probe(self, rotary, prompt, first_sample, n, live, q=None, k=None, num_layers=1):
         """Rotate a probe step's rows before it is decoded."""
         self._call(load().infs_rotate_probe, rotary._h, prompt, first_sample, n, _flags(live, n), num_layers, q, k)
+
+    def norm_rotate_step(self, rotary, norms, q=None, k=None, num_layers=1):
+        """rotate_step with the norm of every head ahead of it; norms is make_norms(...)."""
+        st = _lib.infs_norm_rotate_step(self._h, rotary._h, norms, num_layers, q, k)
+        if st != OK:
+            _check(self._h, st)
+
+    def norm_rotate_probe(self, rotary, norms, prompt, first_sample, n, live, q=None, k=None, num_layers=1):
+        """rotate_probe with the norm of every head ahead of it."""
+        self._call(load().infs_norm_rotate_probe, rotary._h, norms, prompt, first_sample, n, _flags(live, n), num_layers, q,
+                   k)
 
     def end_probe_step(self):
         self._call(load().infs_end_probe_step)

@@ -1,0 +1,240 @@
+"""GPU: the choice of tokens against the definition in 64 bits, row by row.  Tokens and counts have to be equal
+(the inputs are fixed, and the library's sums are exact to 2^-45 or better, so that a number would have to fall
+within 1e-12 of a border to tell them apart).  logprob is a double rounded to fp32, its argument within 1e-12:
+2^-24 relative and 1e-11."""
+
+import math
+
+import numpy as np
+import pytest
+
+from paper_2506_22950_amd import infs
+
+pytestmark = pytest.mark.gpu
+
+
+def define(row, u, temperature=0.0, top_k=0, top_p=0.0, min_p=0.0):
+    """(token, logprob, kept) of one row (float64)."""
+    live = row > -np.inf
+    if not live.any() or not (row < np.inf).all() or not 0 <= u < 1:
+        return -1, math.nan, 0
+    w = np.exp((row - row.max()) / (temperature or 1.0))
+    order = np.argsort(-row, kind="stable")
+    order = order[live[order]]
+    if top_k:
+        order = order[:top_k]
+    if 0 < top_p < 1:
+        sums = np.cumsum(w[order])
+        order = order[:1 + int((sums[:-1] < top_p * sums[-1]).sum())]
+    order = order[w[order] >= min_p]
+    kept = np.sort(order)
+    sums = np.cumsum(w[kept])
+    at = min(int((sums <= u * sums[-1]).sum()), len(kept) - 1)
+    while w[kept[at]] == 0:
+        at -= 1
+    return int(kept[at]), math.log(w[kept[at]] / sums[-1]), len(kept)
+
+
+class Run:
+    def __init__(self, z, u, row_stride=0, stream=None, sampler=None, vocab=None, **kw):
+        import torch
+
+        self.z, self.u = z, u
+        n = z.shape[0]
+        v = vocab or z.shape[1]
+        s = sampler or infs.Sampler(infs.make_sampler_config(
+            vocab=v, dtype=infs.BF16 if z.dtype == torch.bfloat16 else infs.F32, max_rows=n),
+            stream=stream or torch.cuda.current_stream())
+        self.token, self.kept = (torch.full((n,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+        self.logprob = torch.full((n,), 7.0, device="cuda")
+        s.sample(n, z, u, self.token, self.logprob, self.kept, row_stride=row_stride, **kw)
+
+    def check(self, rows, each):
+        t, k, lp, u = self.token.cpu().numpy(), self.kept.cpu().numpy(), self.logprob.cpu().numpy(), self.u.cpu().numpy()
+        for i, row in enumerate(rows):
+            want = define(row, float(u[i]), **(each[i] if isinstance(each, list) else each))
+            assert (t[i], k[i]) == (want[0], want[2]), (i, t[i], k[i], want, each)
+            if want[0] < 0:
+                assert math.isnan(lp[i])
+            else:
+                assert abs(lp[i] - want[1]) <= abs(want[1]) * 2.0 ** -24 + 1e-11, (i, lp[i], want)
+
+
+def logits(n, v, bf16, seed, spread=3.0, masked=0):
+    import torch
+
+    gen = torch.Generator().manual_seed(seed)
+    z = torch.randn(n, v, generator=gen) * spread
+    z = z.bfloat16() if bf16 else z
+    if masked:
+        z[:, v - masked:] = -math.inf
+    u = torch.rand(n, generator=gen)
+    return z.cuda(), u.cuda(), z.double().numpy()
+
+
+WAYS = [{}, {"temperature": 0.6}, {"top_k": 1}, {"top_k": 50}, {"top_p": 0.9}, {"top_p": 0.2, "temperature": 1.5}, {"min_p": 0.05},
+        {"min_p": 1.0}, {"top_p": 1.0, "top_k": 10 ** 9}, {"top_k": 40, "top_p": 0.8, "min_p": 0.02, "temperature": 0.7},
+        {"top_p": 0.999, "min_p": 0.001}, {"top_k": 700, "top_p": 0.95}, {"top_p": 1e-12}]
+
+
+@pytest.mark.parametrize("way", WAYS, ids=str)
+@pytest.mark.parametrize("n,v,bf16", [(1, 1, True), (3, 2, False), (4, 63, True), (5, 1000, False), (3, 5003, True),
+                                      (3, 5003, False), (2, 50257, False), (2, 151936, True)])
+def test_against_the_definition(n, v, bf16, way):
+    z, u, z64 = logits(n, v, bf16, v + n, masked=v // 7)
+    Run(z, u, sampling=infs.make_sampling(**way)).check(z64, way)
+
+
+@pytest.mark.parametrize("rows", [1, 7, 64, 300, 1100])
+def test_many_rows(rows):
+    """Batches of every size, so that every kind of launch is met."""
+    way = {"top_p": 0.9, "top_k": 200}
+    z, u, z64 = logits(rows, 4099, True, rows)
+    Run(z, u, sampling=infs.make_sampling(**way)).check(z64, way)
+    Run(z, u).check(z64, {})
+
+
+def test_all_numbers_are_drawn_in_their_share():
+    """Over evenly spaced u the tokens come in index order, each as often as its share says (within one)."""
+    import torch
+
+    z, _, z64 = logits(1, 300, False, 9)
+    n = 4096
+    u = (torch.arange(n) / n).cuda()
+    r = Run(z.expand(n, 300).contiguous(), u, sampling=infs.make_sampling(top_p=0.9))
+    t = r.token.cpu().numpy()
+    assert (np.diff(t) >= 0).all()
+    got = np.bincount(t, minlength=300)
+    w = np.exp(z64[0])
+    order = np.argsort(-z64[0], kind="stable")
+    sums = np.cumsum(w[order])
+    kept = order[:1 + int((sums[:-1] < 0.9 * sums[-1]).sum())]
+    share = np.zeros(300)
+    share[kept] = w[kept] / w[kept].sum()
+    assert np.abs(got - share * n).max() <= 1.0 and (got[share == 0] == 0).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("way", [{}, {"top_k": 3}, {"top_k": 100, "top_p": 0.5}, {"top_p": 0.3}, {"min_p": 1.0}, {"top_k": 4000}])
+def test_equal_logits(bf16, way):
+    """Rows of one value (0 and -0 among them), of two values, of few values: ties go by the lower index."""
+    import torch
+
+    v = 5000
+    gen = torch.Generator().manual_seed(2)
+    rows = [torch.zeros(v), torch.where(torch.rand(v, generator=gen) < 0.5, 0.0, -0.0),
+            torch.where(torch.rand(v, generator=gen) < 0.1, 1.5, -2.0), torch.randint(0, 4, (v,), generator=gen).float(),
+            torch.full((v,), -3e38), torch.arange(v).float().div(100).floor()]
+    z = torch.stack(rows).to(torch.bfloat16 if bf16 else torch.float32)
+    for at in (0.0, 0.37, 1 - 2.0 ** -24):
+        u = torch.full((len(rows),), at).cuda()
+        Run(z.cuda(), u, sampling=infs.make_sampling(**way)).check(z.double().numpy(), way)
+
+
+@pytest.mark.parametrize("way", [{}, {"top_k": 5}, {"top_p": 0.9}, {"top_k": 50, "top_p": 0.9, "min_p": 0.1}])
+def test_extreme_values(way):
+    """The widest range, tiny and denormal values, temperatures at their ends."""
+    import torch
+
+    v = 3001
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(v, generator=gen)
+    wide = x * 1e38
+    wide[0], wide[1], wide[-1] = 3.4e38, -3.4e38, 3.4e38
+    tiny = x * 1e-41  # denormals
+    mixed = torch.cat([x[:1000] * 1e-41, x[1000:2000], x[2000:] * 1e30])
+    one = torch.full((v,), -math.inf)
+    one[1234] = -5.0
+    z = torch.stack([wide, tiny, x * 1e-38, mixed, one, x.clamp(-1, 1)])
+    u = torch.rand(len(z), generator=gen).cuda()
+    Run(z.cuda(), u, sampling=infs.make_sampling(**way)).check(z.double().numpy(), way)
+    for t in (2.0 ** -20, 2.0 ** 20):
+        way = dict(way, temperature=t)
+        Run(z.cuda(), u, sampling=infs.make_sampling(**way)).check(z.double().numpy(), way)
+
+
+def test_rows_without_a_token():
+    """Masked rows, NaN, +inf, numbers outside [0, 1): -1, NaN and 0; the rows beside them are not touched by it."""
+    import torch
+
+    z, u, _ = logits(8, 1003, False, 4)
+    z[1] = -math.inf
+    z[2, 77] = math.nan
+    z[3, 1002] = math.inf
+    u[4], u[5], u[6] = 1.0, -1e-9, math.nan
+    way = {"top_p": 0.9}
+    Run(z, u, sampling=infs.make_sampling(**way)).check(z.double().cpu().numpy(), way)
+
+
+def test_each_row_its_own_way():
+    import ctypes
+
+    import torch
+
+    ways = [{}, {"temperature": 0.5}, {"top_k": 7}, {"top_p": 0.5}, {"min_p": 0.2}, {"top_k": 9, "top_p": 0.7, "min_p": 0.01,
+                                                                                   "temperature": 2.0}]
+    bad = [{"temperature": -1.0}, {"temperature": math.nan}, {"top_k": -1}, {"top_p": 1.5}, {"top_p": math.nan}, {"min_p": -0.5},
+           {"min_p": math.nan}, {"temperature": 2.0 ** 21}]
+    all_ = ways + bad
+    arr = (infs.Sampling * len(all_))(*[infs.make_sampling(**w) for w in all_])
+    each = torch.frombuffer(bytearray(ctypes.string_at(arr, ctypes.sizeof(arr))), dtype=torch.uint8).cuda()
+    z, u, z64 = logits(len(all_), 2003, True, 5)
+    r = Run(z, u, each=each, sampling=infs.make_sampling(top_k=1))
+    t = r.token.cpu().numpy()
+    assert (t[len(ways):] == -1).all() and (r.kept.cpu().numpy()[len(ways):] == 0).all()
+    r.token, r.kept, r.logprob, r.u = (x[:len(ways)] for x in (r.token, r.kept, r.logprob, r.u))
+    r.check(z64[:len(ways)], ways)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_strides_and_alignment(bf16, shift):
+    """Rows apart, rows that begin off 16 bytes, values outside the rows that must not count."""
+    import torch
+
+    v, stride, n = 1501, 1509, 5
+    z, u, z64 = logits(n, v, bf16, 6)
+    buf = torch.full((n * stride + 8 + shift,), 1e30, dtype=z.dtype, device="cuda")
+    rows = buf[shift:shift + n * stride].view(n, stride)
+    rows[:, :v] = z
+    way = {"top_p": 0.8, "top_k": 100}
+    r = Run(rows, u, row_stride=stride, vocab=v, sampling=infs.make_sampling(**way))
+    r.check(z64, way)
+    Run(rows, u, row_stride=stride, vocab=v).check(z64, {})
+
+
+def test_longest_rows():
+    import torch
+
+    v = 1 << 24
+    z = torch.randn(2, v, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    u = torch.tensor([0.25, 0.75], device="cuda")
+    z64 = z.double().cpu().numpy()
+    for way in ({}, {"top_k": 1000000, "top_p": 0.9}):
+        Run(z, u, sampling=infs.make_sampling(**way)).check(z64, way)
+
+
+def test_graph_and_streams():
+    """Captured on a stream of its own and replayed with other logits and numbers, eager calls of another sampler
+    between the replays."""
+    import torch
+
+    n, v = 9, 30011
+    z, u = torch.empty(n, v, dtype=torch.bfloat16, device="cuda"), torch.empty(n, device="cuda")
+    side = torch.cuda.Stream()
+    s = infs.Sampler(infs.make_sampler_config(vocab=v, dtype=infs.BF16, max_rows=n), stream=side)
+    way = {"top_k": 60, "top_p": 0.9}
+    z.normal_(), u.uniform_()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        r = Run(z, u, sampler=s, sampling=infs.make_sampling(**way))
+    for i in range(4):
+        a, b, z64 = logits(n, v, True, 40 + i)
+        z.copy_(a), u.copy_(b)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        r.check(z64, way)
+        Run(z, u, sampling=infs.make_sampling(**way)).check(z64, way)
