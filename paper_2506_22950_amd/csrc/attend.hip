@@ -25,12 +25,21 @@
 //
 // Masked places.  A score that its row does not see is replaced, not added to,
 // and rows behind a sequence are zero in LDS.  Only a product over tokens of
-// one tile, some of them unseen, can meet 0 times an infinity or NaN: where
-// such a tile holds one (seen while it is staged), those elements are taken out
-// and added token by token, to the rows that see them.
+// one tile, some of them unseen, can meet 0 times an infinity or NaN.  Where
+// such a tile holds one (seen while it is staged), the work-group starts over
+// in a second pass over its tiles, in which those elements are taken out
+// of the products and added token by token to the rows that see them, 32
+// elements of the result at a time (so that the pass takes no more registers than
+// the first; inside the first it took those of a wavefront in four).
+//
+// Work-groups.  C wavefronts, of 32 rows each, share the tiles, and there are S
+// such groups, which take turns with the tiles and are joined at the end: many
+// columns for many rows (every byte out of L2 serves 256 of them), many splits
+// where there are too few work-groups to fill the GPU.
 #include "ops.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace infs {
 namespace {
@@ -69,10 +78,13 @@ struct Type<true> {
   }
   // slot j of 8 alone
   static __device__ __forceinline__ u32x4 only(u32x4 x, int j, bool here) {
-    u32x4 r = {0, 0, 0, 0};
-    if (here) r[j >> 1] = x[j >> 1] & ((j & 1) ? 0xffff0000u : 0xffffu);
-    return r;
+    const uint32_t m = !here ? 0u : (j & 1) ? 0xffff0000u : 0xffffu;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] &= k == j >> 1 ? m : 0u;
+    return x;
   }
+  // a sign bit is set where an exponent is all ones
+  static __device__ __forceinline__ uint32_t odd_bits(uint32_t x) { return (x & 0x7f807f80u) + 0x00800080u; }
   // the infinities and NaN alone
   static __device__ __forceinline__ u32x4 odd_part(u32x4 x) {
     u32x4 r;
@@ -107,10 +119,11 @@ struct Type<false> {
     return r;
   }
   static __device__ __forceinline__ u32x4 only(u32x4 x, int j, bool here) {
-    u32x4 r = {0, 0, 0, 0};
-    if (here) r[j] = x[j];
-    return r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = here && k == j ? x[k] : 0u;
+    return x;
   }
+  static __device__ __forceinline__ uint32_t odd_bits(uint32_t x) { return (x & 0x7f800000u) + 0x00800000u; }
   static __device__ __forceinline__ u32x4 odd_part(u32x4 x) {
     u32x4 r;
 #pragma unroll
@@ -182,7 +195,7 @@ __device__ __forceinline__ void mma_seen(f32x16& c, u32x4 a, u32x4 b, int i, int
   const int half = (threadIdx.x >> 5) & 1;
   const u32x4 rest = Type<BF>::odd_part(a);
   c = Type<BF>::mma(c, a ^ rest, b);
-#pragma unroll
+#pragma unroll 1
   for (int j = 0; j < Type<BF>::kRegs; ++j) {
 #pragma unroll 1
     for (int h = 0; h < 2; ++h) {
@@ -272,11 +285,10 @@ struct Stage {
   __device__ __forceinline__ bool odd() const {
     uint32_t r = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const u32x4 y = Type<BF>::odd_part(x[i]);
-      r |= y[0] | y[1] | y[2] | y[3];
-    }
-    return r != 0;
+    for (int i = 0; i < kPer; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r |= Type<BF>::odd_bits(x[i][j]);
+    return r & (BF ? 0x80008000u : 0x80000000u);
   }
 };
 
@@ -291,273 +303,376 @@ __device__ __forceinline__ void load_operands(u32x4 (&f)[STEPS], const char* row
   }
 }
 
-// A lane's row of results times `by`: acc[b] holds elements 32 b + token_of(i) of it.
-template <bool BF, int D>
-__device__ __forceinline__ void store_result(const f32x16 (&acc)[D / 32], float by, char* row, bool there) {
+// Elements 32 b .. 32 b + 31 of a lane's row of results times `by`: register i holds element token_of(i).
+template <bool BF>
+__device__ __forceinline__ void store_block(const f32x16& acc, float by, char* row, int b, bool there) {
   const int half = (threadIdx.x >> 5) & 1;
+  if constexpr (BF) {
 #pragma unroll
-  for (int b = 0; b < D / 32; ++b) {
-    if constexpr (BF) {
+    for (int q = 0; q < 4; q += 2) {
+      uint32_t w[4];
 #pragma unroll
-      for (int q = 0; q < 4; q += 2) {
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int i = 4 * q + 2 * k;
-          w[k] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)(acc[b][i] * by)) |
-                 (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)(acc[b][i + 1] * by)) << 16;
-        }
-        // two halves of 16 bytes each from two lanes: 8 elements from `half` on
-        const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-        const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-        if (there) *(u32x4*)(row + 64 * b + 16 * q + 16 * half) = u32x4{x[0], y[0], x[1], y[1]};
+      for (int k = 0; k < 4; ++k) {
+        const int i = 4 * q + 2 * k;
+        w[k] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)(acc[i] * by)) |
+               (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)(acc[i + 1] * by)) << 16;
       }
-    } else {
+      // two halves of 16 bytes each from two lanes: 8 elements from `half` on
+      const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+      const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+      if (there) *(u32x4*)(row + 64 * b + 16 * q + 16 * half) = u32x4{x[0], y[0], x[1], y[1]};
+    }
+  } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f32x4 v;
+    for (int q = 0; q < 4; ++q) {
+      f32x4 v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = acc[b][4 * q + k] * by;
-        if (there) *(f32x4*)(row + 128 * b + 32 * q + 16 * half) = v;
-      }
+      for (int k = 0; k < 4; ++k) v[k] = acc[4 * q + k] * by;
+      if (there) *(f32x4*)(row + 128 * b + 32 * q + 16 * half) = v;
     }
   }
 }
 
-template <bool BF>
-constexpr int kTileKeys = BF ? 64 : 32;
+// Sums over the S groups of a work-group's wavefronts, in group order, in the registers of group 0.  buffer: 4 KiB a
+// wavefront.
+template <int C, int S, int N>
+__device__ __forceinline__ void join(f32x16 (&acc)[N], char* buffer) {
+  if constexpr (S > 1) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
+      __syncthreads();
+      if (wave >= C)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *(f32x4*)(buffer + ((wave * 4 + i / 4) * 64 + lane) * 16) = f32x4{acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]};
+      __syncthreads();
+      if (wave < C)
+#pragma unroll
+        for (int g = 1; g < S; ++g)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const f32x4 x = *(const f32x4*)(buffer + (((g * C + wave) * 4 + i / 4) * 64 + lane) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[b][i + j] += x[j];
+          }
+    }
+  }
+}
+
+// Sizes of a kernel of C columns and S splits: tokens of a tile, buffers of tiles, LDS.  `values`: bytes ahead.
+template <bool BF, int D, int C, int S>
+struct Shape {
+  static constexpr int kThreads = 64 * C * S;
+  static constexpr int kBlock = BF && C > 2 ? 64 : 32;  // tokens of a group's tile
+  static constexpr int kTokens = kBlock * S;
+  static constexpr int kBuffers = S == 1 ? 2 : 1;
+  static constexpr int kTile = kTokens * Tile<BF, D>::kRow;
+  static constexpr int kJoin = S > 1 ? C * S * 4096 : 0;
+  static constexpr int kLds = 2 * kBuffers * kTile > kJoin ? 2 * kBuffers * kTile : kJoin;
+};
+
+// Walks tiles 0 .. n-1: load(t) brings the next tile's rows into registers, store(buffer, t) takes them into LDS,
+// use(buffer, t) reads them there.  Two buffers: loads of a tile are in flight while the one before is used.
+template <int BUFFERS, class Load, class Store, class Use>
+__device__ __forceinline__ void walk(int n, Load load, Store store, Use use) {
+  if (n <= 0) return;
+  load(0);
+  __syncthreads();
+  store(0, 0);
+  for (int t = 0; t < n; ++t) {
+    __syncthreads();
+    if (t + 1 < n) load(t + 1);
+    use(BUFFERS == 2 ? t & 1 : 0, t);
+    if (t + 1 < n) {
+      if (BUFFERS == 1) __syncthreads();
+      store(BUFFERS == 2 ? (t + 1) & 1 : 0, t + 1);
+    }
+  }
+}
+
+// The rows of a work-group and of its wavefronts, as the kernels of o and of dq have them.
+template <int C>
+struct Rows {
+  Place p;
+  int rows, row0, kb, keys, shift, token, head, last, seen_all, seen_any, seen_first, seen_last;
+  int64_t q_token;
+  bool there;
+  // false: nothing to do
+  __device__ __forceinline__ bool find(const AttendShape& a, int slots) {
+    constexpr int BM = 32 * C;
+    const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
+    const int slot = slots - 1 - (int)(blockIdx.x / (unsigned)a.kv_heads);  // the longest rows first
+    p = find_place(a.q_offsets, a.sequences, a.q_tokens, slot, a.hpk, __builtin_ctz(BM));
+    rows = (p.end - p.begin) * a.hpk, row0 = p.tile * BM;
+    if (p.tile < 0 || row0 >= rows) return false;
+    kb = offset_of(a.k_offsets, p.sequence, a.k_tokens);
+    keys = max(0, offset_of(a.k_offsets, p.sequence + 1, a.k_tokens) - kb);
+    shift = keys - (p.end - p.begin);
+    const int wrow = row0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % C * 32;
+    const int row = min(wrow + ((int)threadIdx.x & 31), rows - 1);
+    there = wrow + ((int)threadIdx.x & 31) < rows;
+    token = divide_rows(row, a.hpk, a.hpk_inv), head = g * a.hpk + row - token * a.hpk;
+    q_token = p.begin + token;
+    last = there ? token + shift : -1;  // the last key that the row sees
+    // .. that the wavefront's first, and its last row see, and the work-group's
+    seen_all = wrow < rows ? divide_rows(wrow, a.hpk, a.hpk_inv) + shift : -1;
+    seen_any = wrow < rows ? divide_rows(min(wrow + 31, rows - 1), a.hpk, a.hpk_inv) + shift : -1;
+    seen_first = divide_rows(row0, a.hpk, a.hpk_inv) + shift;
+    seen_last = divide_rows(min(row0 + BM, rows) - 1, a.hpk, a.hpk_inv) + shift;
+    return true;
+  }
+};
 
 // ---- o and lse -----------------------------------------------------------------
-template <bool BF, int D, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attend_kernel(const AttendArgs a) {
+template <bool BF, int D, int C, int S>
+__global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(const AttendArgs a) {
   using T = Tile<BF, D>;
-  constexpr int BM = NW * 32, BN = kTileKeys<BF>, NB = BN / 32, R = Type<BF>::kRegs;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][BN * T::kRow];  // K and V of two tiles
-  __shared__ int odd[2];  // the tile whose V holds an infinity or NaN
-  const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int slot = a.q_slots - 1 - (int)(blockIdx.x / (unsigned)a.kv_heads);  // the longest rows first
-  const Place p = find_place(a.q_offsets, a.sequences, a.q_tokens, slot, a.hpk, __builtin_ctz(BM));
-  const int rows = (p.end - p.begin) * a.hpk, row0 = p.tile * BM;
-  if (p.tile < 0 || row0 >= rows) return;
-  const int kb = offset_of(a.k_offsets, p.sequence, a.k_tokens);
-  const int keys = max(0, offset_of(a.k_offsets, p.sequence + 1, a.k_tokens) - kb);
-  const int shift = keys - (p.end - p.begin);
+  using H = Shape<BF, D, C, S>;
+  constexpr int BN = H::kBlock, NB = BN / 32, R = Type<BF>::kRegs;
+  __shared__ __attribute__((aligned(16))) char lds[H::kLds];
+  __shared__ float maxima[S][C * 32], sums[S][C * 32];
+  __shared__ int odd;  // V holds an infinity or NaN in a tile that some rows do not see
+  Rows<C> w;
+  if (!w.find(a, a.q_slots)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int wrow = row0 + wave * 32, row = wrow + (lane & 31);
-  const bool there = row < rows;
-  const int token = divide_rows(min(row, rows - 1), a.hpk, a.hpk_inv), head = g * a.hpk + min(row, rows - 1) - token * a.hpk;
-  const int last = there ? token + shift : -1;  // the last key that the row sees
-  // of the wavefront: the first row's, and the last row's
-  const int seen_all = wrow < rows ? divide_rows(wrow, a.hpk, a.hpk_inv) + shift : -1;
-  const int seen_any = wrow < rows ? divide_rows(min(wrow + 31, rows - 1), a.hpk, a.hpk_inv) + shift : -1;
-  const int seen_last = divide_rows(min(row0 + BM, rows) - 1, a.hpk, a.hpk_inv) + shift;
-  const int tiles = seen_last < 0 ? 0 : seen_last / BN + 1;
-
-  const char* kbase = a.k + kb * a.k_row + g * a.k_head;
-  const char* vbase = a.v + kb * a.v_row + g * a.v_head;
-  const int64_t q_token = p.begin + token;
-  u32x4 q[T::kSteps];
-  load_operands(q, a.q + q_token * a.q_row + head * a.q_head, there);
-
-  const T tile;
-  Stage<BF, D, BN, NW * 64> sk, sv;
-  f32x16 acc[T::kBlocks] = {};
-  float m = -INFINITY, sum = 0.f;
+  const int column = wave % C, group = wave / C, g = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  const int tiles = w.seen_last < 0 ? 0 : w.seen_last / H::kTokens + 1;
+  const char* kbase = a.k + w.kb * a.k_row + g * a.k_head;
+  const char* vbase = a.v + w.kb * a.v_row + g * a.v_head;
   const float c = a.scale * kLog2e;
-  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-  if (tiles > 0) {
-    sk.load(kbase, a.k_row, 0, keys);
-    sv.load(vbase, a.v_row, 0, keys);
-    __syncthreads();
-    sk.store(lds[0][0]);
-    sv.store(lds[0][1]);
-    if (sv.odd()) odd[0] = 0;
-  }
-  __syncthreads();
-  for (int t = 0; t < tiles; ++t) {
-    if (t + 1 < tiles) {
-      sk.load(kbase, a.k_row, (t + 1) * BN, keys);
-      sv.load(vbase, a.v_row, (t + 1) * BN, keys);
-    }
-    const int key0 = t * BN;
-    if (key0 <= seen_any) {
-      const char *lk = lds[t & 1][0], *lv = lds[t & 1][1];
-      f32x16 s[NB] = {};
+  const T tile;
+  if (threadIdx.x == 0) odd = 0;
+
+  const auto pass = [&](auto careful, int b0) {
+    constexpr int KB = careful ? 1 : T::kBlocks;  // blocks of 32 elements of the result, from b0 on
+    Stage<BF, D, H::kTokens, H::kThreads> sk, sv;
+    u32x4 q[T::kSteps];
+    load_operands(q, a.q + w.q_token * a.q_row + w.head * a.q_head, w.there);
+    f32x16 acc[KB] = {};
+    float m = -INFINITY, sum = 0.f;
+    walk<careful ? 1 : H::kBuffers>(
+        tiles,
+        [&](int t) {
+          sk.load(kbase, a.k_row, t * H::kTokens, w.keys);
+          sv.load(vbase, a.v_row, t * H::kTokens, w.keys);
+        },
+        [&](int buffer, int t) {
+          sk.store(lds + 2 * buffer * H::kTile);
+          sv.store(lds + (2 * buffer + 1) * H::kTile);
+          if (!careful && t * H::kTokens + H::kTokens - 1 > w.seen_first && sv.odd()) odd = 1;
+        },
+        [&](int buffer, int t) {
+          const int key0 = t * H::kTokens + group * BN;
+          if (key0 > w.seen_any) return;
+          const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kRow;
+          const char* lv = lk + H::kTile;
+          f32x16 s[NB] = {};
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+          for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int e = 0; e < T::kSteps; ++e) s[n] = Type<BF>::mma(s[n], tile.rows(lk, 32 * n, e), q[e]);
-      const bool masked = key0 + BN - 1 > seen_all;
-      if (masked) {
+            for (int e = 0; e < T::kSteps; ++e) s[n] = Type<BF>::mma(s[n], tile.rows(lk, 32 * n, e), q[e]);
+          if (key0 + BN - 1 > w.seen_all) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[n][i] = key0 + 32 * n + token_of(i, half) <= last ? s[n][i] : -INFINITY;
-      }
+              for (int i = 0; i < 16; ++i) s[n][i] = key0 + 32 * n + token_of(i, half) <= w.last ? s[n][i] : -INFINITY;
+          }
+          float top = -INFINITY;
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+          top = fmaxf(m, fmaxf(top, other_half(top)));
+          if (__any(top > m)) {
+            const float by = exp2_((m - (top == -INFINITY ? 0.f : top)) * c);
+            sum *= by;
+#pragma unroll
+            for (int b = 0; b < KB; ++b) acc[b] *= by;
+            m = top;
+          }
+          const float off = m == -INFINITY ? 0.f : -m * c;
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              s[n][i] = exp2_(fmaf(s[n][i], c, off));
+              sum += s[n][i];
+            }
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; i += R) {
+              const u32x4 p = Type<BF>::operand(s[n], i);
+#pragma unroll
+              for (int b = 0; b < KB; ++b) {
+                const u32x4 v = tile.columns(lv, 32 * n, i, b0 + b);
+                if constexpr (careful)
+                  mma_seen<BF>(acc[b], v, p, i, 0, w.last - key0 - 32 * n);
+                else
+                  acc[b] = Type<BF>::mma(acc[b], v, p);
+              }
+            }
+        });
+    sum += other_half(sum);
+    if constexpr (S > 1) {
+      __syncthreads();
+      if (half == 0) maxima[group][column * 32 + lane] = m, sums[group][column * 32 + lane] = sum;
+      __syncthreads();
+      const int at = column * 32 + (lane & 31);
       float top = -INFINITY;
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+      for (int i = 0; i < S; ++i) top = fmaxf(top, maxima[i][at]);
+      const float base = top == -INFINITY ? 0.f : top;
+      const float by = exp2_((m - base) * c);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-      top = fmaxf(m, fmaxf(top, other_half(top)));
-      if (__any(top > m)) {
-        const float by = exp2_((m - (top == -INFINITY ? 0.f : top)) * c);
-        sum *= by;
+      for (int b = 0; b < KB; ++b) acc[b] *= by;
+      m = top, sum = 0.f;
 #pragma unroll
-        for (int b = 0; b < T::kBlocks; ++b) acc[b] *= by;
-        m = top;
-      }
-      const float off = m == -INFINITY ? 0.f : -m * c;
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[n][i] = exp2_(fmaf(s[n][i], c, off));
-          sum += s[n][i];
-        }
-      const bool careful = masked && odd[t & 1] == t;
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; i += R) {
-          const u32x4 w = Type<BF>::operand(s[n], i);
-#pragma unroll
-          for (int b = 0; b < T::kBlocks; ++b) {
-            const u32x4 v = tile.columns(lv, 32 * n, i, b);
-            if (careful)
-              mma_seen<BF>(acc[b], v, w, i, 0, last - key0 - 32 * n);
-            else
-              acc[b] = Type<BF>::mma(acc[b], v, w);
-          }
-        }
+      for (int i = 0; i < S; ++i) sum = fmaf(sums[i][at], exp2_((maxima[i][at] - base) * c), sum);
+      join<C, S>(acc, lds);
+      if (group > 0) return;
     }
-    if (t + 1 < tiles) {
-      sk.store(lds[(t + 1) & 1][0]);
-      sv.store(lds[(t + 1) & 1][1]);
-      if (sv.odd()) odd[(t + 1) & 1] = t + 1;
+    const float by = w.last < 0 ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) store_block<BF>(acc[b], by, a.o + w.q_token * a.o_row + w.head * a.o_head, b0 + b, w.there);
+    if (w.there && half == 0 && a.lse)
+      a.lse[w.q_token * a.q_heads + w.head] =
+          w.last < 0 ? -INFINITY : (m == -INFINITY ? 0.f : m * a.scale) + __log2f(sum) * kLn2;
+  };
+  pass(std::false_type{}, 0);
+  __syncthreads();
+  if (odd)
+    for (int b = 0; b < T::kBlocks; ++b) {
+      __syncthreads();
+      pass(std::true_type{}, b);
     }
-    __syncthreads();
-  }
-  sum += other_half(sum);
-  const float by = last < 0 ? 0.f : 1.f / sum;
-  store_result<BF, D>(acc, by, a.o + q_token * a.o_row + head * a.o_head, there);
-  if (there && half == 0 && a.lse)
-    a.lse[q_token * a.q_heads + head] = last < 0 ? -INFINITY : (m == -INFINITY ? 0.f : m * a.scale) + __log2f(sum) * kLn2;
 }
 
 // ---- dq (and D) ----------------------------------------------------------------
-// The loop of the forward kernel with the scores' exponentials from lse: s^T and (v up)^T of a tile, ds^T from
+// The walk of the forward kernel with the scores' exponentials from lse: s^T and (v up)^T of a tile, ds^T from
 // them, dq^T += K^T ds^T.  D = up.o of every row is left in a.delta for the kernel of dk and dv.
-template <bool BF, int D, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attend_dq_kernel(const AttendGradArgs a) {
+template <bool BF, int D, int C, int S>
+__global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kernel(const AttendGradArgs a) {
   using T = Tile<BF, D>;
-  constexpr int BM = NW * 32, BN = kTileKeys<BF>, NB = BN / 32, R = Type<BF>::kRegs;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][BN * T::kRow];
-  __shared__ int odd[2];  // the tile whose K holds an infinity or NaN
-  const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int slot = a.q_slots - 1 - (int)(blockIdx.x / (unsigned)a.kv_heads);
-  const Place p = find_place(a.q_offsets, a.sequences, a.q_tokens, slot, a.hpk, __builtin_ctz(BM));
-  const int rows = (p.end - p.begin) * a.hpk, row0 = p.tile * BM;
-  if (p.tile < 0 || row0 >= rows) return;
-  const int kb = offset_of(a.k_offsets, p.sequence, a.k_tokens);
-  const int keys = max(0, offset_of(a.k_offsets, p.sequence + 1, a.k_tokens) - kb);
-  const int shift = keys - (p.end - p.begin);
+  using H = Shape<BF, D, C, S>;
+  constexpr int BN = H::kBlock, NB = BN / 32, R = Type<BF>::kRegs;
+  __shared__ __attribute__((aligned(16))) char lds[H::kLds];
+  __shared__ int odd;  // K holds an infinity or NaN in a tile that some rows do not see
+  Rows<C> w;
+  if (!w.find(a, a.q_slots)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int wrow = row0 + wave * 32, row = wrow + (lane & 31);
-  const bool there = row < rows;
-  const int token = divide_rows(min(row, rows - 1), a.hpk, a.hpk_inv), head = g * a.hpk + min(row, rows - 1) - token * a.hpk;
-  const int last = there ? token + shift : -1;
-  const int seen_all = wrow < rows ? divide_rows(wrow, a.hpk, a.hpk_inv) + shift : -1;
-  const int seen_any = wrow < rows ? divide_rows(min(wrow + 31, rows - 1), a.hpk, a.hpk_inv) + shift : -1;
-  const int seen_last = divide_rows(min(row0 + BM, rows) - 1, a.hpk, a.hpk_inv) + shift;
-  const int tiles = seen_last < 0 ? 0 : seen_last / BN + 1;
-
-  const char* kbase = a.k + kb * a.k_row + g * a.k_head;
-  const char* vbase = a.v + kb * a.v_row + g * a.v_head;
-  const int64_t q_token = p.begin + token;
-  u32x4 q[T::kSteps], up[T::kSteps];
-  float delta = 0.f;
-  load_operands(q, a.o + q_token * a.o_row + head * a.o_head, there);
-  load_operands(up, a.d_o + q_token * a.do_row + head * a.do_head, there);
-#pragma unroll
-  for (int s = 0; s < T::kSteps; ++s) delta += Type<BF>::dot(q[s], up[s]);
-  delta += other_half(delta);
-  load_operands(q, a.q + q_token * a.q_row + head * a.q_head, there);
-  const int64_t at = q_token * a.q_heads + head;
-  if (there && half == 0) a.delta[at] = delta;
-  const float c = a.scale * kLog2e, off = there ? -a.lse[at] * kLog2e : 0.f;
-
+  const int group = wave / C, g = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  const int tiles = w.seen_last < 0 ? 0 : w.seen_last / H::kTokens + 1;
+  const char* kbase = a.k + w.kb * a.k_row + g * a.k_head;
+  const char* vbase = a.v + w.kb * a.v_row + g * a.v_head;
+  const int64_t at = w.q_token * a.q_heads + w.head;
+  const float c = a.scale * kLog2e, off = w.there ? -a.lse[at] * kLog2e : 0.f;
   const T tile;
-  Stage<BF, D, BN, NW * 64> sk, sv;
-  f32x16 acc[T::kBlocks] = {};
-  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-  if (tiles > 0) {
-    sk.load(kbase, a.k_row, 0, keys);
-    sv.load(vbase, a.v_row, 0, keys);
-    __syncthreads();
-    sk.store(lds[0][0]);
-    sv.store(lds[0][1]);
-    if (sk.odd()) odd[0] = 0;
-  }
-  __syncthreads();
-  for (int t = 0; t < tiles; ++t) {
-    if (t + 1 < tiles) {
-      sk.load(kbase, a.k_row, (t + 1) * BN, keys);
-      sv.load(vbase, a.v_row, (t + 1) * BN, keys);
-    }
-    const int key0 = t * BN;
-    if (key0 <= seen_any) {
-      const char *lk = lds[t & 1][0], *lv = lds[t & 1][1];
-      const bool masked = key0 + BN - 1 > seen_all, careful = masked && odd[t & 1] == t;
+  if (threadIdx.x == 0) odd = 0;
+
+  const auto pass = [&](auto careful, int b0) {
+    constexpr int KB = careful ? 1 : T::kBlocks;
+    Stage<BF, D, H::kTokens, H::kThreads> sk, sv;
+    u32x4 q[T::kSteps], up[T::kSteps];
+    float delta = 0.f;
+    load_operands(q, a.o + w.q_token * a.o_row + w.head * a.o_head, w.there);
+    load_operands(up, a.d_o + w.q_token * a.do_row + w.head * a.do_head, w.there);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        f32x16 s = {}, ds = {};
+    for (int s = 0; s < T::kSteps; ++s) delta += Type<BF>::dot(q[s], up[s]);
+    delta += other_half(delta);
+    load_operands(q, a.q + w.q_token * a.q_row + w.head * a.q_head, w.there);
+    if (w.there && half == 0 && group == 0) a.delta[at] = delta;
+    f32x16 acc[KB] = {};
+    walk<careful ? 1 : H::kBuffers>(
+        tiles,
+        [&](int t) {
+          sk.load(kbase, a.k_row, t * H::kTokens, w.keys);
+          sv.load(vbase, a.v_row, t * H::kTokens, w.keys);
+        },
+        [&](int buffer, int t) {
+          sk.store(lds + 2 * buffer * H::kTile);
+          sv.store(lds + (2 * buffer + 1) * H::kTile);
+          if (!careful && t * H::kTokens + H::kTokens - 1 > w.seen_first && sk.odd()) odd = 1;
+        },
+        [&](int buffer, int t) {
+          const int key0 = t * H::kTokens + group * BN;
+          if (key0 > w.seen_any) return;
+          const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kRow;
+          const char* lv = lk + H::kTile;
+          const bool masked = key0 + BN - 1 > w.seen_all;
 #pragma unroll
-        for (int e = 0; e < T::kSteps; ++e) {
-          s = Type<BF>::mma(s, tile.rows(lk, 32 * n, e), q[e]);
-          ds = Type<BF>::mma(ds, tile.rows(lv, 32 * n, e), up[e]);
-        }
+          for (int n = 0; n < NB; ++n) {
+            f32x16 s = {}, ds = {};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ds[i] = exp2_(fmaf(s[i], c, off)) * (ds[i] - delta);
-        if (masked) {
+            for (int e = 0; e < T::kSteps; ++e) {
+              s = Type<BF>::mma(s, tile.rows(lk, 32 * n, e), q[e]);
+              ds = Type<BF>::mma(ds, tile.rows(lv, 32 * n, e), up[e]);
+            }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) ds[i] = key0 + 32 * n + token_of(i, half) <= last ? ds[i] : 0.f;
-        }
+            for (int i = 0; i < 16; ++i) ds[i] = exp2_(fmaf(s[i], c, off)) * (ds[i] - delta);
+            if (masked) {
 #pragma unroll
-        for (int i = 0; i < 16; i += R) {
-          const u32x4 w = Type<BF>::operand(ds, i);
+              for (int i = 0; i < 16; ++i) ds[i] = key0 + 32 * n + token_of(i, half) <= w.last ? ds[i] : 0.f;
+            }
 #pragma unroll
-          for (int b = 0; b < T::kBlocks; ++b) {
-            const u32x4 k = tile.columns(lk, 32 * n, i, b);
-            if (careful)
-              mma_seen<BF>(acc[b], k, w, i, 0, last - key0 - 32 * n);
-            else
-              acc[b] = Type<BF>::mma(acc[b], k, w);
+            for (int i = 0; i < 16; i += R) {
+              const u32x4 p = Type<BF>::operand(ds, i);
+#pragma unroll
+              for (int b = 0; b < KB; ++b) {
+                const u32x4 k = tile.columns(lk, 32 * n, i, b0 + b);
+                if constexpr (careful)
+                  mma_seen<BF>(acc[b], k, p, i, 0, w.last - key0 - 32 * n);
+                else
+                  acc[b] = Type<BF>::mma(acc[b], k, p);
+              }
+            }
           }
-        }
-      }
+        });
+    join<C, S>(acc, lds);
+    if (group > 0) return;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+      store_block<BF>(acc[b], a.scale, a.dq + w.q_token * a.dq_row + w.head * a.dq_head, b0 + b, w.there);
+  };
+  pass(std::false_type{}, 0);
+  __syncthreads();
+  if (odd)
+    for (int b = 0; b < T::kBlocks; ++b) {
+      __syncthreads();
+      pass(std::true_type{}, b);
     }
-    if (t + 1 < tiles) {
-      sk.store(lds[(t + 1) & 1][0]);
-      sv.store(lds[(t + 1) & 1][1]);
-      if (sk.odd()) odd[(t + 1) & 1] = t + 1;
-    }
-    __syncthreads();
-  }
-  store_result<BF, D>(acc, a.scale, a.dq + q_token * a.dq_row + head * a.dq_head, there);
 }
 
 // ---- dk and dv -----------------------------------------------------------------
 // A wavefront's 32 keys are the columns: s = Q k^T and up v^T over a tile of rows, p and ds from them, then
 // dv^T += up^T p and dk^T += Q^T ds with the rows as the tokens of the sum.  A key is seen by the rows from
 // (key - shift) hpk on.
-template <bool BF, int D, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attend_dkv_kernel(const AttendGradArgs a) {
+//
+// Registers: two operands and two results of 32 keys, 192 of them for bf16 heads of 128 and twice as many operands in
+// fp32.  For bf16 the values' operand stays in LDS (a quarter more to read there; in registers the kernel spilled);
+// fp32 heads of 128, and splits, take a wavefront's whole file.
+template <bool BF, int D, int C, int S>
+struct KeyShape {
+  static constexpr int kThreads = 64 * C * S;
+  static constexpr int kBlock = BF && D == 64 && C > 1 ? 64 : 32;  // rows of a group's tile
+  static constexpr int kTokens = kBlock * S;
+  static constexpr int kBuffers = S == 1 ? 2 : 1;
+  static constexpr int kTile = kTokens * Tile<BF, D>::kRow;
+  static constexpr bool kValues = D == 128 && BF == (S == 1);  // in LDS
+  static constexpr int kValueBytes = kValues ? 32 * C * Tile<BF, D>::kRow : 0;
+  static constexpr int kJoin = S > 1 ? C * S * 4096 : 0;
+  static constexpr int kTiles = 2 * kBuffers * kTile > kJoin ? 2 * kBuffers * kTile : kJoin;
+};
+
+template <bool BF, int D, int C, int S>
+__global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dkv_kernel(const AttendGradArgs a) {
   using T = Tile<BF, D>;
-  constexpr int BK = NW * 32, BR = BF && D == 64 ? 64 : 32, R = Type<BF>::kRegs;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][BR * T::kRow];  // Q and d_o of two tiles
-  __shared__ __attribute__((aligned(16))) float stats[2][2][BR];  // -lse log2(e) and D of their rows
-  __shared__ int odd[2];  // the tile that holds an infinity or NaN
+  using H = KeyShape<BF, D, C, S>;
+  constexpr int BK = 32 * C, BR = H::kBlock, R = Type<BF>::kRegs;
+  __shared__ __attribute__((aligned(16))) char lds[H::kTiles + H::kValueBytes];  // Q and d_o of tiles, V
+  __shared__ __attribute__((aligned(16))) float stats[2][2][H::kTokens];         // -lse log2(e) and D of their rows
+  __shared__ int odd;  // Q or d_o holds an infinity or NaN in a tile of which some keys are not seen
   const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
   const int slot = (int)(blockIdx.x / (unsigned)a.kv_heads);
   const Place p = find_place(a.k_offsets, a.sequences, a.k_tokens, slot, 1, __builtin_ctz(BK));
@@ -567,140 +682,170 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_dkv_kernel(const AttendGrad
   const int queries = max(0, offset_of(a.q_offsets, p.sequence + 1, a.q_tokens) - qb);
   const int shift = keys - queries, rows = queries * a.hpk;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int wkey = key0 + wave * 32, key = wkey + (lane & 31);
+  const int group = wave / C, wkey = key0 + wave % C * 32, key = wkey + (lane & 31);
   const bool there = key < keys;
   const auto first_row = [&](int k) { return max(0, k - shift) * a.hpk; };
-  const int first = there ? first_row(key) : INT32_MAX;       // the first row that sees the key
+  const int first = there ? first_row(key) : INT32_MAX;          // the first row that sees the key
   const int wfirst = wkey < keys ? first_row(wkey) : INT32_MAX;  // .. any, and all, of the wavefront's
   const int wall = first_row(min(wkey + 31, keys - 1));
-  const int begin = first_row(key0), tiles = rows > begin ? (rows - begin + BR - 1) / BR : 0;
-
+  const int all = first_row(min(key0 + BK, keys) - 1);           // .. all of the work-group's
+  const int begin = first_row(key0), tiles = rows > begin ? (rows - begin + H::kTokens - 1) / H::kTokens : 0;
   const int64_t k_token = p.begin + (there ? key : key0);
-  u32x4 k[T::kSteps], v[T::kSteps];
-  load_operands(k, a.k + k_token * a.k_row + g * a.k_head, there);
-  load_operands(v, a.v + k_token * a.v_row + g * a.v_head, there);
   const char* qbase = a.q + qb * a.q_row + (int64_t)g * a.hpk * a.q_head;
   const char* dobase = a.d_o + qb * a.do_row + (int64_t)g * a.hpk * a.do_head;
-  const float* stat = half ? a.delta : a.lse;
-  float st = 0.f;
-  // the first wavefronts: one of a row's two values a lane
-  const auto load_stats = [&](int r0) {
-    const int r = r0 + wave * 32 + (lane & 31);
-    st = 0.f;
-    if (wave < BR / 32 && r < rows) {
-      const int t = divide_rows(r, a.hpk, a.hpk_inv);
-      st = stat[(int64_t)(qb + t) * a.q_heads + g * a.hpk + r - t * a.hpk];
-    }
-  };
-  const auto store_stats = [&](int buf) {
-    if (wave < BR / 32) stats[buf][half][wave * 32 + (lane & 31)] = half ? st : -st * kLog2e;
-  };
-
-  const T tile;
-  Stage<BF, D, BR, NW * 64> sq, so;
-  f32x16 dk[T::kBlocks] = {}, dv[T::kBlocks] = {};
   const float c = a.scale * kLog2e;
-  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-  if (tiles > 0) {
-    sq.load_rows(qbase, a.q_row, a.q_head, begin, rows, a.hpk, a.hpk_inv);
-    so.load_rows(dobase, a.do_row, a.do_head, begin, rows, a.hpk, a.hpk_inv);
-    load_stats(begin);
-    __syncthreads();
-    sq.store(lds[0][0]);
-    so.store(lds[0][1]);
-    store_stats(0);
-    if (sq.odd() || so.odd()) odd[0] = 0;
+  const T tile;
+  if (threadIdx.x == 0) odd = 0;
+  char* values = lds + H::kTiles;
+  if constexpr (H::kValues) {
+    Stage<BF, D, BK, H::kThreads> sv;
+    sv.load(a.v + p.begin * a.v_row + g * a.v_head, a.v_row, key0, keys);
+    sv.store(values);
   }
-  __syncthreads();
-  for (int t = 0; t < tiles; ++t) {
-    const int row0 = begin + t * BR;
-    if (t + 1 < tiles) {
-      sq.load_rows(qbase, a.q_row, a.q_head, row0 + BR, rows, a.hpk, a.hpk_inv);
-      so.load_rows(dobase, a.do_row, a.do_head, row0 + BR, rows, a.hpk, a.hpk_inv);
-      load_stats(row0 + BR);
-    }
-    if (row0 + BR > wfirst) {
-      const char *lq = lds[t & 1][0], *lo = lds[t & 1][1];
-      const bool masked = row0 < wall || row0 + BR > rows, careful = masked && odd[t & 1] == t;
-#pragma unroll
-      for (int n = 0; n < BR; n += 32) {
-        f32x16 s = {}, ds = {};
-#pragma unroll
-        for (int e = 0; e < T::kSteps; ++e) {
-          s = Type<BF>::mma(s, tile.rows(lq, n, e), k[e]);
-          ds = Type<BF>::mma(ds, tile.rows(lo, n, e), v[e]);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const f32x4 off = *(const f32x4*)&stats[t & 1][0][n + token_of(i, half)];
-          const f32x4 delta = *(const f32x4*)&stats[t & 1][1][n + token_of(i, half)];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            s[i + j] = exp2_(fmaf(s[i + j], c, off[j]));
-            ds[i + j] = s[i + j] * (ds[i + j] - delta[j]);
+  const char* own_values = values + wave % C * 32 * T::kRow;
+
+  const auto pass = [&](auto careful, int b0) {
+    constexpr int KB = careful ? 1 : T::kBlocks;
+    Stage<BF, D, H::kTokens, H::kThreads> sq, so;
+    u32x4 k[T::kSteps], v[H::kValues ? 1 : T::kSteps];
+    load_operands(k, a.k + k_token * a.k_row + g * a.k_head, there);
+    if constexpr (!H::kValues) load_operands(v, a.v + k_token * a.v_row + g * a.v_head, there);
+    const float* stat = half ? a.delta : a.lse;
+    float st = 0.f;  // the first wavefronts: one of a row's two values a lane
+    f32x16 dk[KB] = {}, dv[KB] = {};
+    walk<careful ? 1 : H::kBuffers>(
+        tiles,
+        [&](int t) {
+          const int row0 = begin + t * H::kTokens, r = row0 + wave * 32 + (lane & 31);
+          sq.load_rows(qbase, a.q_row, a.q_head, row0, rows, a.hpk, a.hpk_inv);
+          so.load_rows(dobase, a.do_row, a.do_head, row0, rows, a.hpk, a.hpk_inv);
+          st = 0.f;
+          if (wave < H::kTokens / 32 && r < rows) {
+            const int i = divide_rows(r, a.hpk, a.hpk_inv);
+            st = stat[(int64_t)(qb + i) * a.q_heads + g * a.hpk + r - i * a.hpk];
           }
-        }
-        if (masked) {
+        },
+        [&](int buffer, int t) {
+          sq.store(lds + 2 * buffer * H::kTile);
+          so.store(lds + (2 * buffer + 1) * H::kTile);
+          if (wave < H::kTokens / 32) stats[buffer][half][wave * 32 + (lane & 31)] = half ? st : -st * kLog2e;
+          if (!careful && begin + t * H::kTokens < all && (sq.odd() || so.odd())) odd = 1;
+        },
+        [&](int buffer, int t) {
+          const int row0 = begin + t * H::kTokens + group * BR;
+          if (row0 + BR <= wfirst || row0 >= rows) return;
+          const char* lq = lds + 2 * buffer * H::kTile + group * BR * T::kRow;
+          const char* lo = lq + H::kTile;
+          const bool masked = row0 < wall || row0 + BR > rows;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int r = row0 + n + token_of(i, half);
-            const bool seen = r >= first && r < rows;
-            s[i] = seen ? s[i] : 0.f;
-            ds[i] = seen ? ds[i] : 0.f;
-          }
-        }
-        // rows of the block that see the key
-        const int from = first - row0 - n, to = rows - 1 - row0 - n;
+          for (int n = 0; n < BR; n += 32) {
+            f32x16 s = {}, ds = {};
 #pragma unroll
-        for (int i = 0; i < 16; i += R) {
-          const u32x4 w = Type<BF>::operand(s, i), dw = Type<BF>::operand(ds, i);
+            for (int e = 0; e < T::kSteps; ++e) {
+              s = Type<BF>::mma(s, tile.rows(lq, n, e), k[e]);
+              ds = Type<BF>::mma(ds, tile.rows(lo, n, e), H::kValues ? tile.rows(own_values, 0, e) : v[H::kValues ? 0 : e]);
+            }
 #pragma unroll
-          for (int b = 0; b < T::kBlocks; ++b) {
-            const u32x4 o = tile.columns(lo, n, i, b), q = tile.columns(lq, n, i, b);
-            if (careful) {
-              mma_seen<BF>(dv[b], o, w, i, from, to);
-              mma_seen<BF>(dk[b], q, dw, i, from, to);
-            } else {
-              dv[b] = Type<BF>::mma(dv[b], o, w);
-              dk[b] = Type<BF>::mma(dk[b], q, dw);
+            for (int i = 0; i < 16; i += 4) {
+              const f32x4 off = *(const f32x4*)&stats[buffer][0][group * BR + n + token_of(i, half)];
+              const f32x4 delta = *(const f32x4*)&stats[buffer][1][group * BR + n + token_of(i, half)];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                s[i + j] = exp2_(fmaf(s[i + j], c, off[j]));
+                ds[i + j] = s[i + j] * (ds[i + j] - delta[j]);
+              }
+            }
+            if (masked) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int r = row0 + n + token_of(i, half);
+                const bool seen = r >= first && r < rows;
+                s[i] = seen ? s[i] : 0.f;
+                ds[i] = seen ? ds[i] : 0.f;
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += R) {
+              const u32x4 pw = Type<BF>::operand(s, i), dw = Type<BF>::operand(ds, i);
+#pragma unroll
+              for (int b = 0; b < KB; ++b) {
+                const u32x4 o = tile.columns(lo, n, i, b0 + b), q = tile.columns(lq, n, i, b0 + b);
+                if constexpr (careful) {
+                  const int from = first - row0 - n, to = rows - 1 - row0 - n;  // rows of the block that see the key
+                  mma_seen<BF>(dv[b], o, pw, i, from, to);
+                  mma_seen<BF>(dk[b], q, dw, i, from, to);
+                } else {
+                  dv[b] = Type<BF>::mma(dv[b], o, pw);
+                  dk[b] = Type<BF>::mma(dk[b], q, dw);
+                }
+              }
             }
           }
-        }
-      }
+        });
+    join<C, S>(dk, lds);
+    join<C, S>(dv, lds);
+    if (group > 0) return;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      store_block<BF>(dk[b], a.scale, a.dk + k_token * a.dk_row + g * a.dk_head, b0 + b, there);
+      store_block<BF>(dv[b], 1.f, a.dv + k_token * a.dv_row + g * a.dv_head, b0 + b, there);
     }
-    if (t + 1 < tiles) {
-      sq.store(lds[(t + 1) & 1][0]);
-      so.store(lds[(t + 1) & 1][1]);
-      store_stats((t + 1) & 1);
-      if (sq.odd() || so.odd()) odd[(t + 1) & 1] = t + 1;
+  };
+  pass(std::false_type{}, 0);
+  __syncthreads();
+  if (odd)
+    for (int b = 0; b < T::kBlocks; ++b) {
+      __syncthreads();
+      pass(std::true_type{}, b);
     }
-    __syncthreads();
-  }
-  store_result<BF, D>(dk, a.scale, a.dk + k_token * a.dk_row + g * a.dk_head, there);
-  store_result<BF, D>(dv, 1.f, a.dv + k_token * a.dv_row + g * a.dv_head, there);
 }
 
 // Slots of the tiles of `tile` rows (per_token rows a token).
-int64_t slots_of(int64_t tokens, int per_token, int sequences, int tile) { return tokens * per_token / tile + sequences; }
+int slots_of(int64_t tokens, int per_token, int sequences, int tile) { return (int)(tokens * per_token / tile + sequences); }
+
+// Whether rows fill work-groups of `tile` rows, and these the GPU; else 32 rows a work-group and splits.
+constexpr int kWideBlocks = 256;
+bool wide(int64_t tokens, int per_token, int kv_heads, int tile) { return tokens * per_token / tile * kv_heads >= kWideBlocks; }
+
+template <bool BF, int D, int C, int S>
+hipError_t attend(AttendArgs& a, hipStream_t stream) {
+  a.q_slots = slots_of(a.q_tokens, a.hpk, a.sequences, C * 32);
+  hipLaunchKernelGGL((attend_kernel<BF, D, C, S>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(64 * C * S), 0, stream, a);
+  return hipGetLastError();
+}
+template <bool BF, int D, int C, int S>
+hipError_t attend_dq(AttendGradArgs& a, hipStream_t stream) {
+  a.q_slots = slots_of(a.q_tokens, a.hpk, a.sequences, C * 32);
+  hipLaunchKernelGGL((attend_dq_kernel<BF, D, C, S>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(64 * C * S), 0, stream, a);
+  return hipGetLastError();
+}
+template <bool BF, int D, int C, int S>
+hipError_t attend_dkv(AttendGradArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((attend_dkv_kernel<BF, D, C, S>),
+                     dim3((unsigned)slots_of(a.k_tokens, 1, a.sequences, C * 32) * a.kv_heads), dim3(64 * C * S), 0, stream, a);
+  return hipGetLastError();
+}
 
 template <bool BF, int D>
 hipError_t attend(AttendArgs& a, hipStream_t stream) {
-  constexpr int NW = 8;
-  a.q_slots = (int32_t)slots_of(a.q_tokens, a.hpk, a.sequences, NW * 32);
-  hipLaunchKernelGGL((attend_kernel<BF, D, NW>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(NW * 64), 0, stream, a);
-  return hipGetLastError();
+  constexpr bool kLarge = !BF && D == 128;  // rows of 512 bytes
+  if (wide(a.q_tokens, a.hpk, a.kv_heads, 256)) return attend<BF, D, 8, 1>(a, stream);
+  return attend<BF, D, 1, kLarge ? 4 : 8>(a, stream);
 }
 
 template <bool BF, int D>
 hipError_t attend_grad(AttendGradArgs& a, hipStream_t stream) {
-  constexpr int NW = 8;
-  a.q_slots = (int32_t)slots_of(a.q_tokens, a.hpk, a.sequences, NW * 32);
-  a.k_slots = (int32_t)slots_of(a.k_tokens, 1, a.sequences, NW * 32);
-  hipLaunchKernelGGL((attend_dq_kernel<BF, D, NW>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(NW * 64), 0, stream, a);
-  const hipError_t e = hipGetLastError();
+  constexpr bool kLarge = !BF && D == 128;
+  hipError_t e;
+  if (wide(a.q_tokens, a.hpk, a.kv_heads, 256))
+    e = attend_dq<BF, D, 8, 1>(a, stream);
+  else
+    e = attend_dq<BF, D, 1, D == 128 ? 4 : 8>(a, stream);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attend_dkv_kernel<BF, D, NW>), dim3((unsigned)a.k_slots * a.kv_heads), dim3(NW * 64), 0, stream, a);
-  return hipGetLastError();
+  constexpr int kKeys = kLarge ? 4 : 8;
+  if (wide(a.k_tokens, 1, a.kv_heads, 32 * kKeys))
+    return attend_dkv<BF, D, kKeys, 1>(a, stream);
+  return attend_dkv<BF, D, 1, BF && D == 64 ? 8 : 4>(a, stream);
 }
 
 }  // namespace

@@ -275,7 +275,7 @@ struct AttendGradArgs : AttendShape {
   float* delta;  // [q_tokens, q_heads]: d_o.o of every row
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, do_row, do_head, dq_row, dq_head, dk_row, dk_head,
       dv_row, dv_head;           // bytes
-  int32_t q_slots, k_slots;      // launch_attend_grad
+  int32_t q_slots;               // launch_attend_grad
 };
 
 hipError_t launch_attend(AttendArgs& args, bool bf16, int head_dim, hipStream_t stream);

@@ -184,6 +184,10 @@ CASES = [
     (2, 1, 64, True, [60, 90], None, {"spread": 30.0}),                 # one key takes nearly all
     (2, 1, 128, False, [60, 90], None, {"spread": 30.0}),
     (3, 3, 64, False, [200], None, {"scale": 4.0}),
+    (64, 64, 64, True, [700, 3, 400, 1], None, {}),                     # enough rows to fill the GPU with the largest tiles
+    (48, 16, 128, True, [520, 130, 700], [600, 130, 901], {}),
+    (64, 64, 64, False, [640, 411], None, {"layout": "fused"}),
+    (32, 32, 128, False, [300, 1900], [333, 1900], {}),
     (32, 4, 128, True, [2, 1, 3, 1, 1, 5, 8, 1, 2, 1, 1, 1, 4] * 6, None, {}),  # more sequences than lanes
 ]
 
@@ -247,13 +251,16 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.parametrize("bf16,d", [(True, 64), (True, 128), (False, 64), (False, 128)])
-def test_unseen_infinities_and_nans(bf16, d):
+@pytest.mark.parametrize("copies", [1, 300])
+def test_unseen_infinities_and_nans(bf16, d, copies):
     """A token's infinities and NaN change nothing that does not see it: later tokens' rows in V, K, Q and d_o, rows
-    behind the sequence, another sequence's, another KV head's."""
+    behind the sequence, another sequence's, another KV head's.  With many more sequences behind, so that the
+    largest tiles are taken too."""
     import torch
 
     q_lens, bad = [70, 45], 37  # token 37 of sequence 0, in the middle of a tile
-    c = Case(4, 2, d, bf16, q_lens, tail=5)
+    c = Case(4, 2, d, bf16, q_lens + [115] * (2 * (copies - 1)), tail=5)
+    end = sum(c.q_lens)
     clean_o, clean_lse = c.outputs()
     a = c.attention()
     c.attend(a, clean_o, clean_lse)
@@ -265,7 +272,7 @@ def test_unseen_infinities_and_nans(bf16, d):
         if which == "tail":
             kept = [t.clone() for t in (c.q, c.k, c.v, c.d_o)]
             for t in (c.q, c.k, c.v, c.d_o):
-                t[115:] = nan
+                t[end:] = nan  # rows behind the last sequence
         else:
             kept = x.clone()
             x[bad, 1, 3] = nan
