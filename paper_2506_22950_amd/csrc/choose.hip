@@ -7,11 +7,22 @@
 // Weights and sums.  Which token it is hangs on where u falls between sums of up to 2^24 terms, so each weight
 // is formed in double and held as a whole number of units of 2^-s (s = 62 - log2 n, at most 50): sums are exact,
 // the same whatever the order.  A weight below half a unit is none
-// (but for u = 0, which takes the first entry of all).  exp2(y) = 2^i exp(f ln 2), |f| <= 1/2, with
-// the Taylor sum to f^10 (relative error below 3e-13).
+// (but for u = 0, which takes the first entry of all).
 //
-// Finding z*.  The entries of a range of values are counted and weighed in kBins bins of equal width; the bin that
-// holds the wanted count or sum becomes the range, until its entries are equal.
+// Two launches, each over pieces of rows (kPieceThreads threads, at most 32 entries of each in registers); the last
+// piece of a row to arrive joins them (nothing waits).
+//   weigh   reads the row: its maximum and, as the way of choosing needs, the sum of its weights and a histogram over
+//           the logarithm of the weights (kBins bins of 1/kBinsPerOctave octave below the maximum).  Without a
+//           filter the join takes the token; else it finds the bin in which z* lies.
+//   gather  reads the row again (out of a cache): entries of that bin, and for small top-k those above it too, go
+//           into a list, which the join ranks; the weights above it go into sums.  The join cuts the list at z*
+//           and finds the token by the sums.
+// Pieces weigh by their own maximum; the join scales their sums in double, in piece order.
+//
+// Rows for which that does not do (a list of more than kList entries, as where logits are equal; z* beyond the bins;
+// a large top-k with top-p; u = 0) the last piece takes alone: the entries of a range of values are counted and
+// weighed in bins of equal width, and the bin that holds the wanted count or sum becomes the range, until its
+// entries are equal.
 #include "ops.h"
 #include "rows.h"
 
@@ -22,27 +33,27 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kThreads = 1024, kWavesOf = kThreads / 64, kBins = 2048;
+constexpr int kThreads = kPieceThreads, kWavesOf = kThreads / 64, kRangeBins = 2048;
 
-// exp2(y) 2^s, y <= 0, as a whole number.
+// exp2(y) 2^s, y <= 0, as a whole number.  2^f on [-1/2, 1/2] by the polynomial of degree 8 of the least relative
+// error (by exchange), its constant then set to 1, so that equal largest entries weigh 1 (1e-12); n = round(y) by an addition that leaves it in the sum's low bits.
 __device__ __forceinline__ u64 weight(double y, int s) {
   // (bounded first: y is a product, and of a fused product with n only its rounding would be left far down)
   y = fmax(y, -200.0);
-  const double n = rint(y), f = (y - n) * 0.69314718055994530942;
-  double p = 1.0 / 3628800.0;
-  p = fma(p, f, 1.0 / 362880.0);
-  p = fma(p, f, 1.0 / 40320.0);
-  p = fma(p, f, 1.0 / 5040.0);
-  p = fma(p, f, 1.0 / 720.0);
-  p = fma(p, f, 1.0 / 120.0);
-  p = fma(p, f, 1.0 / 24.0);
-  p = fma(p, f, 1.0 / 6.0);
-  p = fma(p, f, 0.5);
+  const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
+  double p = 1.3175858111453815e-06;
+  p = fma(p, f, 1.5309737421943565e-05);
+  p = fma(p, f, 0.00015403851748740978);
+  p = fma(p, f, 0.0013333452062248836);
+  p = fma(p, f, 0.009618128542862378);
+  p = fma(p, f, 0.05550410939341711);
+  p = fma(p, f, 0.24022650698880368);
+  p = fma(p, f, 0.6931471805465141);
   p = fma(p, f, 1.0);
-  p = fma(p, f, 1.0);
+  const int n = (int)(uint32_t)__double_as_longlong(t) + s;
+  p = __longlong_as_double(__double_as_longlong(p) + ((long long)n << 52));
   // below 2^52: the sum's low bits are the number, rounded to nearest
-  const double x = ldexp(p, (int)n + s) + 0x1p52;
-  return (u64)__double_as_longlong(x) & ((1ull << 52) - 1);
+  return (u64)__double_as_longlong(p + 0x1p52) & ((1ull << 52) - 1);
 }
 
 __device__ __forceinline__ u64 wave_sum(u64 x) {
@@ -62,6 +73,15 @@ struct RowOf {
     vectors = (n + off + N - 1) / N;
   }
   __device__ __forceinline__ int index(int v, int j) const { return v * N + j - off; }
+  // As it lies in memory, -inf outside the row.
+  __device__ __forceinline__ u32x4 packed(int v) const {
+    const int i0 = index(v, 0);
+    if (i0 >= 0 && i0 + N <= n) return *(const u32x4*)(base + (int64_t)i0 * ES);
+    float x[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = i0 + j >= 0 && i0 + j < n ? E::load(base, i0 + j) : -INFINITY;
+    return E::pack(x);
+  }
   __device__ __forceinline__ void load(int v, float (&x)[N]) const {
     const int i0 = index(v, 0);
     if (i0 >= 0 && i0 + N <= n) {
@@ -76,8 +96,8 @@ struct RowOf {
 };
 
 struct Shared {
-  int count[kBins];
-  u64 mass[kBins];
+  int count[kRangeBins];
+  u64 mass[kRangeBins];
   u64 sums[kWavesOf];
   float lows[kWavesOf], highs[kWavesOf];
   int counts[kWavesOf];
@@ -129,10 +149,10 @@ struct Chooser {
     while (true) {
       // halves, so that the widest range is finite; tiny values scaled up, so that differences are no denormals
       const float up = fmaxf(fabsf(hi), fabsf(lo)) < 0x1p-60f ? 0x1p80f : 0.5f;
-      const float width = hi * up - lo * up, by = width > 0.f ? (kBins - 1) / width : 0.f;
+      const float width = hi * up - lo * up, by = width > 0.f ? (kRangeBins - 1) / width : 0.f;
       const float hi_up = hi * up;
-      const auto bin_of = [&](float z) { return min(kBins - 1, (int)((hi_up - z * up) * by)); };
-      for (int i = threadIdx.x; i < kBins; i += kThreads) sh.count[i] = 0, sh.mass[i] = 0;
+      const auto bin_of = [&](float z) { return min(kRangeBins - 1, (int)((hi_up - z * up) * by)); };
+      for (int i = threadIdx.x; i < kRangeBins; i += kThreads) sh.count[i] = 0, sh.mass[i] = 0;
       __syncthreads();
       for (int v = threadIdx.x; v < row.vectors; v += kThreads) {
         float x[N];
@@ -148,7 +168,7 @@ struct Chooser {
       __syncthreads();
       // the first bin with which the wanted is reached, by the first wavefront
       if (wave == 0) {
-        constexpr int P = kBins / 64;
+        constexpr int P = kRangeBins / 64;
         int n = 0;
         u64 m = 0;
         for (int i = 0; i < P; ++i) n += sh.count[lane * P + i], m += sh.mass[lane * P + i];
@@ -278,10 +298,13 @@ __device__ __forceinline__ bool allowed(const Sampling& p) {
          p.min_p <= 1.0 && p.top_k >= 0;
 }
 
+// A whole row by one work-group.  Not inlined: rare, and inside a kernel its registers were the kernel's (182, without
+// it 82).
+typedef __attribute__((address_space(3))) Shared LdsShared;
 template <bool BF>
-__global__ __launch_bounds__(kThreads) void choose_kernel(const ChooseArgs a) {
-  __shared__ Shared sh;
-  const int64_t r = blockIdx.x;
+__device__ __attribute__((noinline)) void choose_row(const ChooseArgs a, int64_t r, LdsShared* lds) {
+  Shared& sh = *(Shared*)lds;
+  __syncthreads();  // what else lay in sh is no longer read
   const Sampling p = a.each ? a.each[r] : a.all;
   const float u = a.uniform[r];
   Chooser<BF> ch{RowOf<BF>((const char*)a.logits + r * a.row_stride * (BF ? 2 : 4), a.vocab), sh, 0.0, 0.0, a.unit};
@@ -368,17 +391,650 @@ __global__ __launch_bounds__(kThreads) void choose_kernel(const ChooseArgs a) {
   }
 }
 
+
+// ---- pieces -------------------------------------------------------------------
+constexpr int kPieceWaves = kPieceThreads / 64;
+
+template <class T>
+__device__ __forceinline__ void publish(T* p, T x) {  // past the caches of this XCD
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class T>
+__device__ __forceinline__ T collect(const T* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Whether this work-group is the last of `pieces` to come here, with what it published.  Leaves the counter 0.
+__device__ __forceinline__ bool arrive(int32_t* counter, int pieces) {
+  __shared__ bool last;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have reached the coherence point
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
+    if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+  }
+  __syncthreads();
+  return last;
+}
+
+// A running sum over the threads of a work-group, in thread order; x becomes the sum up to and with it.  Returns the
+// whole.  scratch: kPieceWaves.
+template <class T>
+__device__ __forceinline__ T running(T& x, T* scratch) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int i = 1; i < 64; i <<= 1) {
+    const T y = __shfl_up(x, i);
+    if (lane >= i) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) scratch[wave] = x;
+  __syncthreads();
+  T whole = 0;
+  for (int i = 0; i < kPieceWaves; ++i) {
+    if (i == wave) x += whole;
+    whole += scratch[i];
+  }
+  return whole;
+}
+
+// Order of a value as an unsigned number, and back; keys rank by value, then by the lower index.
+__device__ __forceinline__ uint32_t order_of(float z) {
+  const uint32_t b = __float_as_uint(z);
+  return b ^ ((b & 0x80000000u) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(u64 key) {
+  const uint32_t o = (uint32_t)(key >> 32);
+  return __uint_as_float(o ^ ((o & 0x80000000u) ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ u64 key_of(float z, int i) { return (u64)order_of(z) << 32 | (0xffffffffu - (uint32_t)i); }
+__device__ __forceinline__ int index_of(u64 key) { return (int)(0xffffffffu - (uint32_t)key); }
+
+// How a row is chosen from, as its parameters say.
+struct Way {
+  double c;     // log2(e) / T
+  float bins;   // kBinsPerOctave times that: a value's bin is floor(z * bins)
+  bool by_count, by_mass, by_share, ok;
+  __device__ __forceinline__ Way(const Sampling& p, float u, int vocab) {
+    ok = u >= 0.f && u < 1.f && allowed(p);
+    c = 1.4426950408889634074 / (p.temperature == 0.0 ? 1.0 : p.temperature);
+    bins = (float)(c * kBinsPerOctave);
+    by_count = p.top_k > 0 && p.top_k < vocab;
+    by_mass = p.top_p > 0.0 && p.top_p < 1.0;
+    by_share = p.min_p > 0.0;
+  }
+  __device__ __forceinline__ bool whole() const { return !by_count && !by_mass && !by_share; }
+};
+
+__device__ __forceinline__ void write_token(const ChooseArgs& a, int64_t r, int token, double logprob, int kept) {
+  a.token[r] = token;
+  if (a.logprob) a.logprob[r] = (float)logprob;
+  if (a.kept) a.kept[r] = kept;
+}
+
+// The place in a wavefront's 64 vectors at which the running sum of value(z, index) is above target, by a whole
+// work-group (each thread an entry or less): the index, left in *found.  first: the first of these vectors.
+template <bool BF, class F>
+__device__ __forceinline__ void find_entry(const RowOf<BF>& row, int first, u64 target, F value, u64* scratch, int* found) {
+  constexpr int N = RowOf<BF>::N;
+  static_assert(64 * N <= kPieceThreads, "an entry a thread");
+  const int t = threadIdx.x, i = row.index(first, 0) + t;
+  u64 w = 0;
+  if (t < 64 * N && i >= 0 && i < row.n) w = value(Elem<BF>::load(row.base, i) + 0.f, i);
+  u64 sum = w;
+  running(sum, scratch);
+  if (w > 0 && sum > target && sum - w <= target) *found = i;
+  __syncthreads();
+}
+
+// A piece of a row: vector i of a thread is i * kPieceThreads behind its first.
+template <bool BF>
+struct Piece {
+  static constexpr int N = RowOf<BF>::N, V = kPieceVectors;
+  u32x4 x[V];
+  RowOf<BF> row;
+  int first, batches, wave, lane;
+  __device__ __forceinline__ Piece(const ChooseArgs& a, int64_t r, int piece)
+      : row((const char*)a.logits + r * a.row_stride * (BF ? 2 : 4), a.vocab) {
+    wave = threadIdx.x >> 6, lane = threadIdx.x & 63, batches = a.batches;
+    first = piece * batches * kPieceThreads;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < batches) x[i] = row.packed(vector(i));
+  }
+  __device__ __forceinline__ int vector(int i) const { return first + i * kPieceThreads + (int)threadIdx.x; }
+  __device__ __forceinline__ float at(int i, int j) const { return Elem<BF>::get(x[i], j) + 0.f; }  // -0 counts as 0
+};
+
+template <bool BF>
+__global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArgs a) {
+  constexpr int N = RowOf<BF>::N, V = Piece<BF>::V, W = kPieceWaves;
+  __shared__ __attribute__((aligned(16))) char lds[std::max(sizeof(Shared), (size_t)kChoosePieces * 12)];
+  u64* bins = (u64*)lds;
+  __shared__ u64 scratch[W];
+  __shared__ double dscratch[W];
+  __shared__ float tops[W];
+  __shared__ int lives[W], found, found_piece;
+  __shared__ u64 inner;
+  const int rec = blockIdx.x, local = rec / a.pieces, piece = rec - local * a.pieces;
+  const int64_t r = a.row0 + local;
+  const Sampling p = a.each ? a.each[r] : a.all;
+  const float u = a.uniform[r];
+  const Way way(p, u, a.vocab);
+  RowState& state = a.state[local];
+  if (!way.ok) {
+    if (piece == 0 && threadIdx.x == 0) state.mode = kDone, write_token(a, r, -1, NAN, 0);
+    return;
+  }
+  Piece<BF> pc(a, r, piece);
+  for (int i = threadIdx.x; i < kBins; i += kPieceThreads) bins[i] = 0;
+  float m = -INFINITY;
+  int live = 0;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int j = 0; j < N && i < pc.batches; ++j) {
+      const float z = pc.at(i, j);
+      odd |= !(z < INFINITY);
+      m = fmaxf(m, z);
+      live += z > -INFINITY;
+    }
+  for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i)), live += __shfl_xor(live, i);
+  if (pc.lane == 0) tops[pc.wave] = m, lives[pc.wave] = live;
+  odd = __syncthreads_or(odd);
+  m = tops[0], live = lives[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) m = fmaxf(m, tops[i]), live += lives[i];
+  const bool weigh = way.whole() || (way.by_mass && !way.by_count);
+  const bool binned = way.by_count ? p.top_k <= kListCount || !way.by_mass : way.by_mass;
+  const float top_bin = floorf(m * way.bins);
+  u64 sum = 0;
+  if (m > -INFINITY && !odd && (weigh || binned)) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (i >= pc.batches) break;
+      u64 part = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float z = pc.at(i, j);
+        const u64 w = weigh && z > -INFINITY ? weight(((double)z - m) * way.c, a.unit) : 0;
+        part += w;
+        if (binned) {
+          const float b = top_bin - floorf(z * way.bins);
+          if (b < (float)kBins) atomicAdd(&bins[(int)b], way.by_count ? 1ull : w);
+        }
+      }
+      if (weigh) {
+        part = wave_sum(part);
+        sum += part;
+        if (way.whole() && pc.lane == 0) publish(a.subs + ((int64_t)rec * V + i) * W + pc.wave, part);
+      }
+    }
+    if (weigh) {
+      __syncthreads();
+      if (pc.lane == 0) scratch[pc.wave] = sum;
+    }
+  } else {
+    __syncthreads();
+    if (pc.lane == 0) {
+      scratch[pc.wave] = 0;
+      if (way.whole())
+        for (int i = 0; i < pc.batches; ++i) publish(a.subs + ((int64_t)rec * V + i) * W + pc.wave, (u64)0);
+    }
+  }
+  __syncthreads();
+  PieceState& mine = a.piece[rec];
+  if (threadIdx.x == 0) {
+    sum = 0;
+    for (int i = 0; i < W; ++i) sum += scratch[i];
+    publish(&mine.top, odd ? NAN : m);
+    publish(&mine.live, live);
+    publish(&mine.sum, weigh ? sum : 0);
+  }
+  if (binned)
+    for (int i = threadIdx.x; i < kBins; i += kPieceThreads) publish(a.bins + (int64_t)rec * kBins + i, bins[i]);
+  if (!arrive(a.arrived + local * kCounterStride, a.pieces)) return;
+
+  // ---- the row ----
+  const PieceState* all = a.piece + (int64_t)local * a.pieces;
+  m = -INFINITY, live = 0, odd = false;
+  for (int i = threadIdx.x; i < a.pieces; i += kPieceThreads) {
+    const float t = collect(&all[i].top);
+    odd |= t != t;
+    m = fmaxf(m, t);
+    live += collect(&all[i].live);
+  }
+  for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i)), live += __shfl_xor(live, i);
+  if (pc.lane == 0) tops[pc.wave] = m, lives[pc.wave] = live;
+  odd = __syncthreads_or(odd);
+  m = tops[0], live = lives[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) m = fmaxf(m, tops[i]), live += lives[i];
+  if (odd || live == 0) {
+    if (threadIdx.x == 0) state.mode = kDone, write_token(a, r, -1, NAN, 0);
+    return;
+  }
+  // pieces' sums in units of the row's maximum: thread t has pieces t * per .. (a piece's scale is 2^-unit and more)
+  const int per = (a.pieces + kPieceThreads - 1) / kPieceThreads, from_piece = min(a.pieces, (int)threadIdx.x * per),
+            to_piece = min(a.pieces, from_piece + per);
+  const auto scale_of = [&](float t) { return exp2(((double)t - m) * way.c); };
+  double whole = 0.0, before = 0.0;
+  if (weigh) {
+    double own = 0.0;
+    for (int i = from_piece; i < to_piece; ++i) {
+      const u64 w = collect(&all[i].sum);
+      if (w) own += (double)w * scale_of(collect(&all[i].top));
+    }
+    before = own;
+    whole = running(before, dscratch);
+    before -= own;
+  }
+  if (way.whole()) {
+    if (u == 0.f) {
+      choose_row<BF>(a, r, (LdsShared*)lds);
+      return;
+    }
+    const double target = (double)u * whole;
+    if (threadIdx.x == 0) found = -1, found_piece = -1;
+    __syncthreads();
+    // running sums of one thread and of the next may differ by a rounding: the first piece wins, and the last piece of
+    // any weight takes what is left
+    double with = before;
+    for (int i = from_piece; i < to_piece; ++i) {
+      const u64 w = collect(&all[i].sum);
+      if (!w) continue;
+      with += (double)w * scale_of(collect(&all[i].top));
+      if (with > target) atomicMin((unsigned*)&found_piece, (unsigned)i);
+      atomicMax(&found, i);
+    }
+    __syncthreads();
+    const int at = found_piece >= 0 ? found_piece : found;
+    if (at >= from_piece && at < to_piece) {
+      double under = before;
+      for (int i = from_piece; i < at; ++i) {
+        const u64 w = collect(&all[i].sum);
+        if (w) under += (double)w * scale_of(collect(&all[i].top));
+      }
+      const u64 w = collect(&all[at].sum);
+      const double rest = fmax(0.0, (target - under) / scale_of(collect(&all[at].top)));
+      inner = rest < (double)w ? min((u64)rest, w - 1) : w - 1;
+    }
+    __syncthreads();
+    u64 want = inner;
+    const float t = collect(&all[at].top);
+    // its wavefront's batch
+    const u64* subs = a.subs + ((int64_t)local * a.pieces + at) * V * W;
+    u64 part = (int)threadIdx.x < a.batches * W ? collect(subs + threadIdx.x) : 0, upto = part;
+    running(upto, scratch);
+    if (part > 0 && upto > want && upto - part <= want) found = threadIdx.x, inner = upto - part;
+    __syncthreads();
+    want -= inner;
+    const int sub = found;
+    __syncthreads();
+    const int from = at * a.batches * kPieceThreads + sub / W * kPieceThreads + sub % W * 64;
+    find_entry<BF>(pc.row, from, want,
+                   [&](float z, int) -> u64 { return z > -INFINITY ? weight(((double)z - t) * way.c, a.unit) : 0; }, scratch,
+                   &found);
+    if (threadIdx.x == 0) {
+      const double y = ((double)Elem<BF>::load(pc.row.base, found) - m) * way.c;
+      write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log(whole), live);
+      state.mode = kDone;
+    }
+    return;
+  }
+  // The bins of the entries to list.  hi_bin, lo_bin: floor(z bins) of the highest and lowest.
+  const float row_bin = floorf(m * way.bins);
+  const bool count = way.by_count && p.top_k < live, mass = way.by_mass;
+  int mode = kSums;
+  float lo_bin = -INFINITY, hi_bin = -INFINITY;
+  // (bins are whole numbers of float32)
+  if (!(fabsf(row_bin) < 0x1p22f) || (mass && way.by_count && (p.top_k > kListCount || !count))) mode = kLeft;
+  if (mode != kLeft && (count || mass)) {
+    const bool by_mass = !count;
+    // pieces' scales, and where their bin 0 is in the row's (kBins: nowhere)
+    double* scales = (double*)lds;
+    int* offs = (int*)(scales + kChoosePieces);
+    static_assert(sizeof(lds) >= kChoosePieces * 12, "scales and bins of the pieces");
+    for (int i = threadIdx.x; i < a.pieces; i += kPieceThreads) {
+      const float t = collect(&all[i].top), off = row_bin - floorf(t * way.bins);
+      offs[i] = off < (float)kBins ? (int)off : kBins;
+      scales[i] = by_mass && off < (float)kBins ? scale_of(t) : 1.0;
+    }
+    __syncthreads();
+    constexpr int B = kBins / kPieceThreads;
+    double own[B] = {}, total = 0.0;
+    const u64* h = a.bins + (int64_t)local * a.pieces * kBins;
+#pragma unroll 4
+    for (int i = 0; i < a.pieces; ++i) {
+      u64 x[B];
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        const int b = (int)threadIdx.x * B + k - offs[i];
+        x[k] = collect(h + (int64_t)i * kBins + max(b, 0));
+        if (b < 0) x[k] = 0;
+      }
+#pragma unroll
+      for (int k = 0; k < B; ++k) own[k] += (double)x[k] * scales[i];
+    }
+#pragma unroll
+    for (int k = 0; k < B; ++k) total += own[k];
+    double under = total;
+    running(under, dscratch);
+    under -= total;
+    if (threadIdx.x == 0) found = -1;
+    __syncthreads();
+    const double want = by_mass ? p.top_p * whole : (double)p.top_k;
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      under += own[k];
+      if (under >= want) atomicMin((unsigned*)&found, (unsigned)(threadIdx.x * B + k));
+    }
+    __syncthreads();
+    const int b = found;
+    if (b < 0)
+      mode = kLeft;
+    else
+      lo_bin = hi_bin = row_bin - (float)b;
+    if (count && p.top_k <= kListCount) hi_bin = INFINITY, mode = mode == kLeft ? kLeft : kListed;
+  }
+  if (mode != kLeft && way.by_share && mode != kListed) {
+    // the least weight's bin, by a formula that may be off by one
+    const float s = floorf((float)(((double)m * way.c + log2(p.min_p)) * kBinsPerOctave));
+    if (lo_bin > s + 1.f) {
+    } else if (hi_bin < s - 1.f) {
+      lo_bin = s - 1.f, hi_bin = s + 1.f;
+    } else {
+      lo_bin = fminf(lo_bin, s - 1.f), hi_bin = fmaxf(hi_bin, s + 1.f);
+    }
+  }
+  // (a top_k that leaves all: nothing is cut by count)
+  if (mode == kLeft || (mode == kSums && lo_bin == -INFINITY)) {
+    if (threadIdx.x == 0) state.mode = kDone;
+    choose_row<BF>(a, r, (LdsShared*)lds);
+    return;
+  }
+  if (threadIdx.x == 0) state = RowState{m, lo_bin, hi_bin, mode, live, 0, whole};
+}
+
+template <bool BF>
+__global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseArgs a) {
+  constexpr int N = RowOf<BF>::N, V = Piece<BF>::V, W = kPieceWaves;
+  __shared__ __attribute__((aligned(16))) u64 lds[2 * kList];
+  static_assert(sizeof(Shared) <= sizeof(lds), "a row alone");
+  u64 *keys = lds, *upto = lds + kList;
+  __shared__ u64 scratch[W], extra[kPieceThreads];
+  __shared__ int counts[W], listed, base, found;
+  __shared__ u64 inner;
+  const int rec = blockIdx.x, local = rec / a.pieces, piece = rec - local * a.pieces;
+  const RowState st = a.state[local];
+  if (st.mode != kListed && st.mode != kSums) return;
+  const int64_t r = a.row0 + local;
+  const Sampling p = a.each ? a.each[r] : a.all;
+  const float u = a.uniform[r];
+  const Way way(p, u, a.vocab);
+  Piece<BF> pc(a, r, piece);
+  if (threadIdx.x == 0) listed = 0;
+  __syncthreads();
+  const auto w_of = [&](float z) { return weight(((double)z - st.m) * way.c, a.unit); };
+  u64 sum = 0;
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (i >= pc.batches) break;
+    u64 part = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float z = pc.at(i, j), b = floorf(z * way.bins);
+      if (z > -INFINITY && b >= st.lo_bin) {
+        if (b <= st.hi_bin) {
+          const int at = atomicAdd(&listed, 1);
+          if (at < kList) keys[at] = key_of(z, pc.row.index(pc.vector(i), j));
+        } else {
+          part += w_of(z);
+          ++above;
+        }
+      }
+    }
+    if (st.mode == kSums) {
+      part = wave_sum(part);
+      sum += part;
+      if (pc.lane == 0) publish(a.subs + ((int64_t)rec * V + i) * W + pc.wave, part);
+    }
+  }
+  if (st.mode == kSums) {
+    for (int i = 1; i < 64; i <<= 1) above += __shfl_xor(above, i);
+    if (pc.lane == 0) scratch[pc.wave] = sum, counts[pc.wave] = above;
+  }
+  __syncthreads();
+  PieceState& mine = a.piece[rec];
+  int32_t* list_n = a.list_n + local * kCounterStride;
+  u64* list = a.list + (int64_t)local * kList;
+  if (threadIdx.x == 0) {
+    if (st.mode == kSums) {
+      sum = 0, above = 0;
+      for (int i = 0; i < W; ++i) sum += scratch[i], above += counts[i];
+      publish(&mine.sum, sum);
+      publish(&mine.live, above);
+    }
+    base = listed ? __hip_atomic_fetch_add(list_n, listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < min(listed, kList); i += kPieceThreads)
+    if (base < kList - i) publish(list + base + i, keys[i]);
+  if (!arrive(a.arrived + local * kCounterStride, a.pieces)) return;
+
+  // ---- the row ----
+  const int n = collect(list_n);
+  __syncthreads();
+  if (threadIdx.x == 0) publish(list_n, (int32_t)0);
+  if (n > kList || u == 0.f) {
+    choose_row<BF>(a, r, (LdsShared*)lds);
+    return;
+  }
+  // ranked: keys descending, zeros behind
+  int size = 64;
+  while (size < n) size <<= 1;
+  for (int i = threadIdx.x; i < size; i += kPieceThreads) keys[i] = i < n ? collect(list + i) : 0;
+  // keys[0 .. n) in descending order, up to `size`
+  const auto sort = [&](int n, int size) {
+    if (n <= kPieceThreads) {  // by each key's rank, as many comparisons as keys (28 + 45 steps with barriers otherwise)
+      __syncthreads();
+      const u64 own = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;
+      int rank = 0;
+      if ((int)(threadIdx.x & ~63u) < n) {
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) rank += keys[i] > own;
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < n) keys[rank] = own;
+      __syncthreads();
+      return;
+    }
+    for (int k = 2; k <= size; k <<= 1)
+      for (int j = k >> 1; j > 0; j >>= 1) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < size / 2; i += kPieceThreads) {
+          const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x + j;
+          const u64 s = keys[x], t = keys[y];
+          if ((s < t) == ((x & k) == 0)) keys[x] = t, keys[y] = s;
+        }
+      }
+    __syncthreads();
+  };
+  sort(n, size);
+  // running weights of the ranking
+  constexpr int P = kList / kPieceThreads;
+  u64 w[P], own = 0;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    const int i = (int)threadIdx.x * P + k;
+    w[k] = i < n ? w_of(value_of(keys[i])) : 0;
+    own += w[k];
+  }
+  u64 under = own;
+  running(under, scratch);
+  under -= own;
+  // what lies above the list
+  u64 over = 0;
+  int over_count = 0;
+  const PieceState* all = a.piece + (int64_t)local * a.pieces;
+  const int per = (a.pieces + kPieceThreads - 1) / kPieceThreads, from_piece = min(a.pieces, (int)threadIdx.x * per),
+            to_piece = min(a.pieces, ((int)threadIdx.x + 1) * per);
+  if (st.mode == kSums) {
+    u64 x = 0;
+    int c = 0;
+    for (int i = from_piece; i < to_piece; ++i) x += collect(&all[i].sum), c += collect(&all[i].live);
+    over = running(x, scratch);
+    over_count = running(c, counts);
+  }
+  const bool count = way.by_count && p.top_k < st.live;
+  // the share that predecessors weigh less than
+  u64 share = ~0ull;
+  if (way.by_mass) {
+    double limit = st.whole;  // of all entries (a unit's worth is 1)
+    if (count) {  // a list with all of the first top_k
+      u64 first = 0;
+      for (int k = 0; k < P; ++k) {
+        const int i = (int)threadIdx.x * P + k;
+        if (i < p.top_k) first += w[k];
+      }
+      limit = (double)running(first, scratch);
+    }
+    share = (u64)ceil(p.top_p * limit);
+  }
+  const double least = p.min_p * (double)(1ull << a.unit);
+  int kept = 0;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    const int i = (int)threadIdx.x * P + k;
+    const bool in = i < n && (!count || over_count + i < p.top_k) && (!way.by_mass || over + under < share) &&
+                    (!way.by_share || value_of(keys[i]) == st.m || (double)w[k] >= least);
+    kept += in;
+    under += w[k];
+    upto[i] = in ? w[k] : 0;
+  }
+  const int kept_list = running(kept, counts);  // the first of the ranking: what leaves an entry in leaves those before it in
+  u64 weight_list = 0;
+#pragma unroll
+  for (int k = 0; k < P; ++k) weight_list += upto[threadIdx.x * P + k];
+  const u64 whole = over + running(weight_list, scratch);
+  const int kept_all = over_count + kept_list;
+  u64 target = (u64)((double)u * (double)whole);
+  if (target >= whole) target = whole - 1;
+  if (threadIdx.x == 0) found = 0;
+  __syncthreads();
+  if (st.mode == kListed) {
+    // by index: keys (kept entries first, the lowest index highest) with their places in the ranking
+    const int m = kept_list;
+    int size2 = 64;
+    while (size2 < m) size2 <<= 1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < size2; i += kPieceThreads) {
+      const u64 key = keys[i];
+      keys[i] = i < m ? (u64)(uint32_t)key << 32 | (uint32_t)i : 0;
+    }
+    sort(m, size2);
+    u64 v[P], mine_ = 0;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      const int i = (int)threadIdx.x * P + k;
+      v[k] = i < m ? upto[(uint32_t)keys[i]] : 0;
+      mine_ += v[k];
+    }
+    u64 ahead = mine_;
+    running(ahead, scratch);
+    ahead -= mine_;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      const int i = (int)threadIdx.x * P + k;
+      if (v[k] > 0 && ahead <= target && ahead + v[k] > target) found = (int)(0xffffffffu - (uint32_t)(keys[i] >> 32));
+      ahead += v[k];
+    }
+    __syncthreads();
+  } else {
+    // pieces (by ranges, a thread each), then a piece's wavefronts' batches, then entries, each with the kept entries
+    // of the list in them
+    const u64 cut = kept_list > 0 ? keys[kept_list - 1] : ~0ull;
+    const int entries = a.batches * kPieceThreads * N;  // of a piece
+    const auto piece_of = [&](int e) { return (e + pc.row.off) / entries; };
+    const auto add_list = [&](auto place) {  // adds the list's weights to extra[place(entry)] (-1: none)
+      extra[threadIdx.x] = 0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < kept_list; i += kPieceThreads) {
+        const int at = place(index_of(keys[i]));
+        if (at >= 0) atomicAdd(&extra[at], upto[i]);
+      }
+      __syncthreads();
+    };
+    add_list([&](int e) { return piece_of(e) / per; });
+    u64 x = extra[threadIdx.x];
+    for (int i = from_piece; i < to_piece; ++i) x += collect(&all[i].sum);
+    u64 ahead = x;
+    running(ahead, scratch);
+    ahead -= x;
+    if (x > 0 && ahead <= target && ahead + x > target) {
+      int i = from_piece;
+      for (; i < to_piece - 1; ++i) {
+        u64 y = collect(&all[i].sum);
+        for (int k = 0; k < kept_list; ++k)
+          if (piece_of(index_of(keys[k])) == i) y += upto[k];
+        if (ahead + y > target) break;
+        ahead += y;
+      }
+      found = i, inner = target - ahead;
+    }
+    __syncthreads();
+    const int at = found;
+    u64 want = inner;
+    __syncthreads();
+    add_list([&](int e) { return piece_of(e) == at ? ((e + pc.row.off) / (64 * N)) % (a.batches * W) : -1; });
+    const u64* subs = a.subs + ((int64_t)local * a.pieces + at) * V * W;
+    const u64 part = (int)threadIdx.x < a.batches * W ? collect(subs + threadIdx.x) + extra[threadIdx.x] : 0;
+    u64 sums = part;
+    running(sums, scratch);
+    if (part > 0 && sums > want && sums - part <= want) found = threadIdx.x, inner = sums - part;
+    __syncthreads();
+    want -= inner;
+    const int from = (at * a.batches * W + found) * 64;
+    __syncthreads();
+    find_entry<BF>(pc.row, from, want,
+                   [&](float z, int i) -> u64 {
+                     if (!(z > -INFINITY)) return 0;
+                     const float b = floorf(z * way.bins);
+                     const bool in = b > st.hi_bin || (b >= st.lo_bin && kept_list > 0 && key_of(z, i) >= cut);
+                     return in ? w_of(z) : 0;
+                   },
+                   scratch, &found);
+  }
+  if (threadIdx.x == 0) {
+    const double y = ((double)Elem<BF>::load(pc.row.base, found) - st.m) * way.c;
+    write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log((double)whole), kept_all);
+  }
+}
+
 }  // namespace
 
+// Launches go over as many rows at a time as the records hold.
 hipError_t launch_choose(ChooseArgs& a, bool bf16, hipStream_t stream) {
   a.unit = 62;
   while ((int64_t(1) << (62 - a.unit)) < a.vocab) --a.unit;
   a.unit = std::min(a.unit, 50);
-  if (bf16)
-    hipLaunchKernelGGL(choose_kernel<true>, dim3(a.rows), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(choose_kernel<false>, dim3(a.rows), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  a.batches = choose_batches(a.rows, a.vocab, bf16);
+  a.pieces = choose_pieces(a.vocab, a.batches, bf16);
+  const int per_launch = choose_rows(a.pieces);
+  const infs_sampling& p = a.all;
+  const bool whole = !a.each && (p.top_k == 0 || p.top_k >= a.vocab) && (p.top_p == 0.0 || p.top_p == 1.0) && p.min_p == 0.0;
+  const int rows = a.rows;
+  for (a.row0 = 0; a.row0 < rows; a.row0 += per_launch) {
+    const int n = std::min(per_launch, rows - a.row0);
+    const dim3 grid((unsigned)n * a.pieces), block(kPieceThreads);
+    hipLaunchKernelGGL(bf16 ? weigh_kernel<true> : weigh_kernel<false>, grid, block, 0, stream, a);
+    if (!whole) hipLaunchKernelGGL(bf16 ? gather_kernel<true> : gather_kernel<false>, grid, block, 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace infs

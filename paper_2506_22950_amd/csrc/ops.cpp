@@ -109,6 +109,9 @@ struct infs_sampler {
   bool dry = false, bf16 = false;
   hipStream_t stream = nullptr;
   int device = 0;
+  // Counters (zero before the first launch), states, lists and sums of rows and pieces (see ChooseArgs).
+  char* workspace = nullptr;
+  size_t list_n = 0, state = 0, list = 0, piece = 0, subs = 0, bins = 0;  // offsets
 };
 
 struct infs_attention {
@@ -175,6 +178,33 @@ infs_status check_rows(const infs_scorer* s, int32_t rows, const void* logits, i
   if (rows > 0 && !s->dry && !logits) return op_fail(INFS_E_ARG, "%s: null buffer", what);
   if ((uintptr_t)logits % s->es) return op_fail(INFS_E_ARG, "%s must be aligned to an element", what);
   return INFS_OK;
+}
+
+// Lays out a sampler's workspace for its largest call; returns its bytes.
+size_t lay_out(infs_sampler* s) {
+  int64_t rows = 0, pieces = 0;  // of one launch
+  const auto call = [&](int n) {
+    const int p = infs::choose_pieces(s->cfg.vocab, infs::choose_batches(n, s->cfg.vocab, s->bf16), s->bf16);
+    const int64_t r = std::min(n, infs::choose_rows(p));
+    rows = std::max(rows, r);
+    pieces = std::max(pieces, r * p);
+  };
+  for (int n = 1; n <= std::min(s->cfg.max_rows, infs::kChooseRows); ++n) call(n);
+  call(s->cfg.max_rows);
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t begin = at;
+    at += (bytes + 255) / 256 * 256;
+    return begin;
+  };
+  take(sizeof(int32_t) * infs::kCounterStride * rows);
+  s->list_n = take(sizeof(int32_t) * infs::kCounterStride * rows);
+  s->state = take(sizeof(infs::RowState) * rows);
+  s->list = take(sizeof(unsigned long long) * infs::kList * rows);
+  s->piece = take(sizeof(infs::PieceState) * pieces);
+  s->subs = take(sizeof(unsigned long long) * infs::kChooseSubs * pieces);
+  s->bins = take(sizeof(unsigned long long) * infs::kBins * pieces);
+  return at;
 }
 
 size_t workspace_bytes(const infs_scorer& s) {
@@ -536,9 +566,14 @@ infs_status infs_sampler_create(const infs_sampler_config* cfg, void* hip_stream
     infs::StreamDevice dev(s->stream);
     hipError_t e = dev.status();
     if (e == hipSuccess) e = hipGetDevice(&s->device);
+    const size_t bytes = lay_out(s);
+    if (e == hipSuccess) e = hipMalloc((void**)&s->workspace, bytes);
+    if (e == hipSuccess) e = hipMemset(s->workspace, 0, s->state);  // the counters
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);  // the stream need not wait for the null stream
     if (e != hipSuccess) {
+      if (s->workspace) (void)hipFree(s->workspace);
       delete s;
-      return op_fail(INFS_E_DEVICE, "a sampler's device: %s", hipGetErrorString(e));
+      return op_fail(e == hipErrorOutOfMemory ? INFS_E_NOMEM : INFS_E_DEVICE, "a sampler's workspace: %s", hipGetErrorString(e));
     }
   }
   *out = s;
@@ -550,6 +585,7 @@ void infs_sampler_destroy(infs_sampler* s) {
   if (!s->dry) {
     infs::StreamDevice dev(s->stream, s->device);
     (void)hipStreamSynchronize(s->stream);
+    (void)hipFree(s->workspace);
   }
   delete s;
 }
@@ -576,7 +612,15 @@ infs_status infs_choose_tokens(infs_sampler* s, int32_t rows, const void* logits
     if (p.reserved != 0) return op_fail(INFS_E_ARG, "reserved must be 0");
   }
   if (s->dry || rows == 0) return INFS_OK;
-  infs::ChooseArgs a{logits_dev, row_stride, uniform_dev, each_dev, p, token_dev, logprob_dev, kept_dev, rows, s->cfg.vocab, 0};
+  infs::ChooseArgs a{logits_dev, row_stride, uniform_dev, each_dev, p, token_dev, logprob_dev, kept_dev, rows, s->cfg.vocab};
+  char* ws = s->workspace;
+  a.arrived = (int32_t*)ws;
+  a.list_n = (int32_t*)(ws + s->list_n);
+  a.state = (infs::RowState*)(ws + s->state);
+  a.list = (unsigned long long*)(ws + s->list);
+  a.piece = (infs::PieceState*)(ws + s->piece);
+  a.subs = (unsigned long long*)(ws + s->subs);
+  a.bins = (unsigned long long*)(ws + s->bins);
   infs::StreamDevice dev(s->stream, s->device);
   hipError_t e = dev.status();
   if (e == hipSuccess) e = infs::launch_choose(a, s->bf16, s->stream);

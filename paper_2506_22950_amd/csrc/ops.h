@@ -232,7 +232,30 @@ hipError_t launch_import(const PageFormat& f, MoveArgs& args, int layers, hipStr
 
 // ---- the choice of tokens ---------------------------------------------------------
 using Sampling = infs_sampling;
-constexpr int kChooseMaxRows = 1 << 22;  // a work-group of up to 1024 threads a row
+constexpr int kChooseMaxRows = 1 << 22;
+constexpr int kPieceThreads = 512;
+constexpr int kPieceVectors = 8;             // most of a thread, of 16 bytes
+constexpr int kChooseSubs = kPieceVectors * kPieceThreads / 64;  // sums of a piece
+constexpr int kBins = 1024, kBinsPerOctave = 32;
+constexpr int kList = 4096;                  // entries of a row that are ranked
+constexpr int kListCount = 1024;             // a top_k whose entries are all listed
+constexpr int kChooseRecords = 8192;         // pieces, and ..
+constexpr int kChooseRows = 2048;            // .. rows, of a launch
+constexpr int kChooseFill = 256;             // pieces that fill the GPU
+constexpr int kChoosePieces = 2048;          // most of a row
+
+enum RowMode { kDone, kListed, kSums, kLeft };  // what the launch that weighs a row leaves to do
+struct RowState {
+  float m, lo_bin, hi_bin;  // maximum; bins of the entries to list
+  int32_t mode, live;       // RowMode; entries that are not masked
+  int32_t pad;
+  double whole;             // sum of the weights, in units (by mass)
+};
+struct PieceState {
+  float top;                // NaN: one or +inf in the piece
+  int32_t live;             // entries not masked; above the listed bins
+  unsigned long long sum;
+};
 
 struct ChooseArgs {
   const void* logits;
@@ -244,8 +267,36 @@ struct ChooseArgs {
   float* logprob;  // these two may be null
   int32_t* kept;
   int32_t rows, vocab;
-  int32_t unit;  // a weight is a number of units of 2^-unit (launch_choose)
+  // launch_choose
+  int32_t unit;              // a weight is a number of units of 2^-unit
+  int32_t row0;              // of the launch
+  int32_t batches, pieces;   // vectors a thread of a piece, pieces of a row
+  // The workspace: counters (0 between launches) kCounterStride apart per row, then per row and per piece
+  int32_t *arrived, *list_n;
+  RowState* state;
+  unsigned long long* list;  // [rows][kList]
+  PieceState* piece;
+  unsigned long long* subs;  // [pieces][kChooseSubs]: sums of a wavefront's 64 vectors
+  unsigned long long* bins;  // [pieces][kBins]
 };
+
+// Vectors a thread (few rows: fewer, so that the pieces fill the GPU), pieces of a row, rows of a launch.
+inline int choose_pieces(int vocab, int batches, bool bf16) {
+  const int n = 16 / (bf16 ? 2 : 4);
+  return ((vocab + 2 * n - 2) / n + batches * kPieceThreads - 1) / (batches * kPieceThreads);  // at any alignment
+}
+inline int choose_batches(int rows, int vocab, bool bf16) {
+  int b = kPieceVectors;
+  while (b > 1 && (int64_t)rows * choose_pieces(vocab, b, bf16) < kChooseFill &&
+         choose_pieces(vocab, b / 2, bf16) <= kChoosePieces)
+    b /= 2;
+  return b;
+}
+inline int choose_rows(int pieces) {
+  const int n = kChooseRecords / pieces;
+  return n < 1 ? 1 : n < kChooseRows ? n : kChooseRows;
+}
+
 
 hipError_t launch_choose(ChooseArgs& args, bool bf16, hipStream_t stream);
 
