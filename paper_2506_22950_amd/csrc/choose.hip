@@ -17,7 +17,8 @@
 //   gather  reads the row again (out of a cache): entries of that bin, and for small top-k those above it too, go
 //           into a list, which the join ranks; the weights above it go into sums.  The join cuts the list at z*
 //           and finds the token by the sums.
-// Pieces weigh by their own maximum; the join scales their sums in double, in piece order.
+// Pieces weigh by their own maximum; the join scales their sums in double, in piece order.  Where all rows go one way,
+// the whole distribution and a small top-k take one launch (whole_kernel, top_kernel).
 //
 // Rows for which that does not do (a list of more than kList entries, as where logits are equal; z* beyond the bins;
 // a large top-k with top-p; u = 0) the last piece takes alone: the entries of a range of values are counted and
@@ -35,9 +36,10 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = kPieceThreads, kWavesOf = kThreads / 64, kRangeBins = 2048;
 
-// exp2(y) 2^s, y <= 0, as a whole number.  2^f on [-1/2, 1/2] by the polynomial of degree 8 of the least relative
-// error (by exchange), its constant then set to 1, so that equal largest entries weigh 1 (1e-12); n = round(y) by an addition that leaves it in the sum's low bits.
-__device__ __forceinline__ u64 weight(double y, int s) {
+// exp2(y) 2^s, y <= 0 (from -200 on).  2^f on [-1/2, 1/2] by the polynomial of degree 8 of the least relative error (by
+// exchange), its constant then set to 1, so that equal largest entries weigh 1 (1e-12); n = round(y) by an addition
+// that leaves it in the sum's low bits.
+__device__ __forceinline__ double power(double y, int s) {
   // (bounded first: y is a product, and of a fused product with n only its rounding would be left far down)
   y = fmax(y, -200.0);
   const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
@@ -51,14 +53,55 @@ __device__ __forceinline__ u64 weight(double y, int s) {
   p = fma(p, f, 0.6931471805465141);
   p = fma(p, f, 1.0);
   const int n = (int)(uint32_t)__double_as_longlong(t) + s;
-  p = __longlong_as_double(__double_as_longlong(p) + ((long long)n << 52));
-  // below 2^52: the sum's low bits are the number, rounded to nearest
-  return (u64)__double_as_longlong(p + 0x1p52) & ((1ull << 52) - 1);
+  return __longlong_as_double(__double_as_longlong(p) + ((long long)n << 52));
 }
 
-__device__ __forceinline__ u64 wave_sum(u64 x) {
-  for (int i = 1; i < 64; i <<= 1) x += __shfl_xor(x, i);
+// The same as a whole number: added to 2^52, the sum's low bits are it, rounded to nearest.
+__device__ __forceinline__ u64 weight(double y, int s) {
+  return (u64)__double_as_longlong(power(y, s) + 0x1p52) & ((1ull << 52) - 1);
+}
+
+// x of another lane, by a move between lanes (DPP control C, of the rows in ROWS), 0 where there is none.
+template <int C, int ROWS, class T>
+__device__ __forceinline__ T moved(T x) {
+  static_assert(sizeof(T) == 4 || sizeof(T) == 8, "one or two registers");
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), C, ROWS, 0xf, false));
+  } else {
+    const long long v = __builtin_bit_cast(long long, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, C, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), C, ROWS, 0xf, false);
+    return __builtin_bit_cast(T, (long long)((u64)hi << 32 | lo));
+  }
+}
+
+// Running sum over a wavefront: shifts by 1, 2, 4, 8 in rows of 16, then rows' last lanes into the rows behind.
+template <class T>
+__device__ __forceinline__ T wave_running(T x) {
+  x += moved<0x111, 0xf>(x);
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);
+  x += moved<0x143, 0xc>(x);
   return x;
+}
+
+// The value of lane 63, the same in all.
+template <class T>
+__device__ __forceinline__ T last_lane(T x) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+  } else {
+    const long long v = __builtin_bit_cast(long long, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)v, 63), hi = (uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63);
+    return __builtin_bit_cast(T, (long long)((u64)hi << 32 | lo));
+  }
+}
+
+template <class T>
+__device__ __forceinline__ T wave_sum(T x) {
+  return last_lane(wave_running(x));
 }
 
 // A row of logits, in vectors of 16 aligned bytes; entries outside it are -inf.
@@ -82,17 +125,7 @@ struct RowOf {
     for (int j = 0; j < N; ++j) x[j] = i0 + j >= 0 && i0 + j < n ? E::load(base, i0 + j) : -INFINITY;
     return E::pack(x);
   }
-  __device__ __forceinline__ void load(int v, float (&x)[N]) const {
-    const int i0 = index(v, 0);
-    if (i0 >= 0 && i0 + N <= n) {
-      const u32x4 w = *(const u32x4*)(base + (int64_t)i0 * ES);
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = E::get(w, j) + 0.f;  // -0 counts as 0
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = i0 + j >= 0 && i0 + j < n ? E::load(base, i0 + j) + 0.f : -INFINITY;
-    }
-  }
+  __device__ __forceinline__ float at(int i) const { return E::load(base, i) + 0.f; }  // -0 counts as 0
 };
 
 struct Shared {
@@ -108,7 +141,6 @@ struct Shared {
 template <bool BF>
 struct Chooser {
   using R = RowOf<BF>;
-  static constexpr int N = R::N;
   R row;
   Shared& sh;
   double c, top;  // log2(e) / T, m
@@ -121,12 +153,10 @@ struct Chooser {
   template <class F>
   __device__ __forceinline__ void range(F use, float& lo, float& hi) {
     float a = INFINITY, b = -INFINITY;
-    for (int v = threadIdx.x; v < row.vectors; v += kThreads) {
-      float x[N];
-      row.load(v, x);
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (use(x[j])) a = fminf(a, x[j]), b = fmaxf(b, x[j]);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < row.n; i += kThreads) {
+      const float x = row.at(i);
+      if (use(x)) a = fminf(a, x), b = fmaxf(b, x);
     }
     for (int i = 1; i < 64; i <<= 1) a = fminf(a, __shfl_xor(a, i)), b = fmaxf(b, __shfl_xor(b, i));
     if (lane == 0) sh.lows[wave] = a, sh.highs[wave] = b;
@@ -154,16 +184,14 @@ struct Chooser {
       const auto bin_of = [&](float z) { return min(kRangeBins - 1, (int)((hi_up - z * up) * by)); };
       for (int i = threadIdx.x; i < kRangeBins; i += kThreads) sh.count[i] = 0, sh.mass[i] = 0;
       __syncthreads();
-      for (int v = threadIdx.x; v < row.vectors; v += kThreads) {
-        float x[N];
-        row.load(v, x);
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (x[j] >= lo && x[j] <= hi) {
-            const int b = bin_of(x[j]);
-            atomicAdd(&sh.count[b], 1);
-            if (BY_MASS) atomicAdd(&sh.mass[b], w(x[j]));
-          }
+#pragma unroll 1
+      for (int i = threadIdx.x; i < row.n; i += kThreads) {
+        const float x = row.at(i);
+        if (x >= lo && x <= hi) {
+          const int b = bin_of(x);
+          atomicAdd(&sh.count[b], 1);
+          if (BY_MASS) atomicAdd(&sh.mass[b], w(x));
+        }
       }
       __syncthreads();
       // the first bin with which the wanted is reached, by the first wavefront
@@ -171,6 +199,7 @@ struct Chooser {
         constexpr int P = kRangeBins / 64;
         int n = 0;
         u64 m = 0;
+        #pragma unroll 1
         for (int i = 0; i < P; ++i) n += sh.count[lane * P + i], m += sh.mass[lane * P + i];
         int before = n;
         u64 under = m;
@@ -213,17 +242,13 @@ struct Chooser {
   // The first index at which the sum of value(z, index) is above target (at least one is).
   template <class F>
   __device__ __forceinline__ int locate(F value, u64 target) {
-    int from = 0, to = row.vectors;
+    int from = 0, to = row.n;
     while (true) {
       const int part = ((to - from + kWavesOf - 1) / kWavesOf + 63) / 64 * 64;
       const int a = from + wave * part, b = min(to, a + part);
       u64 sum = 0;
-      for (int v = a + lane; v < b; v += 64) {
-        float x[N];
-        row.load(v, x);
-#pragma unroll
-        for (int j = 0; j < N; ++j) sum += value(x[j], row.index(v, j));
-      }
+#pragma unroll 1
+      for (int i = a + lane; i < b; i += 64) sum += value(row.at(i), i);
       sum = wave_sum(sum);
       if (lane == 0) sh.sums[wave] = sum;
       __syncthreads();
@@ -236,31 +261,12 @@ struct Chooser {
       to = min(to, from + part);
       if (part <= 64) break;
     }
-    // 64 vectors: by the first wavefront
+    // 64 entries: by the first wavefront
     if (wave == 0) {
-      float x[N];
-      const int v = from + lane;
-      if (v < to) row.load(v, x);
-      u64 sum = 0;
-#pragma unroll
-      for (int j = 0; j < N; ++j) sum += v < to ? value(x[j], row.index(v, j)) : 0;
-      u64 under = sum;
-      for (int i = 1; i < 64; i <<= 1) {
-        const u64 y = __shfl_up(under, i);
-        if (lane >= i) under += y;
-      }
+      const int i = from + lane;
+      const u64 under = wave_running(i < to ? value(row.at(i), i) : 0);
       const u64 mask = __ballot(under > target);
-      if (lane == (mask ? __builtin_ctzll(mask) : 63)) {
-        under -= sum;
-        int at = 0;
-        bool done = false;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          under += v < to ? value(x[j], row.index(v, j)) : 0;
-          if (!done && under > target) at = row.index(v, j), done = true;
-        }
-        sh.found = at;
-      }
+      if (lane == 0) sh.found = from + (mask ? __builtin_ctzll(mask) : 0);
     }
     __syncthreads();
     const int at = sh.found;
@@ -273,15 +279,12 @@ struct Chooser {
   __device__ __forceinline__ u64 total(F use, int& count) {
     u64 sum = 0;
     int n = 0;
-    for (int v = threadIdx.x; v < row.vectors; v += kThreads) {
-      float x[N];
-      row.load(v, x);
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (use(x[j], row.index(v, j))) sum += w(x[j]), ++n;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < row.n; i += kThreads) {
+      const float x = row.at(i);
+      if (use(x, i)) sum += w(x), ++n;
     }
-    sum = wave_sum(sum);
-    for (int i = 1; i < 64; i <<= 1) n += __shfl_xor(n, i);
+    sum = wave_sum(sum), n = wave_sum(n);
     if (lane == 0) sh.sums[wave] = sum, sh.counts[wave] = n;
     __syncthreads();
     sum = 0, n = 0;
@@ -298,29 +301,23 @@ __device__ __forceinline__ bool allowed(const Sampling& p) {
          p.min_p <= 1.0 && p.top_k >= 0;
 }
 
-// A whole row by one work-group.  Not inlined: rare, and inside a kernel its registers were the kernel's (182, without
-// it 82).
-typedef __attribute__((address_space(3))) Shared LdsShared;
+// A whole row by one work-group.  (Its loops are kept rolled: it is inlined into kernels whose registers it should not
+// raise, and as a call it took scratch memory, for which a launch pays.)
 template <bool BF>
-__device__ __attribute__((noinline)) void choose_row(const ChooseArgs a, int64_t r, LdsShared* lds) {
-  Shared& sh = *(Shared*)lds;
+__device__ __forceinline__ void choose_row(const ChooseArgs& a, int64_t r, Shared& sh) {
   __syncthreads();  // what else lay in sh is no longer read
   const Sampling p = a.each ? a.each[r] : a.all;
   const float u = a.uniform[r];
   Chooser<BF> ch{RowOf<BF>((const char*)a.logits + r * a.row_stride * (BF ? 2 : 4), a.vocab), sh, 0.0, 0.0, a.unit};
-  constexpr int N = RowOf<BF>::N;
   // the largest and smallest finite values, how many are not masked, and whether any is NaN or +inf
   float lo = INFINITY, hi = -INFINITY;
   int live = 0;
   bool odd = false;
-  for (int v = threadIdx.x; v < ch.row.vectors; v += kThreads) {
-    float x[N];
-    ch.row.load(v, x);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      odd |= !(x[j] < INFINITY);
-      if (x[j] > -INFINITY) lo = fminf(lo, x[j]), hi = fmaxf(hi, x[j]), ++live;
-    }
+#pragma unroll 1
+  for (int i = threadIdx.x; i < a.vocab; i += kThreads) {
+    const float x = ch.row.at(i);
+    odd |= !(x < INFINITY);
+    if (x > -INFINITY) lo = fminf(lo, x), hi = fmaxf(hi, x), ++live;
   }
   for (int i = 1; i < 64; i <<= 1) {
     lo = fminf(lo, __shfl_xor(lo, i)), hi = fmaxf(hi, __shfl_xor(hi, i));
@@ -423,18 +420,17 @@ __device__ __forceinline__ bool arrive(int32_t* counter, int pieces) {
 template <class T>
 __device__ __forceinline__ T running(T& x, T* scratch) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = 1; i < 64; i <<= 1) {
-    const T y = __shfl_up(x, i);
-    if (lane >= i) x += y;
-  }
+  x = wave_running(x);
   __syncthreads();
   if (lane == 63) scratch[wave] = x;
   __syncthreads();
-  T whole = 0;
+  T whole = 0, ahead = 0;
+#pragma unroll
   for (int i = 0; i < kPieceWaves; ++i) {
-    if (i == wave) x += whole;
+    if (i == wave) ahead = whole;
     whole += scratch[i];
   }
+  x += ahead;
   return whole;
 }
 
@@ -480,7 +476,7 @@ __device__ __forceinline__ void find_entry(const RowOf<BF>& row, int first, u64 
   static_assert(64 * N <= kPieceThreads, "an entry a thread");
   const int t = threadIdx.x, i = row.index(first, 0) + t;
   u64 w = 0;
-  if (t < 64 * N && i >= 0 && i < row.n) w = value(Elem<BF>::load(row.base, i) + 0.f, i);
+  if (t < 64 * N && i >= 0 && i < row.n) w = value(row.at(i), i);
   u64 sum = w;
   running(sum, scratch);
   if (w > 0 && sum > target && sum - w <= target) *found = i;
@@ -506,11 +502,150 @@ struct Piece {
   __device__ __forceinline__ float at(int i, int j) const { return Elem<BF>::get(x[i], j) + 0.f; }  // -0 counts as 0
 };
 
+// keys[0 .. n) in descending order, in the first `size` (a power of two, zeros behind n).
+__device__ __forceinline__ void sort_keys(u64* keys, int n, int size) {
+  if (n <= kPieceThreads) {  // by each key's rank, as many comparisons as keys (28 to 45 steps with barriers otherwise)
+    __syncthreads();
+    const u64 own = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;
+    int rank = 0;
+    if ((int)(threadIdx.x & ~63u) < n) {
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) rank += keys[i] > own;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < n) keys[rank] = own;
+    __syncthreads();
+    return;
+  }
+  for (int k = 2; k <= size; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < size / 2; i += kPieceThreads) {
+        const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x + j;
+        const u64 s = keys[x], t = keys[y];
+        if ((s < t) == ((x & k) == 0)) keys[x] = t, keys[y] = s;
+      }
+    }
+  __syncthreads();
+}
+
+// A row's list of n keys into LDS, ranked.
+__device__ __forceinline__ void rank_list(u64* keys, const u64* list, int n) {
+  int size = 64;
+  while (size < n) size <<= 1;
+  for (int i = threadIdx.x; i < size; i += kPieceThreads) keys[i] = i < n ? collect(list + i) : 0;
+  sort_keys(keys, n, size);
+}
+
+// What a ranked list keeps: its first `count` entries.  upto[i]: an entry's weight, 0 if it is not kept; target: u of
+// the whole sum.  over, over_count: the sum and number of the entries above the list.
+struct Kept {
+  int count;
+  u64 whole, target;
+};
+template <class F>
+__device__ __forceinline__ Kept cut_list(const Sampling& p, const Way& way, float u, int unit, float m, bool count, double whole,
+                                         u64 over, int over_count, const u64* keys, u64* upto, int n, F w_of, u64* scratch,
+                                         int* counts) {
+  constexpr int P = kList / kPieceThreads;
+  const int each = (n + kPieceThreads - 1) / kPieceThreads, first = threadIdx.x * each;  // of a thread
+  u64 w[P], own = 0, limited = 0;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    w[k] = 0;
+    if (k < each && first + k < n) {
+      w[k] = w_of(value_of(keys[first + k]));
+      own += w[k];
+      if (first + k < p.top_k) limited += w[k];
+    }
+  }
+  u64 under = own;
+  running(under, scratch);
+  under -= own;
+  // the share that an entry's predecessors weigh less than: of all entries, or of a list that has all of the top_k
+  u64 share = ~0ull;
+  if (way.by_mass) share = (u64)ceil(p.top_p * (count ? (double)running(limited, scratch) : whole));
+  const double least = p.min_p * (double)(1ull << unit);
+  int kept = 0;
+  u64 sum = 0;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    const int i = first + k;
+    if (k < each && i < n) {
+      const bool in = (!count || over_count + i < p.top_k) && (!way.by_mass || over + under < share) &&
+                      (!way.by_share || value_of(keys[i]) == m || (double)w[k] >= least);
+      kept += in;
+      under += w[k];
+      upto[i] = in ? w[k] : 0;
+      sum += upto[i];
+    }
+  }
+  Kept x;
+  x.count = running(kept, counts);  // what leaves an entry in leaves those before it in
+  x.whole = over + running(sum, scratch);
+  x.target = (u64)((double)u * (double)x.whole);
+  if (x.target >= x.whole) x.target = x.whole - 1;
+  return x;
+}
+
+// The entry at which the kept weights by index are above the target, where all of them are in the list; its index in
+// *found.
+__device__ __forceinline__ void find_listed(const Kept& x, u64* keys, const u64* upto, u64* scratch, int* found) {
+  constexpr int P = kList / kPieceThreads;
+  // keys by index (the lowest is the highest) with their places in the ranking
+  const int m = x.count;
+  int size = 64;
+  while (size < m) size <<= 1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < size; i += kPieceThreads) keys[i] = i < m ? (u64)(uint32_t)keys[i] << 32 | (uint32_t)i : 0;
+  sort_keys(keys, m, size);
+  const int each = (m + kPieceThreads - 1) / kPieceThreads, first = threadIdx.x * each;
+  u64 v[P], own = 0;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    v[k] = k < each && first + k < m ? upto[(uint32_t)keys[first + k]] : 0;
+    own += v[k];
+  }
+  u64 ahead = own;
+  running(ahead, scratch);
+  ahead -= own;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    if (v[k] > 0 && ahead <= x.target && ahead + v[k] > x.target) *found = index_of((u64)(keys[first + k] >> 32));
+    ahead += v[k];
+  }
+  __syncthreads();
+}
+
+// The keys of a thread's `here` entries with in(z) go to the list in LDS (what does not fit is counted), a place for all
+// of them at once.
+template <bool BF, class F>
+__device__ __forceinline__ void list_entries(const Piece<BF>& pc, int here, F in, u64* keys, int* listed) {
+  if (here == 0) return;
+  int at = atomicAdd(listed, here);
+#pragma unroll
+  for (int i = 0; i < Piece<BF>::V; ++i)
+#pragma unroll
+    for (int j = 0; j < Piece<BF>::N && i < pc.batches; ++j) {
+      const float z = pc.at(i, j);
+      if (!in(z)) continue;
+      if (at < kList) keys[at] = key_of(z, pc.row.index(pc.vector(i), j));
+      ++at;
+    }
+}
+
+// Weight of an entry `f` of a bin above its beginning, in units of 2^-16 of the least weight in the bin: kPieceThreads *
+// kPieceVectors * 8 of them, 2^(1/32) at most each, fit 32 bits.
+__device__ __forceinline__ uint32_t bin_mass(float f) {
+  return (uint32_t)(__builtin_amdgcn_exp2f(f * (1.f / kBinsPerOctave)) * 65536.f + 0.5f);
+}
+static_assert(kPieceThreads * kPieceVectors * 8 * 66974ull < (1ull << 32), "a bin's sum");
+
 template <bool BF>
 __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArgs a) {
   constexpr int N = RowOf<BF>::N, V = Piece<BF>::V, W = kPieceWaves;
-  __shared__ __attribute__((aligned(16))) char lds[std::max(sizeof(Shared), (size_t)kChoosePieces * 12)];
-  u64* bins = (u64*)lds;
+  __shared__ __attribute__((aligned(16))) char lds[sizeof(Shared)];
+  uint32_t* bins = (uint32_t*)lds;
   __shared__ u64 scratch[W];
   __shared__ double dscratch[W];
   __shared__ float tops[W];
@@ -561,8 +696,8 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
         const u64 w = weigh && z > -INFINITY ? weight(((double)z - m) * way.c, a.unit) : 0;
         part += w;
         if (binned) {
-          const float b = top_bin - floorf(z * way.bins);
-          if (b < (float)kBins) atomicAdd(&bins[(int)b], way.by_count ? 1ull : w);
+          const float g = z * way.bins, f = floorf(g), b = top_bin - f;
+          if (b < (float)kBins) atomicAdd(&bins[(int)b], way.by_count ? 1u : bin_mass(g - f));
         }
       }
       if (weigh) {
@@ -618,7 +753,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
   // pieces' sums in units of the row's maximum: thread t has pieces t * per .. (a piece's scale is 2^-unit and more)
   const int per = (a.pieces + kPieceThreads - 1) / kPieceThreads, from_piece = min(a.pieces, (int)threadIdx.x * per),
             to_piece = min(a.pieces, from_piece + per);
-  const auto scale_of = [&](float t) { return exp2(((double)t - m) * way.c); };
+  const auto scale_of = [&](float t) { return power(((double)t - m) * way.c, 0); };
   double whole = 0.0, before = 0.0;
   if (weigh) {
     double own = 0.0;
@@ -632,7 +767,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
   }
   if (way.whole()) {
     if (u == 0.f) {
-      choose_row<BF>(a, r, (LdsShared*)lds);
+      choose_row<BF>(a, r, *(Shared*)lds);
       return;
     }
     const double target = (double)u * whole;
@@ -692,50 +827,62 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
   if (!(fabsf(row_bin) < 0x1p22f) || (mass && way.by_count && (p.top_k > kListCount || !count))) mode = kLeft;
   if (mode != kLeft && (count || mass)) {
     const bool by_mass = !count;
-    // pieces' scales, and where their bin 0 is in the row's (kBins: nowhere)
-    double* scales = (double*)lds;
-    int* offs = (int*)(scales + kChoosePieces);
-    static_assert(sizeof(lds) >= kChoosePieces * 12, "scales and bins of the pieces");
+    // where the pieces' bin 0 is in the row's (kBins: nowhere)
+    int* offs = (int*)lds;
+    static_assert(sizeof(lds) >= kChoosePieces * sizeof(int), "bins of the pieces");
     for (int i = threadIdx.x; i < a.pieces; i += kPieceThreads) {
-      const float t = collect(&all[i].top), off = row_bin - floorf(t * way.bins);
+      const float off = row_bin - floorf(collect(&all[i].top) * way.bins);
       offs[i] = off < (float)kBins ? (int)off : kBins;
-      scales[i] = by_mass && off < (float)kBins ? scale_of(t) : 1.0;
     }
     __syncthreads();
     constexpr int B = kBins / kPieceThreads;
-    double own[B] = {}, total = 0.0;
-    const u64* h = a.bins + (int64_t)local * a.pieces * kBins;
-#pragma unroll 4
+    u64 own[B] = {};
+    const uint32_t* h = a.bins + (int64_t)local * a.pieces * kBins;
+#pragma unroll 8
     for (int i = 0; i < a.pieces; ++i) {
-      u64 x[B];
 #pragma unroll
       for (int k = 0; k < B; ++k) {
         const int b = (int)threadIdx.x * B + k - offs[i];
-        x[k] = collect(h + (int64_t)i * kBins + max(b, 0));
-        if (b < 0) x[k] = 0;
+        const uint32_t x = collect(h + (int64_t)i * kBins + max(b, 0));
+        own[k] += b < 0 ? 0 : x;
       }
-#pragma unroll
-      for (int k = 0; k < B; ++k) own[k] += (double)x[k] * scales[i];
     }
+    // by mass: a bin's sum is in units of 2^-16 of its least weight; bin b's begins at floor(m bins) - b, 1/32 octave each
+    double sums[B], total = 0.0;
 #pragma unroll
-    for (int k = 0; k < B; ++k) total += own[k];
+    for (int k = 0; k < B; ++k) {
+      const int b = (int)threadIdx.x * B + k;
+      sums[k] = (double)own[k];
+      if (by_mass)
+        sums[k] *= power(fmin(0.0, ((double)row_bin - b) / kBinsPerOctave - (double)m * way.c), a.unit - 16);
+      total += sums[k];
+    }
     double under = total;
     running(under, dscratch);
     under -= total;
-    if (threadIdx.x == 0) found = -1;
+    if (threadIdx.x == 0) found = found_piece = -1;
     __syncthreads();
-    const double want = by_mass ? p.top_p * whole : (double)p.top_k;
+    // the bins at which the wanted may be reached: sums are within `off` (2^-17 and the rounding of z bins, whose 2^-24
+    // of a bin are 1/46 of a weight; twice that), so the first is sought with sums that much larger, the last smaller
+    const double want = by_mass ? p.top_p * whole : (double)p.top_k, off = by_mass ? 2e-5 + fabsf(row_bin) * 2.6e-9 : 0.0;
+    int first_bin = kBins, last_bin = kBins;
 #pragma unroll
     for (int k = 0; k < B; ++k) {
-      under += own[k];
-      if (under >= want) atomicMin((unsigned*)&found, (unsigned)(threadIdx.x * B + k));
+      under += sums[k];
+      const int b = threadIdx.x * B + k;
+      if (under * (1.0 + off) >= want) first_bin = min(first_bin, b);
+      if (under * (1.0 - off) >= want) last_bin = min(last_bin, b);
     }
+    // (a wavefront at a time: as few steps on one address as there are wavefronts)
+    const u64 reached = __ballot(first_bin < kBins), passed = __ballot(last_bin < kBins);
+    if (reached && pc.lane == __builtin_ctzll(reached)) atomicMin((unsigned*)&found, (unsigned)first_bin);
+    if (passed && pc.lane == __builtin_ctzll(passed)) atomicMin((unsigned*)&found_piece, (unsigned)last_bin);
     __syncthreads();
-    const int b = found;
-    if (b < 0)
+    const int b = found, b_last = found_piece;
+    if (b_last < 0)
       mode = kLeft;
     else
-      lo_bin = hi_bin = row_bin - (float)b;
+      hi_bin = row_bin - (float)b, lo_bin = row_bin - (float)b_last;
     if (count && p.top_k <= kListCount) hi_bin = INFINITY, mode = mode == kLeft ? kLeft : kListed;
   }
   if (mode != kLeft && way.by_share && mode != kListed) {
@@ -751,7 +898,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
   // (a top_k that leaves all: nothing is cut by count)
   if (mode == kLeft || (mode == kSums && lo_bin == -INFINITY)) {
     if (threadIdx.x == 0) state.mode = kDone;
-    choose_row<BF>(a, r, (LdsShared*)lds);
+    choose_row<BF>(a, r, *(Shared*)lds);
     return;
   }
   if (threadIdx.x == 0) state = RowState{m, lo_bin, hi_bin, mode, live, 0, whole};
@@ -778,7 +925,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
   __syncthreads();
   const auto w_of = [&](float z) { return weight(((double)z - st.m) * way.c, a.unit); };
   u64 sum = 0;
-  int above = 0;
+  int above = 0, here = 0;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     if (i >= pc.batches) break;
@@ -788,8 +935,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
       const float z = pc.at(i, j), b = floorf(z * way.bins);
       if (z > -INFINITY && b >= st.lo_bin) {
         if (b <= st.hi_bin) {
-          const int at = atomicAdd(&listed, 1);
-          if (at < kList) keys[at] = key_of(z, pc.row.index(pc.vector(i), j));
+          ++here;
         } else {
           part += w_of(z);
           ++above;
@@ -802,8 +948,12 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
       if (pc.lane == 0) publish(a.subs + ((int64_t)rec * V + i) * W + pc.wave, part);
     }
   }
+  list_entries(pc, here, [&](float z) {
+    const float b = floorf(z * way.bins);
+    return z > -INFINITY && b >= st.lo_bin && b <= st.hi_bin;
+  }, keys, &listed);
   if (st.mode == kSums) {
-    for (int i = 1; i < 64; i <<= 1) above += __shfl_xor(above, i);
+    above = wave_sum(above);
     if (pc.lane == 0) scratch[pc.wave] = sum, counts[pc.wave] = above;
   }
   __syncthreads();
@@ -829,52 +979,10 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
   __syncthreads();
   if (threadIdx.x == 0) publish(list_n, (int32_t)0);
   if (n > kList || u == 0.f) {
-    choose_row<BF>(a, r, (LdsShared*)lds);
+    choose_row<BF>(a, r, *(Shared*)lds);
     return;
   }
-  // ranked: keys descending, zeros behind
-  int size = 64;
-  while (size < n) size <<= 1;
-  for (int i = threadIdx.x; i < size; i += kPieceThreads) keys[i] = i < n ? collect(list + i) : 0;
-  // keys[0 .. n) in descending order, up to `size`
-  const auto sort = [&](int n, int size) {
-    if (n <= kPieceThreads) {  // by each key's rank, as many comparisons as keys (28 + 45 steps with barriers otherwise)
-      __syncthreads();
-      const u64 own = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;
-      int rank = 0;
-      if ((int)(threadIdx.x & ~63u) < n) {
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) rank += keys[i] > own;
-      }
-      __syncthreads();
-      if ((int)threadIdx.x < n) keys[rank] = own;
-      __syncthreads();
-      return;
-    }
-    for (int k = 2; k <= size; k <<= 1)
-      for (int j = k >> 1; j > 0; j >>= 1) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < size / 2; i += kPieceThreads) {
-          const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x + j;
-          const u64 s = keys[x], t = keys[y];
-          if ((s < t) == ((x & k) == 0)) keys[x] = t, keys[y] = s;
-        }
-      }
-    __syncthreads();
-  };
-  sort(n, size);
-  // running weights of the ranking
-  constexpr int P = kList / kPieceThreads;
-  u64 w[P], own = 0;
-#pragma unroll
-  for (int k = 0; k < P; ++k) {
-    const int i = (int)threadIdx.x * P + k;
-    w[k] = i < n ? w_of(value_of(keys[i])) : 0;
-    own += w[k];
-  }
-  u64 under = own;
-  running(under, scratch);
-  under -= own;
+  rank_list(keys, list, n);
   // what lies above the list
   u64 over = 0;
   int over_count = 0;
@@ -888,80 +996,22 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
     over = running(x, scratch);
     over_count = running(c, counts);
   }
-  const bool count = way.by_count && p.top_k < st.live;
-  // the share that predecessors weigh less than
-  u64 share = ~0ull;
-  if (way.by_mass) {
-    double limit = st.whole;  // of all entries (a unit's worth is 1)
-    if (count) {  // a list with all of the first top_k
-      u64 first = 0;
-      for (int k = 0; k < P; ++k) {
-        const int i = (int)threadIdx.x * P + k;
-        if (i < p.top_k) first += w[k];
-      }
-      limit = (double)running(first, scratch);
-    }
-    share = (u64)ceil(p.top_p * limit);
-  }
-  const double least = p.min_p * (double)(1ull << a.unit);
-  int kept = 0;
-#pragma unroll
-  for (int k = 0; k < P; ++k) {
-    const int i = (int)threadIdx.x * P + k;
-    const bool in = i < n && (!count || over_count + i < p.top_k) && (!way.by_mass || over + under < share) &&
-                    (!way.by_share || value_of(keys[i]) == st.m || (double)w[k] >= least);
-    kept += in;
-    under += w[k];
-    upto[i] = in ? w[k] : 0;
-  }
-  const int kept_list = running(kept, counts);  // the first of the ranking: what leaves an entry in leaves those before it in
-  u64 weight_list = 0;
-#pragma unroll
-  for (int k = 0; k < P; ++k) weight_list += upto[threadIdx.x * P + k];
-  const u64 whole = over + running(weight_list, scratch);
-  const int kept_all = over_count + kept_list;
-  u64 target = (u64)((double)u * (double)whole);
-  if (target >= whole) target = whole - 1;
+  const Kept kept = cut_list(p, way, u, a.unit, st.m, way.by_count && p.top_k < st.live, st.whole, over, over_count, keys, upto,
+                             n, w_of, scratch, counts);
   if (threadIdx.x == 0) found = 0;
   __syncthreads();
   if (st.mode == kListed) {
-    // by index: keys (kept entries first, the lowest index highest) with their places in the ranking
-    const int m = kept_list;
-    int size2 = 64;
-    while (size2 < m) size2 <<= 1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < size2; i += kPieceThreads) {
-      const u64 key = keys[i];
-      keys[i] = i < m ? (u64)(uint32_t)key << 32 | (uint32_t)i : 0;
-    }
-    sort(m, size2);
-    u64 v[P], mine_ = 0;
-#pragma unroll
-    for (int k = 0; k < P; ++k) {
-      const int i = (int)threadIdx.x * P + k;
-      v[k] = i < m ? upto[(uint32_t)keys[i]] : 0;
-      mine_ += v[k];
-    }
-    u64 ahead = mine_;
-    running(ahead, scratch);
-    ahead -= mine_;
-#pragma unroll
-    for (int k = 0; k < P; ++k) {
-      const int i = (int)threadIdx.x * P + k;
-      if (v[k] > 0 && ahead <= target && ahead + v[k] > target) found = (int)(0xffffffffu - (uint32_t)(keys[i] >> 32));
-      ahead += v[k];
-    }
-    __syncthreads();
+    find_listed(kept, keys, upto, scratch, &found);
   } else {
     // pieces (by ranges, a thread each), then a piece's wavefronts' batches, then entries, each with the kept entries
     // of the list in them
-    const u64 cut = kept_list > 0 ? keys[kept_list - 1] : ~0ull;
+    const u64 cut = kept.count > 0 ? keys[kept.count - 1] : ~0ull;
     const int entries = a.batches * kPieceThreads * N;  // of a piece
     const auto piece_of = [&](int e) { return (e + pc.row.off) / entries; };
     const auto add_list = [&](auto place) {  // adds the list's weights to extra[place(entry)] (-1: none)
       extra[threadIdx.x] = 0;
       __syncthreads();
-      for (int i = threadIdx.x; i < kept_list; i += kPieceThreads) {
+      for (int i = threadIdx.x; i < kept.count; i += kPieceThreads) {
         const int at = place(index_of(keys[i]));
         if (at >= 0) atomicAdd(&extra[at], upto[i]);
       }
@@ -973,16 +1023,16 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
     u64 ahead = x;
     running(ahead, scratch);
     ahead -= x;
-    if (x > 0 && ahead <= target && ahead + x > target) {
+    if (x > 0 && ahead <= kept.target && ahead + x > kept.target) {
       int i = from_piece;
       for (; i < to_piece - 1; ++i) {
         u64 y = collect(&all[i].sum);
-        for (int k = 0; k < kept_list; ++k)
+        for (int k = 0; k < kept.count; ++k)
           if (piece_of(index_of(keys[k])) == i) y += upto[k];
-        if (ahead + y > target) break;
+        if (ahead + y > kept.target) break;
         ahead += y;
       }
-      found = i, inner = target - ahead;
+      found = i, inner = kept.target - ahead;
     }
     __syncthreads();
     const int at = found;
@@ -1002,14 +1052,297 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
                    [&](float z, int i) -> u64 {
                      if (!(z > -INFINITY)) return 0;
                      const float b = floorf(z * way.bins);
-                     const bool in = b > st.hi_bin || (b >= st.lo_bin && kept_list > 0 && key_of(z, i) >= cut);
+                     const bool in = b > st.hi_bin || (b >= st.lo_bin && kept.count > 0 && key_of(z, i) >= cut);
                      return in ? w_of(z) : 0;
                    },
                    scratch, &found);
   }
   if (threadIdx.x == 0) {
     const double y = ((double)Elem<BF>::load(pc.row.base, found) - st.m) * way.c;
-    write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log((double)whole), kept_all);
+    write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log((double)kept.whole), over_count + kept.count);
+  }
+}
+
+// A small top-k in one launch: an entry of the first top_k of a row is one of the first top_k of its piece, so
+// among those from the bin on that holds the top_k-th largest of the piece's threads' maxima (kBins bins as above).
+// These go into the row's list, which the last piece ranks and cuts.
+template <bool BF>
+__global__ __launch_bounds__(kPieceThreads, 4) void top_kernel(const ChooseArgs a) {
+  constexpr int N = RowOf<BF>::N, V = Piece<BF>::V, W = kPieceWaves;
+  __shared__ __attribute__((aligned(16))) u64 lds[2 * kList];
+  u64 *keys = lds, *upto = lds + kList;
+  int* bins = (int*)upto;
+  __shared__ u64 scratch[W];
+  __shared__ float tops[W];
+  __shared__ int counts[W], listed, found;
+  const int rec = blockIdx.x, local = rec / a.pieces, piece = rec - local * a.pieces;
+  const int64_t r = a.row0 + local;
+  const Sampling& p = a.all;
+  const float u = a.uniform[r];
+  const Way way(p, u, a.vocab);
+  if (!way.ok) {
+    if (piece == 0 && threadIdx.x == 0) write_token(a, r, -1, NAN, 0);
+    return;
+  }
+  Piece<BF> pc(a, r, piece);
+  for (int i = threadIdx.x; i < kBins; i += kPieceThreads) bins[i] = 0;
+  if (threadIdx.x == 0) listed = 0, found = kBins;
+  float top = -INFINITY;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int j = 0; j < N && i < pc.batches; ++j) {
+      odd |= !(pc.at(i, j) < INFINITY);
+      top = fmaxf(top, pc.at(i, j));
+    }
+  float m = top;
+  for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i));
+  if (pc.lane == 0) tops[pc.wave] = m;
+  odd = __syncthreads_or(odd);
+  m = tops[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) m = fmaxf(m, tops[i]);
+  float row_bin = floorf(m * way.bins);
+  const auto bin_of = [&](float z) {  // below the bins, and where they are no numbers: the last
+    const float b = row_bin - floorf(z * way.bins);
+    return b < (float)(kBins - 1) ? (int)b : kBins - 1;
+  };
+  // the first bin with which bins[] has top_k, kBins where it has fewer (found is that before)
+  const auto first_bin = [&] {
+    __syncthreads();
+    constexpr int B = kBins / kPieceThreads;
+    int own = 0;
+#pragma unroll
+    for (int k = 0; k < B; ++k) own += bins[threadIdx.x * B + k];
+    int upto_here = own;
+    running(upto_here, counts);
+    if (upto_here >= p.top_k && upto_here - own < p.top_k) {
+      int b = threadIdx.x * B, n = upto_here - own;
+      while ((n += bins[b]) < p.top_k) ++b;
+      found = b;
+    }
+    __syncthreads();
+    return found;
+  };
+  if (top > -INFINITY) atomicAdd(&bins[bin_of(top)], 1);
+  const int least = first_bin();
+  // each piece has room for `room` keys; kOdd and kMany, above all keys, say that the row has none, and that there is none
+  constexpr u64 kOdd = ~0ull, kMany = ~0ull - 1;
+  const int room = kList / a.pieces;
+  if (!odd) {
+    const auto in = [&](float z) { return z > -INFINITY && bin_of(z) <= least; };
+    int here = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j < N && i < pc.batches; ++j) here += in(pc.at(i, j));
+    list_entries(pc, here, in, keys, &listed);
+  }
+  __syncthreads();
+  u64* list = a.list + (int64_t)local * kList;
+  for (int i = threadIdx.x; i < room; i += kPieceThreads)
+    publish(list + piece * room + i, odd ? kOdd : listed > room ? kMany : i < listed ? keys[i] : 0ull);
+  if (!arrive(a.arrived + local * kCounterStride, a.pieces)) return;
+
+  // ---- the row ----
+  const int n = room * a.pieces;
+  // the list once more from the bin on that holds the top_k-th of all
+  constexpr int P = kList / kPieceThreads;
+  u64 key[P], best = 0;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    const int i = k * kPieceThreads + (int)threadIdx.x;
+    key[k] = i < n ? collect(list + i) : 0;
+    best = max(best, key[k]);
+  }
+  for (int i = threadIdx.x; i < kBins; i += kPieceThreads) bins[i] = 0;
+  for (int i = 1; i < 64; i <<= 1) best = max(best, __shfl_xor(best, i));
+  __syncthreads();
+  if (pc.lane == 0) scratch[pc.wave] = best;
+  if (threadIdx.x == 0) listed = 0, found = kBins;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < W; ++i) best = max(best, scratch[i]);
+  if (best == 0 || best == kOdd) {
+    if (threadIdx.x == 0) write_token(a, r, -1, NAN, 0);
+    return;
+  }
+  if (best == kMany || u == 0.f) {
+    choose_row<BF>(a, r, *(Shared*)lds);
+    return;
+  }
+  m = value_of(best);
+  row_bin = floorf(m * way.bins);
+#pragma unroll
+  for (int k = 0; k < P; ++k)
+    if (key[k]) atomicAdd(&bins[bin_of(value_of(key[k]))], 1);
+  const int cut = first_bin();
+#pragma unroll
+  for (int k = 0; k < P; ++k)
+    if (key[k] && bin_of(value_of(key[k])) <= cut) keys[atomicAdd(&listed, 1)] = key[k];
+  __syncthreads();
+  const int few = listed;
+  int size = 64;
+  while (size < few) size <<= 1;
+  if (few > kPieceThreads)
+    for (int i = few + (int)threadIdx.x; i < size; i += kPieceThreads) keys[i] = 0;
+  sort_keys(keys, few, size);
+  const auto w_of = [&](float z) { return weight(((double)z - m) * way.c, a.unit); };
+  const Kept kept = cut_list(p, way, u, a.unit, m, true, 0.0, 0, 0, keys, upto, few, w_of, scratch, counts);
+  find_listed(kept, keys, upto, scratch, &found);
+  if (threadIdx.x == 0) {
+    const double y = ((double)Elem<BF>::load(pc.row.base, found) - m) * way.c;
+    write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log((double)kept.whole), kept.count);
+  }
+}
+
+// The first place of x > target among the threads with own > 0, or the last of these where rounding leaves none; -1: no
+// own > 0.  x: running sums.
+__device__ __forceinline__ int first_above(double x, double own, double target, int* low, int* high) {
+  __syncthreads();
+  if (threadIdx.x == 0) *low = INT32_MAX, *high = -1;
+  __syncthreads();
+  const u64 some = __ballot(own > 0.0), here = __ballot(own > 0.0 && x > target);
+  const int lane = threadIdx.x & 63;
+  if (here && lane == __builtin_ctzll(here)) atomicMin(low, (int)threadIdx.x);
+  if (some && lane == 63 - __builtin_clzll(some)) atomicMax(high, (int)threadIdx.x);
+  __syncthreads();
+  return *low < INT32_MAX ? *low : *high;
+}
+
+// The whole distribution, read once: the sums of pieces, of their wavefronts' batches and at last of 64 vectors narrow
+// the place down.  Sums are doubles here, added in an order that sizes and alignment fix.
+template <bool BF>
+__global__ __launch_bounds__(kPieceThreads, 4) void whole_kernel(const ChooseArgs a) {
+  constexpr int N = RowOf<BF>::N, V = Piece<BF>::V, W = kPieceWaves;
+  __shared__ __attribute__((aligned(16))) char lds[sizeof(Shared)];
+  __shared__ double scratch[W];
+  __shared__ float tops[W];
+  __shared__ int lives[W], low, high;
+  __shared__ double inner;
+  const int rec = blockIdx.x, local = rec / a.pieces, piece = rec - local * a.pieces;
+  const int64_t r = a.row0 + local;
+  const float u = a.uniform[r];
+  const Way way(a.all, u, a.vocab);
+  if (!way.ok) {
+    if (piece == 0 && threadIdx.x == 0) write_token(a, r, -1, NAN, 0);
+    return;
+  }
+  Piece<BF> pc(a, r, piece);
+  float m = -INFINITY;
+  int live = 0;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int j = 0; j < N && i < pc.batches; ++j) {
+      const float z = pc.at(i, j);
+      odd |= !(z < INFINITY);
+      m = fmaxf(m, z);
+      live += z > -INFINITY;
+    }
+  for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i)), live += __shfl_xor(live, i);
+  if (pc.lane == 0) tops[pc.wave] = m, lives[pc.wave] = live;
+  odd = __syncthreads_or(odd);
+  m = tops[0], live = lives[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) m = fmaxf(m, tops[i]), live += lives[i];
+  double sum = 0.0;
+  double* subs = (double*)a.subs + (int64_t)rec * V * W;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (i >= pc.batches) break;
+    double part = 0.0;
+    if (m > -INFINITY && !odd) {
+      // a masked entry adds 2^-200, which is nothing to the largest one's 1 (find_entry leaves it out)
+#pragma unroll
+      for (int j = 0; j < N; ++j) part += power(((double)Elem<BF>::get(pc.x[i], j) - m) * way.c, 0);
+      part = wave_sum(part);
+    }
+    sum += part;
+    if (pc.lane == 0) publish(subs + i * W + pc.wave, part);
+  }
+  if (pc.lane == 0) scratch[pc.wave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    PieceState& mine = a.piece[rec];
+    sum = 0.0;
+    for (int i = 0; i < W; ++i) sum += scratch[i];
+    publish(&mine.top, odd ? NAN : m);
+    publish(&mine.live, live);
+    publish(&mine.sum, (u64)__double_as_longlong(sum));
+  }
+  if (!arrive(a.arrived + local * kCounterStride, a.pieces)) return;
+
+  // ---- the row ----
+  const PieceState* all = a.piece + (int64_t)local * a.pieces;
+  const int per = (a.pieces + kPieceThreads - 1) / kPieceThreads, from_piece = min(a.pieces, (int)threadIdx.x * per),
+            to_piece = min(a.pieces, from_piece + per);
+  m = -INFINITY, live = 0, odd = false;
+  for (int i = from_piece; i < to_piece; ++i) {
+    const float t = collect(&all[i].top);
+    odd |= t != t;
+    m = fmaxf(m, t);
+    live += collect(&all[i].live);
+  }
+  for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i)), live += __shfl_xor(live, i);
+  if (pc.lane == 0) tops[pc.wave] = m, lives[pc.wave] = live;
+  odd = __syncthreads_or(odd);
+  m = tops[0], live = lives[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) m = fmaxf(m, tops[i]), live += lives[i];
+  if (odd || live == 0) {
+    if (threadIdx.x == 0) write_token(a, r, -1, NAN, 0);
+    return;
+  }
+  if (u == 0.f) {  // the first entry of any weight at all
+    choose_row<BF>(a, r, *(Shared*)lds);
+    return;
+  }
+  const auto sum_of = [&](int i) {  // of a piece, in units of the row's largest weight
+    const float t = collect(&all[i].top);
+    return t > -INFINITY ? __longlong_as_double((long long)collect(&all[i].sum)) * power(((double)t - m) * way.c, 0) : 0.0;
+  };
+  double own = 0.0;
+  for (int i = from_piece; i < to_piece; ++i) own += sum_of(i);
+  double upto = own;
+  const double whole = running(upto, scratch), target = (double)u * whole;
+  const int mine = first_above(upto, own, target, &low, &high);
+  if ((int)threadIdx.x == mine) {
+    double ahead = upto - own;
+    int i = from_piece;
+    for (; i < to_piece - 1; ++i) {
+      const double x = sum_of(i);
+      if (ahead + x > target) break;
+      ahead += x;
+    }
+    high = i;
+    inner = fmax(0.0, target - ahead);
+  }
+  __syncthreads();
+  const int at = high;
+  const float t = collect(&all[at].top);
+  double want = inner / power(((double)t - m) * way.c, 0);  // in the piece's units
+  const double* of = (const double*)a.subs + ((int64_t)local * a.pieces + at) * V * W;
+  const double part = (int)threadIdx.x < a.batches * W ? collect(of + threadIdx.x) : 0.0;
+  double sums = part;
+  running(sums, scratch);
+  const int sub = first_above(sums, part, want, &low, &high);
+  if ((int)threadIdx.x == sub) inner = sums - part;
+  __syncthreads();
+  want -= inner;
+  const int i = pc.row.index((at * a.batches * W + sub) * 64, 0) + (int)threadIdx.x;
+  double w = 0.0;
+  if (threadIdx.x < 64 * N && i >= 0 && i < a.vocab) {
+    const float z = Elem<BF>::load(pc.row.base, i);
+    if (z > -INFINITY) w = power(((double)z - t) * way.c, 0);
+  }
+  sums = w;
+  running(sums, scratch);
+  if ((int)threadIdx.x == first_above(sums, w, want, &low, &high)) {
+    const double y = ((double)Elem<BF>::load(pc.row.base, i) - m) * way.c;
+    write_token(a, r, i, y * 0.69314718055994530942 - log(whole), live);
   }
 }
 
@@ -1025,12 +1358,20 @@ hipError_t launch_choose(ChooseArgs& a, bool bf16, hipStream_t stream) {
   const int per_launch = choose_rows(a.pieces);
   const infs_sampling& p = a.all;
   const bool whole = !a.each && (p.top_k == 0 || p.top_k >= a.vocab) && (p.top_p == 0.0 || p.top_p == 1.0) && p.min_p == 0.0;
+  // lists of all pieces' first top_k, with room for what else lies in their last bins
+  const bool top = !a.each && p.top_k > 0 && p.top_k < a.vocab && p.top_k <= kPieceThreads / 2 && (int64_t)p.top_k * a.pieces <= kList / 2;
   const int rows = a.rows;
   for (a.row0 = 0; a.row0 < rows; a.row0 += per_launch) {
     const int n = std::min(per_launch, rows - a.row0);
     const dim3 grid((unsigned)n * a.pieces), block(kPieceThreads);
-    hipLaunchKernelGGL(bf16 ? weigh_kernel<true> : weigh_kernel<false>, grid, block, 0, stream, a);
-    if (!whole) hipLaunchKernelGGL(bf16 ? gather_kernel<true> : gather_kernel<false>, grid, block, 0, stream, a);
+    if (whole) {
+      hipLaunchKernelGGL(bf16 ? whole_kernel<true> : whole_kernel<false>, grid, block, 0, stream, a);
+    } else if (top) {
+      hipLaunchKernelGGL(bf16 ? top_kernel<true> : top_kernel<false>, grid, block, 0, stream, a);
+    } else {
+      hipLaunchKernelGGL(bf16 ? weigh_kernel<true> : weigh_kernel<false>, grid, block, 0, stream, a);
+      hipLaunchKernelGGL(bf16 ? gather_kernel<true> : gather_kernel<false>, grid, block, 0, stream, a);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

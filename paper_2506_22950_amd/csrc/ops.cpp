@@ -203,7 +203,7 @@ size_t lay_out(infs_sampler* s) {
   s->list = take(sizeof(unsigned long long) * infs::kList * rows);
   s->piece = take(sizeof(infs::PieceState) * pieces);
   s->subs = take(sizeof(unsigned long long) * infs::kChooseSubs * pieces);
-  s->bins = take(sizeof(unsigned long long) * infs::kBins * pieces);
+  s->bins = take(sizeof(uint32_t) * infs::kBins * pieces);
   return at;
 }
 
@@ -620,7 +620,7 @@ infs_status infs_choose_tokens(infs_sampler* s, int32_t rows, const void* logits
   a.list = (unsigned long long*)(ws + s->list);
   a.piece = (infs::PieceState*)(ws + s->piece);
   a.subs = (unsigned long long*)(ws + s->subs);
-  a.bins = (unsigned long long*)(ws + s->bins);
+  a.bins = (uint32_t*)(ws + s->bins);
   infs::StreamDevice dev(s->stream, s->device);
   hipError_t e = dev.status();
   if (e == hipSuccess) e = infs::launch_choose(a, s->bf16, s->stream);

@@ -277,7 +277,7 @@ struct ChooseArgs {
   unsigned long long* list;  // [rows][kList]
   PieceState* piece;
   unsigned long long* subs;  // [pieces][kChooseSubs]: sums of a wavefront's 64 vectors
-  unsigned long long* bins;  // [pieces][kBins]
+  uint32_t* bins;            // [pieces][kBins]: numbers, or sums of weights
 };
 
 // Vectors a thread (few rows: fewer, so that the pieces fill the GPU), pieces of a row, rows of a launch.
