@@ -36,6 +36,12 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = kPieceThreads, kWavesOf = kThreads / 64, kRangeBins = 2048;
 
+// ln of exp2(y)'s share of a sum of weights of unit 2^-s; 0 where it is all of it.
+template <class T>
+__device__ __forceinline__ double log_share(double y, T sum, int s) {
+  return y * 0.69314718055994530942 - log(ldexp((double)sum, -s));
+}
+
 // exp2(y) 2^s, y <= 0 (from -200 on).  2^f on [-1/2, 1/2] by the polynomial of degree 8 of the least relative error (by
 // exchange), its constant then set to 1, so that equal largest entries weigh 1 (1e-12); n = round(y) by an addition
 // that leaves it in the sum's low bits.
@@ -382,7 +388,7 @@ __device__ __forceinline__ void choose_row(const ChooseArgs& a, int64_t r, Share
     a.token[r] = token;
     if (a.logprob) {
       const double y = ((double)Elem<BF>::load(ch.row.base, token) - ch.top) * ch.c;
-      a.logprob[r] = (float)((y + a.unit) * 0.69314718055994530942 - log((double)sum));
+      a.logprob[r] = (float)(log_share(y, sum, a.unit));
     }
     if (a.kept) a.kept[r] = n;
   }
@@ -813,7 +819,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
                    &found);
     if (threadIdx.x == 0) {
       const double y = ((double)Elem<BF>::load(pc.row.base, found) - m) * way.c;
-      write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log(whole), live);
+      write_token(a, r, found, log_share(y, whole, a.unit), live);
       state.mode = kDone;
     }
     return;
@@ -1059,7 +1065,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseAr
   }
   if (threadIdx.x == 0) {
     const double y = ((double)Elem<BF>::load(pc.row.base, found) - st.m) * way.c;
-    write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log((double)kept.whole), over_count + kept.count);
+    write_token(a, r, found, log_share(y, kept.whole, a.unit), over_count + kept.count);
   }
 }
 
@@ -1126,7 +1132,18 @@ __global__ __launch_bounds__(kPieceThreads, 4) void top_kernel(const ChooseArgs 
     return found;
   };
   if (top > -INFINITY) atomicAdd(&bins[bin_of(top)], 1);
-  const int least = first_bin();
+  int least = first_bin();
+  if (least == kBins) {  // fewer threads with an entry than top_k (a piece at the end of a row): by all entries
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kPieceThreads) bins[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j < N && i < pc.batches; ++j)
+        if (pc.at(i, j) > -INFINITY) atomicAdd(&bins[bin_of(pc.at(i, j))], 1);
+    least = first_bin();
+  }
   // each piece has room for `room` keys; kOdd and kMany, above all keys, say that the row has none, and that there is none
   constexpr u64 kOdd = ~0ull, kMany = ~0ull - 1;
   const int room = kList / a.pieces;
@@ -1193,7 +1210,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void top_kernel(const ChooseArgs 
   find_listed(kept, keys, upto, scratch, &found);
   if (threadIdx.x == 0) {
     const double y = ((double)Elem<BF>::load(pc.row.base, found) - m) * way.c;
-    write_token(a, r, found, (y + a.unit) * 0.69314718055994530942 - log((double)kept.whole), kept.count);
+    write_token(a, r, found, log_share(y, kept.whole, a.unit), kept.count);
   }
 }
 

@@ -153,6 +153,17 @@ def test_extreme_values(way):
         Run(z.cuda(), u, sampling=infs.make_sampling(**way)).check(z.double().numpy(), way)
 
 
+def test_one_entry_left_is_certain():
+    """logprob is 0 where one entry is kept: by top-k, top-p, min-p or masks."""
+    z, u, z64 = logits(4, 2001, True, 8)
+    z[3, 1:] = -math.inf
+    for way in ({"top_k": 1}, {"top_p": 1e-9}, {"min_p": 1.0}, {"top_k": 1500, "top_p": 1e-9}):
+        z[0, 7], z[1, 8], z[2, 9] = 30.0, 31.0, 33.0
+        r = Run(z, u, sampling=infs.make_sampling(**way))
+        assert (r.kept == 1).all() and (r.logprob == 0).all()
+    assert Run(z[3:], u[3:]).logprob.tolist() == [0.0]
+
+
 def test_rows_without_a_token():
     """Masked rows, NaN, +inf, numbers outside [0, 1): -1, NaN and 0; the rows beside them are not touched by it."""
     import torch
@@ -201,6 +212,15 @@ def test_strides_and_alignment(bf16, shift):
     r = Run(rows, u, row_stride=stride, vocab=v, sampling=infs.make_sampling(**way))
     r.check(z64, way)
     Run(rows, u, row_stride=stride, vocab=v).check(z64, {})
+
+
+@pytest.mark.parametrize("n,v,bf16", [(16, 8192 * 18 + 90, True), (16, 4096 + 33, True), (40, 8192 * 5 + 40, False)])
+def test_pieces_of_few_entries(n, v, bf16):
+    """Rows whose last piece has fewer entries than top-k, some of them masked."""
+    for masked in (0, 50, 95):
+        z, u, z64 = logits(n, v, bf16, v, masked=min(masked, v - 1))
+        for way in ({"top_k": 50}, {"top_k": 96, "top_p": 0.9}, {}, {"top_p": 0.7}):
+            Run(z, u, sampling=infs.make_sampling(**way)).check(z64, way)
 
 
 def test_longest_rows():
