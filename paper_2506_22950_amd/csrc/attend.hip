@@ -24,7 +24,7 @@
 // fp32 rows take fp32 products.
 //
 // Masked places.  A score that its row does not see is replaced, not added to,
-// and rows behind a sequence are zero in LDS.  Only a product over tokens of
+// and rows behind a sequence hold its last one again in LDS.  Only a product over tokens of
 // one tile, some of them unseen, can meet 0 times an infinity or NaN.  Where
 // such a tile holds one (seen while it is staged), the work-group starts over
 // in a second pass over its tiles, in which those elements are taken out
@@ -53,6 +53,7 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.f;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -141,47 +142,38 @@ struct Type<false> {
 // Token (key or row) of accumulator register i, in its block of 32.
 __device__ __forceinline__ int token_of(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 
-// A tile of rows of D elements in LDS.  Row r's chunk c of 16 bytes lies at chunk c ^ x(r), x from the low four
-// bits of r: the 8 rows (or 4 rows of 64 bytes) that a quarter of a wavefront reads at once lie in different banks.
+// A tile of rows of D elements in LDS, kStride bytes apart: 32 more than a row, so that the 8 rows that 8 lanes read
+// 16 bytes of lie in different banks (and the 4 rows of 64 bytes of a transposed read meet in few), and every
+// address is a lane's own offset plus a constant.  (Rows without a gap, chunks exchanged by row: no conflict at all,
+// but an instruction an address, a sixth of the loop's.)
 template <bool BF, int D>
 struct Tile {
-  static constexpr int kRow = D * (BF ? 2 : 4), kChunks = kRow / 16, kSteps = kChunks / 2, kBlocks = D / 32;
-  static __device__ __forceinline__ int turn(int r) {
-    return kChunks >= 16 ? ((r & 3) << 2 | ((r >> 2) & 3)) : (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
-  }
-  static __device__ __forceinline__ int place(int r, int c) { return r * kRow + ((c ^ turn(r)) << 4); }
+  static constexpr int kRow = D * (BF ? 2 : 4), kStride = kRow + 32;
+  static constexpr int kChunks = kRow / 16, kSteps = kChunks / 2, kBlocks = D / 32;
 
-  int straight, across, across8;  // byte offsets of this lane
+  int straight, across;  // byte offsets of this lane
   __device__ __forceinline__ Tile() {
-    const int l = threadIdx.x & 63, h = l >> 5;
-    straight = place(l & 31, h);
-    if constexpr (BF) {
-      const int a = l & 15, r = 4 * h + (a >> 2), c = 2 * ((l >> 4) & 1) + ((a & 3) >> 1);
-      across = place(r, c) + 8 * (a & 1);
-      across8 = place(r + 8, c) + 8 * (a & 1);
-    } else {
-      across = 4 * h * kRow + ((((l & 31) >> 2) ^ h) << 4) + 4 * (l & 3);
-    }
+    const int l = threadIdx.x & 63, h = l >> 5, a = l & 15;
+    straight = (l & 31) * kStride + 16 * h;
+    across = BF ? (4 * h + (a >> 2)) * kStride + 32 * ((l >> 4) & 1) + 8 * (a & 3) : 4 * h * kStride + 4 * (l & 31);
   }
-  // Step s of the sum over a row's elements, rows row0 .. row0+31 (row0 a multiple of 32).
+  // Step s of the sum over a row's elements, rows row0 .. row0+31.
   __device__ __forceinline__ u32x4 rows(const char* base, int row0, int s) const {
-    return *(const u32x4*)(base + row0 * kRow + (straight ^ (s << 5)));
+    return *(const u32x4*)(base + straight + row0 * kStride + 32 * s);
   }
   // Elements 32 b .. 32 b + 31 of the tokens that an operand from kRegs accumulator registers on (from register
   // i of the block of 32 tokens at token0) stands for, transposed.
   __device__ __forceinline__ u32x4 columns(const char* base, int token0, int i, int b) const {
+    const char* p = base + across + (token0 + 2 * i) * kStride;
     if constexpr (BF) {
-      const char* p = base + (token0 + 2 * i) * kRow;
-      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (across ^ (b << 6))));
-      const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (across8 ^ (b << 6))));
+      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 64 * b));
+      const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 64 * b + 8 * kStride));
       const u32x2 u = __builtin_bit_cast(u32x2, x), v = __builtin_bit_cast(u32x2, y);
       return u32x4{u[0], u[1], v[0], v[1]};
     } else {
       u32x4 r;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        r[j] = *(const uint32_t*)(base + (token0 + 2 * i + j) * kRow +
-                                  (across ^ ((8 * b ^ (j << 2) ^ ((i >> 1) & 2)) << 4)));
+      for (int j = 0; j < 4; ++j) r[j] = *(const uint32_t*)(p + j * kStride + 128 * b);
       return r;
     }
   }
@@ -247,40 +239,45 @@ __device__ __forceinline__ int divide_rows(int r, int hpk, uint32_t inv) {
   return t * hpk > r ? t - 1 : t;
 }
 
-// Rows of a tensor in registers between memory and LDS: `rows` of a tile, by `threads` threads.
+// Rows of a tensor in registers between memory and LDS: `ROWS` of a tile, by `THREADS` threads.  from() sets the
+// first tile's place, each load() goes on by a tile.
 template <bool BF, int D, int ROWS, int THREADS>
 struct Stage {
   using T = Tile<BF, D>;
   static constexpr int kPer = ROWS * T::kChunks / THREADS, kStep = THREADS / T::kChunks;
   static_assert(ROWS * T::kChunks % THREADS == 0 && THREADS % T::kChunks == 0, "whole chunks a thread");
   u32x4 x[kPer];
+  const char* next;  // of the thread's first row
   static __device__ __forceinline__ int row(int i) { return (int)threadIdx.x / T::kChunks + i * kStep; }
   static __device__ __forceinline__ int chunk() { return (int)threadIdx.x % T::kChunks; }
-  // Token rows first .. of `base` (stride bytes apart), zero from `end` on.
-  __device__ __forceinline__ void load(const char* base, int64_t stride, int first, int end) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int r = first + row(i);
-      x[i] = u32x4{0, 0, 0, 0};
-      if (r < end) x[i] = *(const u32x4*)(base + r * stride + chunk() * 16);
-    }
+  // Rows of tokens from `first` on, `stride` bytes apart.
+  __device__ __forceinline__ void from(const char* base, int64_t stride, int first) {
+    next = base + (first + row(0)) * stride + chunk() * 16;
   }
-  // Rows first .. of a group's heads.
+  // The tile of rows first ..; behind the last, row end - 1 again (end > first).
+  __device__ __forceinline__ void load(int64_t stride, int first, int end) {
+    if (first + ROWS <= end) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) x[i] = *(const u32x4*)(next + i * kStep * stride);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) x[i] = *(const u32x4*)(next + (min(first + row(i), end - 1) - first - row(0)) * stride);
+    }
+    next += ROWS * stride;
+  }
+  // Rows first .. of a group's heads, alike; `inv` as in divide_rows.
   __device__ __forceinline__ void load_rows(const char* base, int64_t stride, int64_t head, int first, int end, int hpk,
                                             uint32_t inv) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int r = first + row(i);
-      x[i] = u32x4{0, 0, 0, 0};
-      if (r < end) {
-        const int t = divide_rows(r, hpk, inv);
-        x[i] = *(const u32x4*)(base + t * stride + (r - t * hpk) * head + chunk() * 16);
-      }
+      const int r = min(first + row(i), end - 1), t = divide_rows(r, hpk, inv);
+      x[i] = *(const u32x4*)(base + t * stride + (r - t * hpk) * head + chunk() * 16);
     }
   }
   __device__ __forceinline__ void store(char* lds) const {
+    char* p = lds + row(0) * T::kStride + chunk() * 16;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) *(u32x4*)(lds + T::place(row(i), chunk())) = x[i];
+    for (int i = 0; i < kPer; ++i) *(u32x4*)(p + i * kStep * T::kStride) = x[i];
   }
   __device__ __forceinline__ bool odd() const {
     uint32_t r = 0;
@@ -300,6 +297,24 @@ __device__ __forceinline__ void load_operands(u32x4 (&f)[STEPS], const char* row
   for (int s = 0; s < STEPS; ++s) {
     f[s] = u32x4{0, 0, 0, 0};
     if (there) f[s] = *(const u32x4*)(row + (2 * s + half) * 16);
+  }
+}
+
+// Operands of a block of 32 rows, asked for ahead of the products that take them: what the compiler would move to
+// their use, two at a time, each pair waiting for LDS.
+template <int STEPS, class T>
+__device__ __forceinline__ void fetch_rows(u32x4 (&f)[STEPS], const T& tile, const char* base, int row0) {
+#pragma unroll
+  for (int e = 0; e < STEPS; ++e) f[e] = tile.rows(base, row0, e);
+  __builtin_amdgcn_sched_barrier(0);
+}
+// N times a matrix instruction, then an LDS load: the order of the code ahead of it.
+template <int N>
+__device__ __forceinline__ void paired() {
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
 }
 
@@ -367,7 +382,7 @@ struct Shape {
   static constexpr int kBlock = BF && C > 2 ? 64 : 32;  // tokens of a group's tile
   static constexpr int kTokens = kBlock * S;
   static constexpr int kBuffers = S == 1 ? 2 : 1;
-  static constexpr int kTile = kTokens * Tile<BF, D>::kRow;
+  static constexpr int kTile = kTokens * Tile<BF, D>::kStride;
   static constexpr int kJoin = S > 1 ? C * S * 4096 : 0;
   static constexpr int kLds = 2 * kBuffers * kTile > kJoin ? 2 * kBuffers * kTile : kJoin;
 };
@@ -383,6 +398,7 @@ __device__ __forceinline__ void walk(int n, Load load, Store store, Use use) {
   for (int t = 0; t < n; ++t) {
     __syncthreads();
     if (t + 1 < n) load(t + 1);
+    __builtin_amdgcn_sched_barrier(0);
     use(BUFFERS == 2 ? t & 1 : 0, t);
     if (t + 1 < n) {
       if (BUFFERS == 1) __syncthreads();
@@ -447,15 +463,18 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
   const auto pass = [&](auto careful, int b0) {
     constexpr int KB = careful ? 1 : T::kBlocks;  // blocks of 32 elements of the result, from b0 on
     Stage<BF, D, H::kTokens, H::kThreads> sk, sv;
+    sk.from(kbase, a.k_row, 0);
+    sv.from(vbase, a.v_row, 0);
     u32x4 q[T::kSteps];
     load_operands(q, a.q + w.q_token * a.q_row + w.head * a.q_head, w.there);
     f32x16 acc[KB] = {};
     float m = -INFINITY, sum = 0.f;
+    const float slack = kSlack / c;
     walk<careful ? 1 : H::kBuffers>(
         tiles,
         [&](int t) {
-          sk.load(kbase, a.k_row, t * H::kTokens, w.keys);
-          sv.load(vbase, a.v_row, t * H::kTokens, w.keys);
+          sk.load(a.k_row, t * H::kTokens, w.keys);
+          sv.load(a.v_row, t * H::kTokens, w.keys);
         },
         [&](int buffer, int t) {
           sk.store(lds + 2 * buffer * H::kTile);
@@ -465,13 +484,20 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
         [&](int buffer, int t) {
           const int key0 = t * H::kTokens + group * BN;
           if (key0 > w.seen_any) return;
-          const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kRow;
+          const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kStride;
           const char* lv = lk + H::kTile;
           f32x16 s[NB] = {};
+          u32x4 f[T::kSteps];
+          fetch_rows(f, tile, lk, 0);
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
+          for (int n = 0; n < NB; ++n) {
 #pragma unroll
-            for (int e = 0; e < T::kSteps; ++e) s[n] = Type<BF>::mma(s[n], tile.rows(lk, 32 * n, e), q[e]);
+            for (int e = 0; e < T::kSteps; ++e) {
+              s[n] = Type<BF>::mma(s[n], f[e], q[e]);
+              if (n + 1 < NB) f[e] = tile.rows(lk, 32 * n + 32, e);
+            }
+            if (n + 1 < NB) paired<T::kSteps>();
+          }
           if (key0 + BN - 1 > w.seen_all) {
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -483,13 +509,16 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
           for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-          top = fmaxf(m, fmaxf(top, other_half(top)));
-          if (__any(top > m)) {
-            const float by = exp2_((m - (top == -INFINITY ? 0.f : top)) * c);
+          top = fmaxf(top, other_half(top));
+          // the sums keep their base until a score is 2^kSlack times it: fp32 has room, and the operands of the second
+          // product are as exact at any size
+          const bool grows = top > m + slack;
+          if (__any(grows)) {
+            const float by = grows ? exp2_((m - top) * c) : 1.f;  // (a row of its own: none goes by another's scores)
             sum *= by;
 #pragma unroll
             for (int b = 0; b < KB; ++b) acc[b] *= by;
-            m = top;
+            m = grows ? top : m;
           }
           const float off = m == -INFINITY ? 0.f : -m * c;
 #pragma unroll
@@ -574,6 +603,8 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
   const auto pass = [&](auto careful, int b0) {
     constexpr int KB = careful ? 1 : T::kBlocks;
     Stage<BF, D, H::kTokens, H::kThreads> sk, sv;
+    sk.from(kbase, a.k_row, 0);
+    sv.from(vbase, a.v_row, 0);
     u32x4 q[T::kSteps], up[T::kSteps];
     float delta = 0.f;
     load_operands(q, a.o + w.q_token * a.o_row + w.head * a.o_head, w.there);
@@ -587,8 +618,8 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
     walk<careful ? 1 : H::kBuffers>(
         tiles,
         [&](int t) {
-          sk.load(kbase, a.k_row, t * H::kTokens, w.keys);
-          sv.load(vbase, a.v_row, t * H::kTokens, w.keys);
+          sk.load(a.k_row, t * H::kTokens, w.keys);
+          sv.load(a.v_row, t * H::kTokens, w.keys);
         },
         [&](int buffer, int t) {
           sk.store(lds + 2 * buffer * H::kTile);
@@ -598,7 +629,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
         [&](int buffer, int t) {
           const int key0 = t * H::kTokens + group * BN;
           if (key0 > w.seen_any) return;
-          const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kRow;
+          const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kStride;
           const char* lv = lk + H::kTile;
           const bool masked = key0 + BN - 1 > w.seen_all;
 #pragma unroll
@@ -658,9 +689,9 @@ struct KeyShape {
   static constexpr int kBlock = BF && D == 64 && C > 1 ? 64 : 32;  // rows of a group's tile
   static constexpr int kTokens = kBlock * S;
   static constexpr int kBuffers = S == 1 ? 2 : 1;
-  static constexpr int kTile = kTokens * Tile<BF, D>::kRow;
+  static constexpr int kTile = kTokens * Tile<BF, D>::kStride;
   static constexpr bool kValues = D == 128 && BF == (S == 1);  // in LDS
-  static constexpr int kValueBytes = kValues ? 32 * C * Tile<BF, D>::kRow : 0;
+  static constexpr int kValueBytes = kValues ? 32 * C * Tile<BF, D>::kStride : 0;
   static constexpr int kJoin = S > 1 ? C * S * 4096 : 0;
   static constexpr int kTiles = 2 * kBuffers * kTile > kJoin ? 2 * kBuffers * kTile : kJoin;
 };
@@ -699,10 +730,11 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dkv_ker
   char* values = lds + H::kTiles;
   if constexpr (H::kValues) {
     Stage<BF, D, BK, H::kThreads> sv;
-    sv.load(a.v + p.begin * a.v_row + g * a.v_head, a.v_row, key0, keys);
+    sv.from(a.v + p.begin * a.v_row + g * a.v_head, a.v_row, key0);
+    sv.load(a.v_row, key0, keys);
     sv.store(values);
   }
-  const char* own_values = values + wave % C * 32 * T::kRow;
+  const char* own_values = values + wave % C * 32 * T::kStride;
 
   const auto pass = [&](auto careful, int b0) {
     constexpr int KB = careful ? 1 : T::kBlocks;
@@ -734,7 +766,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dkv_ker
         [&](int buffer, int t) {
           const int row0 = begin + t * H::kTokens + group * BR;
           if (row0 + BR <= wfirst || row0 >= rows) return;
-          const char* lq = lds + 2 * buffer * H::kTile + group * BR * T::kRow;
+          const char* lq = lds + 2 * buffer * H::kTile + group * BR * T::kStride;
           const char* lo = lq + H::kTile;
           const bool masked = row0 < wall || row0 + BR > rows;
 #pragma unroll
