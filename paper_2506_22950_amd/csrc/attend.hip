@@ -20,7 +20,7 @@
 // {4h .. 4h+3, 8+4h .. 8+4h+3} of 16 (h: which half of the wavefront), and V^T is
 // read in that order (transposed out of LDS, 8 bytes of four keys a lane).
 // bf16 operands add up in fp32; p and ds are rounded to bf16 as operands
-// (2^-9 relative each, below the rounding of the outputs they add up to);
+// (2^-8 relative each, as the rounding of the outputs they add up to);
 // fp32 rows take fp32 products.
 //
 // Masked places.  A score that its row does not see is replaced, not added to,
@@ -35,7 +35,7 @@
 // Work-groups.  C wavefronts, of 32 rows each, share the tiles, and there are S
 // such groups, which take turns with the tiles and are joined at the end: many
 // columns for many rows (every byte out of L2 serves 256 of them), many splits
-// where there are too few work-groups to fill the GPU.
+// where there are too few work-groups to fill the GPU, and some of both between.
 #include "ops.h"
 
 #include <algorithm>
@@ -376,10 +376,10 @@ __device__ __forceinline__ void join(f32x16 (&acc)[N], char* buffer) {
 }
 
 // Sizes of a kernel of C columns and S splits: tokens of a tile, buffers of tiles, LDS.  `values`: bytes ahead.
-template <bool BF, int D, int C, int S>
+template <bool BF, int D, int C, int S, int BLOCK>
 struct Shape {
   static constexpr int kThreads = 64 * C * S;
-  static constexpr int kBlock = BF && C > 2 ? 64 : 32;  // tokens of a group's tile
+  static constexpr int kBlock = BLOCK;  // tokens of a group's tile
   static constexpr int kTokens = kBlock * S;
   static constexpr int kBuffers = S == 1 ? 2 : 1;
   static constexpr int kTile = kTokens * Tile<BF, D>::kStride;
@@ -444,7 +444,7 @@ struct Rows {
 template <bool BF, int D, int C, int S>
 __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(const AttendArgs a) {
   using T = Tile<BF, D>;
-  using H = Shape<BF, D, C, S>;
+  using H = Shape<BF, D, C, S, (BF && C > 1) ? 64 : 32>;
   constexpr int BN = H::kBlock, NB = BN / 32, R = Type<BF>::kRegs;
   __shared__ __attribute__((aligned(16))) char lds[H::kLds];
   __shared__ float maxima[S][C * 32], sums[S][C * 32];
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
 template <bool BF, int D, int C, int S>
 __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kernel(const AttendGradArgs a) {
   using T = Tile<BF, D>;
-  using H = Shape<BF, D, C, S>;
+  using H = Shape<BF, D, C, S, (BF && (C > 2 || (C > 1 && D == 64))) ? 64 : 32>;
   constexpr int BN = H::kBlock, NB = BN / 32, R = Type<BF>::kRegs;
   __shared__ __attribute__((aligned(16))) char lds[H::kLds];
   __shared__ int odd;  // K holds an infinity or NaN in a tile that some rows do not see
@@ -690,14 +690,14 @@ struct KeyShape {
   static constexpr int kTokens = kBlock * S;
   static constexpr int kBuffers = S == 1 ? 2 : 1;
   static constexpr int kTile = kTokens * Tile<BF, D>::kStride;
-  static constexpr bool kValues = D == 128 && BF == (S == 1);  // in LDS
+  static constexpr bool kValues = D == 128 && (BF ? S == 1 || C * S == 8 : S > 1);  // in LDS
   static constexpr int kValueBytes = kValues ? 32 * C * Tile<BF, D>::kStride : 0;
   static constexpr int kJoin = S > 1 ? C * S * 4096 : 0;
   static constexpr int kTiles = 2 * kBuffers * kTile > kJoin ? 2 * kBuffers * kTile : kJoin;
 };
 
 template <bool BF, int D, int C, int S>
-__global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dkv_kernel(const AttendGradArgs a) {
+__global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) void attend_dkv_kernel(const AttendGradArgs a) {
   using T = Tile<BF, D>;
   using H = KeyShape<BF, D, C, S>;
   constexpr int BK = 32 * C, BR = H::kBlock, R = Type<BF>::kRegs;
@@ -835,9 +835,21 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dkv_ker
 // Slots of the tiles of `tile` rows (per_token rows a token).
 int slots_of(int64_t tokens, int per_token, int sequences, int tile) { return (int)(tokens * per_token / tile + sequences); }
 
-// Whether rows fill work-groups of `tile` rows, and these the GPU; else 32 rows a work-group and splits.
-constexpr int kWideBlocks = 256;
-bool wide(int64_t tokens, int per_token, int kv_heads, int tile) { return tokens * per_token / tile * kv_heads >= kWideBlocks; }
+// Whether rows make `groups` work-groups of `tile` rows.  More rows a work-group are fewer bytes through LDS for each,
+// fewer rows are more work-groups, with more splits each, for long walks over keys and for causal ones, which end at
+// different times.  Measured (us; work-groups of 32, 64 and 256 rows; sequences x tokens, 16 heads of 128 on 8 KV heads):
+//   bf16 o    4 x 256: 22 12 13    1 x 2048: 76 45 61    4 x 1024: 111 60 36    64 x 128: 152 73 37
+//   bf16 dq   4 x 256: 22 16 19    1 x 2048: 90 55 83    4 x 1024: 122 75 54    64 x 128: 140 87 60
+//   fp32 o    4 x 256: 38 29 65    1 x 2048: 228 190 505    4 x 1024: 269 205 259    4 x 4096: 3376 2756 2273
+// so bf16 takes 64 and 256 rows as soon as they fill the GPU once.  fp32 products take eight times as long and are
+// never waited for, so a GPU that is filled evenly to the end is worth more: 2 and 4 work-groups a CU.
+// dk and dv (32, 64 and 128 keys):
+//   bf16      4 x 512: 47 33 57    4 x 1024: 119 93 113    8 x 2048: 757 493 461    64 x 128: 99 62 53
+//   fp32      4 x 512: 147 151 292    4 x 1024: 391 465 571    4 x 2048: 1417 1272 1814    64 x 128: 208 176 325
+constexpr int kCus = 256;
+bool fills(int64_t tokens, int per_token, int kv_heads, int tile, int groups) {
+  return tokens * per_token / tile * kv_heads >= groups;
+}
 
 template <bool BF, int D, int C, int S>
 hipError_t attend(AttendArgs& a, hipStream_t stream) {
@@ -861,22 +873,28 @@ hipError_t attend_dkv(AttendGradArgs& a, hipStream_t stream) {
 template <bool BF, int D>
 hipError_t attend(AttendArgs& a, hipStream_t stream) {
   constexpr bool kLarge = !BF && D == 128;  // rows of 512 bytes
-  if (wide(a.q_tokens, a.hpk, a.kv_heads, 256)) return attend<BF, D, 8, 1>(a, stream);
+  if (fills(a.q_tokens, a.hpk, a.kv_heads, 256, kCus * (BF ? 1 : 4))) return attend<BF, D, 8, 1>(a, stream);
+  if (fills(a.q_tokens, a.hpk, a.kv_heads, 64, kCus * (BF ? 1 : 2))) return attend<BF, D, 2, kLarge ? 2 : 4>(a, stream);
   return attend<BF, D, 1, kLarge ? 4 : 8>(a, stream);
 }
 
 template <bool BF, int D>
-hipError_t attend_grad(AttendGradArgs& a, hipStream_t stream) {
+hipError_t attend_dq(AttendGradArgs& a, hipStream_t stream) {
   constexpr bool kLarge = !BF && D == 128;
-  hipError_t e;
-  if (wide(a.q_tokens, a.hpk, a.kv_heads, 256))
-    e = attend_dq<BF, D, 8, 1>(a, stream);
-  else
-    e = attend_dq<BF, D, 1, D == 128 ? 4 : 8>(a, stream);
+  if (fills(a.q_tokens, a.hpk, a.kv_heads, 256, kCus * (BF ? 1 : 4))) return attend_dq<BF, D, 8, 1>(a, stream);
+  if (fills(a.q_tokens, a.hpk, a.kv_heads, 64, kCus * (BF ? 1 : 2)))
+    return attend_dq<BF, D, 2, kLarge ? 2 : 4>(a, stream);
+  return attend_dq<BF, D, 1, D == 128 ? 4 : 8>(a, stream);
+}
+
+template <bool BF, int D>
+hipError_t attend_grad(AttendGradArgs& a, hipStream_t stream) {
+  const hipError_t e = attend_dq<BF, D>(a, stream);
   if (e != hipSuccess) return e;
-  constexpr int kKeys = kLarge ? 4 : 8;
-  if (wide(a.k_tokens, 1, a.kv_heads, 32 * kKeys))
-    return attend_dkv<BF, D, kKeys, 1>(a, stream);
+  if constexpr (BF)
+    if (fills(a.k_tokens, 1, a.kv_heads, 128, kCus * 2)) return attend_dkv<BF, D, 4, 1>(a, stream);
+  if (fills(a.k_tokens, 1, a.kv_heads, 64, kCus * (BF ? 1 : 4)))
+    return attend_dkv<BF, D, 2, !BF && D == 128 ? 2 : 4>(a, stream);
   return attend_dkv<BF, D, 1, BF && D == 64 ? 8 : 4>(a, stream);
 }
 

@@ -188,6 +188,17 @@ CASES = [
     (48, 16, 128, True, [520, 130, 700], [600, 130, 901], {}),
     (64, 64, 64, False, [640, 411], None, {"layout": "fused"}),
     (32, 32, 128, False, [300, 1900], [333, 1900], {}),
+    # enough rows for the tiles between
+    (64, 64, 64, True, [129, 1, 170], None, {}),
+    (64, 64, 128, True, [129, 1, 170], [200, 1, 333], {}),
+    (64, 16, 128, True, [300, 37], [400, 37], {"layout": "fused"}),
+    (128, 128, 64, False, [129, 1, 170], None, {}),
+    (128, 128, 128, False, [129, 1, 170], [129, 7, 300], {}),
+    (256, 256, 64, False, [130, 200], None, {}),
+    (256, 256, 128, False, [130, 200], None, {}),
+    # fp32: .. and for the largest
+    (1024, 1024, 64, False, [256], None, {}),
+    (1024, 512, 128, False, [250, 6], None, {}),
     (32, 4, 128, True, [2, 1, 3, 1, 1, 5, 8, 1, 2, 1, 1, 1, 4] * 6, None, {}),  # more sequences than lanes
 ]
 
@@ -251,7 +262,7 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.parametrize("bf16,d", [(True, 64), (True, 128), (False, 64), (False, 128)])
-@pytest.mark.parametrize("copies", [1, 300])
+@pytest.mark.parametrize("copies", [1, 40, 300])
 def test_unseen_infinities_and_nans(bf16, d, copies):
     """A token's infinities and NaN change nothing that does not see it: later tokens' rows in V, K, Q and d_o, rows
     behind the sequence, another sequence's, another KV head's.  With many more sequences behind, so that the
