@@ -53,7 +53,13 @@ def prefill_prompts(ctx: infs.Context, prompt_lens: Sequence[int], num_layers: i
         raise ValueError("norms go with rotary positions")
     if rotary is not None and positions is None:
         raise ValueError("rotary positions need the tokens' positions")
-    c, tokens = ctx.config, sum(prompt_lens)
+    c, a, tokens = ctx.config, attention.config, sum(prompt_lens)
+    if (a.num_q_heads, a.num_kv_heads, a.head_dim, a.dtype) != (c.num_q_heads, c.num_kv_heads, c.head_dim, c.dtype):
+        raise ValueError("the attention has other heads, or another type, than the context")
+    if (attention.stream or 0) != (ctx.stream or 0):
+        raise ValueError("the attention has to be on the context's stream")
+    if len(prompt_lens) > c.num_prompts:
+        raise ValueError(f"{len(prompt_lens)} prompts for a context of {c.num_prompts}")
     size = c.num_kv_heads * c.head_dim * (4 if c.dtype == infs.F32 else 2)  # bytes of a token's K or V
     for layer in range(num_layers):
         q, k, v, o = (infs._ptr(x) for x in provide(layer))

@@ -363,7 +363,8 @@ class Attention:
 
     def __init__(self, config: AttentionConfig, stream=None):
         h = ctypes.c_void_p()
-        _check(None, load().infs_attention_create(ctypes.byref(config), _stream(stream), ctypes.byref(h)))
+        self.stream = _stream(stream)
+        _check(None, load().infs_attention_create(ctypes.byref(config), self.stream, ctypes.byref(h)))
         self._h = h
         self.config = config
 
