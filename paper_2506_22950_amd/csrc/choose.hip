@@ -1376,7 +1376,15 @@ hipError_t launch_choose(ChooseArgs& a, bool bf16, hipStream_t stream) {
   const infs_sampling& p = a.all;
   const bool whole = !a.each && (p.top_k == 0 || p.top_k >= a.vocab) && (p.top_p == 0.0 || p.top_p == 1.0) && p.min_p == 0.0;
   // lists of all pieces' first top_k, with room for what else lies in their last bins
-  const bool top = !a.each && p.top_k > 0 && p.top_k < a.vocab && p.top_k <= kPieceThreads / 2 && (int64_t)p.top_k * a.pieces <= kList / 2;
+  bool top = !a.each && p.top_k > 0 && p.top_k < a.vocab && p.top_k <= kPieceThreads / 2;
+  // (for few long rows that takes pieces of more entries: one row of 243428, top-k 64: 48 us in two launches of 60 pieces,
+  // 17 in one of 30)
+  for (; top && (int64_t)p.top_k * a.pieces > kList / 2; a.pieces = choose_pieces(a.vocab, a.batches, bf16)) {
+    if (a.batches < kPieceVectors)
+      a.batches *= 2;
+    else
+      top = false;
+  }
   const int rows = a.rows;
   for (a.row0 = 0; a.row0 < rows; a.row0 += per_launch) {
     const int n = std::min(per_launch, rows - a.row0);

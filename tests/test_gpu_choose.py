@@ -223,6 +223,18 @@ def test_pieces_of_few_entries(n, v, bf16):
             Run(z, u, sampling=infs.make_sampling(**way)).check(z64, way)
 
 
+@pytest.mark.parametrize("n,v,bf16", [(1, 243429, True), (3, 120001, False), (2, 1 << 20, False)])
+def test_few_long_rows(n, v, bf16):
+    """Of few rows the pieces are as many as fill the GPU, or as few as their first top_k fit a list."""
+    import torch
+
+    z, u, z64 = logits(n, v, bf16, v, masked=v // 3)
+    s = infs.Sampler(infs.make_sampler_config(vocab=v, dtype=infs.BF16 if bf16 else infs.F32, max_rows=n),
+                     stream=torch.cuda.current_stream())
+    for way in ({"top_k": 256, "min_p": 0.001}, {"top_k": 31}, {}, {"top_k": 64, "top_p": 0.95}, {"top_k": 257}, {"top_p": 0.9}):
+        Run(z, u, sampler=s, sampling=infs.make_sampling(**way)).check(z64, way)
+
+
 def test_longest_rows():
     import torch
 
