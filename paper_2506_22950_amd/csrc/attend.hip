@@ -375,6 +375,73 @@ __device__ __forceinline__ void join(f32x16 (&acc)[N], char* buffer) {
   }
 }
 
+// ---- walks that several work-groups share ----
+// One sequence's few rows over many keys (or a key over many rows) would be one long walk on one CU.  Work-groups of 32
+// rows (C = 1) share it: each takes a run of its tiles, its results go to memory, and the last one to arrive adds
+// them up in their order (nothing waits).
+constexpr int kMostParts = 32;
+template <bool BF>
+constexpr int kLeastTiles = BF ? 2 : 1;  // a part; an fp32 tile takes as long as handing a part over
+
+// The place of a work-group: walk `slot` of head g, and part `part` of the walk.  Parts that are not needed come last.
+struct Walker {
+  int g, slot, part, id;
+  __device__ __forceinline__ Walker(const AttendShape& a, bool shared) {
+    const int i = (int)(blockIdx.x / (unsigned)a.kv_heads);
+    g = (int)blockIdx.x - i * a.kv_heads;
+    part = shared ? (int)((unsigned)i / (unsigned)a.slots) : 0;
+    slot = i - part * a.slots;
+    id = slot * a.kv_heads + g;
+  }
+};
+// Its tiles, first .. first + n - 1 of a walk of `tiles`, which takes `parts` of them; `part` may be none of these.
+struct Share {
+  int parts, first, n;
+  __device__ __forceinline__ Share(int tiles, int part, int most, int least) {
+    parts = min(most, max(1, tiles / least));
+    first = (int)((int64_t)tiles * part / parts), n = (int)((int64_t)tiles * (part + 1) / parts) - first;
+  }
+};
+
+__device__ __forceinline__ void publish(float* p, float x, float y) {  // past the caches of this XCD
+  const uint64_t w = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+  __hip_atomic_store((uint64_t*)p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 collect(const float* p) {
+  const uint64_t w = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return float2{__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32))};
+}
+
+// A block of results in a wavefront's place `at` of the parts' results: 1024 floats.
+__device__ __forceinline__ void publish_block(float* at, const f32x16& x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) publish(at + (i / 2 * 64 + lane) * 2, x[i], x[i + 1]);
+}
+// c = c * keep + the block * by
+__device__ __forceinline__ void collect_block(f32x16& c, const float* at, float keep, float by) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    const float2 x = collect(at + (i / 2 * 64 + lane) * 2);
+    c[i] = fmaf(x.x, by, c[i] * keep), c[i + 1] = fmaf(x.y, by, c[i + 1] * keep);
+  }
+}
+
+// Whether this work-group is the last of `parts` to come here, with what it published.  Leaves the counter 0.
+__device__ __forceinline__ bool arrive(int32_t* counter, int parts) {
+  __shared__ bool last;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have reached the coherence point
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+  }
+  __syncthreads();
+  return last;
+}
+
 // Sizes of a kernel of C columns and S splits: tokens of a tile, buffers of tiles, LDS.  `values`: bytes ahead.
 template <bool BF, int D, int C, int S, int BLOCK>
 struct Shape {
@@ -415,10 +482,9 @@ struct Rows {
   int64_t q_token;
   bool there;
   // false: nothing to do
-  __device__ __forceinline__ bool find(const AttendShape& a, int slots) {
+  __device__ __forceinline__ bool find(const AttendShape& a, const Walker& at) {
     constexpr int BM = 32 * C;
-    const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
-    const int slot = slots - 1 - (int)(blockIdx.x / (unsigned)a.kv_heads);  // the longest rows first
+    const int g = at.g, slot = a.slots - 1 - at.slot;  // the longest rows first
     p = find_place(a.q_offsets, a.sequences, a.q_tokens, slot, a.hpk, __builtin_ctz(BM));
     rows = (p.end - p.begin) * a.hpk, row0 = p.tile * BM;
     if (p.tile < 0 || row0 >= rows) return false;
@@ -443,6 +509,7 @@ struct Rows {
 // ---- o and lse -----------------------------------------------------------------
 template <bool BF, int D, int C, int S>
 __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(const AttendArgs a) {
+  constexpr bool kShared = C == 1;
   using T = Tile<BF, D>;
   using H = Shape<BF, D, C, S, (BF && C > 1) ? 64 : 32>;
   constexpr int BN = H::kBlock, NB = BN / 32, R = Type<BF>::kRegs;
@@ -450,39 +517,79 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
   __shared__ float maxima[S][C * 32], sums[S][C * 32];
   __shared__ int odd;  // V holds an infinity or NaN in a tile that some rows do not see
   Rows<C> w;
-  if (!w.find(a, a.q_slots)) return;
+  const Walker at(a, kShared);
+  if (!w.find(a, at)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int column = wave % C, group = wave / C, g = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int tiles = w.seen_last < 0 ? 0 : w.seen_last / H::kTokens + 1;
+  const int column = wave % C, group = wave / C, g = at.g;
+  const Share share(w.seen_last < 0 ? 0 : w.seen_last / H::kTokens + 1,
+                    at.part, kShared ? a.parts : 1, kLeastTiles<BF>);
+  if (at.part >= share.parts) return;
+  // of the walk: [parts][blocks][1024], [parts][32][2]
+  float* results = a.part + (int64_t)at.id * a.parts * (32 * (D + 2));
+  float* statistics = results + a.parts * (32 * D);
   const char* kbase = a.k + w.kb * a.k_row + g * a.k_head;
   const char* vbase = a.v + w.kb * a.v_row + g * a.v_head;
   const float c = a.scale * kLog2e;
   const T tile;
   if (threadIdx.x == 0) odd = 0;
 
+  // Joins the groups; blocks b0 .. of the result, to its rows or to the parts'.
+  const auto finish = [&](auto& acc, float m, float sum, int b0, bool to_parts) {
+    constexpr int KB = sizeof(acc) / sizeof(f32x16);
+    if constexpr (S > 1) {
+      __syncthreads();
+      if (half == 0) maxima[group][column * 32 + lane] = m, sums[group][column * 32 + lane] = sum;
+      __syncthreads();
+      const int own = column * 32 + (lane & 31);
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < S; ++i) top = fmaxf(top, maxima[i][own]);
+      const float base = top == -INFINITY ? 0.f : top;
+      const float by = exp2_((m - base) * c);
+#pragma unroll
+      for (int b = 0; b < KB; ++b) acc[b] *= by;
+      m = top, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < S; ++i) sum = fmaf(sums[i][own], exp2_((maxima[i][own] - base) * c), sum);
+      join<C, S>(acc, lds);
+      if (group > 0) return;
+      if (kShared && to_parts) {
+        if (half == 0) publish(statistics + (at.part * 32 + lane) * 2, m, sum);
+#pragma unroll
+        for (int b = 0; b < KB; ++b) publish_block(results + (at.part * T::kBlocks + b0 + b) * 1024, acc[b]);
+        return;
+      }
+    }
+    const float by = w.last < 0 ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) store_block<BF>(acc[b], by, a.o + w.q_token * a.o_row + w.head * a.o_head, b0 + b, w.there);
+    if (w.there && half == 0 && a.lse)
+      a.lse[w.q_token * a.q_heads + w.head] =
+          w.last < 0 ? -INFINITY : (m == -INFINITY ? 0.f : m * a.scale) + __log2f(sum) * kLn2;
+  };
   const auto pass = [&](auto careful, int b0) {
     constexpr int KB = careful ? 1 : T::kBlocks;  // blocks of 32 elements of the result, from b0 on
     Stage<BF, D, H::kTokens, H::kThreads> sk, sv;
-    sk.from(kbase, a.k_row, 0);
-    sv.from(vbase, a.v_row, 0);
+    sk.from(kbase, a.k_row, share.first * H::kTokens);
+    sv.from(vbase, a.v_row, share.first * H::kTokens);
     u32x4 q[T::kSteps];
     load_operands(q, a.q + w.q_token * a.q_row + w.head * a.q_head, w.there);
     f32x16 acc[KB] = {};
     float m = -INFINITY, sum = 0.f;
     const float slack = kSlack / c;
     walk<careful ? 1 : H::kBuffers>(
-        tiles,
+        share.n,
         [&](int t) {
-          sk.load(a.k_row, t * H::kTokens, w.keys);
-          sv.load(a.v_row, t * H::kTokens, w.keys);
+          sk.load(a.k_row, (share.first + t) * H::kTokens, w.keys);
+          sv.load(a.v_row, (share.first + t) * H::kTokens, w.keys);
         },
         [&](int buffer, int t) {
           sk.store(lds + 2 * buffer * H::kTile);
           sv.store(lds + (2 * buffer + 1) * H::kTile);
-          if (!careful && t * H::kTokens + H::kTokens - 1 > w.seen_first && sv.odd()) odd = 1;
+          if (!careful && (share.first + t + 1) * H::kTokens - 1 > w.seen_first && sv.odd()) odd = 1;
         },
         [&](int buffer, int t) {
-          const int key0 = t * H::kTokens + group * BN;
+          const int key0 = (share.first + t) * H::kTokens + group * BN;
           if (key0 > w.seen_any) return;
           const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kStride;
           const char* lv = lk + H::kTile;
@@ -544,30 +651,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
             }
         });
     sum += other_half(sum);
-    if constexpr (S > 1) {
-      __syncthreads();
-      if (half == 0) maxima[group][column * 32 + lane] = m, sums[group][column * 32 + lane] = sum;
-      __syncthreads();
-      const int at = column * 32 + (lane & 31);
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < S; ++i) top = fmaxf(top, maxima[i][at]);
-      const float base = top == -INFINITY ? 0.f : top;
-      const float by = exp2_((m - base) * c);
-#pragma unroll
-      for (int b = 0; b < KB; ++b) acc[b] *= by;
-      m = top, sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < S; ++i) sum = fmaf(sums[i][at], exp2_((maxima[i][at] - base) * c), sum);
-      join<C, S>(acc, lds);
-      if (group > 0) return;
-    }
-    const float by = w.last < 0 ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int b = 0; b < KB; ++b) store_block<BF>(acc[b], by, a.o + w.q_token * a.o_row + w.head * a.o_head, b0 + b, w.there);
-    if (w.there && half == 0 && a.lse)
-      a.lse[w.q_token * a.q_heads + w.head] =
-          w.last < 0 ? -INFINITY : (m == -INFINITY ? 0.f : m * a.scale) + __log2f(sum) * kLn2;
+    finish(acc, m, sum, b0, share.parts > 1);
   };
   pass(std::false_type{}, 0);
   __syncthreads();
@@ -576,6 +660,21 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
       __syncthreads();
       pass(std::true_type{}, b);
     }
+  if constexpr (kShared) {
+    if (share.parts == 1 || !arrive(a.arrived + at.id, share.parts)) return;
+    // the parts, in turn over the groups
+    f32x16 acc[T::kBlocks] = {};
+    float m = -INFINITY, sum = 0.f;
+    for (int i = group; i < share.parts; i += S) {
+      const float2 x = collect(statistics + (i * 32 + (lane & 31)) * 2);
+      const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
+      const float keep = exp2_((m - base) * c), by = exp2_((x.x - base) * c);
+      m = top, sum = fmaf(x.y, by, sum * keep);
+#pragma unroll
+      for (int b = 0; b < T::kBlocks; ++b) collect_block(acc[b], results + (i * T::kBlocks + b) * 1024, keep, by);
+    }
+    finish(acc, m, sum, 0, false);
+  }
 }
 
 // ---- dq (and D) ----------------------------------------------------------------
@@ -583,28 +682,45 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
 // them, dq^T += K^T ds^T.  D = up.o of every row is left in a.delta for the kernel of dk and dv.
 template <bool BF, int D, int C, int S>
 __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kernel(const AttendGradArgs a) {
+  constexpr bool kShared = C == 1;
   using T = Tile<BF, D>;
   using H = Shape<BF, D, C, S, (BF && (C > 2 || (C > 1 && D == 64))) ? 64 : 32>;
   constexpr int BN = H::kBlock, NB = BN / 32, R = Type<BF>::kRegs;
   __shared__ __attribute__((aligned(16))) char lds[H::kLds];
   __shared__ int odd;  // K holds an infinity or NaN in a tile that some rows do not see
   Rows<C> w;
-  if (!w.find(a, a.q_slots)) return;
+  const Walker at(a, kShared);
+  if (!w.find(a, at)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int group = wave / C, g = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int tiles = w.seen_last < 0 ? 0 : w.seen_last / H::kTokens + 1;
+  const int group = wave / C, g = at.g;
+  const Share share(w.seen_last < 0 ? 0 : w.seen_last / H::kTokens + 1,
+                    at.part, kShared ? a.parts : 1, kLeastTiles<BF>);
+  if (at.part >= share.parts) return;
+  float* results = a.part + (int64_t)at.id * a.parts * (32 * D);  // of the walk: [parts][blocks][1024]
   const char* kbase = a.k + w.kb * a.k_row + g * a.k_head;
   const char* vbase = a.v + w.kb * a.v_row + g * a.v_head;
-  const int64_t at = w.q_token * a.q_heads + w.head;
-  const float c = a.scale * kLog2e, off = w.there ? -a.lse[at] * kLog2e : 0.f;
+  const int64_t row = w.q_token * a.q_heads + w.head;
+  const float c = a.scale * kLog2e, off = w.there ? -a.lse[row] * kLog2e : 0.f;
   const T tile;
   if (threadIdx.x == 0) odd = 0;
 
+  const auto finish = [&](auto& acc, int b0, bool to_parts) {
+    constexpr int KB = sizeof(acc) / sizeof(f32x16);
+    join<C, S>(acc, lds);
+    if (group > 0) return;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      if (kShared && to_parts)
+        publish_block(results + (at.part * T::kBlocks + b0 + b) * 1024, acc[b]);
+      else
+        store_block<BF>(acc[b], a.scale, a.dq + w.q_token * a.dq_row + w.head * a.dq_head, b0 + b, w.there);
+    }
+  };
   const auto pass = [&](auto careful, int b0) {
     constexpr int KB = careful ? 1 : T::kBlocks;
     Stage<BF, D, H::kTokens, H::kThreads> sk, sv;
-    sk.from(kbase, a.k_row, 0);
-    sv.from(vbase, a.v_row, 0);
+    sk.from(kbase, a.k_row, share.first * H::kTokens);
+    sv.from(vbase, a.v_row, share.first * H::kTokens);
     u32x4 q[T::kSteps], up[T::kSteps];
     float delta = 0.f;
     load_operands(q, a.o + w.q_token * a.o_row + w.head * a.o_head, w.there);
@@ -613,21 +729,21 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
     for (int s = 0; s < T::kSteps; ++s) delta += Type<BF>::dot(q[s], up[s]);
     delta += other_half(delta);
     load_operands(q, a.q + w.q_token * a.q_row + w.head * a.q_head, w.there);
-    if (w.there && half == 0 && group == 0) a.delta[at] = delta;
+    if (w.there && half == 0 && group == 0 && at.part == 0) a.delta[row] = delta;
     f32x16 acc[KB] = {};
     walk<careful ? 1 : H::kBuffers>(
-        tiles,
+        share.n,
         [&](int t) {
-          sk.load(a.k_row, t * H::kTokens, w.keys);
-          sv.load(a.v_row, t * H::kTokens, w.keys);
+          sk.load(a.k_row, (share.first + t) * H::kTokens, w.keys);
+          sv.load(a.v_row, (share.first + t) * H::kTokens, w.keys);
         },
         [&](int buffer, int t) {
           sk.store(lds + 2 * buffer * H::kTile);
           sv.store(lds + (2 * buffer + 1) * H::kTile);
-          if (!careful && t * H::kTokens + H::kTokens - 1 > w.seen_first && sk.odd()) odd = 1;
+          if (!careful && (share.first + t + 1) * H::kTokens - 1 > w.seen_first && sk.odd()) odd = 1;
         },
         [&](int buffer, int t) {
-          const int key0 = t * H::kTokens + group * BN;
+          const int key0 = (share.first + t) * H::kTokens + group * BN;
           if (key0 > w.seen_any) return;
           const char* lk = lds + 2 * buffer * H::kTile + group * BN * T::kStride;
           const char* lv = lk + H::kTile;
@@ -660,11 +776,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
             }
           }
         });
-    join<C, S>(acc, lds);
-    if (group > 0) return;
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-      store_block<BF>(acc[b], a.scale, a.dq + w.q_token * a.dq_row + w.head * a.dq_head, b0 + b, w.there);
+    finish(acc, b0, share.parts > 1);
   };
   pass(std::false_type{}, 0);
   __syncthreads();
@@ -673,6 +785,14 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
       __syncthreads();
       pass(std::true_type{}, b);
     }
+  if constexpr (kShared) {
+    if (share.parts == 1 || !arrive(a.arrived + at.id, share.parts)) return;
+    f32x16 acc[T::kBlocks] = {};
+    for (int i = group; i < share.parts; i += S)
+#pragma unroll
+      for (int b = 0; b < T::kBlocks; ++b) collect_block(acc[b], results + (i * T::kBlocks + b) * 1024, 1.f, 1.f);
+    finish(acc, 0, false);
+  }
 }
 
 // ---- dk and dv -----------------------------------------------------------------
@@ -698,14 +818,15 @@ struct KeyShape {
 
 template <bool BF, int D, int C, int S>
 __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) void attend_dkv_kernel(const AttendGradArgs a) {
+  constexpr bool kShared = C == 1;
   using T = Tile<BF, D>;
   using H = KeyShape<BF, D, C, S>;
   constexpr int BK = 32 * C, BR = H::kBlock, R = Type<BF>::kRegs;
   __shared__ __attribute__((aligned(16))) char lds[H::kTiles + H::kValueBytes];  // Q and d_o of tiles, V
   __shared__ __attribute__((aligned(16))) float stats[2][2][H::kTokens];         // -lse log2(e) and D of their rows
   __shared__ int odd;  // Q or d_o holds an infinity or NaN in a tile of which some keys are not seen
-  const int g = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int slot = (int)(blockIdx.x / (unsigned)a.kv_heads);
+  const Walker at(a, kShared);
+  const int g = at.g, slot = at.slot;
   const Place p = find_place(a.k_offsets, a.sequences, a.k_tokens, slot, 1, __builtin_ctz(BK));
   const int keys = p.end - p.begin, key0 = p.tile * BK;
   if (p.tile < 0 || key0 >= keys) return;
@@ -720,7 +841,12 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
   const int wfirst = wkey < keys ? first_row(wkey) : INT32_MAX;  // .. any, and all, of the wavefront's
   const int wall = first_row(min(wkey + 31, keys - 1));
   const int all = first_row(min(key0 + BK, keys) - 1);           // .. all of the work-group's
-  const int begin = first_row(key0), tiles = rows > begin ? (rows - begin + H::kTokens - 1) / H::kTokens : 0;
+  const int from = first_row(key0);
+  const Share share(rows > from ? (rows - from + H::kTokens - 1) / H::kTokens : 0,
+                    at.part, kShared ? a.parts : 1, kLeastTiles<BF>);
+  if (at.part >= share.parts) return;
+  const int begin = from + share.first * H::kTokens;
+  float* results = a.part + (int64_t)at.id * a.parts * (2 * 32 * D);  // of the walk: [parts][blocks][2][1024]
   const int64_t k_token = p.begin + (there ? key : key0);
   const char* qbase = a.q + qb * a.q_row + (int64_t)g * a.hpk * a.q_head;
   const char* dobase = a.d_o + qb * a.do_row + (int64_t)g * a.hpk * a.do_head;
@@ -736,6 +862,23 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
   }
   const char* own_values = values + wave % C * 32 * T::kStride;
 
+  const auto finish = [&](auto& dk, auto& dv, int b0, bool to_parts) {
+    constexpr int KB = sizeof(dk) / sizeof(f32x16);
+    join<C, S>(dk, lds);
+    join<C, S>(dv, lds);
+    if (group > 0) return;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      if (kShared && to_parts) {
+        float* to = results + (at.part * T::kBlocks + b0 + b) * 2048;
+        publish_block(to, dk[b]);
+        publish_block(to + 1024, dv[b]);
+      } else {
+        store_block<BF>(dk[b], a.scale, a.dk + k_token * a.dk_row + g * a.dk_head, b0 + b, there);
+        store_block<BF>(dv[b], 1.f, a.dv + k_token * a.dv_row + g * a.dv_head, b0 + b, there);
+      }
+    }
+  };
   const auto pass = [&](auto careful, int b0) {
     constexpr int KB = careful ? 1 : T::kBlocks;
     Stage<BF, D, H::kTokens, H::kThreads> sq, so;
@@ -746,7 +889,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
     float st = 0.f;  // the first wavefronts: one of a row's two values a lane
     f32x16 dk[KB] = {}, dv[KB] = {};
     walk<careful ? 1 : H::kBuffers>(
-        tiles,
+        share.n,
         [&](int t) {
           const int row0 = begin + t * H::kTokens, r = row0 + wave * 32 + (lane & 31);
           sq.load_rows(qbase, a.q_row, a.q_head, row0, rows, a.hpk, a.hpk_inv);
@@ -814,14 +957,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
             }
           }
         });
-    join<C, S>(dk, lds);
-    join<C, S>(dv, lds);
-    if (group > 0) return;
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      store_block<BF>(dk[b], a.scale, a.dk + k_token * a.dk_row + g * a.dk_head, b0 + b, there);
-      store_block<BF>(dv[b], 1.f, a.dv + k_token * a.dv_row + g * a.dv_head, b0 + b, there);
-    }
+    finish(dk, dv, b0, share.parts > 1);
   };
   pass(std::false_type{}, 0);
   __syncthreads();
@@ -830,6 +966,18 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
       __syncthreads();
       pass(std::true_type{}, b);
     }
+  if constexpr (kShared) {
+    if (share.parts == 1 || !arrive(a.arrived + at.id, share.parts)) return;
+    f32x16 dk[T::kBlocks] = {}, dv[T::kBlocks] = {};
+    for (int i = group; i < share.parts; i += S)
+#pragma unroll
+      for (int b = 0; b < T::kBlocks; ++b) {
+        const float* from = results + (i * T::kBlocks + b) * 2048;
+        collect_block(dk[b], from, 1.f, 1.f);
+        collect_block(dv[b], from + 1024, 1.f, 1.f);
+      }
+    finish(dk, dv, 0, false);
+  }
 }
 
 // Slots of the tiles of `tile` rows (per_token rows a token).
@@ -851,22 +999,32 @@ bool fills(int64_t tokens, int per_token, int kv_heads, int tile, int groups) {
   return tokens * per_token / tile * kv_heads >= groups;
 }
 
+// Work-groups that may share a walk: as many as there is room for (two a CU), and as the longest walk there can be has
+// tiles for.
+void share_walks(AttendShape& a, bool shared, int64_t longest, int tile, int least) {
+  const int64_t walks = (int64_t)a.slots * a.kv_heads, most = (longest + tile - 1) / tile / least;
+  a.parts = shared ? (int)std::max<int64_t>(1, std::min({kAttendParts / walks, most, (int64_t)kMostParts})) : 1;
+}
+
 template <bool BF, int D, int C, int S>
 hipError_t attend(AttendArgs& a, hipStream_t stream) {
-  a.q_slots = slots_of(a.q_tokens, a.hpk, a.sequences, C * 32);
-  hipLaunchKernelGGL((attend_kernel<BF, D, C, S>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(64 * C * S), 0, stream, a);
+  a.slots = slots_of(a.q_tokens, a.hpk, a.sequences, C * 32);
+  share_walks(a, C == 1, a.k_tokens, 32 * S, kLeastTiles<BF>);
+  hipLaunchKernelGGL((attend_kernel<BF, D, C, S>), dim3((unsigned)a.slots * a.kv_heads * a.parts), dim3(64 * C * S), 0, stream, a);
   return hipGetLastError();
 }
 template <bool BF, int D, int C, int S>
 hipError_t attend_dq(AttendGradArgs& a, hipStream_t stream) {
-  a.q_slots = slots_of(a.q_tokens, a.hpk, a.sequences, C * 32);
-  hipLaunchKernelGGL((attend_dq_kernel<BF, D, C, S>), dim3((unsigned)a.q_slots * a.kv_heads), dim3(64 * C * S), 0, stream, a);
+  a.slots = slots_of(a.q_tokens, a.hpk, a.sequences, C * 32);
+  share_walks(a, C == 1, a.k_tokens, 32 * S, kLeastTiles<BF>);
+  hipLaunchKernelGGL((attend_dq_kernel<BF, D, C, S>), dim3((unsigned)a.slots * a.kv_heads * a.parts), dim3(64 * C * S), 0, stream, a);
   return hipGetLastError();
 }
 template <bool BF, int D, int C, int S>
 hipError_t attend_dkv(AttendGradArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((attend_dkv_kernel<BF, D, C, S>),
-                     dim3((unsigned)slots_of(a.k_tokens, 1, a.sequences, C * 32) * a.kv_heads), dim3(64 * C * S), 0, stream, a);
+  a.slots = slots_of(a.k_tokens, 1, a.sequences, C * 32);
+  share_walks(a, C == 1, (int64_t)a.q_tokens * a.hpk, 32 * S, kLeastTiles<BF>);
+  hipLaunchKernelGGL((attend_dkv_kernel<BF, D, C, S>), dim3((unsigned)a.slots * a.kv_heads * a.parts), dim3(64 * C * S), 0, stream, a);
   return hipGetLastError();
 }
 

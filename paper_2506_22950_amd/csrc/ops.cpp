@@ -119,7 +119,10 @@ struct infs_attention {
   bool dry = false, bf16 = false;
   hipStream_t stream = nullptr;
   int device = 0;
-  float* delta = nullptr;  // [max_tokens, Hq] (AttendGradArgs)
+  // [max_tokens, Hq] (AttendGradArgs), behind the parts of shared walks and their counters (AttendShape)
+  float* delta = nullptr;
+  float* part = nullptr;
+  int32_t* arrived = nullptr;
 };
 
 namespace {
@@ -166,7 +169,7 @@ infs_status check_attend(const infs_attention* a, int32_t sequences, int64_t q_t
       (*k_tokens / 32 + sequences) * a->cfg.num_kv_heads > infs::kAttendMostBlocks)
     return op_fail(INFS_E_ARG, "more than 2^22 work-groups");
   *s = {q_offsets, *k_offsets, sequences, (int32_t)q_tokens, (int32_t)*k_tokens, a->cfg.num_q_heads, a->cfg.num_kv_heads, hpk,
-        (uint32_t)(((uint64_t(1) << 32) + hpk - 1) / hpk), a->cfg.scale};
+        (uint32_t)(((uint64_t(1) << 32) + hpk - 1) / hpk), a->cfg.scale, a->part, a->arrived, 1, 0};
   return INFS_OK;
 }
 
@@ -382,8 +385,18 @@ infs_status infs_attention_create(const infs_attention_config* cfg, void* hip_st
     infs::StreamDevice dev(a->stream);
     hipError_t e = dev.status();
     if (e == hipSuccess) e = hipGetDevice(&a->device);
-    if (e == hipSuccess) e = hipMalloc((void**)&a->delta, sizeof(float) * k.max_tokens * k.num_q_heads);
+    const size_t counters = sizeof(int32_t) * infs::kAttendParts,
+                 parts = sizeof(float) * infs::kAttendParts * infs::kAttendPartFloats * k.head_dim,
+                 delta = sizeof(float) * k.max_tokens * k.num_q_heads;
+    char* all = nullptr;
+    if (e == hipSuccess) e = hipMalloc((void**)&all, counters + parts + delta);
+    if (e == hipSuccess) {
+      a->arrived = (int32_t*)all, a->part = (float*)(all + counters), a->delta = (float*)(all + counters + parts);
+      e = hipMemset(a->arrived, 0, counters);
+      if (e == hipSuccess) e = hipStreamSynchronize(nullptr);  // the stream need not wait for the null stream
+    }
     if (e != hipSuccess) {
+      if (all) (void)hipFree(all);
       delete a;
       return op_fail(e == hipErrorOutOfMemory ? INFS_E_NOMEM : INFS_E_DEVICE, "an attention's workspace: %s",
                      hipGetErrorString(e));
@@ -398,7 +411,7 @@ void infs_attention_destroy(infs_attention* a) {
   if (!a->dry) {
     infs::StreamDevice dev(a->stream, a->device);
     (void)hipStreamSynchronize(a->stream);
-    (void)hipFree(a->delta);
+    (void)hipFree(a->arrived);
   }
   delete a;
 }

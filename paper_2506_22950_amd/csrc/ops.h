@@ -309,14 +309,20 @@ struct AttendShape {
   int32_t sequences, q_tokens, k_tokens, q_heads, kv_heads, hpk;
   uint32_t hpk_inv;                      // 2^32 / hpk, rounded up
   float scale;
+  // Walks that several work-groups share: their parts' results, and how many have come (zero between launches).
+  float* part;
+  int32_t* arrived;
+  int32_t parts, slots;  // launch_attend, launch_attend_grad
 };
+constexpr int kAttendParts = 512;                  // work-groups of a launch with shared walks
+constexpr int kAttendPartFloats = 2 * 32;  // of an element of the head: two results (or one with a maximum and a sum)
+                                           // of 32 rows
 
 struct AttendArgs : AttendShape {
   const char *q, *k, *v;
   char* o;
   float* lse;  // [q_tokens, q_heads], or null
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;  // bytes
-  int32_t q_slots;  // launch_attend
 };
 
 struct AttendGradArgs : AttendShape {
@@ -326,7 +332,6 @@ struct AttendGradArgs : AttendShape {
   float* delta;  // [q_tokens, q_heads]: d_o.o of every row
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, do_row, do_head, dq_row, dq_head, dk_row, dk_head,
       dv_row, dv_head;           // bytes
-  int32_t q_slots;               // launch_attend_grad
 };
 
 hipError_t launch_attend(AttendArgs& args, bool bf16, int head_dim, hipStream_t stream);

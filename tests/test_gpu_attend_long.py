@@ -1,0 +1,123 @@
+"""GPU: attention whose walks over keys (or, for their gradients, over rows) several work-groups share: few rows over
+many keys, and their gradients.  The bounds are those of tests/test_gpu_attend.py (sums of n terms: the joins add no
+terms, and a rescaling of a part is one rounding more, within them)."""
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_attend import Case, starts
+from tests.test_gpu_attend import test_against_formulas as against_formulas
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    (2, 1, 128, True, [1], [20001]),                       # one token, as many parts as there are
+    (2, 2, 64, True, [1], [70000]),
+    (4, 2, 64, False, [1, 3], [9000, 513]),                # walks of different lengths, some of one part
+    (8, 1, 128, False, [1], [5000]),
+    (16, 8, 128, True, [1] * 8, [4000, 5000, 1, 3000, 512, 513, 7001, 300]),
+    (4, 2, 64, True, [700], None),                         # causal: rows of a tile see parts, or nothing of them
+    (2, 1, 128, True, [900, 0, 40], [900, 700, 1300]),
+    (6, 2, 64, False, [129, 300, 1, 77], None),
+    (4, 1, 128, False, [600], None),
+    (32, 1, 128, True, [150], None),                       # many rows for few keys: the keys' gradients are shared
+    (4, 2, 64, True, [1000], [300]),                       # rows that see no key, ahead of those that do
+    (2, 1, 64, False, [3], [9000]),
+]
+
+
+@pytest.mark.parametrize("hq,hkv,d,bf16,q_lens,k_lens", CASES)
+def test_shared_walks_against_formulas(hq, hkv, d, bf16, q_lens, k_lens):
+    against_formulas(hq, hkv, d, bf16, q_lens, k_lens, {})
+
+
+@pytest.mark.parametrize("bf16,d", [(True, 64), (True, 128), (False, 64), (False, 128)])
+def test_unseen_infinities_and_nans_in_parts(bf16, d):
+    """A late token's NaN and infinities change nothing that does not see it, in whichever part of a walk they are."""
+    import torch
+
+    n, bad = 1500, 1131
+    c = Case(4, 2, d, bf16, [n], tail=5)
+    a = c.attention()
+    clean_o, clean_lse = c.outputs()
+    c.attend(a, clean_o, clean_lse)
+    clean = c.grads()
+    c.grad(a, clean, clean_o, clean_lse)
+    for which in ("v", "k", "q", "d_o"):
+        x = getattr(c, which)
+        kept = x.clone()
+        x[bad, 0, 3], x[bad, 0, 9], x[bad + 1, 0, 20] = float("nan"), float("inf"), -float("inf")
+        o, lse = c.outputs()
+        c.attend(a, o, lse)
+        out = c.grads()
+        c.grad(a, out, clean_o, clean_lse)
+        torch.cuda.synchronize()
+        group = [2, 3]  # heads that it does not reach at all
+        assert torch.equal(o[:, group], clean_o[:, group]) and torch.equal(lse[:, group], clean_lse[:, group])
+        assert torch.equal(o[:bad], clean_o[:bad]) and torch.equal(lse[:bad], clean_lse[:bad])
+        dq, dk, dv = out
+        assert torch.equal(dq[:, group], clean[0][:, group])
+        assert torch.equal(dk[:, 1], clean[1][:, 1]) and torch.equal(dv[:, 1], clean[2][:, 1])
+        assert torch.equal(dq[:bad], clean[0][:bad])
+        if which in ("q", "d_o"):  # the keys behind it do not see it
+            assert torch.equal(dk[bad + 2:], clean[1][bad + 2:]) and torch.equal(dv[bad + 2:], clean[2][bad + 2:])
+            assert torch.equal(o[bad + 2:], clean_o[bad + 2:]) and torch.equal(dq[bad + 2:], clean[0][bad + 2:])
+        if which == "v":
+            assert bool(torch.isnan(o[bad:n, :2, 3]).all()) and not bool(torch.isnan(o[bad:n, :2, 4:9]).any())
+            assert bool((o[bad:n, :2, 9] == float("inf")).all()) and bool((o[bad + 1:n, :2, 20] == -float("inf")).all())
+        x.copy_(kept)
+
+
+def test_graph_of_shared_walks():
+    """Captured and replayed with other offsets, walks of other lengths: the counters are left as they were."""
+    import torch
+
+    c = Case(4, 2, 128, True, [300, 2, 5], [1500, 4000, 900], tail=0)
+    side = torch.cuda.Stream()
+    a, b = c.attention(side), c.attention()
+    o, lse = c.outputs()
+    out = c.grads()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        c.attend(a, o, lse)
+        c.grad(a, out, o, lse)
+    for i, (q_lens, k_lens) in enumerate((([300, 2, 5], [1500, 4000, 900]), ([1, 305, 1], [6000, 399, 1]),
+                                          ([0, 1, 306], [0, 6100, 300]), ([300, 2, 5], [1500, 4000, 900]))):
+        gen = torch.Generator().manual_seed(80 + i)
+        for x in (c.q, c.k, c.v, c.d_o):
+            x.copy_(torch.randn(x.shape, generator=gen).to(x.dtype))
+        c.q_off.copy_(torch.tensor(starts(q_lens), dtype=torch.int32))
+        c.k_off.copy_(torch.tensor(starts(k_lens), dtype=torch.int32))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        eo, el = c.outputs()
+        c.attend(b, eo, el)
+        eg = c.grads()
+        c.grad(b, eg, eo, el)
+        torch.cuda.synchronize()
+        assert torch.equal(o[:sum(q_lens)], eo[:sum(q_lens)]) and torch.equal(lse[:sum(q_lens)], el[:sum(q_lens)])
+        for x, y, n in zip(out, eg, (sum(q_lens), sum(k_lens), sum(k_lens))):
+            assert torch.equal(x[:n], y[:n])
+
+
+def test_two_attentions_at_once():
+    """Shared walks of two attentions on two streams: each has counters and parts of its own."""
+    import torch
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    cs = [Case(8, 2, 64, True, [1, 200], [8000, 3000], seed=3 + i) for i in range(2)]
+    at = [c.attention(s) for c, s in zip(cs, streams)]
+    outs = [[(*c.outputs(), c.grads()) for _ in range(12)] for c in cs]
+    torch.cuda.synchronize()
+    for i in range(12):
+        for c, a, o in zip(cs, at, outs):
+            c.attend(a, o[i][0], o[i][1])
+            c.grad(a, o[i][2], o[i][0], o[i][1])
+    torch.cuda.synchronize()
+    for o in outs:
+        for x in o[1:]:
+            assert torch.equal(x[0], o[0][0]) and torch.equal(x[1], o[0][1])
+            assert all(torch.equal(p, q) for p, q in zip(x[2], o[0][2]))
+    assert np.isfinite(outs[0][0][0].double().cpu().numpy()).all()
