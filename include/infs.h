@@ -593,9 +593,10 @@ typedef struct infs_attention_config {
     uint32_t flags;        /* INFS_FLAG_DRY_RUN: arguments are checked, nothing is allocated or launched */
 } infs_attention_config;
 
-/* An attention: its stream and a workspace on the current device (of hip_stream where given).  Calls on one
-   attention are ordered by its stream; captured graphs that hold its calls must not run at the same time as other
-   work of the same attention.  Messages: infs_last_error(NULL).  One host thread at a time. */
+/* An attention: its stream and a workspace on the current device (of hip_stream where given), of 4 max_tokens Hq + 2^17
+   head_dim bytes and a little.  Calls on one attention are ordered by its stream; captured graphs that hold its calls
+   must not run at the same time as other work of the same attention.  Messages: infs_last_error(NULL).  One host
+   thread at a time. */
 typedef struct infs_attention infs_attention;
 infs_status infs_attention_create(const infs_attention_config* cfg, void* hip_stream, infs_attention** out);
 /* Waits for the attention's stream first.  NULL is a no-op. */
@@ -718,8 +719,9 @@ void infs_sampler_destroy(infs_sampler* s);
                          not in [0, 1) and where each_dev[i] is not allowed
      logprob_dev [rows]  log of its weight's share of the kept weights, or NULL (NaN for token -1)
      kept_dev [rows]     how many entries are kept, int32, or NULL (0 for token -1)
-   Weights are held in 64 bits as whole multiples of 2^-(62 - log2 vocab) of the largest (2^-50 at finest), so that
-   their sums are exact whatever the order. */
+   Weights are formed and added up in 64 bits: as whole multiples of 2^-(62 - log2 vocab) of the largest (2^-50 at
+   finest), so that their sums are exact whatever the order, or, where nothing is left out, as doubles in an order that
+   sizes, strides and alignment fix.  The same call gives the same tokens. */
 infs_status infs_choose_tokens(infs_sampler* s, int32_t rows, const void* logits_dev, int64_t row_stride,
                                const float* uniform_dev, const infs_sampling* all, const infs_sampling* each_dev,
                                int32_t* token_dev, float* logprob_dev, int32_t* kept_dev);
