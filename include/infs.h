@@ -588,7 +588,7 @@ typedef struct infs_attention_config {
     int32_t num_kv_heads;  /* Hkv */
     int32_t head_dim;      /* 64 or 128 */
     int32_t dtype;         /* infs_dtype of all rows */
-    float scale;           /* finite, > 0; 0: 1/sqrt(head_dim) */
+    float scale;           /* in [2^-64, 2^64]; 0: 1/sqrt(head_dim) */
     int32_t max_tokens;    /* packed query rows of one call, >= 1; max_tokens * Hq / Hkv below 2^31 */
     uint32_t flags;        /* INFS_FLAG_DRY_RUN: arguments are checked, nothing is allocated or launched */
 } infs_attention_config;

@@ -370,7 +370,8 @@ infs_status infs_attention_create(const infs_attention_config* cfg, void* hip_st
     return op_fail(INFS_E_ARG, "num_q_heads must be a multiple of num_kv_heads, up to 4096");
   if (k.head_dim != 64 && k.head_dim != 128) return op_fail(INFS_E_ARG, "head_dim must be 64 or 128");
   if (k.dtype != INFS_F32 && k.dtype != INFS_BF16) return op_fail(INFS_E_ARG, "dtype must be INFS_F32 or INFS_BF16");
-  if (!(k.scale >= 0.f) || !std::isfinite(k.scale)) return op_fail(INFS_E_ARG, "scale must be finite and > 0, or 0");
+  if (k.scale != 0.f && !(k.scale >= 0x1p-64f && k.scale <= 0x1p64f))
+    return op_fail(INFS_E_ARG, "scale must be in [2^-64, 2^64], or 0");
   if (k.max_tokens < 1 || (int64_t)k.max_tokens * (k.num_q_heads / k.num_kv_heads) > INT32_MAX)
     return op_fail(INFS_E_ARG, "max_tokens must be at least 1, times Hq / Hkv below 2^31");
   if (k.flags & ~INFS_FLAG_DRY_RUN) return op_fail(INFS_E_ARG, "unknown flags");

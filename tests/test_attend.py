@@ -79,3 +79,15 @@ def test_null_attention():
     assert lib.infs_attend(None, 0, 0, None, 0, None, None, None, None, None) == infs.E_ARG
     assert lib.infs_attend_grad(None, 0, 0, None, 0, None, None, None, None, None, None, None) == infs.E_ARG
     lib.infs_attention_destroy(None)
+
+
+@pytest.mark.parametrize("scale,ok", [(2.0 ** -64, True), (2.0 ** 64, True), (1e-38, False), (2.0 ** -65, False),
+                                      (2.0 ** 65, False), (3e38, False)])
+def test_range_of_the_scale(scale, ok):
+    c = infs.make_attention_config(num_q_heads=4, num_kv_heads=2, head_dim=64, dtype=infs.BF16, scale=scale, max_tokens=9,
+                                   flags=infs.FLAG_DRY_RUN)
+    if ok:
+        infs.Attention(c).destroy()
+    else:
+        with pytest.raises(infs.InfsError, match="scale"):
+            infs.Attention(c)

@@ -121,3 +121,35 @@ def test_two_attentions_at_once():
             assert torch.equal(x[0], o[0][0]) and torch.equal(x[1], o[0][1])
             assert all(torch.equal(p, q) for p, q in zip(x[2], o[0][2]))
     assert np.isfinite(outs[0][0][0].double().cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("q_lens,k_lens", [([70, 9], [70, 9]), ([3], [2000]), ([700], [700])])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [20, 40, 60])
+def test_scores_far_out(power, d, q_lens, k_lens):
+    """Keys that are 0 but for one element, which counts down from 2^power to 2^power / 2: exact scores, of which each is so far
+    below the one before that a row takes its first key's value alone, and lse is that score (to fp32's rounding of a
+    product with the scale).  Equal scores share.  The gradients are finite."""
+    import torch
+
+    c = Case(2, 1, d, False, q_lens, k_lens, scale=1.0, tail=0)
+    m = sum(k_lens)
+    c.q.zero_(), c.k.zero_()
+    c.q[:, :, 5] = 2.0 ** (power - 20)
+    c.k[:, 0, 5] = 2.0 ** 20 - torch.arange(m, device="cuda").float() // 2 * 256  # two of each
+    a = c.attention()
+    o, lse = c.outputs()
+    c.attend(a, o, lse)
+    out = c.grads()
+    c.grad(a, out, o, lse)
+    torch.cuda.synchronize()
+    ks, qs = starts(k_lens), starts(q_lens)
+    for i, (n, mm) in enumerate(zip(q_lens, k_lens)):
+        first = c.k[ks[i], 0, 5].double().item() * 2.0 ** (power - 20)
+        pair = 2 if mm > 1 and c.k[ks[i], 0, 5] == c.k[ks[i] + 1, 0, 5] else 1
+        for t in range(n):
+            some = min(pair, t + mm - n + 1)
+            want = c.v[ks[i]:ks[i] + some, 0].double().mean(0)
+            assert (o[qs[i] + t].double() - want).abs().max() <= 2.0 ** -20 * 8, (i, t)
+            assert abs(lse[qs[i] + t].double() - first).max() <= abs(first) * 2.0 ** -23 + 1, (i, t)
+    assert all(bool(torch.isfinite(x).all()) for x in out)
