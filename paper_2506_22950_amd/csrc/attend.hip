@@ -57,8 +57,7 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;
 // Scores this far out (in powers of 2) are taken off the row's base before they are scaled, since the rounding of the
-// scaled base, 2^-24 of it, is on its way to be a power by itself.  The gradient, which has the fp32 lse alone, takes
-// p for 1 where it comes out larger.
+// scaled base, 2^-24 of it, is on its way to be a power by itself.
 constexpr float kFar = 0x1p20f;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -698,6 +697,13 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_kernel(
   }
 }
 
+// -lse in powers of 2.  Where its roundings (lse's own, the product's, that of the scale) may come to powers that leave
+// fp32, lower by twice their bound, so that no p is above 1.
+__device__ __forceinline__ float base_of(float lse) {
+  const float off = -lse * kLog2e, size = fminf(fabsf(off), 3e38f);
+  return size > 0x1p26f ? off - size * 0x1p-21f : off;
+}
+
 // ---- dq (and D) ----------------------------------------------------------------
 // The walk of the forward kernel with the scores' exponentials from lse: s^T and (v up)^T of a tile, ds^T from
 // them, dq^T += K^T ds^T.  D = up.o of every row is left in a.delta for the kernel of dk and dv.
@@ -722,7 +728,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
   const char* kbase = a.k + w.kb * a.k_row + g * a.k_head;
   const char* vbase = a.v + w.kb * a.v_row + g * a.v_head;
   const int64_t row = w.q_token * a.q_heads + w.head;
-  const float c = a.scale * kLog2e, off = w.there ? -a.lse[row] * kLog2e : 0.f;
+  const float c = a.scale * kLog2e, off = w.there ? base_of(a.lse[row]) : 0.f;
   const T tile;
   if (threadIdx.x == 0) odd = 0;
 
@@ -779,13 +785,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
               ds = Type<BF>::mma(ds, tile.rows(lv, 32 * n, e), up[e]);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], c, off);
-            if (__any(fabsf(off) > kFar)) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) s[i] = fabsf(off) > kFar && s[i] > 0.f ? 0.f : s[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) ds[i] = exp2_(s[i]) * (ds[i] - delta);
+            for (int i = 0; i < 16; ++i) ds[i] = exp2_(fmaf(s[i], c, off)) * (ds[i] - delta);
             if (masked) {
 #pragma unroll
               for (int i = 0; i < 16; ++i) ds[i] = key0 + 32 * n + token_of(i, half) <= w.last ? ds[i] : 0.f;
@@ -856,7 +856,6 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
   __shared__ __attribute__((aligned(16))) char lds[H::kTiles + H::kValueBytes];  // Q and d_o of tiles, V
   __shared__ __attribute__((aligned(16))) float stats[2][2][H::kTokens];         // -lse log2(e) and D of their rows
   __shared__ int odd;  // Q or d_o holds an infinity or NaN in a tile of which some keys are not seen
-  __shared__ int far;  // some row's lse is beyond kFar
   const Walker at(a, kShared);
   const int g = at.g, slot = at.slot;
   const Place p = find_place(a.k_offsets, a.sequences, a.k_tokens, slot, 1, __builtin_ctz(BK));
@@ -884,7 +883,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
   const char* dobase = a.d_o + qb * a.do_row + (int64_t)g * a.hpk * a.do_head;
   const float c = a.scale * kLog2e;
   const T tile;
-  if (threadIdx.x == 0) odd = far = 0;
+  if (threadIdx.x == 0) odd = 0;
   char* values = lds + H::kTiles;
   if constexpr (H::kValues) {
     Stage<BF, D, BK, H::kThreads> sv;
@@ -935,10 +934,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
         [&](int buffer, int t) {
           sq.store(lds + 2 * buffer * H::kTile);
           so.store(lds + (2 * buffer + 1) * H::kTile);
-          if (wave < H::kTokens / 32) {
-            stats[buffer][half][wave * 32 + (lane & 31)] = half ? st : -st * kLog2e;
-            if (!half && fabsf(st) * kLog2e > kFar) far = 1;
-          }
+          if (wave < H::kTokens / 32) stats[buffer][half][wave * 32 + (lane & 31)] = half ? st : base_of(st);
           if (!careful && begin + t * H::kTokens < all && (sq.odd() || so.odd())) odd = 1;
         },
         [&](int buffer, int t) {
@@ -960,17 +956,11 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
               const f32x4 off = *(const f32x4*)&stats[buffer][0][group * BR + n + token_of(i, half)];
               const f32x4 delta = *(const f32x4*)&stats[buffer][1][group * BR + n + token_of(i, half)];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) s[i + j] = fmaf(s[i + j], c, off[j]), ds[i + j] -= delta[j];
-            }
-            if (far) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const float off = stats[buffer][0][group * BR + n + token_of(i, half)];
-                s[i] = fabsf(off) > kFar && s[i] > 0.f ? 0.f : s[i];
+              for (int j = 0; j < 4; ++j) {
+                s[i + j] = exp2_(fmaf(s[i + j], c, off[j]));
+                ds[i + j] = s[i + j] * (ds[i + j] - delta[j]);
               }
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = exp2_(s[i]), ds[i] *= s[i];
             if (masked) {
 #pragma unroll
               for (int i = 0; i < 16; ++i) {

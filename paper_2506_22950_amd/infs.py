@@ -369,7 +369,8 @@ class Attention:
         self.config = config
 
     def attend(self, sequences, q_tokens, q_offsets, q, k, v, lse=None, k_tokens=None, k_offsets=None):
-        """infs_attend; q (queries, and where their outputs go), k and v are rotary_rows(...)."""
+        """infs_attend; q (queries, and where their outputs go), k and v are rotary_rows(...);
+        k_tokens: q_tokens where not given."""
         st = _lib.infs_attend(self._h, sequences, q_tokens, _ptr(q_offsets), q_tokens if k_tokens is None else k_tokens,
                               _ptr(k_offsets), q, k, v, _ptr(lse))
         if st != OK:
