@@ -1390,7 +1390,7 @@ hipError_t launch_choose(ChooseArgs& a, bool bf16, hipStream_t stream) {
   // 17 in one of 30)
   for (; top && (int64_t)p.top_k * a.pieces > kList / 2; a.pieces = choose_pieces(a.vocab, a.batches, bf16)) {
     if (a.batches < kPieceVectors)
-      a.batches *= 2;
+      ++a.batches;
     else
       top = false;
   }

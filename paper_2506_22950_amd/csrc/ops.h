@@ -241,7 +241,7 @@ constexpr int kList = 4096;                  // entries of a row that are ranked
 constexpr int kListCount = 1024;             // a top_k whose entries are all listed
 constexpr int kChooseRecords = 8192;         // pieces, and ..
 constexpr int kChooseRows = 2048;            // .. rows, of a launch
-constexpr int kChooseFill = 256;             // pieces that fill the GPU
+constexpr int kChooseFill = 512;             // pieces that fill the GPU, two a CU
 constexpr int kChoosePieces = 2048;          // most of a row
 
 enum RowMode { kDone, kListed, kSums, kLeft };  // what the launch that weighs a row leaves to do
@@ -280,17 +280,20 @@ struct ChooseArgs {
   uint32_t* bins;            // [pieces][kBins]: numbers, or sums of weights
 };
 
-// Vectors a thread (few rows: fewer, so that the pieces fill the GPU), pieces of a row, rows of a launch.
-inline int choose_pieces(int vocab, int batches, bool bf16) {
+// Vectors a thread, pieces of a row, rows of a launch.  Pieces are as small as two a CU allow for all rows together, and
+// no larger than the registers hold (top-p of 101 rows of 50257 in fp32: 53 us in 404 pieces, of which some CUs had two
+// of the largest, 42 in 505 smaller ones, 60 in 909; 64 rows of 151936 in bf16: 74, 59, 73 in 320, 512, 960).
+inline int choose_vectors(int vocab, bool bf16) {  // of a row, at any alignment
   const int n = 16 / (bf16 ? 2 : 4);
-  return ((vocab + 2 * n - 2) / n + batches * kPieceThreads - 1) / (batches * kPieceThreads);  // at any alignment
+  return (vocab + 2 * n - 2) / n;
+}
+inline int choose_pieces(int vocab, int batches, bool bf16) {
+  return (choose_vectors(vocab, bf16) + batches * kPieceThreads - 1) / (batches * kPieceThreads);
 }
 inline int choose_batches(int rows, int vocab, bool bf16) {
-  int b = kPieceVectors;
-  while (b > 1 && (int64_t)rows * choose_pieces(vocab, b, bf16) < kChooseFill &&
-         choose_pieces(vocab, b / 2, bf16) <= kChoosePieces)
-    b /= 2;
-  return b;
+  const int64_t least = choose_pieces(vocab, kPieceVectors, bf16), fill = kChooseFill / (rows < 1 ? 1 : rows);
+  const int64_t pieces = fill < least ? least : fill;
+  return (int)((choose_vectors(vocab, bf16) + pieces * kPieceThreads - 1) / (pieces * kPieceThreads));
 }
 inline int choose_rows(int pieces) {
   const int n = kChooseRecords / pieces;
