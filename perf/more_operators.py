@@ -263,6 +263,9 @@ def _prepare_norm(st, seed):
             st.dw = torch.empty(2, case["head_dim"], device="cuda")
             st.workspace = torch.empty(infs.norm_rotate_grad_workspace(case["tokens"], case["head_dim"]),
                                        dtype=torch.uint8, device="cuda")
+        elif case["entry"] == "step" and case["q_heads"] // case["kv_heads"] not in (1, 2, 4, 8):
+            # heads that no context decodes: their rows, layer by layer
+            st.ctx, st.positions = None, torch.tensor(_positions(case), dtype=torch.int32, device="cuda")
         elif case["entry"] == "step":
             # a context whose slots hold responses of the positions' lengths
             n, cap, first = case["tokens"], 1024, case["first"]
@@ -346,9 +349,16 @@ def _rows(x, out=None):
 
 
 def _own_norm(st):
+    from paper_2506_22950_amd import infs
+
     case = st.case
     q, k = _rows(st.q, st.q_out), _rows(st.k, st.k_out)
-    if case["entry"] == "step":
+    if case["entry"] == "step" and st.ctx is None:
+        for i in range(case["layers"]):
+            st.rotary.norm_rotate_rows(_own_type(case["dtype"]), case["tokens"], infs.layer_norms(st.norms, i),
+                                       _rows(st.q[i], st.q_out[i]), _rows(st.k[i], st.k_out[i]), positions=st.positions,
+                                       stream=torch.cuda.current_stream())
+    elif case["entry"] == "step":
         st.ctx.norm_rotate_step(st.rotary, st.norms, q, k, num_layers=case["layers"])
     else:
         st.rotary.norm_rotate_rows(_own_type(case["dtype"]), case["tokens"], st.norms, q, k, first_position=case["first"],
