@@ -1021,14 +1021,18 @@ int slots_of(int64_t tokens, int per_token, int sequences, int tile) { return (i
 //   bf16 dq   4 x 256: 22 16 19    1 x 2048: 90 55 83    4 x 1024: 122 75 54    64 x 128: 140 87 60
 //   fp32 o    4 x 256: 38 29 65    1 x 2048: 228 190 505    4 x 1024: 269 205 259    4 x 4096: 3376 2756 2273
 // so bf16 takes 64 and 256 rows as soon as they fill the GPU once.  fp32 products take eight times as long and are
-// never waited for, so a GPU that is filled evenly to the end is worth more: 2 and 4 work-groups a CU.
+// never waited for, so a GPU that is filled evenly to the end is worth more: 4 work-groups of 256 a CU, and of 64 two
+// where walks are long (1 x 1024: 68 89; 300 to 800 tokens, 8 heads on 2: 57 73), one where they are short (20 sequences of
+// 1 to 381 tokens: 69 55).
 // dk and dv (32, 64 and 128 keys):
 //   bf16      4 x 512: 47 33 57    4 x 1024: 119 93 113    8 x 2048: 757 493 461    64 x 128: 99 62 53
 //   fp32      4 x 512: 147 151 292    4 x 1024: 391 465 571    4 x 2048: 1417 1272 1814    64 x 128: 208 176 325
-constexpr int kCus = 256;
+constexpr int kCus = 256, kShortWalk = 384;  // kShortWalk: keys of a sequence, on average
 bool fills(int64_t tokens, int per_token, int kv_heads, int tile, int groups) {
   return tokens * per_token / tile * kv_heads >= groups;
 }
+
+bool short_walks(const AttendShape& a) { return a.k_tokens / a.sequences <= kShortWalk; }
 
 // Work-groups that may share a walk: as many as there is room for (two a CU), and as the longest walk there can be has
 // tiles for.
@@ -1066,7 +1070,8 @@ template <bool BF, int D>
 hipError_t attend(AttendArgs& a, hipStream_t stream) {
   constexpr bool kLarge = !BF && D == 128;  // rows of 512 bytes
   if (fills(a.q_tokens, a.hpk, a.kv_heads, 256, kCus * (BF ? 1 : 4))) return attend<BF, D, 8, 1>(a, stream);
-  if (fills(a.q_tokens, a.hpk, a.kv_heads, 64, kCus * (BF ? 1 : 2))) return attend<BF, D, 2, kLarge ? 2 : 4>(a, stream);
+  if (fills(a.q_tokens, a.hpk, a.kv_heads, 64, kCus * (BF || short_walks(a) ? 1 : 2)))
+    return attend<BF, D, 2, kLarge ? 2 : 4>(a, stream);
   return attend<BF, D, 1, kLarge ? 4 : 8>(a, stream);
 }
 
@@ -1074,7 +1079,7 @@ template <bool BF, int D>
 hipError_t attend_dq(AttendGradArgs& a, hipStream_t stream) {
   constexpr bool kLarge = !BF && D == 128;
   if (fills(a.q_tokens, a.hpk, a.kv_heads, 256, kCus * (BF ? 1 : 4))) return attend_dq<BF, D, 8, 1>(a, stream);
-  if (fills(a.q_tokens, a.hpk, a.kv_heads, 64, kCus * (BF ? 1 : 2)))
+  if (fills(a.q_tokens, a.hpk, a.kv_heads, 64, kCus * (BF || short_walks(a) ? 1 : 2)))
     return attend_dq<BF, D, 2, kLarge ? 2 : 4>(a, stream);
   return attend_dq<BF, D, 1, D == 128 ? 4 : 8>(a, stream);
 }

@@ -196,6 +196,8 @@ CASES = [
     (128, 128, 128, False, [129, 1, 170], [129, 7, 300], {}),
     (256, 256, 64, False, [130, 200], None, {}),
     (256, 256, 128, False, [130, 200], None, {}),
+    (64, 64, 64, False, [150, 1, 111], None, {}),                       # fp32: with short walks
+    (64, 64, 128, False, [150, 1, 111], [150, 30, 300], {}),
     # fp32: .. and for the largest
     (1024, 1024, 64, False, [256], None, {}),
     (1024, 512, 128, False, [250, 6], None, {}),
