@@ -516,7 +516,8 @@ struct Rows {
 // ---- o and lse -----------------------------------------------------------------
 // Bound by the chain of a tile: first product, maximum, exponentials, second product, each of which waits for the one
 // before, with two wavefronts a SIMD to fill in (256 registers each).  Four packed prompts of 256 to 4096 tokens, 32
-// heads of 128 on 8 KV heads: 203 us, 890 TFLOP/s, where a large matrix product of the same type reaches 1290.
+// heads of 128 on 8 KV heads: 203 to 221 us (one card and another), 820 to 890 TFLOP/s, where a large matrix product of
+// the same type reaches 1290.
 // Leaving out loads, exponentials or either product gained a tenth each; wavefronts half a tile apart (three buffers),
 // operands asked for a whole product ahead, and two work-groups of 128 rows a CU gained nothing.
 template <bool BF, int D, int C, int S>

@@ -647,9 +647,9 @@ __device__ __forceinline__ uint32_t bin_mass(float f) {
 }
 static_assert(kPieceThreads * kPieceVectors * 8 * 66974ull < (1ull << 32), "a bin's sum");
 
-// The weighing launch.  101 rows of 50257 in fp32, top-p and min-p: 27 us, of which 3.5 until the piece is there, 7.5
-// for the weights (a degree-8 polynomial in double each, at half rate) and the bins, 6 for the join; the rest is the
-// launch and rows that end later.
+// The weighing launch.  101 rows of 50257 in fp32, top-p and min-p: 21 us, of which 2.5 until the piece is there, 5 for the
+// weights (a degree-8 polynomial in double each) and the bins, 6.5 for the join; the rest is the launch and what CUs with two
+// pieces take longer.
 template <bool BF>
 __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArgs a) {
   constexpr int N = RowOf<BF>::N, V = Piece<BF>::V, W = kPieceWaves;
@@ -913,8 +913,8 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
   if (threadIdx.x == 0) state = RowState{m, lo_bin, hi_bin, mode, live, 0, whole};
 }
 
-// The gathering launch: 27 us for the same rows, 10 of them for the piece (loaded again, the weights above the list), 1
-// for its list, 8 for the join.
+// The gathering launch: 21 us for the same rows, 7 of them for the piece (loaded again, its list, the weights above it) and
+// 7 for the join.
 template <bool BF>
 __global__ __launch_bounds__(kPieceThreads, 4) void gather_kernel(const ChooseArgs a) {
   constexpr int N = RowOf<BF>::N, V = Piece<BF>::V, W = kPieceWaves;
