@@ -173,6 +173,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_kernel(const NormArg
   int t;
   bool k;
   bool there = place(first, in, out, t, k);
+  if (!there) t = 0;  // angles of a token that is there
   float x[H::M], y[H::M];
   head.load(in, there, x);
   for (int e = threadIdx.x; e < 2 * INFS_ROTARY_MAX_DIM; e += blockDim.x) {
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotate_kernel(const NormArg
     i += step;
     if (i - first >= total) break;  // the same for all threads
     there = place(i, in, out, t, k);
-    if (!there) t = 0;  // angles of a token that is there
+    if (!there) t = 0;
     head.load(in, there, x);
   }
 }
