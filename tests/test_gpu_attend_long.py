@@ -153,3 +153,50 @@ def test_scores_far_out(power, d, q_lens, k_lens):
             assert (o[qs[i] + t].double() - want).abs().max() <= 2.0 ** -20 * 8, (i, t)
             assert abs(lse[qs[i] + t].double() - first).max() <= abs(first) * 2.0 ** -23 + 1, (i, t)
     assert all(bool(torch.isfinite(x).all()) for x in out)
+
+
+@pytest.mark.parametrize("q_len", [1, 700])
+def test_offsets_beyond_32_bits(q_len):
+    """A sequence whose rows begin 4.3 GB into K, V and their gradients: what the same rows give in small buffers."""
+    import torch
+
+    from paper_2506_22950_amd import infs
+
+    h, d, m, n = 16, 128, 700, (1 << 20) + 4000
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    q, d_o = (torch.randn(q_len, h, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    k, v, dk, dv = (torch.empty(n, h, d, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    for x in (k, v):
+        x[n - m:] = torch.randn(m, h, d, generator=gen, device="cuda").bfloat16()
+    a = infs.Attention(infs.make_attention_config(num_q_heads=h, num_kv_heads=h, head_dim=d, dtype=infs.BF16, max_tokens=q_len),
+                       stream=torch.cuda.current_stream())
+
+    def rows(x, out=None):
+        return infs.rotary_rows(x, out, h)
+
+    q_off, got = torch.tensor([0, q_len], dtype=torch.int32, device="cuda"), []
+    for ks, vs, dks, dvs, total in ((k, v, dk, dv, n), (k[n - m:], v[n - m:], torch.empty_like(k[:m]), torch.empty_like(k[:m]), m)):
+        k_off = torch.tensor([total - m, total], dtype=torch.int32, device="cuda")
+        o, lse, dq = torch.empty_like(q), torch.empty(q_len, h, device="cuda"), torch.empty_like(q)
+        a.attend(1, q_len, q_off, rows(q, o), rows(ks), rows(vs), lse, k_tokens=total, k_offsets=k_off)
+        a.grad(1, q_len, q_off, rows(q, dq), rows(ks, dks), rows(vs, dvs), rows(o), rows(d_o), lse, k_tokens=total,
+               k_offsets=k_off)
+        got.append((o, lse, dq, dks[total - m:], dvs[total - m:]))
+    torch.cuda.synchronize()
+    for x, y in zip(got[0][:3], got[1][:3]):
+        assert torch.equal(x, y)
+    assert bool(torch.isfinite(got[0][0]).all())
+    # The keys' gradients take work-groups by the number of keys, another one here: the same operands (p and ds in bf16) are
+    # added in another order.  Two fp32 sums of q_len terms differ by at most 2 q_len 2^-24 of the sum of their sizes (formed
+    # here with errors of 1e-3 at most), and each is rounded to bf16 by half a step: 2 * 2^-8 of the larger.
+    kf, vf, qf, uf = (x.float().transpose(0, 1).contiguous() for x in (k[n - m:], v[n - m:], q, d_o))
+    o, lse = got[0][0].float().transpose(0, 1).contiguous(), got[0][1].t().contiguous()
+    seen = torch.ones(q_len, m, device="cuda").tril(m - q_len).bool()
+    s = torch.bmm(qf, kf.transpose(1, 2).contiguous()) / d ** 0.5
+    p = (s - lse[..., None]).exp() * seen
+    ds = p * (torch.bmm(uf, vf.transpose(1, 2).contiguous()) - (uf * o).sum(-1, keepdim=True))
+    sizes = (torch.bmm(ds.abs().transpose(1, 2).contiguous(), qf.abs()) / d ** 0.5,
+             torch.bmm(p.transpose(1, 2).contiguous(), uf.abs()))
+    for x, y, size in zip(got[0][3:], got[1][3:], sizes):
+        bound = 2 * q_len * 2.0 ** -24 * 1.01 * size.transpose(0, 1) + 2.0 ** -7 * torch.maximum(x.float().abs(), y.float().abs())
+        assert bool(((x.float() - y.float()).abs() <= bound).all())

@@ -235,6 +235,19 @@ def test_few_long_rows(n, v, bf16):
         Run(z, u, sampler=s, sampling=infs.make_sampling(**way)).check(z64, way)
 
 
+def test_rows_far_apart():
+    """Rows 4.3 GB apart."""
+    import torch
+
+    z, u, z64 = logits(3, 5003, True, 4)
+    far = torch.empty(2 * (1 << 31) + 6000, dtype=torch.bfloat16, device="cuda")
+    for i in range(3):
+        far[i << 31:][:5003] = z[i]
+    rows = far.as_strided((3, 5003), (1 << 31, 1))
+    for way in ({}, {"top_k": 50}, {"top_p": 0.9}):
+        Run(rows, u, row_stride=1 << 31, sampling=infs.make_sampling(**way)).check(z64, way)
+
+
 def test_longest_rows():
     import torch
 
