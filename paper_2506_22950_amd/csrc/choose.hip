@@ -1290,9 +1290,11 @@ __global__ __launch_bounds__(kPieceThreads, 4) void whole_kernel(const ChooseArg
   Piece<BF> pc(a, r, piece);
   float m = -INFINITY;
   int live = 0;
+  uint32_t some = 0;  // batches with an entry that is not masked
   bool odd = false;
 #pragma unroll
-  for (int i = 0; i < V; ++i)
+  for (int i = 0; i < V; ++i) {
+    const int before = live;
 #pragma unroll
     for (int j = 0; j < N && i < pc.batches; ++j) {
       const float z = pc.at(i, j);
@@ -1300,6 +1302,8 @@ __global__ __launch_bounds__(kPieceThreads, 4) void whole_kernel(const ChooseArg
       m = fmaxf(m, z);
       live += z > -INFINITY;
     }
+    some |= live > before ? 1u << i : 0u;
+  }
   for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i)), live += __shfl_xor(live, i);
   if (pc.lane == 0) tops[pc.wave] = m, lives[pc.wave] = live;
   odd = __syncthreads_or(odd);
@@ -1312,8 +1316,10 @@ __global__ __launch_bounds__(kPieceThreads, 4) void whole_kernel(const ChooseArg
   for (int i = 0; i < V; ++i) {
     if (i >= pc.batches) break;
     double part = 0.0;
-    if (m > -INFINITY && !odd) {
-      // a masked entry adds 2^-200, which is nothing to the largest one's 1 (find_entry leaves it out)
+    // A masked entry next to others adds 2^-200 of the largest weight, which its batch's sum may hold: an entry that is not
+    // masked is there to take the place.  A batch of masked entries alone must not have one, so it weighs 0: a target that
+    // is exactly the sum ahead of it (0 here) would stop at anything more.
+    if (m > -INFINITY && !odd && __any(some >> i & 1)) {
 #pragma unroll
       for (int j = 0; j < N; ++j) part += power(((double)Elem<BF>::get(pc.x[i], j) - m) * way.c, 0);
       part = wave_sum(part);
@@ -1368,12 +1374,13 @@ __global__ __launch_bounds__(kPieceThreads, 4) void whole_kernel(const ChooseArg
   const double whole = running(upto, scratch), target = (double)u * whole;
   const int mine = first_above(upto, own, target, &low, &high);
   if ((int)threadIdx.x == mine) {
-    double ahead = upto - own;
-    int i = from_piece;
-    for (; i < to_piece - 1; ++i) {
-      const double x = sum_of(i);
+    double ahead = upto - own, x = 0.0;
+    int i = from_piece;  // of the pieces with any weight (one has: own > 0), the last if rounding leaves none
+    for (int j = from_piece; j < to_piece; ++j) {
+      const double y = sum_of(j);
+      if (y == 0.0) continue;
+      ahead += x, x = y, i = j;
       if (ahead + x > target) break;
-      ahead += x;
     }
     high = i;
     inner = fmax(0.0, target - ahead);
