@@ -24,7 +24,7 @@
 // fp32 rows take fp32 products.
 //
 // Masked places.  A score that its row does not see is replaced, not added to,
-// and rows behind a sequence hold its last one again in LDS.  Only a product over tokens of
+// and rows behind a sequence hold its last one again in LDS, unseen by all.  Only a product over tokens of
 // one tile, some of them unseen, can meet 0 times an infinity or NaN.  Where
 // such a tile holds one (seen while it is staged), the work-group starts over
 // in a second pass over its tiles, in which those elements are taken out
@@ -856,7 +856,7 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
   constexpr int BK = 32 * C, BR = H::kBlock, R = Type<BF>::kRegs;
   __shared__ __attribute__((aligned(16))) char lds[H::kTiles + H::kValueBytes];  // Q and d_o of tiles, V
   __shared__ __attribute__((aligned(16))) float stats[2][2][H::kTokens];         // -lse log2(e) and D of their rows
-  __shared__ int odd;  // Q or d_o holds an infinity or NaN in a tile of which some keys are not seen
+  __shared__ int odd;  // Q or d_o holds an infinity or NaN in a tile of which some keys are not seen, or behind its rows
   const Walker at(a, kShared);
   const int g = at.g, slot = at.slot;
   const Place p = find_place(a.k_offsets, a.sequences, a.k_tokens, slot, 1, __builtin_ctz(BK));
@@ -936,7 +936,8 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 || (BF && S == 1) ? 2 : 1) v
           sq.store(lds + 2 * buffer * H::kTile);
           so.store(lds + (2 * buffer + 1) * H::kTile);
           if (wave < H::kTokens / 32) stats[buffer][half][wave * 32 + (lane & 31)] = half ? st : base_of(st);
-          if (!careful && begin + t * H::kTokens < all && (sq.odd() || so.odd())) odd = 1;
+          const int row0 = begin + t * H::kTokens;
+          if (!careful && (row0 < all || row0 + H::kTokens > rows) && (sq.odd() || so.odd())) odd = 1;
         },
         [&](int buffer, int t) {
           const int row0 = begin + t * H::kTokens + group * BR;

@@ -425,3 +425,43 @@ def test_graph_streams_and_two_attentions():
         for x, y in zip(out, eg):
             assert torch.equal(x, y)
         check_forward(c, eo, el)
+
+
+@pytest.mark.parametrize("bf16,d", [(True, 64), (True, 128), (False, 64), (False, 128)])
+@pytest.mark.parametrize("copies", [1, 5, 20])
+def test_infinities_of_a_last_token(bf16, d, copies):
+    """An infinite gradient of a sequence's last token reaches dv of every key as that infinity (p is above 0 for scores
+    as near as these), also where the rows of the sequence end inside a tile; other elements of dv stay finite, other
+    sequences' and KV heads' as they were.  With more sequences behind, so that every tile of keys is taken."""
+    import torch
+
+    lens = [300, 155]
+    c = Case(16, 8, d, bf16, lens * copies, tail=2)
+    a = c.attention()
+    o, lse = c.outputs()
+    c.attend(a, o, lse)
+    clean = c.grads()
+    c.grad(a, clean, o, lse)
+    inf = float("inf")
+    starts_of = starts(c.q_lens)
+    bad = [0, len(c.q_lens) - 1]  # sequences
+    for i in bad:
+        c.d_o[int(starts_of[i + 1]) - 1, 5, 9] = inf     # KV head 2
+        c.d_o[int(starts_of[i + 1]) - 1, 4, 21] = -inf
+    out = c.grads()
+    c.grad(a, out, o, lse)
+    torch.cuda.synchronize()
+    hit = torch.zeros(c.tk, dtype=torch.bool, device="cuda")
+    for i in bad:
+        hit[int(starts_of[i]):int(starts_of[i + 1])] = True
+    dv = out[2]
+    assert bool((dv[hit, 2, 9] == inf).all()), int(torch.isnan(dv[hit, 2, 9]).sum())
+    assert bool((dv[hit, 2, 21] == -inf).all())
+    rest = [e for e in range(d) if e not in (9, 21)]
+    # what is finite is the same sum, of which the second pass may add some elements in another order
+    want, got = clean[2][hit, 2][:, rest].double(), dv[hit, 2][:, rest].double()
+    assert bool(torch.isfinite(got).all())
+    assert float((got - want).abs().max()) <= (2.0 ** -8 if bf16 else 2.0 ** -18) * float(want.abs().max())
+    others = [h for h in range(8) if h != 2]
+    assert torch.equal(dv[:, others], clean[2][:, others]) and torch.equal(dv[~hit], clean[2][~hit])
+    assert torch.equal(out[1][:, others], clean[1][:, others]) and torch.equal(out[1][~hit], clean[1][~hit])
