@@ -538,8 +538,9 @@ infs_status infs_rotate_probe(infs_ctx* ctx, const infs_rotary* r, int32_t promp
  * Norms of heads with the rotation in the same pass: what models whose queries and keys are normed head by
  * head apply in the place of infs_rotate_*.  For a head x of d = head_dim elements with weights w:
  *     n = sqrt(sum x_e^2 / d + eps),   z_e = w_e x_e / n,   out = the rotation of z
- * Sums and products are held in fp32, outputs rounded once.  A head that holds an infinity or NaN is NaN
- * wherever the formula is (an infinity makes n infinite); one of zeros stays zero.
+ * Sums and products are held in fp32, outputs rounded once; heads whose squares leave its range are taken times a
+ * power of two.  A head that holds an infinity or NaN is NaN wherever the formula is (an infinity makes n infinite);
+ * one of zeros stays zero, also with eps = 0, where its gradient is zero too.
  * ------------------------------------------------------------------------------------------- */
 typedef struct infs_norms {
     const void* weight_q;   /* device, [head_dim] elements, a layer's at + layer * layer_stride; NULL: ones */
