@@ -304,7 +304,7 @@ struct Chooser {
 __device__ __forceinline__ bool allowed(const Sampling& p) {
   const double t = p.temperature;
   return (t == 0.0 || (t >= 0x1p-20 && t <= 0x1p20)) && p.top_p >= 0.0 && p.top_p <= 1.0 && p.min_p >= 0.0 &&
-         p.min_p <= 1.0 && p.top_k >= 0;
+         p.min_p <= 1.0 && p.top_k >= 0 && p.reserved == 0;
 }
 
 // A whole row by one work-group.  (Its loops are kept rolled: it is inlined into kernels whose registers it should not

@@ -116,3 +116,20 @@ def test_masked_batches_weigh_nothing():
             allowed = {at[min(int((sums <= i / n * sums[-1] + d).sum()), 3)] for d in (-slack, 0.0, slack)}
             assert int(t[i]) in allowed, (values, i, t[i], allowed)
         assert (r.kept.cpu().numpy() == 4).all()
+
+
+def test_rows_with_reserved_set():
+    """What a call refuses for all rows is no token for one of them."""
+    import torch
+
+    v, n = 1003, 6
+    live, u = [np.array([7, 900])] * n, [0.5] * n
+    ways = [WAYS[i] for i in (0, 2, 4, 0, 2, 4)]
+    each = array_of(ways)
+    words = each.view(torch.int32).view(n, -1)
+    words[3:, -1] = 1  # reserved, the last of a row's parameters
+    r = Run(rows_of(live, v, True, 0), torch.tensor(u, device="cuda"), each=each)
+    t, k, lp = r.token.cpu().numpy(), r.kept.cpu().numpy(), r.logprob.cpu().numpy()
+    assert (t[3:] == -1).all() and (k[3:] == 0).all() and np.isnan(lp[3:]).all(), (t, k, lp)
+    r.token, r.kept, r.logprob = r.token[:3], r.kept[:3], r.logprob[:3]
+    check(r, live, u, ways[:3])
