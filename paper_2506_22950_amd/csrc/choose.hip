@@ -776,6 +776,7 @@ __global__ __launch_bounds__(kPieceThreads, 4) void weigh_kernel(const ChooseArg
   }
   if (way.whole()) {
     if (u == 0.f) {
+      if (threadIdx.x == 0) state.mode = kDone;
       choose_row<BF>(a, r, *(Shared*)lds);
       return;
     }

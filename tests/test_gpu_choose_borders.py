@@ -133,3 +133,22 @@ def test_rows_with_reserved_set():
     assert (t[3:] == -1).all() and (k[3:] == 0).all() and np.isnan(lp[3:]).all(), (t, k, lp)
     r.token, r.kept, r.logprob = r.token[:3], r.kept[:3], r.logprob[:3]
     check(r, live, u, ways[:3])
+
+
+def test_first_entries_after_other_calls():
+    """u = 0 without a filter, row by row, on a sampler whose rows were listed and summed by the call before: the first
+    entry of any weight, whatever that call left in the workspace."""
+    import torch
+
+    from tests.test_gpu_choose import define, logits
+
+    v, n = 50257, 6
+    z, u, z64 = logits(n, v, True, 12, masked=70)
+    z[:, :3] = -math.inf
+    z64[:, :3] = -np.inf
+    s = infs.Sampler(infs.make_sampler_config(vocab=v, dtype=infs.BF16, max_rows=n), stream=torch.cuda.current_stream())
+    for before in ({"top_p": 0.9}, {"top_k": 900}, {"top_k": 900, "top_p": 0.9}):
+        Run(z, u, sampler=s, each=array_of([before] * n)).check(z64, before)
+        r = Run(z, torch.zeros(n, device="cuda"), sampler=s, each=array_of([{}] * n))
+        assert (r.token == 3).all() and (r.kept == v - 73).all()
+        assert all(define(row, 0.0)[0] == 3 for row in z64)
