@@ -1427,7 +1427,8 @@ hipError_t launch_choose(ChooseArgs& a, bool bf16, hipStream_t stream) {
   // lists of all pieces' first top_k, with room for what else lies in their last bins
   bool top = !a.each && p.top_k > 0 && p.top_k < a.vocab && p.top_k <= kPieceThreads / 2;
   // (for few long rows that takes pieces of more entries: one row of 243428, top-k 64: 48 us in two launches of 60 pieces,
-  // 17 in one of 30)
+  // 17 in one of 30; where the largest are still too many, the two launches keep them, since their joins go by pieces: one
+  // row of 151936 in fp32, top-k 250: 37 us in 10 pieces, 61 in 75)
   for (; top && (int64_t)p.top_k * a.pieces > kList / 2; a.pieces = choose_pieces(a.vocab, a.batches, bf16)) {
     if (a.batches < kPieceVectors)
       ++a.batches;
