@@ -47,7 +47,7 @@ void set_rotary(const infs_rotary& r, bool inverse, RotaryArgs* a) {
   a->sign = inverse ? -1.f : 1.f;
 }
 
-infs_status pack_norms(const infs_norms* n, int head_dim, int layers, NormWeights* out) {
+infs_status pack_norms(const infs_norms* n, NormWeights* out) {
   if (!n) return op_fail(INFS_E_ARG, "null norms");
   if (n->dtype != INFS_F32 && n->dtype != INFS_BF16) return op_fail(INFS_E_ARG, "norms: dtype must be INFS_F32 or INFS_BF16");
   if (!(n->eps >= 0.f) || !std::isfinite(n->eps)) return op_fail(INFS_E_ARG, "norms: eps must be finite and >= 0");
@@ -307,7 +307,7 @@ infs_status infs_norm_rotate_rows(const infs_rotary* r, void* hip_stream, int32_
                                   const int32_t* positions_dev, int32_t first_position) {
   infs::NormArgs a{};
   infs_status st = infs::pack_rotation(r, dtype, tokens, q, k, positions_dev, first_position, &a.r);
-  if (st == INFS_OK) st = infs::pack_norms(norms, r->cfg.head_dim, 1, &a);
+  if (st == INFS_OK) st = infs::pack_norms(norms, &a);
   if (st != INFS_OK || tokens == 0) return st;
   infs::set_rotary(*r, false, &a.r);
   infs::StreamDevice dev((hipStream_t)hip_stream);
@@ -328,7 +328,7 @@ infs_status infs_norm_rotate_grad(const infs_rotary* r, void* hip_stream, int32_
                                   const int32_t* positions_dev, int32_t first_position) {
   infs::NormGradArgs a{};
   infs_status st = infs::pack_rotation(r, dtype, tokens, q, k, positions_dev, first_position, &a.r);
-  if (st == INFS_OK) st = infs::pack_norms(norms, r->cfg.head_dim, 1, &a);
+  if (st == INFS_OK) st = infs::pack_norms(norms, &a);
   if (st != INFS_OK) return st;
   if (!q != !dq || !k != !dk) return op_fail(INFS_E_ARG, "q and dq go together, and k and dk");
   const infs_rows* rows[2] = {q, k};

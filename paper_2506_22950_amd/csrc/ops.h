@@ -112,8 +112,8 @@ inline int norm_grad_parts(int64_t tokens) { return (int)(tokens < kNormGradPart
 // Fill in what the structs leave to them.
 hipError_t launch_norm_rotate(NormArgs& args, bool bf16, bool interleaved, int layers, hipStream_t stream);
 hipError_t launch_norm_rotate_grad(NormGradArgs& args, bool bf16, bool interleaved, hipStream_t stream);
-// E_ARG (op_fail), or the weights of `layers` layers.
-infs_status pack_norms(const infs_norms* n, int head_dim, int layers, NormWeights* out);
+// E_ARG (op_fail), or the weights of every layer.
+infs_status pack_norms(const infs_norms* n, NormWeights* out);
 
 // ---- scores of tokens -----------------------------------------------------------
 constexpr int kScoreMaxRows = 1 << 23;

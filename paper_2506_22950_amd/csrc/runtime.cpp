@@ -1590,7 +1590,7 @@ infs_status rotate_slots(infs_ctx* c, const infs_rotary* r, int32_t num_layers, 
   infs::NormArgs na{};
   infs::RotaryArgs& a = na.r;
   if (normed) {
-    const infs_status st = infs::pack_norms(norms, c->D, num_layers, &na);
+    const infs_status st = infs::pack_norms(norms, &na);
     if (st != INFS_OK) return fail(c, st, "%s", g_thread_error.c_str());
   }
   const infs_rows* rows[2] = {q, k};
