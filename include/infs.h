@@ -582,7 +582,9 @@ int64_t infs_norm_rotate_grad_workspace(int64_t tokens, int32_t head_dim);
  * where that is negative, then o = 0 and lse = -inf).  Query head h goes with KV head h / (Hq / Hkv), and over the
  * keys that a query sees
  *     s_j = scale q.k_j,   lse = ln sum_j e^(s_j),   o = sum_j e^(s_j - lse) v_j
- * Sums are held in fp32.  No output depends on a token that it does not see, whatever that holds.
+ * Sums, maxima and exponentials are held in fp32.  With bf16 rows the operands of the matrix products are bf16 too: the
+ * rows as they are, and the weights of the keys (in the gradient p and ds below) rounded to it, 2^-8 of themselves at
+ * most.  No output depends on a token that it does not see, whatever that holds.
  * ------------------------------------------------------------------------------------------- */
 typedef struct infs_attention_config {
     int32_t num_q_heads;   /* Hq, a multiple of num_kv_heads, up to 4096 */
@@ -616,9 +618,13 @@ infs_status infs_attend(infs_attention* a, int32_t sequences, int64_t q_tokens, 
                         const infs_rows* v, float* lse_dev);
 
 /* Its gradient: q, k, v: in as in infs_attend, out the gradients with respect to them; o, d_o: in the outputs and
-   their gradients; lse_dev as infs_attend wrote it.  dk and dv are sums over the queries of a group's heads,
-   added in an order that depends on sizes and offsets alone; keys that no query sees get zeros.  The gradients may
-   not overlap the inputs. */
+   their gradients; lse_dev as infs_attend wrote it.  With p_j = e^(s_j - lse) and ds_j = p_j (d_o.v_j - d_o.o):
+       dq = scale sum_j ds_j k_j,   dk_j = scale sum ds_j q,   dv_j = sum p_j d_o
+   dk and dv are sums over the queries of a group's heads, added in an order that depends on sizes and offsets alone;
+   keys that no query sees get zeros.  The gradients may not overlap the inputs.
+   lse is all that is kept of a row, in fp32, so p_j is right within a factor of e^(|lse| 2^-21) on top of what the score's
+   own sum is off by; where |lse| is above 2^26 ln 2 (4.6e7) it is lowered by 2^-32 and more, so that no gradient
+   leaves fp32 by it. */
 infs_status infs_attend_grad(infs_attention* a, int32_t sequences, int64_t q_tokens, const int32_t* q_offsets_dev,
                              int64_t k_tokens, const int32_t* k_offsets_dev, const infs_rows* q, const infs_rows* k,
                              const infs_rows* v, const infs_rows* o, const infs_rows* d_o, const float* lse_dev);

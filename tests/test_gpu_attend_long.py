@@ -200,3 +200,37 @@ def test_offsets_beyond_32_bits(q_len):
     for x, y, size in zip(got[0][3:], got[1][3:], sizes):
         bound = 2 * q_len * 2.0 ** -24 * 1.01 * size.transpose(0, 1) + 2.0 ** -7 * torch.maximum(x.float().abs(), y.float().abs())
         assert bool(((x.float() - y.float()).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradient_of_far_scores(d):
+    """What the gradient's p is off by where scores lie far from 0: sequences of one token, whose only weight is 1, read off dv
+    = p d_o.  Scores are one product (exact).  Roundings of 2^-24 of the exponent each: in lse the score times the scale, the
+    base of its exponential (taken off again by the sum's logarithm) and the sum of both; here scale log2(e) and the base:
+    5 2^-24 < 2^-21, so p is within a factor of e^(|lse| 2^-21), and 2^-21 for the exponential and the products.  Beyond
+    2^26 powers of 2 (where lse's base is exact: 3 2^-24) it is lowered by 2^-21 of the exponent: below 2^-20.  o is p v / p:
+    three roundings."""
+    import torch
+
+    n, scale = 2000, 0.3
+    c = Case(1, 1, d, False, [1] * n, scale=scale, tail=0)
+    c.q.zero_(), c.k.zero_()
+    c.d_o.fill_(1.0)
+    gen = torch.Generator().manual_seed(11)
+    size = 2.0 ** (torch.rand(n, generator=gen).double() * 40 - 4)
+    c.q[:, 0, 7] = (size / 1000).float().cuda()
+    c.k[:, 0, 7] = (1000 * torch.randn(n, generator=gen).sign()).cuda()
+    a = c.attention()
+    o, lse = c.outputs()
+    c.attend(a, o, lse)
+    out = c.grads()
+    c.grad(a, out, o, lse)
+    torch.cuda.synchronize()
+    far = lse[:, 0].double().abs()
+    p = out[2][:, 0, 0].double()
+    near = far <= 2.0 ** 26 * np.log(2.0)
+    assert 1000 < int(near.sum()) < n - 100
+    assert bool(((o - c.v).double().abs() <= 3.01 * 2.0 ** -24 * c.v.double().abs()).all())
+    off = far[near] * 2.0 ** -21 + 2.0 ** -21
+    assert bool(torch.isfinite(p).all()) and bool((p[near].log().abs() <= off).all())
+    assert bool((p[~near] <= 2.0 ** -20).all())
