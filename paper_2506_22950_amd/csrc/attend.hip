@@ -831,9 +831,10 @@ __global__ __launch_bounds__(64 * C * S, C * S >= 8 ? 2 : 1) void attend_dq_kern
 //
 // Registers: two operands and two results of 32 keys, 192 of them for bf16 heads of 128 and twice as many operands in
 // fp32.  For bf16 the values' operand stays in LDS (a quarter more to read there; in registers the kernel spilled);
-// fp32 heads of 128, and splits, take a wavefront's whole file.
+// fp32 heads of 128, and splits, take a wavefront's whole file.  bf16 keys of two wavefronts and four splits still spill, 15
+// registers for heads of 128 and 12 for 64.
 // Bound by LDS: of 32 x 32 products whose operands both serve once, 400 cycles of reads for 1024 of the matrix unit,
-// and eight wavefronts on one LDS.  290 us for the sequences above (four products); work-groups of 256 keys, one a CU
+// and eight wavefronts on one LDS.  287 us for the sequences above (four products); work-groups of 256 keys, one a CU
 // instead of two of 128, took 310.
 template <bool BF, int D, int C, int S>
 struct KeyShape {

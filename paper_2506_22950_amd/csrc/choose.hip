@@ -1270,7 +1270,7 @@ __device__ __forceinline__ int first_above(double x, double own, double target, 
 
 // The whole distribution, read once: the sums of pieces, of their wavefronts' batches and at last of 64 vectors narrow
 // the place down.  Sums are doubles here, added in an order that sizes and alignment fix.
-// 512 rows of 151936 in bf16: 100 us, 1.6 TB/s: bound by the weights in double, some 40 us of them, and by the chain of
+// 512 rows of 151936 in bf16: 101 us, 1.5 TB/s: bound by the weights in double, some 40 us of them, and by the chain of
 // a piece in front of and behind them (138 in two launches).
 template <bool BF>
 __global__ __launch_bounds__(kPieceThreads, 4) void whole_kernel(const ChooseArgs a) {
