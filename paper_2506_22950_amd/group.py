@@ -56,6 +56,8 @@ def prefill_prompts(ctx: infs.Context, prompt_lens: Sequence[int], num_layers: i
     c, a, tokens = ctx.config, attention.config, sum(prompt_lens)
     if (a.num_q_heads, a.num_kv_heads, a.head_dim, a.dtype) != (c.num_q_heads, c.num_kv_heads, c.head_dim, c.dtype):
         raise ValueError("the attention has other heads, or another type, than the context")
+    if rotary is not None and rotary.config.head_dim != c.head_dim:
+        raise ValueError(f"rotary head_dim {rotary.config.head_dim} is not the context's {c.head_dim}")
     if (attention.stream or 0) != (ctx.stream or 0):
         raise ValueError("the attention has to be on the context's stream")
     if len(prompt_lens) > c.num_prompts:

@@ -69,3 +69,22 @@ def test_prompts_that_do_not_fit_together():
         prefill_prompts(ctx, [8, 8, 8], L, provide, attention, None)
     assert not asked
     ctx.destroy()
+
+
+def attention_for(ctx, max_tokens=64):
+    c = ctx.config
+    return infs.Attention(infs.make_attention_config(
+        num_q_heads=c.num_q_heads, num_kv_heads=c.num_kv_heads, head_dim=c.head_dim, dtype=c.dtype, max_tokens=max_tokens,
+        flags=infs.FLAG_DRY_RUN))
+
+
+def test_prompts_with_a_rotary_of_other_heads():
+    """Dense rows of the context's heads, taken for larger ones, would be read and written past their end."""
+    ctx, asked = context(prefill=False), []
+    for d in (32, 128):
+        rotary = infs.Rotary(config(head_dim=d, rotary_dim=d))
+        for norms in (None, infs.make_norms(dtype=infs.F32)):
+            with pytest.raises(ValueError, match="rotary"):
+                prefill_prompts(ctx, [8, 8], L, asked.append, attention_for(ctx), None, rotary, norms, positions=1 << 16)
+    assert not asked
+    ctx.destroy()
