@@ -62,6 +62,13 @@ def prefill_prompts(ctx: infs.Context, prompt_lens: Sequence[int], num_layers: i
         raise ValueError("the attention has to be on the context's stream")
     if len(prompt_lens) > c.num_prompts:
         raise ValueError(f"{len(prompt_lens)} prompts for a context of {c.num_prompts}")
+    if num_layers > c.num_layers:
+        raise ValueError(f"{num_layers} layers for a context of {c.num_layers}")
+    for p, n in enumerate(prompt_lens):
+        if not 0 <= n <= c.max_prompt_len:
+            raise ValueError(f"prompt {p} has {n} tokens, the context takes up to {c.max_prompt_len}")
+    if tokens > a.max_tokens:
+        raise ValueError(f"{tokens} tokens for an attention of {a.max_tokens}")
     size = c.num_kv_heads * c.head_dim * (4 if c.dtype == infs.F32 else 2)  # bytes of a token's K or V
     for layer in range(num_layers):
         q, k, v, o = (infs._ptr(x) for x in provide(layer))

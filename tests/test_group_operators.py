@@ -88,3 +88,17 @@ def test_prompts_with_a_rotary_of_other_heads():
                 prefill_prompts(ctx, [8, 8], L, asked.append, attention_for(ctx), None, rotary, norms, positions=1 << 16)
     assert not asked
     ctx.destroy()
+
+
+@pytest.mark.parametrize("lens,layers,max_tokens,match", [
+    ([8, 17], L, 64, "prompt 1"), ([17], L, 64, "prompt 0"), ([8, -4], L, 64, "prompt 1"), ([16, 16], L, 31, "tokens"),
+    ([8, 8], L + 1, 64, "layers")])
+def test_prompts_that_no_pass_takes(lens, layers, max_tokens, match):
+    """What the context or the attention would refuse later, behind rows that are rotated in place and prompts that are
+    stored, is refused before anything is done."""
+    ctx, asked = context(prefill=False), []
+    with pytest.raises(ValueError, match=match):
+        prefill_prompts(ctx, lens, layers, asked.append, attention_for(ctx, max_tokens), None)
+    assert not asked
+    prefill_prompts(ctx, [16, 0], L, lambda layer: NONE, attention_for(ctx, 16), None)
+    ctx.destroy()
