@@ -100,5 +100,5 @@ def test_prompts_that_no_pass_takes(lens, layers, max_tokens, match):
     with pytest.raises(ValueError, match=match):
         prefill_prompts(ctx, lens, layers, asked.append, attention_for(ctx, max_tokens), None)
     assert not asked
-    prefill_prompts(ctx, [16, 0], L, lambda layer: NONE, attention_for(ctx, 16), None)
+    prefill_prompts(ctx, [16, 0], L, lambda layer: [i << 20 for i in range(1, 5)], attention_for(ctx, 16), None)
     ctx.destroy()
