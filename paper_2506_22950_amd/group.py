@@ -71,7 +71,8 @@ def prefill_prompts(ctx: infs.Context, prompt_lens: Sequence[int], num_layers: i
         raise ValueError(f"{tokens} tokens for an attention of {a.max_tokens}")
     size = c.num_kv_heads * c.head_dim * (4 if c.dtype == infs.F32 else 2)  # bytes of a token's K or V
     for layer in range(num_layers):
-        q, k, v, o = (infs._ptr(x) for x in provide(layer))
+        buffers = provide(layer)  # held until the layer's calls are made
+        q, k, v, o = (infs._ptr(x) for x in buffers)
         if rotary is not None:
             rows = infs.rotary_rows(q, q, c.num_q_heads), infs.rotary_rows(k, k, c.num_kv_heads)
             if norms is not None:

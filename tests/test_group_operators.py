@@ -102,3 +102,37 @@ def test_prompts_that_no_pass_takes(lens, layers, max_tokens, match):
     assert not asked
     prefill_prompts(ctx, [16, 0], L, lambda layer: [i << 20 for i in range(1, 5)], attention_for(ctx, 16), None)
     ctx.destroy()
+
+
+def test_buffers_of_a_layer_live_through_its_calls():
+    """provide()'s buffers may be its only references: they are held until the layer's calls are made."""
+    import weakref
+
+    class Buffer:
+        def __init__(self, at):
+            self.at = at
+
+        def data_ptr(self):
+            return self.at
+
+    alive = []
+
+    class Spy:
+        def __init__(self, ctx):
+            self.config, self.stream, self.ctx = ctx.config, ctx.stream, ctx
+
+        def prefill_shared(self, *a):
+            alive.append(sum(r() is not None for r in refs))
+            self.ctx.prefill_shared(*a)
+
+    refs = []
+
+    def provide(layer):
+        b = [Buffer(i << 20) for i in range(1, 5)]
+        refs[:] = [weakref.ref(x) for x in b]
+        return b
+
+    ctx = context(prefill=False)
+    prefill_prompts(Spy(ctx), [8, 3], L, provide, attention_for(ctx), 1 << 16)
+    assert alive == [4] * (2 * L)
+    ctx.destroy()
